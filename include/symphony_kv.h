@@ -298,6 +298,81 @@ int sym_pred_layer(sym_ctx* ctx, int32_t layer, const void* q, const void* k_new
                    const void* v_new, float* out, void* stream);
 int sym_pred_end(sym_ctx* ctx);
 
+/* ---- rotary positions, bounds of pages, sparse preds --------------------------------- */
+/* Pair i of a head (i < dims / 2) turns by position * f_i radians: with c and s the cosine and sine of that, times magnitude,
+ *   y1 = x1 c - x2 s,  y2 = x2 c + x1 s
+ * where (x1, x2) are elements (i, i + dims/2) of the head, or (2i, 2i + 1).  f_i = base^(-2i / dims), scaled for
+ * contexts longer than a model was made for:
+ *   original_len = 0: f_i / factor;
+ *   original_len > 0: by parts.  A pair that turns more than high_turns times over original_len tokens keeps f_i, one that
+ *     turns less than low_turns times gets f_i / factor, between the two the share kept rises linearly with the turns.
+ * Everything is computed in 64 bits and rounded to the storage type (by way of 32 bits).     */
+#define SYM_ROPE_HALVES      0   /* element i pairs with i + dims / 2   */
+#define SYM_ROPE_INTERLEAVED 1   /* element 2i pairs with 2i + 1        */
+typedef struct sym_rope {
+  int32_t layout;
+  int32_t dims;            /* leading elements of a head that turn: even; 0 = head_dim.  The others stay as they are  */
+  double  base;            /* > 0                                                        */
+  double  factor;          /* > 0; 0 = 1                                                 */
+  int64_t original_len;
+  double  low_turns, high_turns;   /* with original_len: high_turns > low_turns          */
+  double  magnitude;       /* 0 = 1                                                      */
+} sym_rope;
+/* Query rows q [n][Hq][D] and key rows k [n][Hkv][D] of n tokens turned to their positions (device int32 [n], any sign), for preds that
+ * take rows as they are (sym_pred_batch, sym_pred_layer).  Either pair of pointers may be NULL.  An output may be its own
+ * input; any other overlap is refused.  Rows 16-byte aligned.  Touches neither files nor workspace: allowed while a batch is
+ * open, and may be recorded into a graph.                                                 */
+int sym_rope_rows(sym_ctx* ctx, const sym_rope* rope, int32_t n, const int32_t* positions,
+                  const void* q, void* q_out, const void* k, void* k_out, void* stream);
+/* kv_append of n_tokens[b] >= 1 rows to each of n_files files (distinct, else SYM_EBUSY), keys turned on the way.  k, v: device,
+ * [n_layers][T][Hkv][D], files in order, 16-byte aligned; positions: device int32 [T], or NULL: the tokens' indices in their
+ * files; rope NULL: rows are appended as they are.  Bounds of the pages that become full are written too where a buffer is
+ * attached.  Not to be recorded into a graph (SYM_EINVAL), like every call below.          */
+int sym_kv_append_rope(sym_ctx* ctx, int32_t n_files, const sym_kv* kv, const int32_t* n_tokens,
+                       const sym_rope* rope, const int32_t* positions, const void* k, const void* v, void* stream);
+
+/* Bounds of a page: per layer and kv head the elementwise minimum and maximum of its 16 keys (a NaN makes both NaN), in the storage
+ * type, [n_layers][n_pages][Hkv][2 (minimum, maximum)][D], in a buffer of the caller.  Only full pages have them: a file's
+ * last, partly filled page is always read.
+ *   sym_bounds_bytes: size of the buffer.  sym_bounds_attach: device memory, 256-byte aligned, owned by the caller; NULL detaches it.
+ *     Files start without bounds whatever the buffer holds.
+ *   sym_kv_bounds: computes the bounds of every full page of n files (in a host-only context only what is recorded of them).
+ *   sym_kv_bounded: the leading pages of the file that have bounds.  Appends leave them, forks inherit them, truncate
+ *     and offload lower the number; sparse preds compute what is missing for the files of their batch.     */
+int64_t sym_bounds_bytes(const sym_config* cfg);
+int     sym_bounds_attach(sym_ctx* ctx, void* bounds, int64_t bytes);
+int     sym_kv_bounds(sym_ctx* ctx, int32_t n, const sym_kv* kv, void* stream);
+int64_t sym_kv_bounded(sym_ctx* ctx, sym_kv kv);
+
+/* pred over a choice of pages.  A new token whose visible tokens lie in n pages (the last one as far as visible) reads, for each kv head,
+ * all of them if n <= budget, else: the first `first`, the last `last`, and of the others the budget - first - last of highest
+ * score.  The score of a page is
+ *   sum_d A_d maximum_d + B_d minimum_d,   A_d = sum_h max(q_hd, 0),  B_d = sum_h min(q_hd, 0)
+ * over the query heads h of the kv head: what the sum of their logits with any key of the page does not exceed.  Summed in 64
+ * bits, rounded to 32; of equal scores the lower index is taken, NaN counts as above all.  The softmax runs over the tokens read.
+ *   rope: NULL, or the new tokens' q and k rows are turned first (q and k_new themselves stay as they are);
+ *   positions: device int32 [T] (with a rope), read by every layer; NULL: the tokens' indices in their files;
+ *   dense_layers: sym_pred_begin_sparse also prepares the batch for sym_pred_layer.
+ * sym_pred_sparse: appends and attends like sym_pred_batch (same rules and errors; single-layer contexts).  picked: NULL, or
+ *   device int32 [T][Hkv][budget], receives the indices of the pages read, in order, -1 behind the last.
+ * sym_pred_begin_sparse / sym_pred_layer_sparse: the same over layers, like sym_pred_begin / sym_pred_layer and under the same rules; with
+ *   dense_layers each layer is run by either sym_pred_layer_sparse or sym_pred_layer (rows as they are: it knows no rope).
+ * Rows and outputs 16-byte aligned.  A buffer for bounds has to be attached.  SYM_ENOSPC if the workspace does not hold the batch:
+ * beside the page tables about T * Hq * 256 bytes with a rope, and for one token Hkv * 4 bytes per page of the longest file and
+ * per page read.                                                                          */
+typedef struct sym_sparse {
+  int32_t budget, first, last;     /* first >= 0, last >= 1, first + last <= budget      */
+  int32_t dense_layers;
+  const sym_rope* rope;            /* host; copied by the call                           */
+  const int32_t* positions;
+} sym_sparse;
+int sym_pred_sparse(sym_ctx* ctx, int32_t n_lips, const sym_kv* kv, const int32_t* n_tokens, const sym_sparse* sparse,
+                    const void* q, const void* k_new, const void* v_new, float* out, int32_t* picked, void* stream);
+int sym_pred_begin_sparse(sym_ctx* ctx, int32_t n_lips, const sym_kv* kv, const int32_t* n_tokens,
+                          const sym_sparse* sparse, void* stream);
+int sym_pred_layer_sparse(sym_ctx* ctx, int32_t layer, const void* q, const void* k_new, const void* v_new,
+                          float* out, int32_t* picked, void* stream);
+
 /* Kernel-level entry without the allocator: attention only, over page tables the caller
  * supplies.  K/V of every token (new ones included) must already be in the pool.
  * page_table_flat: host int32, LIP b's page ids at [pt_offsets[b], pt_offsets[b+1]);
@@ -439,8 +514,8 @@ int     sym_sched_state(sym_sched* s, double* rate_per_us, double* target_batch,
 
 /* ---- measurement ------------------------------------------------------------------- */
 /* Kernel ids for sym_profile_read. */
-#define SYM_K_PROLOGUE 0   /* descriptor copy + copy-on-write copies + KV append, one launch */
-#define SYM_K_ATTN     1   /* attention over the page tables: decode ranges + MFMA tiles     */
+#define SYM_K_PROLOGUE 0   /* descriptor copy + copy-on-write copies + KV append, one launch; rope, rotated appends, bounds */
+#define SYM_K_ATTN     1   /* attention over the page tables: decode ranges + MFMA tiles; scores, choice and attention of a sparse pred */
 #define SYM_K_MERGE    2   /* merge of the partial results of ranges that were cut           */
 #define SYM_K_MOVE     3   /* token copies of sym_kv_extract / sym_kv_merge                  */
 #define SYM_K_SWAP     4   /* page copies of sym_kv_offload / sym_kv_restore                 */

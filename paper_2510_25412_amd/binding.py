@@ -13,6 +13,7 @@ LIB_PATH = os.environ.get("SYMPHONY_KV_LIB") or os.path.join(_HERE, "libsymphony
 
 SYM_OK, SYM_EINVAL, SYM_EBADF, SYM_ENOSPC, SYM_ENOENT, SYM_EEXIST, SYM_EBUSY, SYM_EHIP = 0, -1, -2, -3, -4, -5, -6, -7
 SYM_F32, SYM_BF16 = 0, 1
+ROPE_LAYOUTS = {"halves": 0, "interleaved": 1}
 K_PROLOGUE, K_ATTN, K_MERGE, K_MOVE, K_SWAP = 0, 1, 2, 3, 4
 
 
@@ -39,6 +40,16 @@ class SymStats(C.Structure):
                                          "host_ns_plan", "host_ns_pred", "tokens_moved", "pages_referenced",
                                          "pages_offloaded", "pages_restored", "host_slots", "last_batch_tiles",
                                          "last_batch_shared_rows")]
+
+
+class SymRope(C.Structure):
+    _fields_ = [("layout", C.c_int32), ("dims", C.c_int32), ("base", C.c_double), ("factor", C.c_double), ("original_len", C.c_int64),
+                ("low_turns", C.c_double), ("high_turns", C.c_double), ("magnitude", C.c_double)]
+
+
+class SymSparse(C.Structure):
+    _fields_ = [("budget", C.c_int32), ("first", C.c_int32), ("last", C.c_int32), ("dense_layers", C.c_int32),
+                ("rope", C.POINTER(SymRope)), ("positions", C.c_void_p)]
 
 
 class SymError(RuntimeError):
@@ -80,6 +91,15 @@ _SIGNATURES = {
     "sym_pred_end": (C.c_int, [C.c_void_p]),
     "sym_kv_read_layer": (C.c_int, [C.c_void_p, C.c_int32, C.c_int32, C.c_int64, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p]),
     "sym_pred_batch_raw": (C.c_int, [C.c_void_p, C.c_int32, _I32P, _I32P, _I64P, _I64P, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "sym_rope_rows": (C.c_int, [C.c_void_p, C.POINTER(SymRope), C.c_int32] + [C.c_void_p] * 6),
+    "sym_kv_append_rope": (C.c_int, [C.c_void_p, C.c_int32, _I32P, _I32P, C.POINTER(SymRope)] + [C.c_void_p] * 4),
+    "sym_bounds_bytes": (C.c_int64, [C.POINTER(SymConfig)]),
+    "sym_bounds_attach": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int64]),
+    "sym_kv_bounds": (C.c_int, [C.c_void_p, C.c_int32, _I32P, C.c_void_p]),
+    "sym_kv_bounded": (C.c_int64, [C.c_void_p, C.c_int32]),
+    "sym_pred_sparse": (C.c_int, [C.c_void_p, C.c_int32, _I32P, _I32P, C.POINTER(SymSparse)] + [C.c_void_p] * 6),
+    "sym_pred_begin_sparse": (C.c_int, [C.c_void_p, C.c_int32, _I32P, _I32P, C.POINTER(SymSparse), C.c_void_p]),
+    "sym_pred_layer_sparse": (C.c_int, [C.c_void_p, C.c_int32] + [C.c_void_p] * 6),
     "sym_kv_pages": (C.c_int64, [C.c_void_p, C.c_int32, _I32P, C.c_int64]),
     "sym_page_refcount": (C.c_int32, [C.c_void_p, C.c_int32]),
     "sym_free_pages": (C.c_int64, [C.c_void_p]),
@@ -160,6 +180,21 @@ def _ptr(t):
     return t.data_ptr()
 
 
+def _batch(kv, n_tokens):
+    """Files and their new tokens as int32 arrays of one length."""
+    kv, n_tokens = np.ascontiguousarray(kv, np.int32), np.ascontiguousarray(n_tokens, np.int32)
+    if kv.shape != n_tokens.shape or kv.ndim != 1:
+        raise ValueError(f"{kv.shape} files, but {n_tokens.shape} numbers of tokens")
+    return kv, n_tokens
+
+
+def _positions(t):
+    """Address of int32 positions."""
+    if t is not None and not isinstance(t, int) and str(t.dtype) != "torch.int32":
+        raise TypeError(f"positions must be int32, got {t.dtype}")
+    return _ptr(t)
+
+
 def make_config(n_q_heads, n_kv_heads, head_dim, page_tokens, dtype, n_pages, device=-1, pool=None, workspace=None,
                 workspace_bytes=0, free_order=None, softmax_scale=0.0, decode_waves=0, n_layers=1, tuning=None):
     """`tuning`: dict of sym_tuning fields to change from the library's defaults for this shape."""
@@ -185,6 +220,22 @@ def make_config(n_q_heads, n_kv_heads, head_dim, page_tokens, dtype, n_pages, de
         cfg._tuning = t
         cfg.tuning = C.pointer(t)
     return cfg
+
+
+def make_rope(layout="halves", dims=0, base=10000.0, factor=1.0, original_len=0, low_turns=1.0, high_turns=32.0, magnitude=1.0):
+    """How rows turn to their positions (struct sym_rope of the header)."""
+    return SymRope(ROPE_LAYOUTS.get(layout, layout), dims, base, factor, original_len, low_turns, high_turns, magnitude)
+
+
+def make_sparse(budget, first=1, last=1, rope=None, positions=None, dense_layers=False):
+    """Which pages a sparse pred reads (struct sym_sparse of the header); positions: int32 tensor on the device or None."""
+    s = SymSparse(budget, first, last, 1 if dense_layers else 0, C.pointer(rope) if rope is not None else None, _positions(positions))
+    s._keep = (rope, positions)
+    return s
+
+
+def bounds_bytes(cfg):
+    return load().sym_bounds_bytes(C.byref(cfg))
 
 
 def page_bytes(cfg):
@@ -357,6 +408,43 @@ class Context:
         kv_a, kv_p = _i32(kv)
         nt_a, nt_p = _i32(n_tokens)
         self._chk(self._fn.sym_pred_batch_static(self.h, len(kv_a), kv_p, nt_p, _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(out), stream))
+
+    # ---- rotary positions, bounds of pages, sparse preds ----
+    def rope_rows(self, rope, positions, q, q_out, k, k_out, stream=None):
+        """Rows of len(positions) tokens turned; q or k (and its output) may be None.  positions: int32 tensor on the device."""
+        n = positions.numel()
+        for x, heads in ((q, self.cfg.n_q_heads), (q_out, self.cfg.n_q_heads), (k, self.cfg.n_kv_heads), (k_out, self.cfg.n_kv_heads)):
+            if x is not None and not isinstance(x, int) and x.numel() != n * heads * self.cfg.head_dim:
+                raise ValueError(f"{n} positions, but rows of shape {tuple(x.shape)}")
+        self._chk(self.lib.sym_rope_rows(self.h, C.byref(rope), n, _positions(positions), _ptr(q), _ptr(q_out), _ptr(k), _ptr(k_out), stream))
+
+    def kv_append_rope(self, kv, n_tokens, rope, k, v, positions=None, stream=None):
+        kv_a, nt_a = _batch(kv, n_tokens)
+        self._chk(self._fn.sym_kv_append_rope(self.h, len(kv_a), kv_a.ctypes.data, nt_a.ctypes.data, None if rope is None else C.byref(rope), _positions(positions), _ptr(k), _ptr(v), stream))
+
+    def bounds_attach(self, bounds):
+        """bounds: device tensor of at least bounds_bytes(cfg) bytes, or None.  Kept alive by the context."""
+        self._chk(self.lib.sym_bounds_attach(self.h, _ptr(bounds), 0 if bounds is None else bounds.numel() * bounds.element_size()))
+        self._bounds = bounds
+
+    def kv_bounds(self, kv, stream=None):
+        kv_a, kv_p = _i32(kv)
+        self._chk(self._fn.sym_kv_bounds(self.h, len(kv_a), kv_p, stream))
+
+    def kv_bounded(self, kv):
+        return self._chk(self.lib.sym_kv_bounded(self.h, kv))
+
+    def pred_sparse(self, kv, n_tokens, sparse, q, k_new, v_new, out, picked=None, stream=None):
+        kv_a, nt_a = _batch(kv, n_tokens)
+        self._chk(self._fn.sym_pred_sparse(self.h, len(kv_a), kv_a.ctypes.data, nt_a.ctypes.data, C.byref(sparse), _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(out), _ptr(picked), stream))
+
+    def pred_begin_sparse(self, kv, n_tokens, sparse, stream=None):
+        kv_a, nt_a = _batch(kv, n_tokens)
+        self._chk(self._fn.sym_pred_begin_sparse(self.h, len(kv_a), kv_a.ctypes.data, nt_a.ctypes.data, C.byref(sparse), stream))
+        self._sparse = sparse                    # its positions are read by every layer
+
+    def pred_layer_sparse(self, layer, q, k_new, v_new, out, picked=None, stream=None):
+        self._chk(self.lib.sym_pred_layer_sparse(self.h, layer, _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(out), _ptr(picked), stream))
 
     def test_fail_staging(self, count):
         self._chk(self.lib.sym_test_fail_staging(self.h, count))

@@ -17,6 +17,7 @@
 #include "kernels.hpp"
 #include "kvfs.hpp"
 #include "sched.hpp"
+#include "sparse.hpp"
 
 using namespace symkv;
 
@@ -57,6 +58,27 @@ sym_tuning default_tuning(const sym_config* cfg) {
 }
 }  // namespace
 
+// What the sparse layers of a batch need, planned once: where the sections lie in the blob, and how its rows go through the scratch.
+struct SparsePlan {
+  bool on = false, dense = false;                  // sparse layers may run; dense ones may too
+  int32_t budget = 0, first = 0, last = 0;
+  bool turns = false;                              // a rope is given
+  RopeTable rope;
+  const int32_t* pos = nullptr;
+  int64_t off_rows = 0, off_tables = 0, off_groups = 0, off_runs = 0, off_pages = 0, off_merge = 0;   // word offsets in the blob
+  int64_t entries = 0;                             // page ids in the tables
+  int32_t n_rows = 0, n_runs = 0;
+  int32_t n_stale = 0, n_done = 0;                 // full pages without bounds: from before the batch, then those that it completes
+  int32_t splits = 1, score_stride = 0, list_stride = 0, group_rows = 1;
+  int64_t q_bytes = 0, row_bytes = 0;              // scratch: turned query rows of the batch; per row and slab
+  struct Slab {
+    int32_t row0, rows, group0, groups, most_scored;
+  };
+  int64_t slab_rows = 0;                           // rows that fit the scratch at a time
+  std::vector<Slab> slabs;
+  std::vector<sym_kv> kv;                          // the batch's files
+};
+
 // A batch planned by sym_pred_begin: where its parts lie in the device copy of the blob, until every layer has run.
 struct OpenPred {
   bool open = false;
@@ -66,6 +88,7 @@ struct OpenPred {
   int64_t partials = 0;                            // partial slots behind the blob in the workspace
   std::vector<uint8_t> done;                       // per layer: sym_pred_layer has run
   int32_t n_done = 0;
+  SparsePlan sparse;
 };
 
 struct sym_ctx {
@@ -94,6 +117,8 @@ struct sym_ctx {
   AppendPlan plan;
   GatherPlan gplan;
   SwapPlan splan;
+  uint8_t* bounds = nullptr;                       // caller's buffer for the bounds of the pages' keys (sym_bounds_attach)
+  std::vector<int32_t> words;                      // scratch: runs of an append, page ids
   std::vector<uint8_t*> host_chunks;   // pinned memory of the host slots, kHostChunk pages each
   int64_t pages_offloaded = 0, pages_restored = 0;
   BatchDesc desc;
@@ -545,8 +570,9 @@ int64_t partials_behind(const sym_ctx* c, const Scratch& ws, int64_t bound_words
   const int64_t fit = (ws.bytes - align_up(bound_words * 4, 256) - 512) / slot_bytes;
   return std::max(ws.partials, std::min<int64_t>(fit, 1 << 20));
 }
+// extra: words that the caller will put behind the blob.
 int pred_plan_locked(sym_ctx* c, int32_t n_lips, const sym_kv* kv, const int32_t* n_tokens, const Scratch& ws, bool no_alloc,
-                     PlannedBatch* pb) {
+                     PlannedBatch* pb, int64_t extra = 0) {
   const int P = c->cfg.page_tokens;
   // sizes after the append, for the checks that must precede any state change
   int64_t T = 0, entries = 0;
@@ -557,7 +583,7 @@ int pred_plan_locked(sym_ctx* c, int32_t n_lips, const sym_kv* kv, const int32_t
     T += n_tokens[b];
     entries += (f->len + n_tokens[b] + P - 1) / P;
   }
-  const int64_t bound = blob_words_bound(c, n_lips, T, entries);
+  const int64_t bound = blob_words_bound(c, n_lips, T, entries) + extra;
   if (no_alloc && bound > kStaticBlobWords) return fail(c, SYM_ENOSPC, "pred_batch_static: batch too large (descriptor beyond the static limit)");
   const int64_t partials = no_alloc ? ws.partials : partials_behind(c, ws, bound);
   pb->partials = partials;
@@ -574,9 +600,9 @@ int pred_plan_locked(sym_ctx* c, int32_t n_lips, const sym_kv* kv, const int32_t
     c->len_after[b] = f->len;
   }
   // behind the descriptor lie the copy list (3 words per LIP at most) and the slot map
-  const DescParams prm = desc_params(c, partials, bound - 3 * n_lips - T - 64, true);
+  const DescParams prm = desc_params(c, partials, bound - extra - 3 * n_lips - T - 64, true);
   // The descriptor is built straight into the pinned staging buffer; copy list and slot map follow it.
-  const int64_t tail_words = (int64_t)c->plan.cow.size() + (int64_t)c->plan.slots.size() + 4;
+  const int64_t tail_words = (int64_t)c->plan.cow.size() + (int64_t)c->plan.slots.size() + 4 + extra;
   int si = -1;
   c->desc.alloc = [&](int64_t words) -> int32_t* {
     const auto w0 = std::chrono::steady_clock::now();
@@ -634,6 +660,398 @@ int pred_batch_locked(sym_ctx* c, int32_t n_lips, const sym_kv* kv, const int32_
   c->host_ns_plan += ns(t_planned - t_begin) - pb.wait_ns;
   c->host_ns_pred += ns(t_end - t_begin) - pb.wait_ns;
   return rc;
+}
+
+// ---- rotary positions, page bounds, sparse preds ------------------------------------------------------------------------------
+
+// Makes the context's device current for a call.
+struct OnDevice {
+  int before;
+  explicit OnDevice(const sym_ctx* c) : before(c->cfg.device >= 0 && enter_device ? enter_device(c->cfg.device) : -1) {}
+  ~OnDevice() {
+    if (before >= 0) leave_device(before);
+  }
+};
+// The call's body with nothing thrown past the C boundary.
+template <typename F>
+int guarded(sym_ctx* c, F f) {
+  try {
+    return f();
+  } catch (const std::exception&) {
+    return fail(c, SYM_ENOSPC, "out of host memory");
+  }
+}
+bool aligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
+bool overlap(const void* a, int64_t na, const void* b, int64_t nb) {
+  return (uintptr_t)a < (uintptr_t)b + (uintptr_t)nb && (uintptr_t)b < (uintptr_t)a + (uintptr_t)na;
+}
+int64_t row_bytes_of(int64_t tokens, int32_t heads) { return tokens * heads * 256; }
+int64_t page_bounds_bytes(const sym_config& cfg) { return (int64_t)cfg.n_kv_heads * 512; }
+int64_t layer_bounds(const sym_ctx* c) { return c->cfg.n_pages * page_bounds_bytes(c->cfg); }
+
+// The table of a rope for this context's heads; null: rows stay as they are.
+int rope_table(sym_ctx* c, const sym_rope* r, RopeTable* t) {
+  *t = RopeTable{};
+  t->path = ROPE_NONE;
+  if (!r) return SYM_OK;
+  const int32_t D = c->cfg.head_dim, dims = r->dims == 0 ? D : r->dims;
+  if (r->layout != SYM_ROPE_HALVES && r->layout != SYM_ROPE_INTERLEAVED) return fail(c, SYM_EINVAL, "rope: unknown layout");
+  if (dims < 2 || dims > D || dims % 2) return fail(c, SYM_EINVAL, "rope: dims must be even, 2 .. head_dim");
+  const double factor = r->factor == 0.0 ? 1.0 : r->factor, mag = r->magnitude == 0.0 ? 1.0 : r->magnitude;
+  if (!(r->base > 0.0) || !std::isfinite(r->base) || !(factor > 0.0) || !std::isfinite(factor) || !std::isfinite(mag))
+    return fail(c, SYM_EINVAL, "rope: base and factor must be positive, magnitude finite");
+  if (r->original_len < 0) return fail(c, SYM_EINVAL, "rope: original_len must not be negative");
+  if (r->original_len > 0 && (!std::isfinite(r->low_turns) || !std::isfinite(r->high_turns) || !(r->high_turns > r->low_turns)))
+    return fail(c, SYM_EINVAL, "rope: high_turns must be above low_turns");
+  const double two_pi = 6.283185307179586476925286766559;
+  for (int32_t i = 0; i < dims / 2; ++i) {
+    double f = std::pow(r->base, -2.0 * i / dims) / two_pi;        // turns per position
+    if (r->original_len > 0) {
+      const double turns = (double)r->original_len * f;
+      const double keep = std::min(std::max((turns - r->low_turns) / (r->high_turns - r->low_turns), 0.0), 1.0);
+      f *= keep + (1.0 - keep) / factor;
+    } else {
+      f /= factor;
+    }
+    if (!std::isfinite(f) || f > 0.5e9) return fail(c, SYM_EINVAL, "rope: a frequency is out of range");
+    t->turns[i] = f;
+  }
+  const int32_t chunk = c->cfg.dtype == SYM_BF16 ? 8 : 4;
+  t->path = r->layout == SYM_ROPE_INTERLEAVED ? ROPE_INTERLEAVED : (dims / 2) % chunk == 0 ? ROPE_HALVES : ROPE_HALVES_ANY;
+  t->dims = dims;
+  t->mag = mag;
+  return SYM_OK;
+}
+
+// What the calls that stage lists for one run refuse: a recorded launch would be run again, on lists long overwritten.
+int refuse_capture(sym_ctx* c, hipStream_t st, const char* what) {
+  if (!stream_captures || !launch_append_rope) return fail(c, SYM_EHIP, std::string(what) + ": this build has no kernels");
+  if (stream_captures(st)) return fail(c, SYM_EINVAL, std::string(what) + ": cannot be recorded into a graph");
+  return SYM_OK;
+}
+
+// The runs of c->plan, tokens in consecutive slots of one page, as RUN_WORDS words each; the files as they are after the append.
+void append_runs(const sym_ctx* c, int32_t n_files, const sym_kv* kv, const int32_t* n_tokens, std::vector<int32_t>* out) {
+  const int32_t P = c->cfg.page_tokens;
+  out->clear();
+  int32_t t = 0;
+  for (int32_t b = 0; b < n_files; ++b) {
+    const int64_t before = c->fs->len(kv[b]) - n_tokens[b];
+    for (int32_t i = 0; i < n_tokens[b];) {
+      const int32_t s = (int32_t)((before + i) % P), n = std::min(n_tokens[b] - i, P - s);
+      out->push_back(t + i);
+      out->push_back(c->plan.slots[(size_t)(t + i)]);
+      out->push_back(n | (s + n == P ? 1 << 8 : 0));
+      out->push_back((int32_t)(before + i));
+      i += n;
+    }
+    t += n_tokens[b];
+  }
+}
+int64_t runs_of(int64_t before, int64_t n, int32_t P) { return (before + n + P - 1) / P - before / P; }
+
+// Files of a batch, their tokens and lengths: what the new calls check of them before anything changes (the append checks the rest).
+int check_batch(sym_ctx* c, int32_t n_files, const sym_kv* kv, const int32_t* n_tokens, const char* what, int64_t* tokens, int64_t* runs) {
+  *tokens = *runs = 0;
+  for (int32_t b = 0; b < n_files; ++b) {
+    const KvFile* f = c->fs->file_of(kv[b]);
+    if (!f) return fail(c, SYM_EBADF, std::string(what) + ": bad file handle");
+    if (n_tokens[b] < 1) return fail(c, SYM_EINVAL, std::string(what) + ": n_tokens must be >= 1");
+    if (f->len + n_tokens[b] > 0x7fffffff) return fail(c, SYM_ENOSPC, std::string(what) + ": file too long");
+    *tokens += n_tokens[b];
+    *runs += runs_of(f->len, n_tokens[b], c->cfg.page_tokens);
+  }
+  if (*tokens > (1 << 26)) return fail(c, SYM_ENOSPC, std::string(what) + ": too many tokens for one call");
+  return SYM_OK;
+}
+
+AppendRopeArgs append_args(const sym_ctx* c, int32_t layer, int32_t n_layers, int64_t tokens, const void* k, const void* v, const int32_t* pos) {
+  AppendRopeArgs a{};
+  a.pool = pool_of(c, layer);
+  a.page_bytes = c->page_bytes;
+  a.layer_bytes = c->layer_bytes;
+  a.layer_bounds = layer_bounds(c);
+  a.bounds = c->bounds ? c->bounds + layer * a.layer_bounds : nullptr;
+  a.k = k;
+  a.v = v;
+  a.layer_rows = row_bytes_of(tokens, c->cfg.n_kv_heads);
+  a.pos = pos;
+  a.Hq = c->cfg.n_q_heads;
+  a.Hkv = c->cfg.n_kv_heads;
+  a.n_layers = n_layers;
+  return a;
+}
+
+// Bounds of `n` pages, ids in device memory (or, at most kArgPages, on the host), in layers [layer, layer + n_layers).
+int run_bounds(sym_ctx* c, const int32_t* pages, int64_t n, bool by_args, int32_t layer, int32_t n_layers, hipStream_t st) {
+  constexpr int64_t kChunk = 1 << 20;
+  for (int64_t off = 0; off < n; off += kChunk) {
+    BoundsArgs a{pool_of(c, layer), c->page_bytes, c->layer_bytes, c->bounds + layer * layer_bounds(c), layer_bounds(c), pages + off,
+                 (int32_t)std::min(kChunk, n - off), c->cfg.n_kv_heads, n_layers, by_args ? 1 : 0};
+    Timed t(c, SYM_K_PROLOGUE, st);
+    const hipError_t e = launch_bounds(a, c->cfg.dtype, st);
+    if (e != hipSuccess) return fail_hip(c, e, "bounds launch");
+  }
+  return SYM_OK;
+}
+int batch_bounds(sym_ctx* c, const SparsePlan& sp, const int32_t* blob, int32_t layer, int32_t n, hipStream_t st) {
+  return n > 0 ? run_bounds(c, blob + sp.off_pages, n, false, layer, 1, st) : SYM_OK;
+}
+
+void open_batch(sym_ctx* c, const PlannedBatch& pb) {
+  OpenPred& o = c->pred;
+  o.open = true;
+  o.words = pb.words;
+  o.cow_off = pb.cow_off;
+  o.slots_off = pb.slots_off;
+  o.n_cow = pb.n_cow;
+  o.n_append = pb.n_append;
+  o.copies_first = c->plan.copies_first;
+  o.partials = pb.partials;
+  o.done.assign((size_t)c->n_layers, 0);
+  o.n_done = 0;
+  ++c->pred_batches;
+}
+void layer_done(sym_ctx* c, int32_t layer) {
+  OpenPred& o = c->pred;
+  o.done[layer] = 1;
+  if (++o.n_done < c->n_layers) return;
+  o.open = false;                                                     // the batch is complete
+  if (o.sparse.on)                                                    // ... and every full page of its files has bounds in every layer
+    for (sym_kv h : o.sparse.kv) c->fs->set_bounded(h, c->fs->len(h) / c->cfg.page_tokens);
+  o.sparse.on = false;
+}
+
+constexpr int64_t kMostUnits = 1 << 20;          // (row, kv head, part) workgroups of a launch
+int check_sparse(sym_ctx* c, const sym_sparse* s, SparsePlan* sp) {
+  if (s->budget < 1 || s->first < 0 || s->last < 1 || (int64_t)s->first + s->last > s->budget)
+    return fail(c, SYM_EINVAL, "sparse: budget >= first + last, first >= 0, last >= 1");
+  if (s->positions && !s->rope) return fail(c, SYM_EINVAL, "sparse: positions without a rope");
+  if (!aligned(s->positions, 4)) return fail(c, SYM_EINVAL, "sparse: positions must be 4-byte aligned");
+  if (int rc = rope_table(c, s->rope, &sp->rope)) return rc;
+  if (!c->bounds) return fail(c, SYM_EINVAL, "sparse: no buffer for page bounds is attached (sym_bounds_attach)");
+  sp->turns = s->rope != nullptr;
+  sp->pos = s->positions;
+  sp->budget = s->budget;
+  sp->first = s->first;
+  sp->last = s->last;
+  sp->dense = s->dense_layers != 0;
+  return SYM_OK;
+}
+
+// Sizes of the sparse part of a batch, from the files as they are before it: words of its sections, how it goes through the scratch of
+// `ws_bytes` bytes behind `blob_words` words.
+int size_sparse(sym_ctx* c, SparsePlan* sp, int32_t n_lips, const sym_kv* kv, const int32_t* n_tokens, int64_t tokens, int64_t runs, int64_t* words) {
+  const int64_t P = c->cfg.page_tokens, H = c->cfg.n_kv_heads;
+  int64_t entries = 0, stale = 0, done = 0, most_pages = 0, most_kept = 0;
+  for (int32_t b = 0; b < n_lips; ++b) {
+    const KvFile* f = c->fs->file_of(kv[b]);
+    const int64_t after = f->len + n_tokens[b], pages = (after + P - 1) / P;
+    entries += pages;
+    stale += f->len / P - f->bounded;
+    done += after / P - f->len / P;
+    most_pages = std::max(most_pages, pages);
+    most_kept = std::max(most_kept, std::min<int64_t>(pages, sp->budget));
+  }
+  sp->n_rows = (int32_t)tokens;
+  sp->n_runs = (int32_t)runs;
+  sp->entries = entries;
+  sp->n_stale = (int32_t)stale;
+  sp->n_done = (int32_t)done;
+  sp->kv.assign(kv, kv + n_lips);
+  sp->score_stride = most_pages > sp->budget ? (int32_t)((most_pages - sp->first - sp->last + 3) & ~3ll) : 0;
+  sp->list_stride = (int32_t)((most_kept + 3) & ~3ll);
+  // Parts of a list: enough workgroups for the chip where rows are few, each wavefront with two pages at least.
+  const int64_t units = tokens * H;
+  sp->splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(512 / std::max<int64_t>(units, 1), most_kept / 8));
+  sp->q_bytes = sp->turns ? align_up(row_bytes_of(tokens, c->cfg.n_q_heads), 256) : 0;
+  *words = sp->n_rows * (int64_t)(SPARSE_ROW_WORDS + SPARSE_GROUP_WORDS) + entries + runs * RUN_WORDS + stale + done +
+           (sp->splits > 1 ? units * MERGE_WORDS : 0) + 16;
+  return SYM_OK;
+}
+int fit_sparse(sym_ctx* c, SparsePlan* sp, int64_t ws_bytes, int64_t blob_words) {
+  const int64_t H = c->cfg.n_kv_heads;
+  const int64_t slot = sp->splits > 1 ? (int64_t)sp->splits * c->G * (2 + c->cfg.head_dim) * 4 : 0;
+  sp->row_bytes = H * ((int64_t)(sp->score_stride + sp->list_stride) * 4 + slot);
+  const int64_t room = ws_bytes - align_up(blob_words * 4, 256) - sp->q_bytes - 4 * 256;
+  sp->slab_rows = std::min({room / sp->row_bytes, kMostUnits / std::max<int64_t>(1, H * sp->splits), (int64_t)65535});
+  if (sp->slab_rows < 1 || (sp->splits > 1 && sp->slab_rows < sp->n_rows)) return fail(c, SYM_ENOSPC, "workspace too small for this sparse batch");
+  return SYM_OK;
+}
+// Writes the sections at word `at` of `blob` (after the append): rows, groups, tables, runs, pages without bounds, merge items.
+void fill_sparse(sym_ctx* c, SparsePlan* sp, int32_t n_lips, const sym_kv* kv, const int32_t* n_tokens, int32_t* blob, int64_t at) {
+  const int32_t P = c->cfg.page_tokens, H = c->cfg.n_kv_heads;
+  sp->off_rows = at;
+  sp->off_groups = sp->off_rows + (int64_t)sp->n_rows * SPARSE_ROW_WORDS;
+  sp->off_tables = sp->off_groups + (int64_t)sp->n_rows * SPARSE_GROUP_WORDS;
+  sp->off_runs = sp->off_tables + sp->entries;
+  sp->off_pages = sp->off_runs + (int64_t)sp->n_runs * RUN_WORDS;
+  sp->off_merge = sp->off_pages + sp->n_stale + sp->n_done;
+  int32_t *rows = blob + sp->off_rows, *groups = blob + sp->off_groups, *tables = blob + sp->off_tables;
+  int32_t *stale = blob + sp->off_pages, *done = stale + sp->n_stale;
+  append_runs(c, n_lips, kv, n_tokens, &c->words);
+  copy_bytes(blob + sp->off_runs, c->words.data(), c->words.size() * 4);
+  sp->slabs.clear();
+  sp->group_rows = 1;
+  int32_t row = 0, tbl = 0, n_groups = 0;
+  for (int32_t b = 0; b < n_lips; ++b) {
+    const KvFile* f = c->fs->file_of(kv[b]);
+    const int64_t before = f->len - n_tokens[b];
+    copy_bytes(tables + tbl, f->pages.data(), f->pages.size() * 4);
+    for (int64_t p = f->bounded; p < before / P; ++p) *stale++ = f->pages[(size_t)p];
+    for (int64_t p = before / P; p < f->len / P; ++p) *done++ = f->pages[(size_t)p];
+    int32_t in_group = 0;                          // rows of the group that is being filled (0: none)
+    for (int32_t i = 0; i < n_tokens[b]; ++i, ++row) {
+      const int32_t vis = (int32_t)(before + i + 1), n = (vis + P - 1) / P;
+      int32_t* r = rows + (int64_t)row * SPARSE_ROW_WORDS;
+      r[0] = tbl;
+      r[1] = vis;
+      r[2] = std::min(n, sp->budget);
+      r[3] = 0;
+      if (row % sp->slab_rows == 0) {
+        sp->slabs.push_back({row, 0, n_groups, 0, 0});
+        in_group = 0;
+      }
+      SparsePlan::Slab& slab = sp->slabs.back();
+      ++slab.rows;
+      if (n <= sp->budget) continue;               // every page is read
+      slab.most_scored = std::max(slab.most_scored, n - sp->first - sp->last);
+      if (in_group == 0 || in_group == kGroupRows) {
+        groups[2 * n_groups] = row;
+        groups[2 * n_groups + 1] = 0;
+        ++n_groups;
+        ++slab.groups;
+        in_group = 0;
+      }
+      sp->group_rows = std::max(sp->group_rows, groups[2 * n_groups - 1] = ++in_group);
+    }
+    tbl += (int32_t)f->pages.size();
+  }
+  if (sp->splits > 1)
+    for (int32_t u = 0; u < sp->n_rows * H; ++u) {
+      int32_t* m = blob + sp->off_merge + (int64_t)u * MERGE_WORDS;
+      const int32_t item[MERGE_WORDS] = {u * sp->splits, sp->splits, u / H * c->cfg.n_q_heads + u % H * c->G, 0, 0, 0, 1, 0};
+      std::memcpy(m, item, sizeof(item));
+    }
+}
+
+// One sparse layer: the rows turned and appended, then slab by slab scores, choice, attention.
+int run_sparse_layer(sym_ctx* c, const SparsePlan& sp, uint8_t* ws, int64_t words, int32_t layer, const void* q, const void* k_new, const void* v_new,
+                     float* out, int32_t* picked, hipStream_t st) {
+  const int32_t* blob = (const int32_t*)ws;
+  uint8_t* at = ws + align_up(words * 4, 256);
+  void* q_turned = at;
+  at += sp.q_bytes;
+  const int64_t H = c->cfg.n_kv_heads;
+  {
+    AppendRopeArgs a = append_args(c, layer, 1, sp.n_rows, k_new, v_new, sp.pos);
+    a.q = sp.turns ? q : nullptr;
+    a.q_out = q_turned;
+    a.runs = blob + sp.off_runs;
+    a.n_runs = sp.n_runs;
+    Timed t(c, SYM_K_PROLOGUE, st);
+    const hipError_t e = launch_append_rope(a, sp.rope, c->cfg.dtype, st);
+    if (e != hipSuccess) return fail_hip(c, e, "append launch");
+  }
+  if (int rc = batch_bounds(c, sp, blob, layer, sp.n_stale, st)) return rc;
+  SparseArgs a{};
+  a.pool = pool_of(c, layer);
+  a.page_bytes = c->page_bytes;
+  a.bounds = c->bounds + layer * layer_bounds(c);
+  a.q = sp.turns ? q_turned : q;
+  a.out = out;
+  a.picked = picked;
+  a.rows = blob + sp.off_rows;
+  a.groups = blob + sp.off_groups;
+  a.tables = blob + sp.off_tables;
+  const int64_t slab = std::min<int64_t>(sp.slab_rows, sp.n_rows);
+  a.scores = (float*)at;
+  at += align_up(slab * H * sp.score_stride * 4, 256);
+  a.lists = (int32_t*)at;
+  at += align_up(slab * H * sp.list_stride * 4, 256);
+  a.part_ml = (float*)at;
+  at += align_up(sp.splits > 1 ? slab * H * sp.splits * c->G * 2 * 4 : 0, 256);
+  a.part_acc = (float*)at;
+  a.group_rows = sp.group_rows;
+  a.Hq = c->cfg.n_q_heads;
+  a.Hkv = c->cfg.n_kv_heads;
+  a.budget = sp.budget;
+  a.first = sp.first;
+  a.last = sp.last;
+  a.score_stride = sp.score_stride;
+  a.list_stride = sp.list_stride;
+  a.splits = sp.splits;
+  a.scale_log2e = c->scale_log2e;
+  for (const SparsePlan::Slab& s : sp.slabs) {
+    a.row0 = s.row0;
+    a.n_rows = s.rows;
+    a.group0 = s.group0;
+    a.n_groups = s.groups;
+    a.most_scored = s.most_scored;
+    hipError_t e = hipSuccess;
+    {
+      Timed t(c, SYM_K_ATTN, st, false, true, 2 + (s.groups > 0));
+      if (s.groups > 0) e = launch_sparse_scores(a, c->cfg.dtype, st);
+      if (e == hipSuccess) e = launch_sparse_select(a, st);
+      if (e == hipSuccess) e = launch_sparse_attend(a, c->cfg.dtype, st);
+    }
+    if (e != hipSuccess) return fail_hip(c, e, "sparse attention launch");
+    if (sp.splits > 1) {
+      MergeArgs m{a.part_acc, a.part_ml, blob + sp.off_merge, out, (int32_t)(sp.n_rows * H), sp.splits, nullptr, 0, 0, c->cfg.n_q_heads};
+      Timed t(c, SYM_K_MERGE, st);
+      e = launch_merge(m, c->G, c->cfg.head_dim, st);
+      if (e != hipSuccess) return fail_hip(c, e, "merge launch");
+    }
+  }
+  return SYM_OK;
+}
+
+// The host half of a batch with sparse layers (lock held): plan, commit, blob to the device, batch open.
+int begin_sparse_locked(sym_ctx* c, int32_t n_lips, const sym_kv* kv, const int32_t* n_tokens, const sym_sparse* sparse, hipStream_t st) {
+  SparsePlan sp;
+  int64_t tokens, runs, extra;
+  int rc;
+  if ((rc = check_sparse(c, sparse, &sp)) || (rc = check_batch(c, n_lips, kv, n_tokens, "pred_sparse", &tokens, &runs))) return rc;
+  if (c->cfg.device < 0) return fail(c, SYM_EINVAL, "host-only context");
+  if ((rc = refuse_capture(c, st, "pred_sparse"))) return rc;
+  if ((rc = size_sparse(c, &sp, n_lips, kv, n_tokens, tokens, runs, &extra))) return rc;
+  PlannedBatch pb;
+  if (sp.dense) {
+    int64_t entries = 0;
+    for (int32_t b = 0; b < n_lips; ++b) entries += (c->fs->len(kv[b]) + n_tokens[b] + c->cfg.page_tokens - 1) / c->cfg.page_tokens;
+    if ((rc = fit_sparse(c, &sp, c->cfg.workspace_bytes, blob_words_bound(c, n_lips, tokens, entries) + extra))) return rc;
+    if ((rc = pred_plan_locked(c, n_lips, kv, n_tokens, workspace_of(c), false, &pb, extra))) return rc;
+  } else {
+    const int64_t bound = 3ll * n_lips + extra;
+    if ((rc = fit_sparse(c, &sp, c->cfg.workspace_bytes, bound)) || (rc = stage_reserve(c, bound))) return rc;
+    c->plan.clear();
+    if ((rc = c->fs->append(n_lips, kv, n_tokens, &c->plan, &c->err))) return rc;
+    if ((rc = stage_acquire(c, bound, &pb.si))) return rc;
+    pb.n_cow = (int32_t)(c->plan.cow.size() / 3);
+    copy_bytes(c->stage[pb.si], c->plan.cow.data(), c->plan.cow.size() * 4);
+    pb.words = (int64_t)c->plan.cow.size();
+  }
+  fill_sparse(c, &sp, n_lips, kv, n_tokens, c->stage[pb.si], pb.words);
+  pb.words += extra;
+  sp.on = true;
+  c->pred.sparse = std::move(sp);
+  if ((rc = launch_prologue(c, pb.si, pb.words, nullptr, 0, nullptr, 0, nullptr, nullptr, st, pb.si))) return rc;
+  open_batch(c, pb);
+  return SYM_OK;
+}
+int sparse_layer_locked(sym_ctx* c, int32_t layer, const void* q, const void* k_new, const void* v_new, float* out, int32_t* picked, hipStream_t st) {
+  OpenPred& o = c->pred;
+  uint8_t* ws = (uint8_t*)c->cfg.workspace;
+  if (o.n_cow > 0)       // the copies first: a page that the batch completes is read again for its bounds
+    if (int rc = launch_prologue(c, -1, 0, (const int32_t*)ws + o.cow_off, o.n_cow, nullptr, 0, nullptr, nullptr, st, -1, nullptr, true, layer)) return rc;
+  if (int rc = run_sparse_layer(c, o.sparse, ws, o.words, layer, q, k_new, v_new, out, picked, st)) return rc;
+  layer_done(c, layer);
+  return SYM_OK;
+}
+int check_layer_rows(sym_ctx* c, const void* q, const void* k_new, const void* v_new, const float* out, const int32_t* picked) {
+  if (!aligned(q, 16) || !aligned(k_new, 16) || !aligned(v_new, 16) || !aligned(out, 16) || !aligned(picked, 4))
+    return fail(c, SYM_EINVAL, "sparse: rows and outputs must be 16-byte aligned");
+  return SYM_OK;
 }
 
 }  // namespace
@@ -1090,18 +1508,8 @@ int sym_pred_begin(sym_ctx* c, int32_t n_lips, const sym_kv* kv, const int32_t* 
   // the whole blob (descriptor, copy list, slot map) goes to the device once; the layers read it there
   hipStream_t st = (hipStream_t)stream;
   if ((rc = launch_prologue(c, pb.si, pb.words, nullptr, 0, nullptr, 0, nullptr, nullptr, st, pb.si))) return rc;
-  OpenPred& o = c->pred;
-  o.open = true;
-  o.words = pb.words;
-  o.cow_off = pb.cow_off;
-  o.slots_off = pb.slots_off;
-  o.n_cow = pb.n_cow;
-  o.n_append = pb.n_append;
-  o.copies_first = c->plan.copies_first;
-  o.partials = pb.partials;
-  o.done.assign((size_t)c->n_layers, 0);
-  o.n_done = 0;
-  ++c->pred_batches;
+  open_batch(c, pb);
+  c->pred.sparse.on = false;
   const int64_t ns = std::chrono::duration_cast<std::chrono::nanoseconds>(std::chrono::steady_clock::now() - t_begin).count() - pb.wait_ns;
   c->host_ns_plan += ns;
   c->host_ns_pred += ns;
@@ -1115,6 +1523,7 @@ int sym_pred_layer(sym_ctx* c, int32_t layer, const void* q, const void* k_new, 
   if (!o.open) return fail(c, SYM_EINVAL, "pred_layer: no batch is open (sym_pred_begin first)");
   if (layer < 0 || layer >= c->n_layers) return fail(c, SYM_EINVAL, "pred_layer: no such layer");
   if (o.done[layer]) return fail(c, SYM_EBUSY, "pred_layer: this layer of the batch has already run");
+  if (o.sparse.on && !o.sparse.dense) return fail(c, SYM_EINVAL, "pred_layer: the batch was begun for sparse layers only (dense_layers)");
   const auto t_begin = std::chrono::steady_clock::now();
   hipStream_t st = (hipStream_t)stream;
   const Scratch ws{(uint8_t*)c->cfg.workspace, c->cfg.workspace_bytes, o.partials};
@@ -1129,8 +1538,8 @@ int sym_pred_layer(sym_ctx* c, int32_t layer, const void* q, const void* k_new, 
     if ((rc = launch_prologue(c, -1, 0, cow, n_cow, slots, o.n_append, k_new, v_new, st, -1, nullptr, true, layer))) return rc;
   rc = launch_attention(c, ws, o.words, q, out, st, true, k_new, v_new, layer);
   if (rc) return rc;
-  o.done[layer] = 1;
-  if (++o.n_done == c->n_layers) o.open = false;                      // the batch is complete
+  if (o.sparse.on && (rc = batch_bounds(c, o.sparse, (const int32_t*)ws.base, layer, o.sparse.n_stale + o.sparse.n_done, st))) return rc;
+  layer_done(c, layer);
   c->host_ns_pred += std::chrono::duration_cast<std::chrono::nanoseconds>(std::chrono::steady_clock::now() - t_begin).count();
   return SYM_OK;
 }
@@ -1139,7 +1548,235 @@ int sym_pred_end(sym_ctx* c) {
   if (!c) return SYM_EINVAL;
   std::lock_guard<std::mutex> lk(c->mu);
   c->pred.open = false;
+  c->pred.sparse.on = false;
   return SYM_OK;
+}
+
+int64_t sym_bounds_bytes(const sym_config* cfg) {
+  if (!shape_ok(cfg) || cfg->n_pages < 1) return 0;
+  return std::max(1, cfg->n_layers) * cfg->n_pages * page_bounds_bytes(*cfg);
+}
+
+int sym_bounds_attach(sym_ctx* c, void* bounds, int64_t bytes) {
+  if (!c) return SYM_EINVAL;
+  std::lock_guard<std::mutex> lk(c->mu);
+  if (int busy = refuse_if_open(c, "bounds_attach")) return busy;
+  if (bounds && !aligned(bounds, 256)) return fail(c, SYM_EINVAL, "bounds_attach: the buffer must be 256-byte aligned");
+  if (bounds && bytes < c->n_layers * layer_bounds(c)) return fail(c, SYM_ENOSPC, "bounds_attach: buffer too small (sym_bounds_bytes)");
+  c->bounds = (uint8_t*)bounds;
+  c->fs->clear_bounded();
+  return SYM_OK;
+}
+
+int64_t sym_kv_bounded(sym_ctx* c, sym_kv kv) {
+  if (!c) return SYM_EINVAL;
+  std::lock_guard<std::mutex> lk(c->mu);
+  const KvFile* f = c->fs->file_of(kv);
+  return f ? f->bounded : (int64_t)fail(c, SYM_EBADF, "kv_bounded: bad handle");
+}
+
+int sym_kv_bounds(sym_ctx* c, int32_t n, const sym_kv* kv, void* stream) {
+  if (!c || n < 0 || (n > 0 && !kv)) return SYM_EINVAL;
+  std::lock_guard<std::mutex> lk(c->mu);
+  return guarded(c, [&]() -> int {
+    if (int busy = refuse_if_open(c, "kv_bounds")) return busy;
+    if (!c->bounds) return fail(c, SYM_EINVAL, "kv_bounds: no buffer is attached (sym_bounds_attach)");
+    const int32_t P = c->cfg.page_tokens;
+    int64_t pages = 0;
+    for (int32_t b = 0; b < n; ++b) {
+      const KvFile* f = c->fs->file_of(kv[b]);
+      if (!f) return fail(c, SYM_EBADF, "kv_bounds: bad file handle");
+      if (f->waiting) return fail(c, SYM_EBUSY, "kv_bounds: file is offloaded");
+      pages += f->len / P;
+    }
+    int rc;
+    hipStream_t st = (hipStream_t)stream;
+    if (c->cfg.device >= 0) {
+      if ((rc = refuse_capture(c, st, "kv_bounds"))) return rc;
+      const OnDevice on(c);
+      if (pages <= kArgPages) {
+        c->words.clear();
+        for (int32_t b = 0; b < n; ++b) {
+          const KvFile* f = c->fs->file_of(kv[b]);
+          c->words.insert(c->words.end(), f->pages.begin(), f->pages.begin() + f->len / P);
+        }
+        if (pages > 0 && (rc = run_bounds(c, c->words.data(), pages, true, 0, c->n_layers, st))) return rc;
+      } else {
+        // the ids go to the workspace, as many at a time as it holds
+        const int64_t room = std::min<int64_t>(pages, c->cfg.workspace_bytes / 4 - 16);
+        if ((rc = stage_reserve(c, room + 4))) return rc;
+        int si = -1;
+        int64_t have = 0;
+        auto flush = [&]() -> int {
+          if (have == 0) return SYM_OK;
+          int r = launch_prologue(c, si, have, nullptr, 0, nullptr, 0, nullptr, nullptr, st, si);
+          if (!r) r = run_bounds(c, (const int32_t*)c->cfg.workspace, have, false, 0, c->n_layers, st);
+          have = 0;
+          return r;
+        };
+        for (int32_t b = 0; b < n; ++b) {
+          const KvFile* f = c->fs->file_of(kv[b]);
+          for (int64_t p = 0, full = f->len / P; p < full;) {
+            if (have == 0 && (rc = stage_acquire(c, room, &si))) return rc;
+            const int64_t m = std::min(full - p, room - have);
+            std::memcpy(c->stage[si] + have, f->pages.data() + p, (size_t)m * 4);
+            p += m;
+            have += m;
+            if (have == room && (rc = flush())) return rc;
+          }
+        }
+        if ((rc = flush())) return rc;
+      }
+    }
+    for (int32_t b = 0; b < n; ++b) c->fs->set_bounded(kv[b], c->fs->len(kv[b]) / P);
+    return SYM_OK;
+  });
+}
+
+int sym_rope_rows(sym_ctx* c, const sym_rope* rope, int32_t n, const int32_t* positions, const void* q, void* q_out, const void* k, void* k_out, void* stream) {
+  if (!c || n < 0) return SYM_EINVAL;
+  std::lock_guard<std::mutex> lk(c->mu);
+  return guarded(c, [&]() -> int {
+    if (!rope) return fail(c, SYM_EINVAL, "rope_rows: no rope");
+    RopeTable t;
+    if (int rc = rope_table(c, rope, &t)) return rc;
+    if (!positions && n > 0) return fail(c, SYM_EINVAL, "rope_rows: no positions");
+    if ((q == nullptr) != (q_out == nullptr) || (k == nullptr) != (k_out == nullptr)) return fail(c, SYM_EINVAL, "rope_rows: rows without an output, or the other way round");
+    if (!aligned(q, 16) || !aligned(q_out, 16) || !aligned(k, 16) || !aligned(k_out, 16) || !aligned(positions, 4))
+      return fail(c, SYM_EINVAL, "rope_rows: rows must be 16-byte aligned, positions 4-byte");
+    const int64_t nq = q ? row_bytes_of(n, c->cfg.n_q_heads) : 0, nk = k ? row_bytes_of(n, c->cfg.n_kv_heads) : 0;
+    if ((q != q_out && overlap(q, nq, q_out, nq)) || (k != k_out && overlap(k, nk, k_out, nk)) || overlap(q_out, nq, k, nk) || overlap(k_out, nk, q, nq) ||
+        overlap(q_out, nq, k_out, nk) || overlap(positions, 4ll * n, q_out, nq) || overlap(positions, 4ll * n, k_out, nk))
+      return fail(c, SYM_EINVAL, "rope_rows: an output overlaps other rows (it may be its own input)");
+    if (c->cfg.device < 0) return fail(c, SYM_EINVAL, "host-only context");
+    if (n == 0 || (!q && !k)) return SYM_OK;
+    if (!launch_rope_rows) return fail(c, SYM_EHIP, "rope_rows: this build has no kernels");
+    const OnDevice on(c);
+    hipStream_t st = (hipStream_t)stream;
+    for (int64_t t0 = 0; t0 < n; t0 += kMostRopeRows) {
+      const int64_t oq = row_bytes_of(t0, c->cfg.n_q_heads), ok = row_bytes_of(t0, c->cfg.n_kv_heads);
+      RopeRowsArgs a{};
+      if (q) {
+        a.q = (const uint8_t*)q + oq;
+        a.q_out = (uint8_t*)q_out + oq;
+      }
+      if (k) {
+        a.k = (const uint8_t*)k + ok;
+        a.k_out = (uint8_t*)k_out + ok;
+      }
+      a.pos = positions + t0;
+      a.n = (int32_t)std::min<int64_t>(kMostRopeRows, n - t0);
+      a.Hq = c->cfg.n_q_heads;
+      a.Hkv = c->cfg.n_kv_heads;
+      Timed timed(c, SYM_K_PROLOGUE, st, false, !stream_captures(st));      // (events of a recorded stream could not be read)
+      const hipError_t e = launch_rope_rows(a, t, c->cfg.dtype, st);
+      if (e != hipSuccess) return fail_hip(c, e, "rope launch");
+    }
+    return SYM_OK;
+  });
+}
+
+int sym_kv_append_rope(sym_ctx* c, int32_t n_files, const sym_kv* kv, const int32_t* n_tokens, const sym_rope* rope, const int32_t* positions,
+                       const void* k, const void* v, void* stream) {
+  if (!c || n_files < 0) return SYM_EINVAL;
+  if (n_files == 0) return SYM_OK;
+  if (!kv || !n_tokens || !k || !v) return SYM_EINVAL;
+  std::lock_guard<std::mutex> lk(c->mu);
+  return guarded(c, [&]() -> int {
+    int rc;
+    if ((rc = refuse_if_open(c, "kv_append_rope"))) return rc;
+    RopeTable t;
+    if ((rc = rope_table(c, rope, &t))) return rc;
+    if (positions && !rope) return fail(c, SYM_EINVAL, "kv_append_rope: positions without a rope");
+    if (!aligned(k, 16) || !aligned(v, 16) || !aligned(positions, 4)) return fail(c, SYM_EINVAL, "kv_append_rope: rows must be 16-byte aligned, positions 4-byte");
+    int64_t tokens, runs;
+    if ((rc = check_batch(c, n_files, kv, n_tokens, "kv_append_rope", &tokens, &runs))) return rc;
+    if (c->cfg.device < 0) return fail(c, SYM_EINVAL, "host-only context");
+    hipStream_t st = (hipStream_t)stream;
+    if ((rc = refuse_capture(c, st, "kv_append_rope"))) return rc;
+    const OnDevice on(c);
+    if ((rc = stage_reserve(c, 3ll * n_files + runs * RUN_WORDS))) return rc;      // before any state change
+    c->words.reserve((size_t)runs * RUN_WORDS);
+    c->plan.clear();
+    if ((rc = c->fs->append(n_files, kv, n_tokens, &c->plan, &c->err))) return rc;
+    append_runs(c, n_files, kv, n_tokens, &c->words);
+    const int32_t P = c->cfg.page_tokens, n_cow = (int32_t)(c->plan.cow.size() / 3);
+    const bool by_args = runs <= kArgRuns, staged = n_cow > 0 || !by_args;
+    int si = -1;
+    if (staged) {
+      if ((rc = stage_acquire(c, (int64_t)(c->plan.cow.size() + c->words.size()), &si))) return rc;
+      copy_bytes(c->stage[si], c->plan.cow.data(), c->plan.cow.size() * 4);
+      copy_bytes(c->stage[si] + c->plan.cow.size(), c->words.data(), c->words.size() * 4);
+    }
+    // copies first: they fill slots of a page that the append may complete and then reads for its bounds
+    for (int32_t l = 0; l < c->n_layers && n_cow > 0; ++l)
+      if ((rc = launch_prologue(c, si, 0, c->stage[si], n_cow, nullptr, 0, nullptr, nullptr, st, by_args && l == c->n_layers - 1 ? si : -1, nullptr, true, l))) return rc;
+    AppendRopeArgs a = append_args(c, 0, c->n_layers, tokens, k, v, positions);
+    a.by_args = by_args ? 1 : 0;
+    a.runs = by_args ? c->words.data() : c->stage[si] + c->plan.cow.size();
+    a.n_runs = (int32_t)runs;
+    const StageDone done(c, by_args ? -1 : si);
+    a.done = done.event();
+    {
+      Timed timed(c, SYM_K_PROLOGUE, st);
+      const hipError_t e = launch_append_rope(a, t, c->cfg.dtype, st);
+      if (e != hipSuccess) return fail_hip(c, e, "append launch");
+    }
+    if ((rc = done.launched(st))) return rc;
+    for (int32_t b = 0; c->bounds && b < n_files; ++b) {       // pages completed now have bounds: whole again where none was missing
+      const KvFile* f = c->fs->file_of(kv[b]);
+      if (f->bounded == (f->len - n_tokens[b]) / P) c->fs->set_bounded(kv[b], f->len / P);
+    }
+    return SYM_OK;
+  });
+}
+
+int sym_pred_begin_sparse(sym_ctx* c, int32_t n_lips, const sym_kv* kv, const int32_t* n_tokens, const sym_sparse* sparse, void* stream) {
+  if (!c || n_lips < 1 || !kv || !n_tokens || !sparse) return SYM_EINVAL;
+  std::lock_guard<std::mutex> lk(c->mu);
+  return guarded(c, [&]() -> int {
+    if (int busy = refuse_if_open(c, "pred_begin_sparse")) return busy;
+    const OnDevice on(c);
+    return begin_sparse_locked(c, n_lips, kv, n_tokens, sparse, (hipStream_t)stream);
+  });
+}
+
+int sym_pred_layer_sparse(sym_ctx* c, int32_t layer, const void* q, const void* k_new, const void* v_new, float* out, int32_t* picked, void* stream) {
+  if (!c || !q || !k_new || !v_new || !out) return SYM_EINVAL;
+  std::lock_guard<std::mutex> lk(c->mu);
+  return guarded(c, [&]() -> int {
+    OpenPred& o = c->pred;
+    if (!o.open || !o.sparse.on) return fail(c, SYM_EINVAL, "pred_layer_sparse: no batch with sparse layers is open (sym_pred_begin_sparse first)");
+    if (layer < 0 || layer >= c->n_layers) return fail(c, SYM_EINVAL, "pred_layer_sparse: no such layer");
+    if (o.done[layer]) return fail(c, SYM_EBUSY, "pred_layer_sparse: this layer of the batch has already run");
+    hipStream_t st = (hipStream_t)stream;
+    int rc;
+    if ((rc = check_layer_rows(c, q, k_new, v_new, out, picked)) || (rc = refuse_capture(c, st, "pred_layer_sparse"))) return rc;
+    const OnDevice on(c);
+    return sparse_layer_locked(c, layer, q, k_new, v_new, out, picked, st);
+  });
+}
+
+int sym_pred_sparse(sym_ctx* c, int32_t n_lips, const sym_kv* kv, const int32_t* n_tokens, const sym_sparse* sparse, const void* q, const void* k_new,
+                    const void* v_new, float* out, int32_t* picked, void* stream) {
+  if (!c || n_lips < 0) return SYM_EINVAL;
+  if (n_lips == 0) return SYM_OK;
+  if (!kv || !n_tokens || !sparse || !q || !k_new || !v_new || !out) return SYM_EINVAL;
+  std::lock_guard<std::mutex> lk(c->mu);
+  return guarded(c, [&]() -> int {
+    if (c->n_layers != 1) return fail(c, SYM_EINVAL, "pred_sparse: a context with several layers runs its batches with sym_pred_begin_sparse / sym_pred_layer_sparse");
+    if (int busy = refuse_if_open(c, "pred_sparse")) return busy;
+    hipStream_t st = (hipStream_t)stream;
+    int rc;
+    if ((rc = check_layer_rows(c, q, k_new, v_new, out, picked))) return rc;
+    const OnDevice on(c);
+    sym_sparse only = *sparse;
+    only.dense_layers = 0;
+    if ((rc = begin_sparse_locked(c, n_lips, kv, n_tokens, &only, st))) return rc;
+    rc = sparse_layer_locked(c, 0, q, k_new, v_new, out, picked, st);
+    if (rc) c->pred.open = c->pred.sparse.on = false;
+    return rc;
+  });
 }
 
 int sym_test_fail_staging(sym_ctx* c, int32_t count) {

@@ -88,6 +88,7 @@ int32_t Kvfs::new_file() {
   f.named = false;
   f.alive = true;
   f.waiting = false;
+  f.bounded = 0;
   return id;
 }
 
@@ -144,6 +145,7 @@ int32_t Kvfs::fork(int32_t parent) {
   const KvFile& par = files_[pid];
   child.pages = par.pages;
   child.len = par.len;
+  child.bounded = par.bounded;
   for (int32_t p : child.pages) ++refcount_[p];
   return new_handle(id);
 }
@@ -177,7 +179,18 @@ int Kvfs::truncate(int32_t h, int64_t new_len) {
   if (new_len < 0 || new_len > f.len) return SYM_EINVAL;
   release_entries(handle_file_[h], (size_t)((new_len + P_ - 1) / P_));
   f.len = new_len;
+  f.bounded = std::min(f.bounded, new_len / P_);
   return SYM_OK;
+}
+
+void Kvfs::set_bounded(int32_t h, int64_t pages) {
+  if (!file_of(h)) return;
+  KvFile& f = files_[handle_file_[h]];
+  f.bounded = std::min(pages, f.len / P_);
+}
+
+void Kvfs::clear_bounded() {
+  for (KvFile& f : files_) f.bounded = 0;
 }
 
 void Kvfs::begin_marks() {
@@ -433,7 +446,10 @@ int Kvfs::offload(int32_t n, const int32_t* handles, SwapPlan* plan, std::string
       } else {
         s = n_slots_++;
       }
-      for (const auto& r : w) files_[r.first].pages[r.second] = -(s + 1);
+      for (const auto& r : w) {
+        files_[r.first].pages[r.second] = -(s + 1);
+        files_[r.first].bounded = std::min<int64_t>(files_[r.first].bounded, r.second);      // it comes back as another page
+      }
       host_refs_[s] = std::move(w);
       waiters_.erase(p);
       refcount_[p] = 0;

@@ -18,6 +18,9 @@ struct KvFile {
   int64_t len = 0;
   std::vector<int32_t> pages;      // page ids; -(slot + 1) for a page that is on the host
   bool waiting = false;            // offloaded: its thread waits for I/O (paper section 4.3)
+  // Leading pages whose key bounds are in the attached buffer (all of them full).  What a file sees of its pages never changes
+  // under it (a shared page is copied before it is appended to), so only calls that shorten the file or move its pages lower this.
+  int64_t bounded = 0;
   std::vector<int32_t> handles;
   std::string name;
   bool named = false;
@@ -126,6 +129,9 @@ class Kvfs {
   int64_t len(int32_t h) const;
   int truncate(int32_t h, int64_t new_len);   // drop tokens from new_len on; frees pages no longer needed
   const KvFile* file_of(int32_t h) const;
+  // The file's first `pages` pages have bounds (at most its full pages); nobody has any: another buffer was attached.
+  void set_bounded(int32_t h, int64_t pages);
+  void clear_bounded();
   // Whether a list of handles names a file twice: begin_marks(), then mark() of each (valid) handle says if its file is new.
   void begin_marks();
   bool mark(int32_t h);

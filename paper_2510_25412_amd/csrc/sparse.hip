@@ -1,0 +1,1031 @@
+// HIP kernels (gfx950 / CDNA4) of what comes before and beside dense attention on long files: rotary positions of query and key
+// rows, appends that turn the keys on their way into the pages, bounds of the pages' keys, the choice of pages by those bounds
+// and attention over the chosen pages.
+#include <hip/hip_runtime.h>
+#include <hip/hip_ext.h>
+
+#include <algorithm>
+#include <cstddef>
+#include <cstdint>
+
+#include "device.hpp"
+#include "sparse.hpp"
+
+namespace symkv {
+
+namespace {
+
+#define SYM_AS4 const __attribute__((address_space(4)))
+
+// Storage of two elements in one or two words.
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {      // to nearest even, as every conversion to the storage type
+  const bf16x2_t v = {(__bf16)a, (__bf16)b};
+  return __builtin_bit_cast(uint32_t, v);
+}
+// The rounding to 32 bits on the way to 16, which the compiler would otherwise leave out (it rounds 64 bits to bf16 in one go, in a dozen
+// instructions): a caller who computes a rotation with elementwise operations gets these bits.
+__device__ __forceinline__ float round_f32(double x) {
+  float f = (float)x;
+  asm("" : "+v"(f));
+  return f;
+}
+template <typename E>
+__device__ __forceinline__ u32x4_t pack_chunk(const float* y) {
+  if constexpr (E::kDimsPerChunk == 8) return u32x4_t{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7])};
+  else return u32x4_t{as_u32(y[0]), as_u32(y[1]), as_u32(y[2]), as_u32(y[3])};
+}
+
+// ---------------------------------------------------------------------------------------
+// Rotary positions.  Pair (x1, x2) of a row at position p turns by the angle 2 pi p t, t turns per position:
+//   y1 = m (x1 cos - x2 sin),  y2 = m (x2 cos + x1 sin).
+// In 64 bits: p t loses its fraction in 32 bits at far positions, and a key that is rounded to its neighbour in the storage type
+// (it takes an error of 2^-25 in a cosine) shows in the outputs of attention as 1e-5.  The angle is reduced to p t - round(p t) turns, so that
+// sincospi's argument is exact.  A workgroup computes the angles of its tokens once, into LDS, for all heads; a thread then keeps
+// those of its two 16-byte chunks in registers and walks the token's rows with them.
+// ---------------------------------------------------------------------------------------
+constexpr int kPairs = 64;                       // pairs of a head at most
+constexpr int kRunTokens = kP;                   // most tokens of a workgroup
+
+__device__ __forceinline__ double2 angle_of(SYM_AS4 RopeTable* r, int pos, int i) {
+  double x = (double)pos * r->turns[i], s, c;
+  x -= rint(x);
+  sincospi(2.0 * x, &s, &c);
+  return make_double2(r->mag * c, r->mag * s);
+}
+
+struct RowAt {
+  const uint8_t* src;
+  uint8_t* dst;
+  int half;                                      // bytes from the first to the second 128-byte half of the destination
+  bool turns;
+};
+
+// Rows of `ntok` tokens, `rpt` of each, 2^lg of the workgroup's 256 threads to a token: row_at(token, row) says where from and where to.
+// Eight threads to a row, two chunks each, so that a thread holds both elements of its pairs (a row may be turned in place).
+// angles() fills cs and ends with a barrier; the first U rows of every thread are under way while it runs.
+template <typename E, int PATH, int U, typename R, typename A>
+__device__ __forceinline__ void turn_rows(const R& row_at, const A& angles, const int rpt, const int ntok, const int lg, const int dims,
+                                          const double2 (*cs)[kPairs], uint8_t (*stage)[kRowBytes]) {
+  constexpr int C = E::kDimsPerChunk;
+  const int tid = threadIdx.x, j = tid & 7;
+  const int tok = min(tid >> lg, ntok - 1), rl = (tid & ((1 << lg) - 1)) >> 3, nrl = 1 << (lg - 3);
+  const bool mine = (tid >> lg) < ntok;
+  const int hr = dims / 2 / C;                   // HALVES: chunks of the first half of what turns
+  int c0 = j, c1 = j + 8;
+  bool lane_turns = PATH != ROPE_NONE;
+  if constexpr (PATH == ROPE_HALVES) {
+    lane_turns = j < hr;
+    c0 = lane_turns ? j : 2 * j;                 // the rest of the row, two chunks in a row: 2 hr + 2 (j - hr)
+    c1 = lane_turns ? j + hr : c0 + 1;
+  }
+  u32x4_t x[U][2];
+  auto request = [&](int row0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {                // past the end the last row is read again and not stored
+      const RowAt at = row_at(tok, min(row0 + u * nrl, rpt - 1));
+      x[u][0] = *(const u32x4_t*)(at.src + c0 * 16);
+      x[u][1] = *(const u32x4_t*)(at.src + c1 * 16);
+    }
+  };
+  request(rl);
+  angles();
+  double c[C], s[C];
+  if constexpr (PATH == ROPE_HALVES || PATH == ROPE_INTERLEAVED) {
+#pragma unroll
+    for (int e = 0; e < C; ++e) {
+      const int i = PATH == ROPE_HALVES ? (lane_turns ? j * C + e : 0) : e < C / 2 ? j * (C / 2) + e : (j + 8) * (C / 2) + e - C / 2;
+      const double2 t = cs[tok][i];
+      c[e] = t.x;
+      s[e] = t.y;
+    }
+  }
+  for (int base = 0;; ) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int row = base + u * nrl + rl;
+      const RowAt at = row_at(tok, min(row, rpt - 1));
+      u32x4_t y[2] = {x[u][0], x[u][1]};
+      if constexpr (PATH == ROPE_HALVES) {
+        if (lane_turns && at.turns) {
+          float a[C], b[C], ya[C], yb[C];
+          E::unpack(__builtin_bit_cast(uint4, x[u][0]), a);
+          E::unpack(__builtin_bit_cast(uint4, x[u][1]), b);
+#pragma unroll
+          for (int e = 0; e < C; ++e) {
+            ya[e] = round_f32((double)a[e] * c[e] - (double)b[e] * s[e]);
+            yb[e] = round_f32((double)b[e] * c[e] + (double)a[e] * s[e]);
+          }
+          y[0] = pack_chunk<E>(ya);
+          y[1] = pack_chunk<E>(yb);
+        }
+      } else if constexpr (PATH == ROPE_INTERLEAVED) {
+        if (at.turns) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            float a[C], ya[C];
+            E::unpack(__builtin_bit_cast(uint4, x[u][h]), a);
+#pragma unroll
+            for (int p = 0; p < C / 2; ++p) {
+              const double ce = c[h * (C / 2) + p], se = s[h * (C / 2) + p];
+              ya[2 * p] = round_f32((double)a[2 * p] * ce - (double)a[2 * p + 1] * se);
+              ya[2 * p + 1] = round_f32((double)a[2 * p + 1] * ce + (double)a[2 * p] * se);
+            }
+            const u32x4_t t = pack_chunk<E>(ya);
+#pragma unroll
+            for (int w = 0; w < 4; ++w)          // a word holds one pair (bf16) or half of one
+              if (((h ? c1 : c0) * C + w * (C / 4)) < dims) y[h][w] = t[w];
+          }
+        }
+      } else if constexpr (PATH == ROPE_HALVES_ANY) {
+        // the other element of a pair lies anywhere in the row: through LDS
+        __syncthreads();
+        *(u32x4_t*)(stage[tid >> 3] + c0 * 16) = x[u][0];
+        *(u32x4_t*)(stage[tid >> 3] + c1 * 16) = x[u][1];
+        __syncthreads();
+        if (at.turns) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int d0 = (h ? c1 : c0) * C;
+            float a[C], ya[C];
+            E::unpack(__builtin_bit_cast(uint4, x[u][h]), a);
+#pragma unroll
+            for (int e = 0; e < C; ++e) {
+              const int d = d0 + e, i = d < dims / 2 ? d : d - dims / 2;
+              const bool in = d < dims;
+              const int other = in ? (d < dims / 2 ? d + dims / 2 : i) : d;
+              float o;
+              if constexpr (C == 8) o = as_f32((uint32_t)((const uint16_t*)stage[tid >> 3])[other] << 16);
+              else o = ((const float*)stage[tid >> 3])[other];
+              const double2 t = cs[tok][in ? i : 0];
+              ya[e] = in ? round_f32((double)a[e] * t.x + (d < dims / 2 ? -(double)o : (double)o) * t.y) : a[e];
+            }
+            const u32x4_t t = pack_chunk<E>(ya);
+            if (d0 < dims) y[h] = t;
+          }
+        }
+      }
+      if (mine && row < rpt) {
+        *(u32x4_t*)(at.dst + (c0 >> 3) * at.half + (c0 & 7) * 16) = y[0];
+        *(u32x4_t*)(at.dst + (c1 >> 3) * at.half + (c1 & 7) * 16) = y[1];
+      }
+    }
+    base += U * nrl;
+    if (base >= rpt) break;
+    request(base + rl);
+  }
+}
+
+// Angles of `n` tokens, at positions pos[..] or from pos0 on, into cs.
+template <int PATH>
+__device__ __forceinline__ void fill_angles(SYM_AS4 RopeTable* r, const int32_t* pos, const int pos0, const int n, double2 (*cs)[kPairs]) {
+  if constexpr (PATH != ROPE_NONE) {
+    const int pairs = r->dims / 2;
+    for (int i = threadIdx.x; i < n * kPairs; i += 256)
+      if (i % kPairs < pairs) cs[i / kPairs][i % kPairs] = angle_of(r, pos ? pos[i / kPairs] : pos0 + i / kPairs, i % kPairs);
+  }
+  __syncthreads();
+}
+
+// Query and key rows of a batch, turned on their own.  Bound: HBM, read + write.
+struct RopeRowsKernelArgs {
+  RopeRowsArgs a;
+  RopeTable r;
+};
+template <typename E, int PATH>
+__global__ __launch_bounds__(256) void rope_rows_kernel(RopeRowsKernelArgs) {
+  __shared__ double2 cs[4][kPairs];
+  __shared__ __align__(16) uint8_t stage[PATH == ROPE_HALVES_ANY ? 32 : 1][kRowBytes];
+  // the arguments where they lie: named as a parameter and indexed by the thread, the table would be copied to scratch
+  auto ka = (SYM_AS4 RopeRowsKernelArgs*)__builtin_amdgcn_kernarg_segment_ptr();
+  const int per = ka->a.tokens, t0 = blockIdx.x * per, n = min(per, ka->a.n - t0);
+  const int hq = ka->a.q ? ka->a.Hq : 0, hk = ka->a.k ? ka->a.Hkv : 0;
+  const uint8_t* q = (const uint8_t*)ka->a.q + (int64_t)t0 * hq * kRowBytes;
+  const uint8_t* k = (const uint8_t*)ka->a.k + (int64_t)t0 * hk * kRowBytes;
+  uint8_t* qo = (uint8_t*)ka->a.q_out + (int64_t)t0 * hq * kRowBytes;
+  uint8_t* ko = (uint8_t*)ka->a.k_out + (int64_t)t0 * hk * kRowBytes;
+  const int32_t* pos = ka->a.pos + t0;
+  turn_rows<E, PATH, 4>(
+      [&](int tok, int row) __attribute__((always_inline)) {
+        const bool is_q = row < hq;
+        const int64_t off = (int64_t)(is_q ? tok * hq + row : tok * hk + row - hq) * kRowBytes;
+        return RowAt{(is_q ? q : k) + off, (is_q ? qo : ko) + off, kHalfBytes, true};
+      },
+      [&]() __attribute__((always_inline)) { fill_angles<PATH>(&ka->r, pos, 0, n, cs); }, hq + hk, n, per == 1 ? 8 : 6, ka->r.dims, cs, stage);
+}
+
+// Bounds of one (page, kv head): elementwise minimum and maximum of its 16 keys, by one wavefront.  Lane (r, j) reads chunk j of
+// both halves of tokens r and 8 + r; the eight lanes of a chunk are combined by halving exchanges over the list [lo, -hi]
+// (the minimum of -x is -maximum), which leave lane r with entries r V/8 .. of it.  A NaN makes both bounds of its element NaN.
+__device__ __forceinline__ float least(float a, float b) { return __builtin_elementwise_minimum(a, b); }
+template <typename E>
+__device__ __forceinline__ void page_bounds(const uint8_t* slab, uint8_t* out) {
+  constexpr int C = E::kDimsPerChunk, V = 4 * C;
+  const int lane = threadIdx.x & 63, r = lane >> 3, j = lane & 7;
+  uint4 k[4];
+#pragma unroll
+  for (int x = 0; x < 4; ++x) k[x] = *(const uint4*)(slab + x * 1024 + lane * 16);
+  float v[V];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    float a[C], b[C];
+    E::unpack(k[2 * h], a);
+    E::unpack(k[2 * h + 1], b);
+#pragma unroll
+    for (int e = 0; e < C; ++e) {
+      v[h * C + e] = least(a[e], b[e]);
+      v[V / 2 + h * C + e] = least(-a[e], -b[e]);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < V / 2; ++i) {
+    const auto sw = __builtin_amdgcn_permlane32_swap(as_u32(v[i]), as_u32(v[i + V / 2]), false, false);
+    v[i] = least(as_f32(sw[0]), as_f32(sw[1]));
+  }
+#pragma unroll
+  for (int i = 0; i < V / 4; ++i) {
+    const auto sw = __builtin_amdgcn_permlane16_swap(as_u32(v[i]), as_u32(v[i + V / 4]), false, false);
+    v[i] = least(as_f32(sw[0]), as_f32(sw[1]));
+  }
+  const bool b3 = (lane & 8) != 0;
+#pragma unroll
+  for (int i = 0; i < V / 8; ++i) {
+    const float keep = b3 ? v[i + V / 8] : v[i], send = b3 ? v[i] : v[i + V / 8];
+    v[i] = least(keep, row_xor8(send));
+  }
+  const bool top = r >= 4;
+  const int at = (r & 3) * (V / 8);              // entry of lo (or hi): dim (at / C) 8 C + j C + at % C
+#pragma unroll
+  for (int i = 0; i < V / 8; ++i) v[i] = top ? -v[i] : v[i];
+  uint2 w;
+  if constexpr (C == 8) w = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+  else w = make_uint2(as_u32(v[0]), as_u32(v[1]));
+  *(uint2*)(out + (top ? kRowBytes : 0) + (at / C) * kHalfBytes + j * 16 + (at % C) * (16 / C)) = w;
+}
+
+// ---------------------------------------------------------------------------------------
+// Append with the keys turned on the way.  A workgroup takes a run: the new tokens of a file that go to consecutive slots of one page,
+// one layer.  Few runs travel with the kernel's arguments, so that no request over the host link stands before the first load.  When the
+// run completes its page, the workgroup writes the page's bounds behind its own stores.  Bound: HBM, read + write; few tokens: the launch.
+// ---------------------------------------------------------------------------------------
+struct ArgRuns {
+  int32_t w[kArgRuns * RUN_WORDS];
+};
+struct AppendKernelArgs {
+  AppendRopeArgs a;
+  RopeTable r;
+};
+struct AppendRunsKernelArgs {
+  AppendKernelArgs k;
+  ArgRuns runs;
+};
+template <typename E, int PATH>
+__device__ __forceinline__ void append_run(SYM_AS4 AppendKernelArgs* ka, const int t0, const int slot, const int nf, const int pos0, double2 (*cs)[kPairs], uint8_t (*stage)[kRowBytes]) {
+  const int n = nf & 0xff, Hkv = ka->a.Hkv, Hq = ka->a.q ? ka->a.Hq : 0, layer = blockIdx.y;
+  uint8_t* page = ka->a.pool + layer * ka->a.layer_bytes + (int64_t)(slot / kP) * ka->a.page_bytes;
+  const int ts = slot % kP;
+  const uint8_t* k = (const uint8_t*)ka->a.k + layer * ka->a.layer_rows + (int64_t)t0 * Hkv * kRowBytes;
+  const uint8_t* v = (const uint8_t*)ka->a.v + layer * ka->a.layer_rows + (int64_t)t0 * Hkv * kRowBytes;
+  const uint8_t* q = (const uint8_t*)ka->a.q + (int64_t)t0 * Hq * kRowBytes;
+  uint8_t* qo = (uint8_t*)ka->a.q_out + (int64_t)t0 * Hq * kRowBytes;
+  const int32_t* pos = ka->a.pos ? ka->a.pos + t0 : nullptr;
+  const int lg = n == 1 ? 8 : n == 2 ? 7 : n <= 4 ? 6 : n <= 8 ? 5 : 4;
+  turn_rows<E, PATH, 4>(
+      [=](int tok, int row) __attribute__((always_inline)) {
+        // all three of everything, then the choice: under branches the compiler chooses between addresses of the captured variables,
+        // and these go to memory
+        const bool is_q = row >= 2 * Hkv, is_v = row >= Hkv;
+        const int g = is_v ? row - Hkv : row;
+        const int64_t from_q = (int64_t)(tok * Hq + row - 2 * Hkv) * kRowBytes, from = (int64_t)(tok * Hkv + g) * kRowBytes;
+        const uint8_t *sq = q + from_q, *sv = v + from, *sk = k + from;
+        uint8_t *dq = qo + from_q, *dk = page + (int64_t)g * kSlab + (is_v ? kBlk : 0) + (ts + tok) * kHalfBytes;
+        return RowAt{is_q ? sq : is_v ? sv : sk, is_q ? dq : dk, is_q ? kHalfBytes : kP * kHalfBytes, is_q || !is_v};
+      },
+      [=]() __attribute__((always_inline)) { fill_angles<PATH>(&ka->r, pos, pos0, n, cs); }, 2 * Hkv + Hq, n, lg, ka->r.dims, cs, stage);
+  if ((nf >> 8) && ka->a.bounds) {
+    __syncthreads();                             // the page's last keys are written; the others were there
+    uint8_t* b = ka->a.bounds + layer * ka->a.layer_bounds + (int64_t)(slot / kP) * Hkv * (2 * kRowBytes);
+    for (int g = threadIdx.x >> 6; g < Hkv; g += 4) page_bounds<E>(page + (int64_t)g * kSlab, b + g * (2 * kRowBytes));
+  }
+}
+template <typename E, int PATH>
+__global__ __launch_bounds__(256) void append_rope_kernel(AppendKernelArgs) {
+  __shared__ double2 cs[PATH == ROPE_NONE ? 1 : kRunTokens][kPairs];
+  __shared__ __align__(16) uint8_t stage[PATH == ROPE_HALVES_ANY ? 32 : 1][kRowBytes];
+  auto ka = (SYM_AS4 AppendKernelArgs*)__builtin_amdgcn_kernarg_segment_ptr();
+  const int32_t* w = ka->a.runs + (int64_t)blockIdx.x * RUN_WORDS;
+  append_run<E, PATH>(ka, sload(w), sload(w + 1), sload(w + 2), sload(w + 3), cs, stage);
+}
+template <typename E, int PATH>
+__global__ __launch_bounds__(256) void append_rope_runs_kernel(AppendRunsKernelArgs) {
+  __shared__ double2 cs[PATH == ROPE_NONE ? 1 : kRunTokens][kPairs];
+  __shared__ __align__(16) uint8_t stage[PATH == ROPE_HALVES_ANY ? 32 : 1][kRowBytes];
+  auto ka = (SYM_AS4 AppendRunsKernelArgs*)__builtin_amdgcn_kernarg_segment_ptr();
+  const auto* w = ka->runs.w + blockIdx.x * RUN_WORDS;
+  append_run<E, PATH>(&ka->k, w[0], w[1], w[2], w[3], cs, stage);
+}
+
+// ---------------------------------------------------------------------------------------
+// Bounds of a list of pages: a workgroup to a page and layer, a wavefront to a kv head at a time.  Bound: HBM (4 KiB read for 512 bytes written).
+// ---------------------------------------------------------------------------------------
+struct BoundsKernelArgs {
+  BoundsArgs a;
+  int32_t ids[kArgPages];
+};
+template <typename E, bool ARGS>
+__global__ __launch_bounds__(256) void bounds_kernel(std::conditional_t<ARGS, BoundsKernelArgs, BoundsArgs>) {
+  auto ka = (SYM_AS4 BoundsKernelArgs*)__builtin_amdgcn_kernarg_segment_ptr();
+  const int page = ARGS ? ka->ids[blockIdx.x] : sload(ka->a.pages + blockIdx.x), Hkv = ka->a.Hkv;
+  const uint8_t* p = ka->a.pool + blockIdx.y * ka->a.layer_bytes + page * ka->a.page_bytes;
+  uint8_t* b = ka->a.bounds + blockIdx.y * ka->a.layer_bounds + (int64_t)page * Hkv * (2 * kRowBytes);
+  for (int g = threadIdx.x >> 6; g < Hkv; g += 4) page_bounds<E>(p + (int64_t)g * kSlab, b + g * (2 * kRowBytes));
+}
+
+// ---------------------------------------------------------------------------------------
+// Scores: for a new token and kv head, page p gets  sum_d A_d hi_d + B_d lo_d  with A_d = sum_h max(q_hd, 0), B_d = sum_h min(q_hd, 0) over the
+// G query heads of the kv head: what the sum of their logits with any key of the page does not exceed.  Products and sums in 64 bits
+// (the choice of pages hangs on comparisons of scores that lie close together; with sums in 32 bits it would depend on their order),
+// rounded to 32 at the end.  A wavefront takes one kv head and 32 pages; 32 lanes share a page's 512 bytes, a 16-byte chunk
+// each, with the chunk's coefficients in registers; eight pages a lane are then added up over the 32 lanes by halving exchanges.  Up
+// to RT consecutive tokens of a file share the pass.  Bound: HBM.
+// ---------------------------------------------------------------------------------------
+constexpr int kScorePages = 32;
+__device__ __forceinline__ double as_f64(uint32_t lo, uint32_t hi) { return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo); }
+template <int CTRL>
+__device__ __forceinline__ double dpp_f64(double x) {
+  const uint64_t b = __builtin_bit_cast(uint64_t, x);
+  return as_f64((uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)b, CTRL, 0xf, 0xf, false), (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(b >> 32), CTRL, 0xf, 0xf, false));
+}
+
+template <typename E, int RT>
+__global__ __launch_bounds__(256) void sparse_scores_kernel(SparseArgs a) {
+  constexpr int C = E::kDimsPerChunk;
+  const int32_t* grp = a.groups + (int64_t)(a.group0 + blockIdx.y) * SPARSE_GROUP_WORDS;
+  const int r0 = sload(grp), nr = sload(grp + 1);
+  const int wave = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6)));
+  const int head = wave % a.Hkv, p0 = a.first + wave / a.Hkv * kScorePages;
+  const int32_t* last_row = a.rows + (int64_t)(r0 + nr - 1) * SPARSE_ROW_WORDS;      // of consecutive tokens the last sees most
+  const int tbl = sload(last_row), end = (sload(last_row + 1) + kP - 1) / kP - a.last;
+  if (p0 >= end) return;
+  const int lane = threadIdx.x & 63, sub = lane >> 5, hl = lane & 31, part = hl >> 4, chunk = hl & 15;
+  const uint8_t* rec = a.bounds + head * (2 * kRowBytes) + hl * 16;
+  const int64_t page_rec = (int64_t)a.Hkv * (2 * kRowBytes);
+  const int32_t* pt = a.tables + tbl;
+  int id[kScorePages / 2];
+#pragma unroll
+  for (int s = 0; s < kScorePages / 2; ++s) id[s] = pt[min(p0 + 2 * s + sub, end - 1)];
+  // coefficients of this lane's chunk: lanes 0..15 of a page hold lo, 16..31 hi
+  double cf[RT][C];
+  const int G = a.Hq / a.Hkv;
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+#pragma unroll
+    for (int e = 0; e < C; ++e) cf[t][e] = 0.0;
+    const uint8_t* q = (const uint8_t*)a.q + ((int64_t)(r0 + min(t, nr - 1)) * a.Hq + head * G) * kRowBytes + chunk * 16;
+    for (int h = 0; h < G; ++h) {
+      float x[C];
+      E::unpack(*(const uint4*)(q + h * kRowBytes), x);
+#pragma unroll
+      for (int e = 0; e < C; ++e) cf[t][e] += (double)(part ? (x[e] < 0.f ? 0.f : x[e]) : (x[e] > 0.f ? 0.f : x[e]));
+    }
+  }
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+    uint4 x[8];
+#pragma unroll
+    for (int s = 0; s < 8; ++s) x[s] = *(const uint4*)(rec + (int64_t)id[b * 8 + s] * page_rec);
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      double v[8];
+#pragma unroll
+      for (int s = 0; s < 8; ++s) {
+        float f[C];
+        E::unpack(x[s], f);
+        v[s] = 0.0;
+#pragma unroll
+        for (int e = 0; e < C; ++e) v[s] = __builtin_fma(cf[t][e], (double)f[e], v[s]);
+      }
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {              // lane bit 4: even rows of 16 lanes keep pages 0..3, odd ones 4..7
+        const uint64_t p = __builtin_bit_cast(uint64_t, v[s]), q = __builtin_bit_cast(uint64_t, v[s + 4]);
+        const auto lo = __builtin_amdgcn_permlane16_swap((uint32_t)p, (uint32_t)q, false, false);
+        const auto hi = __builtin_amdgcn_permlane16_swap((uint32_t)(p >> 32), (uint32_t)(q >> 32), false, false);
+        v[s] = as_f64(lo[0], hi[0]) + as_f64(lo[1], hi[1]);
+      }
+      const bool b3 = (lane & 8) != 0;
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {              // lane bit 3
+        const double keep = b3 ? v[s + 2] : v[s], send = b3 ? v[s] : v[s + 2];
+        v[s] = keep + dpp_f64<0x128>(send);      // row_ror:8
+        v[s] += dpp_f64<0xB1>(v[s]);             // the octet's sum
+        v[s] += dpp_f64<0x4E>(v[s]);
+        v[s] += dpp_f64<0x141>(v[s]);
+      }
+      // lane octet (bit 4, bit 3) holds steps 4 bit4 + 2 bit3 + {0, 1} of the eight
+      const int step = b * 8 + ((lane >> 4) & 1) * 4 + ((lane >> 3) & 1) * 2 + (lane & 1), p = p0 + 2 * step + sub;
+      const int row = r0 + t;
+      if (t < nr && (lane & 7) < 2) {
+        const int n = (a.rows[(int64_t)row * SPARSE_ROW_WORDS + 1] + kP - 1) / kP;
+        if (n > a.budget && p < n - a.last)
+          a.scores[((int64_t)(row - a.row0) * a.Hkv + head) * a.score_stride + (p - a.first)] = (float)((lane & 1) ? v[1] : v[0]);
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------------------
+// Choice of pages, a workgroup to a (new token, kv head): the page ids to read, in the order of the file.  Scores become whole numbers of
+// the same order (NaN above all), the smallest chosen one is found bit by bit from the first bit in which the largest and
+// the smallest differ, counting with ballots, and of those equal to it the lowest indices are taken.
+// NT threads hold EPT scores each; EPT = 0: any number of scores, read again for every count.
+// ---------------------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t order_of(float x) {
+  if (x != x) return 0xffffffffu;
+  const uint32_t b = as_u32(x + 0.0f);           // -0 and 0 are equal
+  return (b & 0x80000000u) ? ~b : b | 0x80000000u;
+}
+template <int NT, int EPT>
+__global__ __launch_bounds__(NT) void sparse_select_kernel(SparseArgs a) {
+  constexpr int W = NT / 64, N = EPT > 0 ? EPT : 1;
+  __shared__ uint32_t s_cnt[34], s_max, s_min, s_pre[N * W];
+  const int row = a.row0 + (int)blockIdx.x / a.Hkv, head = (int)blockIdx.x % a.Hkv;
+  const int32_t* rw = a.rows + (int64_t)row * SPARSE_ROW_WORDS;
+  const int32_t* pt = a.tables + sload(rw);
+  const int n = (sload(rw + 1) + kP - 1) / kP, kept = sload(rw + 2);
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  int32_t* list = a.lists + (int64_t)blockIdx.x * a.list_stride;
+  int32_t* picked = a.picked ? a.picked + ((int64_t)row * a.Hkv + head) * a.budget : nullptr;
+  auto put = [&](int at, int p) __attribute__((always_inline)) {
+    list[at] = pt[p];
+    if (picked) picked[at] = p;
+  };
+  if (picked)
+    for (int i = kept + tid; i < a.budget; i += NT) picked[i] = -1;
+  if (kept == n) {
+    for (int i = tid; i < n; i += NT) put(i, i);
+    return;
+  }
+  const int m = n - a.first - a.last, want = kept - a.first - a.last;
+  for (int i = tid; i < a.first; i += NT) put(i, i);
+  for (int i = tid; i < a.last; i += NT) put(kept - a.last + i, n - a.last + i);
+  if (want == 0) return;
+  const float* sc = a.scores + (int64_t)blockIdx.x * a.score_stride;
+  if (tid < 34) s_cnt[tid] = 0;
+  if (tid == 0) {
+    s_max = 0;
+    s_min = 0xffffffffu;
+  }
+  uint32_t key[N];                               // 0: none (order_of never gives it)
+  if constexpr (EPT > 0) {
+#pragma unroll
+    for (int e = 0; e < EPT; ++e) {
+      const int i = e * NT + tid;
+      key[e] = i < m ? order_of(sc[i]) : 0;
+    }
+  }
+  // f(key) of every score of this thread
+  auto each = [&](auto f) __attribute__((always_inline)) {
+    if constexpr (EPT > 0) {
+#pragma unroll
+      for (int e = 0; e < EPT; ++e) f(key[e]);
+    } else {
+      for (int i0 = 0; i0 < m; i0 += NT) f(i0 + tid < m ? order_of(sc[i0 + tid]) : 0u);
+    }
+  };
+  uint32_t hi = 0, lo = 0xffffffffu;
+  each([&](uint32_t k) {
+    hi = max(hi, k);
+    lo = min(lo, k ? k : 0xffffffffu);
+  });
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    hi = max(hi, (uint32_t)__shfl_xor((int)hi, o));
+    lo = min(lo, (uint32_t)__shfl_xor((int)lo, o));
+  }
+  __syncthreads();
+  if (lane == 0) {
+    atomicMax(&s_max, hi);
+    atomicMin(&s_min, lo);
+  }
+  __syncthreads();
+  hi = s_max;
+  lo = s_min;
+  // keys of at least x
+  auto count = [&](uint32_t x, int at) __attribute__((always_inline)) {
+    uint32_t c = 0;
+    each([&](uint32_t k) { c += (uint32_t)__popcll(__builtin_amdgcn_ballot_w64(k >= x)); });
+    if (lane == 0) atomicAdd(&s_cnt[at], c);
+    __syncthreads();
+    return s_cnt[at];
+  };
+  // the largest t with at least `want` keys >= t: from the bits that all keys share, the next lower bit each time
+  uint32_t t = hi;
+  if (hi != lo) {
+    const int top = 31 - __clz((int)(hi ^ lo));
+    t = hi & ~((2u << top) - 1);
+    for (int b = top; b >= 0; --b)
+      if (count(t | (1u << b), b) >= (uint32_t)want) t |= 1u << b;
+  }
+  const uint32_t above = t == 0xffffffffu ? 0 : count(t + 1, 32);
+  const uint32_t need = (uint32_t)want - above;  // of those equal to t
+  // Place of a chosen page among the chosen: those above t before it, and of the equal ones before it at most `need`.
+  if constexpr (EPT > 0) {
+    static_assert(NT * EPT < 65536, "two counts of 16 bits in a word");
+    uint64_t gt[N], eq[N];
+#pragma unroll
+    for (int e = 0; e < EPT; ++e) {
+      gt[e] = __builtin_amdgcn_ballot_w64(key[e] > t);
+      eq[e] = __builtin_amdgcn_ballot_w64(key[e] == t);
+      if (lane == 0) s_pre[e * W + w] = (uint32_t)__popcll(gt[e]) | (uint32_t)__popcll(eq[e]) << 16;
+    }
+    __syncthreads();
+    if (w == 0) {                                // exclusive sums over the N * W words, a stretch to each lane
+      constexpr int PER = (N * W + 63) / 64;
+      uint32_t g = 0, q = 0;
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+        if (lane * PER + i < N * W) {
+          g += s_pre[lane * PER + i] & 0xffff;
+          q += s_pre[lane * PER + i] >> 16;
+        }
+      uint32_t gs = g, qs = q;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t x = (uint32_t)__shfl_up((int)gs, o), y = (uint32_t)__shfl_up((int)qs, o);
+        if (lane >= o) {
+          gs += x;
+          qs += y;
+        }
+      }
+      gs -= g;
+      qs -= q;
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+        if (lane * PER + i < N * W) {
+          const uint32_t c = s_pre[lane * PER + i];
+          s_pre[lane * PER + i] = gs | qs << 16;
+          gs += c & 0xffff;
+          qs += c >> 16;
+        }
+    }
+    __syncthreads();
+    const uint64_t below = (1ull << lane) - 1;
+#pragma unroll
+    for (int e = 0; e < EPT; ++e) {
+      const uint32_t pre = s_pre[e * W + w];
+      const uint32_t g = (pre & 0xffff) + (uint32_t)__popcll(gt[e] & below), q = (pre >> 16) + (uint32_t)__popcll(eq[e] & below);
+      if (key[e] > t || (key[e] == t && q < need)) put(a.first + (int)(g + min(q, need)), a.first + e * NT + tid);
+    }
+  } else {
+    uint32_t g0 = 0, q0 = 0;
+    const uint64_t below = (1ull << lane) - 1;
+    for (int i0 = 0; i0 < m; i0 += NT) {
+      const uint32_t k = i0 + tid < m ? order_of(sc[i0 + tid]) : 0u;
+      const uint64_t gt = __builtin_amdgcn_ballot_w64(k > t), eq = __builtin_amdgcn_ballot_w64(k == t);
+      if (lane == 0) s_pre[w] = (uint32_t)__popcll(gt) | (uint32_t)__popcll(eq) << 16;
+      __syncthreads();
+      uint32_t g = g0, q = q0;
+      for (int x = 0; x < W; ++x) {
+        const uint32_t c = s_pre[x];
+        if (x < w) {
+          g += c & 0xffff;
+          q += c >> 16;
+        }
+        g0 += c & 0xffff;
+        q0 += c >> 16;
+      }
+      __syncthreads();                           // before the next round's counts
+      g += (uint32_t)__popcll(gt & below);
+      q += (uint32_t)__popcll(eq & below);
+      if (k > t || (k == t && q < need)) put(a.first + (int)(g + min(q, need)), a.first + i0 + tid);
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------------------
+// Attention over the listed pages of a (new token, kv head): a workgroup of four wavefronts to each of `splits` equal parts of the list.
+// The list is read like a file's page table: only its last page may be partly filled.  One pass, with the running maximum and sum
+// of the softmax in fp32; the wavefronts' results are combined through LDS, those of several parts by the merge kernel.
+// Bound: HBM (8 KiB for 4 D 16 G flops).
+// ---------------------------------------------------------------------------------------
+// bf16 storage: on the matrix cores, an fp32 weight cut into three bf16 numbers (8 bits each: exact), as in decode_bins_mx.  Where 3 G columns fit
+// into 16 each takes a column of one product.  With 8 heads per kv head there are two products to the same sums: the upper part halved in columns 0..7
+// of both (0 there would make an infinite V NaN), the middle and the lower part in columns 8..15.  (Weights cut to 16 bits in one
+// product: error against 64 bits 4.8e-6 instead of 2e-7.)
+template <int G>
+struct AttendMx {
+  static constexpr int D = 128;
+  static constexpr bool TWICE = G == 8;
+  bf16x8_t q[4];
+  f32x4_t O[8];
+  float m, l;
+  int col, grp, part;
+  uint32_t cut1, cut2;
+  float scale;
+
+  __device__ __forceinline__ void start(const uint8_t* qrows, float scale_log2e) {
+    const int lane = threadIdx.x & 63;
+    col = lane & 15;
+    grp = lane >> 4;
+    part = col / G;
+    cut1 = part >= 1 ? 0xffff0000u : 0u;
+    cut2 = part >= 2 ? 0xffff0000u : 0u;
+    scale = scale_log2e;
+    const uint8_t* qp = qrows + (col % G) * kRowBytes + grp * 16;
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) q[ks] = __builtin_bit_cast(bf16x8_t, *(const u32x4_t*)(qp + ks * 64));
+    m = -1e30f;
+    l = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) O[e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
+  // (a lane's place in a page hangs on nothing that start() sets: the first page is requested before it)
+  __device__ __forceinline__ void request(PageRegs& R, const uint8_t* slab) const {
+    const int col = threadIdx.x & 15, grp = (threadIdx.x & 63) >> 4;
+    const uint8_t* kb = slab + col * kHalfBytes + grp * 16;
+    const uint8_t* vb = slab + kBlk + (col >> 3) * (kP * kHalfBytes) + (4 * grp) * kHalfBytes + (col & 7) * 16;
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) R.k[ks] = *(const uint4*)(kb + (ks >> 1) * (kP * kHalfBytes) + (ks & 1) * 64);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) R.v[u] = *(const uint4*)(vb + u * kHalfBytes);
+  }
+  __device__ __forceinline__ void page(PageRegs& R, const int nvalid) {
+    f32x4_t S = {0.f, 0.f, 0.f, 0.f}, S2 = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      S = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, R.k[ks]), q[ks], S, 0, 0, 0);
+      S2 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, R.k[2 + ks]), q[2 + ks], S2, 0, 0, 0);
+    }
+    S = S + S2;
+    if (nvalid < kP) {                           // slots past the file's end hold anything; weight 0, but 0 * NaN is NaN
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (4 * grp + u >= nvalid) {
+          S[u] = -__builtin_inff();
+          R.v[u] = make_uint4(0, 0, 0, 0);
+        }
+    }
+    const float mx = fmaxf(fmaxf(S[0], S[1]), fmaxf(S[2], S[3])) * scale;
+    if (__builtin_amdgcn_ballot_w64(mx > m + kTau) != 0) {
+      const float mn = pair32_max(pair16_max(fmaxf(m, mx)));
+      const float al = __builtin_amdgcn_exp2f(m - mn);
+      l *= al;
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) O[e][v] *= al;
+      m = mn;
+    }
+    uint32_t w[4], w2[4];
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+      float x = __builtin_amdgcn_exp2f(__builtin_fmaf(S[v], scale, -m));
+      l += x;
+      if constexpr (TWICE) {
+        const float up = as_f32(as_u32(x) & 0xffff0000u), mid = x - up;
+        w[v] = as_u32(part ? mid : 0.5f * up);
+        w2[v] = as_u32(part ? mid - as_f32(as_u32(mid) & 0xffff0000u) : 0.5f * up);
+      } else {
+        x -= as_f32(as_u32(x) & cut1);
+        x -= as_f32(as_u32(x) & cut2);
+        w[v] = as_u32(x);
+      }
+    }
+    auto upper = [](const uint32_t* x) __attribute__((always_inline)) {
+      return __builtin_bit_cast(s16x4_t, make_uint2(__builtin_amdgcn_perm(x[1], x[0], 0x07060302), __builtin_amdgcn_perm(x[3], x[2], 0x07060302)));
+    };
+    const s16x4_t W = upper(w), W2 = TWICE ? upper(w2) : W;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t sel = (e & 1) ? 0x07060302 : 0x05040100;
+      auto word = [&](int u) { return (e >> 1) == 0 ? R.v[u].x : (e >> 1) == 1 ? R.v[u].y : (e >> 1) == 2 ? R.v[u].z : R.v[u].w; };
+      const s16x4_t vt = __builtin_bit_cast(s16x4_t, make_uint2(__builtin_amdgcn_perm(word(1), word(0), sel), __builtin_amdgcn_perm(word(3), word(2), sel)));
+      O[e] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vt, W, O[e], 0, 0, 0);
+      if constexpr (TWICE) O[e] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vt, W2, O[e], 0, 0, 0);
+    }
+  }
+  // this wavefront's unnormalised result, [G][D] and (max, sum) per head
+  __device__ __forceinline__ void finish(float* acc, float* ml) {
+    const float ls = pair32_sum(pair16_sum(l));
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        float low = row_shl<G>(O[e][v]);
+        if constexpr (!TWICE) low += row_shl<2 * G>(O[e][v]);
+        O[e][v] += low == low ? low : 0.f;       // (an infinite V at a lower part of 0: the upper part says what it makes of the output)
+      }
+    if (col < G) {
+      float* o = acc + col * D + 32 * grp;       // + 8 v + e
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        *(float4*)(o + 8 * v) = make_float4(O[0][v], O[1][v], O[2][v], O[3][v]);
+        *(float4*)(o + 8 * v + 4) = make_float4(O[4][v], O[5][v], O[6][v], O[7][v]);
+      }
+      if (grp == 0) *(float2*)(ml + 2 * col) = make_float2(m, ls);
+    }
+  }
+};
+
+// fp32 storage: on the vector units, lane (r, j) holds tokens r and 8 + r of a page and 8 dims; running maximum and sum are each lane's own.
+template <int G>
+struct AttendF32 {
+  static constexpr int C = 4, DPL = 8, D = 64;
+  uint4 q[G][2];
+  float m[G], l[G], acc[G][DPL];
+  int r, j;
+  float scale;
+
+  __device__ __forceinline__ void start(const uint8_t* qrows, float scale_log2e) {
+    const int lane = threadIdx.x & 63;
+    r = lane >> 3;
+    j = lane & 7;
+    scale = scale_log2e;
+#pragma unroll
+    for (int h = 0; h < G; ++h) {
+      q[h][0] = *(const uint4*)(qrows + h * kRowBytes + j * 16);
+      q[h][1] = *(const uint4*)(qrows + h * kRowBytes + kHalfBytes + j * 16);
+      m[h] = -1e30f;
+      l[h] = 0.f;
+#pragma unroll
+      for (int d = 0; d < DPL; ++d) acc[h][d] = 0.f;
+    }
+  }
+  __device__ __forceinline__ void request(PageRegs& R, const uint8_t* slab) const {
+    const uint8_t* b = slab + (threadIdx.x & 63) * 16;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) R.k[x] = *(const uint4*)(b + x * 1024);
+#pragma unroll
+    for (int x = 0; x < 4; ++x) R.v[x] = *(const uint4*)(b + kBlk + x * 1024);
+  }
+  __device__ __forceinline__ void page(PageRegs& R, const int nvalid) {
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf)
+      if (hf * 8 + r >= nvalid) {
+        R.v[hf] = make_uint4(0, 0, 0, 0);
+        R.v[2 + hf] = make_uint4(0, 0, 0, 0);
+      }
+    float s[2][G];
+    bool need = false;
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+      for (int h = 0; h < G; ++h) {
+        float x = ElemF32::dot(R.k[2 + hf], q[h][1], ElemF32::dot(R.k[hf], q[h][0], 0.f));
+        x = octet_sum(x) * scale;
+        s[hf][h] = hf * 8 + r < nvalid ? x : -__builtin_inff();
+      }
+#pragma unroll
+    for (int h = 0; h < G; ++h) need |= fmaxf(s[0][h], s[1][h]) > m[h] + kTau;
+    if (__builtin_amdgcn_ballot_w64(need) != 0) {
+#pragma unroll
+      for (int h = 0; h < G; ++h) {
+        const float mn = fmaxf(m[h], fmaxf(s[0][h], s[1][h])), al = __builtin_amdgcn_exp2f(m[h] - mn);
+        l[h] *= al;
+#pragma unroll
+        for (int d = 0; d < DPL; ++d) acc[h][d] *= al;
+        m[h] = mn;
+      }
+    }
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf) {
+      float w[G];
+#pragma unroll
+      for (int h = 0; h < G; ++h) {
+        w[h] = __builtin_amdgcn_exp2f(s[hf][h] - m[h]);
+        l[h] += w[h];
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        float v[C];
+        ElemF32::unpack(R.v[i * 2 + hf], v);
+#pragma unroll
+        for (int h = 0; h < G; ++h)
+#pragma unroll
+          for (int e = 0; e < C; ++e) acc[h][i * C + e] = __builtin_fmaf(w[h], v[e], acc[h][i * C + e]);
+      }
+    }
+  }
+  __device__ __forceinline__ void finish(float* out, float* ml) {
+#pragma unroll
+    for (int h = 0; h < G; ++h) {
+      const float M = pair32_max(pair16_max(fmaxf(m[h], row_xor8(m[h]))));
+      const float f = __builtin_amdgcn_exp2f(m[h] - M);
+      float ls = l[h] * f;
+      ls = pair32_sum(pair16_sum(ls + row_xor8(ls)));
+      // the eight token slots of a chunk: halving exchanges over lane bits 5, 4, 3 leave lane r with entry r
+      float x[DPL];
+#pragma unroll
+      for (int d = 0; d < DPL; ++d) x[d] = acc[h][d] * f;
+#pragma unroll
+      for (int d = 0; d < 4; ++d) {
+        const auto sw = __builtin_amdgcn_permlane32_swap(as_u32(x[d]), as_u32(x[d + 4]), false, false);
+        x[d] = as_f32(sw[0]) + as_f32(sw[1]);
+      }
+#pragma unroll
+      for (int d = 0; d < 2; ++d) {
+        const auto sw = __builtin_amdgcn_permlane16_swap(as_u32(x[d]), as_u32(x[d + 2]), false, false);
+        x[d] = as_f32(sw[0]) + as_f32(sw[1]);
+      }
+      const bool b3 = (r & 1) != 0;
+      const float keep = b3 ? x[1] : x[0], send = b3 ? x[0] : x[1];
+      out[h * D + (r / C) * (D / 2) + j * C + r % C] = keep + row_xor8(send);
+      if ((threadIdx.x & 63) == 0) *(float2*)(ml + 2 * h) = make_float2(M, ls);
+    }
+  }
+};
+
+constexpr int kAttendWaves = 4;
+template <typename AT, int G>
+__global__ __launch_bounds__(64 * kAttendWaves, 2) void sparse_attend_kernel(SparseArgs a) {
+  constexpr int D = AT::D, NT = 64 * kAttendWaves;
+  __shared__ __align__(16) float s_acc[kAttendWaves][G * D];
+  __shared__ __align__(16) float s_ml[kAttendWaves][2 * G];
+  const int unit = (int)blockIdx.x / a.splits, split = (int)blockIdx.x - unit * a.splits;
+  const int row = a.row0 + unit / a.Hkv, head = unit % a.Hkv;
+  const int32_t* rw = a.rows + (int64_t)row * SPARSE_ROW_WORDS;
+  const int vis = sload(rw + 1), kept = sload(rw + 2);
+  const int tail = (vis - 1) % kP + 1;           // tokens of the last page
+  const int wv = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  const int parts = a.splits * kAttendWaves, mine = split * kAttendWaves + wv;
+  int p = (int)((int64_t)kept * mine / parts);
+  const int pe = (int)((int64_t)kept * (mine + 1) / parts);
+  const int32_t* list = a.lists + (int64_t)unit * a.list_stride;
+  const uint8_t* pool = a.pool + (int64_t)head * kSlab;
+  AT at;
+  PageRegs A, B;
+  auto id = [&](int i) __attribute__((always_inline)) { return (int64_t)sload(list + min(i, kept - 1)); };      // past the part's end: read, not used
+  at.request(A, pool + id(p) * a.page_bytes);
+  at.start((const uint8_t*)a.q + ((int64_t)row * a.Hq + head * G) * kRowBytes, a.scale_log2e);
+  while (p < pe) {
+    at.request(B, pool + id(p + 1) * a.page_bytes);
+    at.page(A, p == kept - 1 ? tail : kP);
+    if (++p >= pe) break;
+    at.request(A, pool + id(p + 1) * a.page_bytes);
+    at.page(B, p == kept - 1 ? tail : kP);
+    ++p;
+  }
+  at.finish(s_acc[wv], s_ml[wv]);
+  __syncthreads();
+  float* out = a.out + ((int64_t)row * a.Hq + head * G) * D;
+  const int64_t slot = (int64_t)unit * a.splits + split;
+  for (int x = threadIdx.x; x < G * D; x += NT) {
+    const int h = x / D;
+    float M = s_ml[0][2 * h], num = 0.f, den = 0.f;
+#pragma unroll
+    for (int w = 1; w < kAttendWaves; ++w) M = fmaxf(M, s_ml[w][2 * h]);
+#pragma unroll
+    for (int w = 0; w < kAttendWaves; ++w) {     // (a wavefront without pages: maximum -1e30, sum 0, zeros)
+      const float f = __builtin_amdgcn_exp2f(s_ml[w][2 * h] - M);
+      num = __builtin_fmaf(s_acc[w][x], f, num);
+      den = __builtin_fmaf(s_ml[w][2 * h + 1], f, den);
+    }
+    if (a.splits == 1) {
+      out[x] = num / den;
+    } else {
+      a.part_acc[slot * G * D + x] = num;
+      if (x % D == 0) *(float2*)(a.part_ml + (slot * G + h) * 2) = make_float2(M, den);
+    }
+  }
+}
+
+}  // namespace
+
+// The element type and the way of turning, as template arguments.
+#define SYM_ROPE_CASES(LAUNCH) \
+  if (dtype == 0) { \
+    switch (r.path) { \
+      case ROPE_NONE: LAUNCH(ElemF32, ROPE_NONE); break; \
+      case ROPE_HALVES: LAUNCH(ElemF32, ROPE_HALVES); break; \
+      case ROPE_HALVES_ANY: LAUNCH(ElemF32, ROPE_HALVES_ANY); break; \
+      case ROPE_INTERLEAVED: LAUNCH(ElemF32, ROPE_INTERLEAVED); break; \
+      default: return hipErrorInvalidValue; \
+    } \
+  } else { \
+    switch (r.path) { \
+      case ROPE_NONE: LAUNCH(ElemBF16, ROPE_NONE); break; \
+      case ROPE_HALVES: LAUNCH(ElemBF16, ROPE_HALVES); break; \
+      case ROPE_HALVES_ANY: LAUNCH(ElemBF16, ROPE_HALVES_ANY); break; \
+      case ROPE_INTERLEAVED: LAUNCH(ElemBF16, ROPE_INTERLEAVED); break; \
+      default: return hipErrorInvalidValue; \
+    } \
+  }
+
+hipError_t launch_rope_rows(RopeRowsArgs a, const RopeTable& r, int dtype, hipStream_t st) {
+  if (a.n <= 0) return hipSuccess;
+  if (a.n > kMostRopeRows) return hipErrorInvalidValue;
+  a.tokens = a.n >= 2048 ? 4 : 1;
+  const RopeRowsKernelArgs ka{a, r};
+  const dim3 grid((unsigned)((a.n + a.tokens - 1) / a.tokens)), block(256);
+#define SYM_LAUNCH(E, PATH) hipLaunchKernelGGL((rope_rows_kernel<E, PATH>), grid, block, 0, st, ka)
+  SYM_ROPE_CASES(SYM_LAUNCH)
+#undef SYM_LAUNCH
+  return hipGetLastError();
+}
+
+hipError_t launch_append_rope(const AppendRopeArgs& a, const RopeTable& r, int dtype, hipStream_t st) {
+  if (a.n_runs <= 0) return a.done ? hipEventRecord(a.done, st) : hipSuccess;
+  if (a.n_layers < 1 || a.n_layers > 65535) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)a.n_runs, (unsigned)a.n_layers), block(256);
+  if (a.by_args) {
+    if (a.n_runs > kArgRuns) return hipErrorInvalidValue;
+    AppendRunsKernelArgs ka;
+    ka.k = AppendKernelArgs{a, r};
+    std::copy_n(a.runs, a.n_runs * RUN_WORDS, ka.runs.w);
+    std::fill(ka.runs.w + a.n_runs * RUN_WORDS, ka.runs.w + kArgRuns * RUN_WORDS, 0);
+    hipError_t e = hipSuccess;
+#define SYM_LAUNCH(E, PATH) e = launch_done(append_rope_runs_kernel<E, PATH>, grid, block, st, a.done, ka)
+    SYM_ROPE_CASES(SYM_LAUNCH)
+#undef SYM_LAUNCH
+    return e;
+  }
+  const AppendKernelArgs ka{a, r};
+  hipError_t e = hipSuccess;
+#define SYM_LAUNCH(E, PATH) e = launch_done(append_rope_kernel<E, PATH>, grid, block, st, a.done, ka)
+  SYM_ROPE_CASES(SYM_LAUNCH)
+#undef SYM_LAUNCH
+  return e;
+}
+
+hipError_t launch_bounds(const BoundsArgs& a, int dtype, hipStream_t st) {
+  if (a.n_pages <= 0) return hipSuccess;
+  if (a.n_layers < 1 || a.n_layers > 65535) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)a.n_pages, (unsigned)a.n_layers), block(256);
+  if (a.by_args) {
+    if (a.n_pages > kArgPages) return hipErrorInvalidValue;
+    BoundsKernelArgs ka;
+    ka.a = a;
+    std::copy_n(a.pages, a.n_pages, ka.ids);
+    std::fill(ka.ids + a.n_pages, ka.ids + kArgPages, 0);
+    if (dtype == 0) hipLaunchKernelGGL((bounds_kernel<ElemF32, true>), grid, block, 0, st, ka);
+    else hipLaunchKernelGGL((bounds_kernel<ElemBF16, true>), grid, block, 0, st, ka);
+  } else {
+    if (dtype == 0) hipLaunchKernelGGL((bounds_kernel<ElemF32, false>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((bounds_kernel<ElemBF16, false>), grid, block, 0, st, a);
+  }
+  return hipGetLastError();
+}
+
+hipError_t launch_sparse_scores(const SparseArgs& a, int dtype, hipStream_t st) {
+  if (a.n_groups <= 0 || a.most_scored <= 0) return hipSuccess;
+  const int64_t waves = (int64_t)((a.most_scored + kScorePages - 1) / kScorePages) * a.Hkv;
+  const dim3 grid((unsigned)((waves + 3) / 4), (unsigned)a.n_groups), block(256);
+  if (a.n_groups > 65535) return hipErrorInvalidValue;
+  if (dtype == 0) {
+    if (a.group_rows == 1) hipLaunchKernelGGL((sparse_scores_kernel<ElemF32, 1>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((sparse_scores_kernel<ElemF32, kGroupRows>), grid, block, 0, st, a);
+  } else {
+    if (a.group_rows == 1) hipLaunchKernelGGL((sparse_scores_kernel<ElemBF16, 1>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((sparse_scores_kernel<ElemBF16, kGroupRows>), grid, block, 0, st, a);
+  }
+  return hipGetLastError();
+}
+
+hipError_t launch_sparse_select(const SparseArgs& a, hipStream_t st) {
+  if (a.n_rows <= 0) return hipSuccess;
+  const dim3 grid((unsigned)a.n_rows * a.Hkv);
+  const int m = a.most_scored;
+#define SYM_SELECT(NT, EPT) hipLaunchKernelGGL((sparse_select_kernel<NT, EPT>), grid, dim3(NT), 0, st, a)
+  if (m <= 256) SYM_SELECT(256, 1);
+  else if (m <= 1024) SYM_SELECT(256, 4);
+  else if (m <= 4096) SYM_SELECT(512, 8);
+  else if (m <= 16384) SYM_SELECT(1024, 16);
+  else SYM_SELECT(1024, 0);
+#undef SYM_SELECT
+  return hipGetLastError();
+}
+
+hipError_t launch_sparse_attend(const SparseArgs& a, int dtype, hipStream_t st) {
+  if (a.n_rows <= 0) return hipSuccess;
+  const dim3 grid((unsigned)(a.n_rows * a.Hkv * a.splits)), block(64 * kAttendWaves);
+#define SYM_ATTEND(GG) \
+  case GG: \
+    if (dtype == 0) hipLaunchKernelGGL((sparse_attend_kernel<AttendF32<GG>, GG>), grid, block, 0, st, a); \
+    else hipLaunchKernelGGL((sparse_attend_kernel<AttendMx<GG>, GG>), grid, block, 0, st, a); \
+    break;
+  switch (a.Hq / a.Hkv) {
+    SYM_ATTEND(1) SYM_ATTEND(2) SYM_ATTEND(4) SYM_ATTEND(8)
+    default: return hipErrorInvalidValue;
+  }
+#undef SYM_ATTEND
+  return hipGetLastError();
+}
+
+int enter_device(int device) {
+  int cur = device;
+  if (hipGetDevice(&cur) != hipSuccess || cur == device) return -1;
+  return hipSetDevice(device) == hipSuccess ? cur : -1;
+}
+void leave_device(int before) {
+  if (before >= 0) (void)hipSetDevice(before);
+}
+
+bool stream_captures(hipStream_t st) {
+  hipStreamCaptureStatus cs = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing(st, &cs) != hipSuccess) {
+    (void)hipGetLastError();
+    return true;
+  }
+  return cs != hipStreamCaptureStatusNone;
+}
+
+}  // namespace symkv
