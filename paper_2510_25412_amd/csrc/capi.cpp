@@ -65,11 +65,12 @@ struct SparsePlan {
   bool turns = false;                              // a rope is given
   RopeTable rope;
   const int32_t* pos = nullptr;
-  int64_t off_rows = 0, off_tables = 0, off_groups = 0, off_runs = 0, off_pages = 0, off_merge = 0;   // word offsets in the blob
+  int64_t off_rows = 0, off_tables = 0, off_groups = 0, off_runs = 0, off_pages = 0, off_counters = 0;   // word offsets in the blob
   int64_t entries = 0;                             // page ids in the tables
+  int64_t n_counters = 0;
   int32_t n_rows = 0, n_runs = 0;
   int32_t n_stale = 0, n_done = 0;                 // full pages without bounds: from before the batch, then those that it completes
-  int32_t splits = 1, score_stride = 0, list_stride = 0, group_rows = 1;
+  int32_t splits = 1, score_stride = 0, group_rows = 1;
   int64_t q_bytes = 0, row_bytes = 0;              // scratch: turned query rows of the batch; per row and slab
   struct Slab {
     int32_t row0, rows, group0, groups, most_scored;
@@ -859,34 +860,34 @@ int size_sparse(sym_ctx* c, SparsePlan* sp, int32_t n_lips, const sym_kv* kv, co
   sp->n_stale = (int32_t)stale;
   sp->n_done = (int32_t)done;
   sp->kv.assign(kv, kv + n_lips);
-  sp->score_stride = most_pages > sp->budget ? (int32_t)((most_pages - sp->first - sp->last + 3) & ~3ll) : 0;
-  sp->list_stride = (int32_t)((most_kept + 3) & ~3ll);
-  // Parts of a list: enough workgroups for the chip where rows are few, each wavefront with two pages at least.
+  sp->score_stride = most_pages > sp->budget ? (int32_t)align_up(most_pages - sp->first - sp->last, 32) : 0;
+  // Parts of a list: enough workgroups for the chip where rows are few, each wavefront with two pages at least; no more pages than a
+  // workgroup's list holds.
   const int64_t units = tokens * H;
-  sp->splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(512 / std::max<int64_t>(units, 1), most_kept / 8));
+  sp->splits = (int32_t)std::max({(int64_t)1, std::min(512 / units, most_kept / 8), (most_kept + kPartPages - 1) / kPartPages});
   sp->q_bytes = sp->turns ? align_up(row_bytes_of(tokens, c->cfg.n_q_heads), 256) : 0;
-  *words = sp->n_rows * (int64_t)(SPARSE_ROW_WORDS + SPARSE_GROUP_WORDS) + entries + runs * RUN_WORDS + stale + done +
-           (sp->splits > 1 ? units * MERGE_WORDS : 0) + 16;
+  sp->n_counters = sp->splits > 1 ? H * std::max<int64_t>(1, std::min(tokens, kMostUnits / (H * sp->splits))) : 0;
+  *words = sp->n_rows * (int64_t)(SPARSE_ROW_WORDS + SPARSE_GROUP_WORDS) + entries + runs * RUN_WORDS + stale + done + sp->n_counters + 16;
   return SYM_OK;
 }
 int fit_sparse(sym_ctx* c, SparsePlan* sp, int64_t ws_bytes, int64_t blob_words) {
   const int64_t H = c->cfg.n_kv_heads;
   const int64_t slot = sp->splits > 1 ? (int64_t)sp->splits * c->G * (2 + c->cfg.head_dim) * 4 : 0;
-  sp->row_bytes = H * ((int64_t)(sp->score_stride + sp->list_stride) * 4 + slot);
+  sp->row_bytes = H * ((int64_t)sp->score_stride * 4 + slot);
   const int64_t room = ws_bytes - align_up(blob_words * 4, 256) - sp->q_bytes - 4 * 256;
-  sp->slab_rows = std::min({room / sp->row_bytes, kMostUnits / std::max<int64_t>(1, H * sp->splits), (int64_t)65535});
-  if (sp->slab_rows < 1 || (sp->splits > 1 && sp->slab_rows < sp->n_rows)) return fail(c, SYM_ENOSPC, "workspace too small for this sparse batch");
+  sp->slab_rows = std::min({room / std::max<int64_t>(sp->row_bytes, 1), std::max<int64_t>(1, kMostUnits / (H * sp->splits)), (int64_t)65535, (int64_t)sp->n_rows});
+  if (sp->slab_rows < 1) return fail(c, SYM_ENOSPC, "workspace too small for this sparse batch");
   return SYM_OK;
 }
-// Writes the sections at word `at` of `blob` (after the append): rows, groups, tables, runs, pages without bounds, merge items.
+// Writes the sections at word `at` of `blob` (after the append): rows, groups, tables, runs, pages without bounds, counters.
 void fill_sparse(sym_ctx* c, SparsePlan* sp, int32_t n_lips, const sym_kv* kv, const int32_t* n_tokens, int32_t* blob, int64_t at) {
-  const int32_t P = c->cfg.page_tokens, H = c->cfg.n_kv_heads;
+  const int32_t P = c->cfg.page_tokens;
   sp->off_rows = at;
   sp->off_groups = sp->off_rows + (int64_t)sp->n_rows * SPARSE_ROW_WORDS;
   sp->off_tables = sp->off_groups + (int64_t)sp->n_rows * SPARSE_GROUP_WORDS;
   sp->off_runs = sp->off_tables + sp->entries;
   sp->off_pages = sp->off_runs + (int64_t)sp->n_runs * RUN_WORDS;
-  sp->off_merge = sp->off_pages + sp->n_stale + sp->n_done;
+  sp->off_counters = sp->off_pages + sp->n_stale + sp->n_done;
   int32_t *rows = blob + sp->off_rows, *groups = blob + sp->off_groups, *tables = blob + sp->off_tables;
   int32_t *stale = blob + sp->off_pages, *done = stale + sp->n_stale;
   append_runs(c, n_lips, kv, n_tokens, &c->words);
@@ -906,8 +907,6 @@ void fill_sparse(sym_ctx* c, SparsePlan* sp, int32_t n_lips, const sym_kv* kv, c
       int32_t* r = rows + (int64_t)row * SPARSE_ROW_WORDS;
       r[0] = tbl;
       r[1] = vis;
-      r[2] = std::min(n, sp->budget);
-      r[3] = 0;
       if (row % sp->slab_rows == 0) {
         sp->slabs.push_back({row, 0, n_groups, 0, 0});
         in_group = 0;
@@ -915,29 +914,28 @@ void fill_sparse(sym_ctx* c, SparsePlan* sp, int32_t n_lips, const sym_kv* kv, c
       SparsePlan::Slab& slab = sp->slabs.back();
       ++slab.rows;
       if (n <= sp->budget) continue;               // every page is read
-      slab.most_scored = std::max(slab.most_scored, n - sp->first - sp->last);
       if (in_group == 0 || in_group == kGroupRows) {
-        groups[2 * n_groups] = row;
-        groups[2 * n_groups + 1] = 0;
+        groups[n_groups * SPARSE_GROUP_WORDS] = row;
         ++n_groups;
         ++slab.groups;
         in_group = 0;
       }
-      sp->group_rows = std::max(sp->group_rows, groups[2 * n_groups - 1] = ++in_group);
+      int32_t* g = groups + (int64_t)(n_groups - 1) * SPARSE_GROUP_WORDS;
+      g[1] = ++in_group;
+      g[2] = tbl;
+      g[3] = n - sp->last;                         // (of a group's tokens the last sees most)
+      sp->group_rows = std::max(sp->group_rows, in_group);
+      slab.most_scored = std::max(slab.most_scored, n - sp->first - sp->last);
     }
     tbl += (int32_t)f->pages.size();
   }
-  if (sp->splits > 1)
-    for (int32_t u = 0; u < sp->n_rows * H; ++u) {
-      int32_t* m = blob + sp->off_merge + (int64_t)u * MERGE_WORDS;
-      const int32_t item[MERGE_WORDS] = {u * sp->splits, sp->splits, u / H * c->cfg.n_q_heads + u % H * c->G, 0, 0, 0, 1, 0};
-      std::memcpy(m, item, sizeof(item));
-    }
+  std::fill_n(blob + sp->off_counters, sp->n_counters, 0);
 }
 
-// One sparse layer: the rows turned and appended, then slab by slab scores, choice, attention.
+// One sparse layer: the rows turned and appended, then slab by slab scores and attention.  stage: the staging buffer whose lists are not
+// on the device yet, or -1.
 int run_sparse_layer(sym_ctx* c, const SparsePlan& sp, uint8_t* ws, int64_t words, int32_t layer, const void* q, const void* k_new, const void* v_new,
-                     float* out, int32_t* picked, hipStream_t st) {
+                     float* out, int32_t* picked, int stage, hipStream_t st) {
   const int32_t* blob = (const int32_t*)ws;
   uint8_t* at = ws + align_up(words * 4, 256);
   void* q_turned = at;
@@ -949,9 +947,20 @@ int run_sparse_layer(sym_ctx* c, const SparsePlan& sp, uint8_t* ws, int64_t word
     a.q_out = q_turned;
     a.runs = blob + sp.off_runs;
     a.n_runs = sp.n_runs;
+    const StageDone done(c, stage);
+    if (stage >= 0) {                              // the lists travel with this launch
+      a.host_words = c->stage[stage];
+      a.dev_words = (int32_t*)ws;
+      a.copy_words = words;
+      a.by_args = sp.n_runs <= kArgRuns ? 1 : 0;
+      a.runs = c->stage[stage] + sp.off_runs;
+      a.done = done.event();
+    }
     Timed t(c, SYM_K_PROLOGUE, st);
     const hipError_t e = launch_append_rope(a, sp.rope, c->cfg.dtype, st);
     if (e != hipSuccess) return fail_hip(c, e, "append launch");
+    if (stage >= 0)
+      if (int rc = done.launched(st)) return rc;
   }
   if (int rc = batch_bounds(c, sp, blob, layer, sp.n_stale, st)) return rc;
   SparseArgs a{};
@@ -964,11 +973,10 @@ int run_sparse_layer(sym_ctx* c, const SparsePlan& sp, uint8_t* ws, int64_t word
   a.rows = blob + sp.off_rows;
   a.groups = blob + sp.off_groups;
   a.tables = blob + sp.off_tables;
+  a.counters = (int32_t*)ws + sp.off_counters;
   const int64_t slab = std::min<int64_t>(sp.slab_rows, sp.n_rows);
-  a.scores = (float*)at;
+  a.scores = (uint32_t*)at;
   at += align_up(slab * H * sp.score_stride * 4, 256);
-  a.lists = (int32_t*)at;
-  at += align_up(slab * H * sp.list_stride * 4, 256);
   a.part_ml = (float*)at;
   at += align_up(sp.splits > 1 ? slab * H * sp.splits * c->G * 2 * 4 : 0, 256);
   a.part_acc = (float*)at;
@@ -979,7 +987,6 @@ int run_sparse_layer(sym_ctx* c, const SparsePlan& sp, uint8_t* ws, int64_t word
   a.first = sp.first;
   a.last = sp.last;
   a.score_stride = sp.score_stride;
-  a.list_stride = sp.list_stride;
   a.splits = sp.splits;
   a.scale_log2e = c->scale_log2e;
   for (const SparsePlan::Slab& s : sp.slabs) {
@@ -990,24 +997,18 @@ int run_sparse_layer(sym_ctx* c, const SparsePlan& sp, uint8_t* ws, int64_t word
     a.most_scored = s.most_scored;
     hipError_t e = hipSuccess;
     {
-      Timed t(c, SYM_K_ATTN, st, false, true, 2 + (s.groups > 0));
+      Timed t(c, SYM_K_ATTN, st, false, true, 1 + (s.groups > 0));
       if (s.groups > 0) e = launch_sparse_scores(a, c->cfg.dtype, st);
-      if (e == hipSuccess) e = launch_sparse_select(a, st);
       if (e == hipSuccess) e = launch_sparse_attend(a, c->cfg.dtype, st);
     }
     if (e != hipSuccess) return fail_hip(c, e, "sparse attention launch");
-    if (sp.splits > 1) {
-      MergeArgs m{a.part_acc, a.part_ml, blob + sp.off_merge, out, (int32_t)(sp.n_rows * H), sp.splits, nullptr, 0, 0, c->cfg.n_q_heads};
-      Timed t(c, SYM_K_MERGE, st);
-      e = launch_merge(m, c->G, c->cfg.head_dim, st);
-      if (e != hipSuccess) return fail_hip(c, e, "merge launch");
-    }
   }
   return SYM_OK;
 }
 
-// The host half of a batch with sparse layers (lock held): plan, commit, blob to the device, batch open.
-int begin_sparse_locked(sym_ctx* c, int32_t n_lips, const sym_kv* kv, const int32_t* n_tokens, const sym_sparse* sparse, hipStream_t st) {
+// The host half of a batch with sparse layers (lock held): plan, commit, lists to the device (unless stage is given: it receives the staging
+// buffer that holds them), batch open.
+int begin_sparse_locked(sym_ctx* c, int32_t n_lips, const sym_kv* kv, const int32_t* n_tokens, const sym_sparse* sparse, int* stage, hipStream_t st) {
   SparsePlan sp;
   int64_t tokens, runs, extra;
   int rc;
@@ -1035,16 +1036,18 @@ int begin_sparse_locked(sym_ctx* c, int32_t n_lips, const sym_kv* kv, const int3
   pb.words += extra;
   sp.on = true;
   c->pred.sparse = std::move(sp);
-  if ((rc = launch_prologue(c, pb.si, pb.words, nullptr, 0, nullptr, 0, nullptr, nullptr, st, pb.si))) return rc;
+  if (stage) *stage = pb.si;
+  else if ((rc = launch_prologue(c, pb.si, pb.words, nullptr, 0, nullptr, 0, nullptr, nullptr, st, pb.si))) return rc;
   open_batch(c, pb);
   return SYM_OK;
 }
-int sparse_layer_locked(sym_ctx* c, int32_t layer, const void* q, const void* k_new, const void* v_new, float* out, int32_t* picked, hipStream_t st) {
+int sparse_layer_locked(sym_ctx* c, int32_t layer, const void* q, const void* k_new, const void* v_new, float* out, int32_t* picked, int stage, hipStream_t st) {
   OpenPred& o = c->pred;
   uint8_t* ws = (uint8_t*)c->cfg.workspace;
+  const int32_t* lists = stage >= 0 ? c->stage[stage] : (const int32_t*)ws;
   if (o.n_cow > 0)       // the copies first: a page that the batch completes is read again for its bounds
-    if (int rc = launch_prologue(c, -1, 0, (const int32_t*)ws + o.cow_off, o.n_cow, nullptr, 0, nullptr, nullptr, st, -1, nullptr, true, layer)) return rc;
-  if (int rc = run_sparse_layer(c, o.sparse, ws, o.words, layer, q, k_new, v_new, out, picked, st)) return rc;
+    if (int rc = launch_prologue(c, -1, 0, lists + o.cow_off, o.n_cow, nullptr, 0, nullptr, nullptr, st, -1, nullptr, true, layer)) return rc;
+  if (int rc = run_sparse_layer(c, o.sparse, ws, o.words, layer, q, k_new, v_new, out, picked, stage, st)) return rc;
   layer_done(c, layer);
   return SYM_OK;
 }
@@ -1737,7 +1740,7 @@ int sym_pred_begin_sparse(sym_ctx* c, int32_t n_lips, const sym_kv* kv, const in
   return guarded(c, [&]() -> int {
     if (int busy = refuse_if_open(c, "pred_begin_sparse")) return busy;
     const OnDevice on(c);
-    return begin_sparse_locked(c, n_lips, kv, n_tokens, sparse, (hipStream_t)stream);
+    return begin_sparse_locked(c, n_lips, kv, n_tokens, sparse, nullptr, (hipStream_t)stream);
   });
 }
 
@@ -1753,7 +1756,7 @@ int sym_pred_layer_sparse(sym_ctx* c, int32_t layer, const void* q, const void* 
     int rc;
     if ((rc = check_layer_rows(c, q, k_new, v_new, out, picked)) || (rc = refuse_capture(c, st, "pred_layer_sparse"))) return rc;
     const OnDevice on(c);
-    return sparse_layer_locked(c, layer, q, k_new, v_new, out, picked, st);
+    return sparse_layer_locked(c, layer, q, k_new, v_new, out, picked, -1, st);
   });
 }
 
@@ -1772,8 +1775,9 @@ int sym_pred_sparse(sym_ctx* c, int32_t n_lips, const sym_kv* kv, const int32_t*
     const OnDevice on(c);
     sym_sparse only = *sparse;
     only.dense_layers = 0;
-    if ((rc = begin_sparse_locked(c, n_lips, kv, n_tokens, &only, st))) return rc;
-    rc = sparse_layer_locked(c, 0, q, k_new, v_new, out, picked, st);
+    int stage = -1;
+    if ((rc = begin_sparse_locked(c, n_lips, kv, n_tokens, &only, &stage, st))) return rc;
+    rc = sparse_layer_locked(c, 0, q, k_new, v_new, out, picked, stage, st);
     if (rc) c->pred.open = c->pred.sparse.on = false;
     return rc;
   });

@@ -307,11 +307,23 @@ __device__ __forceinline__ void append_run(SYM_AS4 AppendKernelArgs* ka, const i
     for (int g = threadIdx.x >> 6; g < Hkv; g += 4) page_bounds<E>(page + (int64_t)g * kSlab, b + g * (2 * kRowBytes));
   }
 }
+// The workgroups behind the runs' copy a batch's lists to the workspace for the launches that follow, 16 bytes per thread.
+__device__ __forceinline__ bool copy_lists(SYM_AS4 AppendKernelArgs* ka) {
+  const int blk = (int)blockIdx.x - ka->a.n_runs;
+  if (blk < 0) return false;
+  const uint4* src = (const uint4*)ka->a.host_words;
+  uint4* dst = (uint4*)ka->a.dev_words;
+  const int64_t n16 = (ka->a.copy_words + 3) / 4;      // the staging buffer is padded to 16 bytes
+  if (blockIdx.y == 0)
+    for (int64_t i = (int64_t)blk * 256 + threadIdx.x; i < n16; i += (int64_t)(gridDim.x - ka->a.n_runs) * 256) dst[i] = src[i];
+  return true;
+}
 template <typename E, int PATH>
 __global__ __launch_bounds__(256) void append_rope_kernel(AppendKernelArgs) {
   __shared__ double2 cs[PATH == ROPE_NONE ? 1 : kRunTokens][kPairs];
   __shared__ __align__(16) uint8_t stage[PATH == ROPE_HALVES_ANY ? 32 : 1][kRowBytes];
   auto ka = (SYM_AS4 AppendKernelArgs*)__builtin_amdgcn_kernarg_segment_ptr();
+  if (copy_lists(ka)) return;
   const int32_t* w = ka->a.runs + (int64_t)blockIdx.x * RUN_WORDS;
   append_run<E, PATH>(ka, sload(w), sload(w + 1), sload(w + 2), sload(w + 3), cs, stage);
 }
@@ -320,6 +332,7 @@ __global__ __launch_bounds__(256) void append_rope_runs_kernel(AppendRunsKernelA
   __shared__ double2 cs[PATH == ROPE_NONE ? 1 : kRunTokens][kPairs];
   __shared__ __align__(16) uint8_t stage[PATH == ROPE_HALVES_ANY ? 32 : 1][kRowBytes];
   auto ka = (SYM_AS4 AppendRunsKernelArgs*)__builtin_amdgcn_kernarg_segment_ptr();
+  if (copy_lists(&ka->k)) return;
   const auto* w = ka->runs.w + blockIdx.x * RUN_WORDS;
   append_run<E, PATH>(&ka->k, w[0], w[1], w[2], w[3], cs, stage);
 }
@@ -341,14 +354,15 @@ __global__ __launch_bounds__(256) void bounds_kernel(std::conditional_t<ARGS, Bo
 }
 
 // ---------------------------------------------------------------------------------------
-// Scores: for a new token and kv head, page p gets  sum_d A_d hi_d + B_d lo_d  with A_d = sum_h max(q_hd, 0), B_d = sum_h min(q_hd, 0) over the
-// G query heads of the kv head: what the sum of their logits with any key of the page does not exceed.  Products and sums in 64 bits
-// (the choice of pages hangs on comparisons of scores that lie close together; with sums in 32 bits it would depend on their order),
-// rounded to 32 at the end.  A wavefront takes one kv head and 32 pages; 32 lanes share a page's 512 bytes, a 16-byte chunk
-// each, with the chunk's coefficients in registers; eight pages a lane are then added up over the 32 lanes by halving exchanges.  Up
-// to RT consecutive tokens of a file share the pass.  Bound: HBM.
+// Choice of pages.  For a new token and kv head, page p scores  sum_d A_d hi_d + B_d lo_d  with A_d = sum_h max(q_hd, 0), B_d = sum_h min(q_hd, 0)
+// over the G query heads of the kv head: what the sum of their logits with any key of the page does not exceed.  Products and sums in 64
+// bits (the choice hangs on comparisons of scores that lie close together; with sums in 32 bits it would depend on their order),
+// rounded to 32 at the end and written down as whole numbers of the same order.
+// A wavefront takes one kv head and 32 pages; 32 lanes share a page's 512 bytes, a 16-byte chunk each, with the chunk's coefficients
+// in registers; eight pages a lane are then added up over the 32 lanes by halving exchanges.  Up to RT consecutive tokens of a file
+// share the pass.  Bound: HBM for one token, 64-bit arithmetic for four.
 // ---------------------------------------------------------------------------------------
-constexpr int kScorePages = 32;
+constexpr int kScorePages = 32;                  // of a wavefront
 __device__ __forceinline__ double as_f64(uint32_t lo, uint32_t hi) { return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo); }
 template <int CTRL>
 __device__ __forceinline__ double dpp_f64(double x) {
@@ -356,20 +370,28 @@ __device__ __forceinline__ double dpp_f64(double x) {
   return as_f64((uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)b, CTRL, 0xf, 0xf, false), (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(b >> 32), CTRL, 0xf, 0xf, false));
 }
 
+// A score as a whole number of the same order (NaN above all; never 0, which stands for none).
+__device__ __forceinline__ uint32_t order_of(float x) {
+  if (x != x) return 0xffffffffu;
+  const uint32_t b = as_u32(x + 0.0f);           // -0 and 0 are equal
+  return (b & 0x80000000u) ? ~b : b | 0x80000000u;
+}
+
 template <typename E, int RT>
 __global__ __launch_bounds__(256) void sparse_scores_kernel(SparseArgs a) {
   constexpr int C = E::kDimsPerChunk;
+  hold(a.groups, a.tables, a.bounds, a.q, a.scores, a.Hq, a.Hkv, a.first, a.score_stride);
   const int32_t* grp = a.groups + (int64_t)(a.group0 + blockIdx.y) * SPARSE_GROUP_WORDS;
-  const int r0 = sload(grp), nr = sload(grp + 1);
+  const int r0 = sload(grp), nr = sload(grp + 1), tbl = sload(grp + 2), end = sload(grp + 3);
   const int wave = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6)));
   const int head = wave % a.Hkv, p0 = a.first + wave / a.Hkv * kScorePages;
-  const int32_t* last_row = a.rows + (int64_t)(r0 + nr - 1) * SPARSE_ROW_WORDS;      // of consecutive tokens the last sees most
-  const int tbl = sload(last_row), end = (sload(last_row + 1) + kP - 1) / kP - a.last;
   if (p0 >= end) return;
+  const int32_t* pt = a.tables + tbl;
+  uint32_t* scores = a.scores + ((int64_t)(r0 - a.row0) * a.Hkv + head) * a.score_stride;
+  const int64_t row_scores = (int64_t)a.Hkv * a.score_stride;
   const int lane = threadIdx.x & 63, sub = lane >> 5, hl = lane & 31, part = hl >> 4, chunk = hl & 15;
   const uint8_t* rec = a.bounds + head * (2 * kRowBytes) + hl * 16;
   const int64_t page_rec = (int64_t)a.Hkv * (2 * kRowBytes);
-  const int32_t* pt = a.tables + tbl;
   int id[kScorePages / 2];
 #pragma unroll
   for (int s = 0; s < kScorePages / 2; ++s) id[s] = pt[min(p0 + 2 * s + sub, end - 1)];
@@ -422,191 +444,186 @@ __global__ __launch_bounds__(256) void sparse_scores_kernel(SparseArgs a) {
       }
       // lane octet (bit 4, bit 3) holds steps 4 bit4 + 2 bit3 + {0, 1} of the eight
       const int step = b * 8 + ((lane >> 4) & 1) * 4 + ((lane >> 3) & 1) * 2 + (lane & 1), p = p0 + 2 * step + sub;
-      const int row = r0 + t;
-      if (t < nr && (lane & 7) < 2) {
-        const int n = (a.rows[(int64_t)row * SPARSE_ROW_WORDS + 1] + kP - 1) / kP;
-        if (n > a.budget && p < n - a.last)
-          a.scores[((int64_t)(row - a.row0) * a.Hkv + head) * a.score_stride + (p - a.first)] = (float)((lane & 1) ? v[1] : v[0]);
-      }
+      // (a row's last pages may be scored beyond its need: its stretch has room for the most pages of any row)
+      if (t < nr && (lane & 7) < 2 && p < end) scores[t * row_scores + (p - a.first)] = order_of((float)((lane & 1) ? v[1] : v[0]));
     }
   }
 }
 
-// ---------------------------------------------------------------------------------------
-// Choice of pages, a workgroup to a (new token, kv head): the page ids to read, in the order of the file.  Scores become whole numbers of
-// the same order (NaN above all), the smallest chosen one is found bit by bit from the first bit in which the largest and
-// the smallest differ, counting with ballots, and of those equal to it the lowest indices are taken.
-// NT threads hold EPT scores each; EPT = 0: any number of scores, read again for every count.
-// ---------------------------------------------------------------------------------------
-__device__ __forceinline__ uint32_t order_of(float x) {
-  if (x != x) return 0xffffffffu;
-  const uint32_t b = as_u32(x + 0.0f);           // -0 and 0 are equal
-  return (b & 0x80000000u) ? ~b : b | 0x80000000u;
+constexpr int kAttendWaves = 4;
+struct ChooseLds {
+  __align__(16) uint32_t hist[4][256];                         // one for every round
+  uint2 total[kAttendWaves];                     // of every wavefront: greatest and least score, then how many are above and equal to the least chosen
+};
+
+// Sum over this lane and the higher ones of the wavefront: four DPP adds inside rows of 16 lanes, then the rows' totals.
+__device__ __forceinline__ uint32_t suffix_sum(uint32_t x) {
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x101, 0xf, 0xf, true);      // row_shl: 0 past the row's end
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x102, 0xf, 0xf, true);
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x104, 0xf, 0xf, true);
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x108, 0xf, 0xf, true);
+  const uint32_t t1 = (uint32_t)__builtin_amdgcn_readlane((int)x, 16), t2 = (uint32_t)__builtin_amdgcn_readlane((int)x, 32), t3 = (uint32_t)__builtin_amdgcn_readlane((int)x, 48);
+  const int row = (threadIdx.x & 63) >> 4;
+  return x + (row < 1 ? t1 : 0) + (row < 2 ? t2 : 0) + (row < 3 ? t3 : 0);
 }
-template <int NT, int EPT>
-__global__ __launch_bounds__(NT) void sparse_select_kernel(SparseArgs a) {
-  constexpr int W = NT / 64, N = EPT > 0 ? EPT : 1;
-  __shared__ uint32_t s_cnt[34], s_max, s_min, s_pre[N * W];
-  const int row = a.row0 + (int)blockIdx.x / a.Hkv, head = (int)blockIdx.x % a.Hkv;
-  const int32_t* rw = a.rows + (int64_t)row * SPARSE_ROW_WORDS;
-  const int32_t* pt = a.tables + sload(rw);
-  const int n = (sload(rw + 1) + kP - 1) / kP, kept = sload(rw + 2);
+// Sum over this lane and the lower ones.
+__device__ __forceinline__ uint32_t prefix_sum(uint32_t x) {
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xf, 0xf, true);      // row_shr
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xf, 0xf, true);
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xf, 0xf, true);
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xf, 0xf, true);
+  const uint32_t t0 = (uint32_t)__builtin_amdgcn_readlane((int)x, 15), t1 = (uint32_t)__builtin_amdgcn_readlane((int)x, 31), t2 = (uint32_t)__builtin_amdgcn_readlane((int)x, 47);
+  const int row = (threadIdx.x & 63) >> 4;
+  return x + (row > 0 ? t0 : 0) + (row > 1 ? t1 : 0) + (row > 2 ? t2 : 0);
+}
+// The greatest x of the wavefront, in every lane.
+__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x121, 0xf, 0xf, false));      // row_ror
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x122, 0xf, 0xf, false));
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x124, 0xf, 0xf, false));
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x128, 0xf, 0xf, false));
+  return max(max((uint32_t)__builtin_amdgcn_readlane((int)x, 0), (uint32_t)__builtin_amdgcn_readlane((int)x, 16)),
+             max((uint32_t)__builtin_amdgcn_readlane((int)x, 32), (uint32_t)__builtin_amdgcn_readlane((int)x, 48)));
+}
+
+// The `want` highest of the m scores (want < m), by the whole workgroup: put(i-th chosen, its index), in order of the index.
+// The smallest chosen score is found in at most four rounds: a histogram of 256 equal steps between the least and the greatest that it can be,
+// and the step in which the wanted one lies.  Usually a step that is wanted whole ends it.  A thread holds EPT scores in a row, so that
+// places are counted thread by thread; EPT = 0: any number of scores, sixteen at a time, read again for every round.
+template <int EPT, typename P>
+__device__ __forceinline__ void pick_highest(const uint32_t* sc, const int m, const int want, ChooseLds& s, const P& put) {
+  constexpr int W = kAttendWaves, NT = 64 * W, N = EPT > 0 ? EPT : 16;
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-  int32_t* list = a.lists + (int64_t)blockIdx.x * a.list_stride;
-  int32_t* picked = a.picked ? a.picked + ((int64_t)row * a.Hkv + head) * a.budget : nullptr;
-  auto put = [&](int at, int p) __attribute__((always_inline)) {
-    list[at] = pt[p];
-    if (picked) picked[at] = p;
-  };
-  if (picked)
-    for (int i = kept + tid; i < a.budget; i += NT) picked[i] = -1;
-  if (kept == n) {
-    for (int i = tid; i < n; i += NT) put(i, i);
-    return;
-  }
-  const int m = n - a.first - a.last, want = kept - a.first - a.last;
-  for (int i = tid; i < a.first; i += NT) put(i, i);
-  for (int i = tid; i < a.last; i += NT) put(kept - a.last + i, n - a.last + i);
-  if (want == 0) return;
-  const float* sc = a.scores + (int64_t)blockIdx.x * a.score_stride;
-  if (tid < 34) s_cnt[tid] = 0;
-  if (tid == 0) {
-    s_max = 0;
-    s_min = 0xffffffffu;
-  }
-  uint32_t key[N];                               // 0: none (order_of never gives it)
-  if constexpr (EPT > 0) {
+  const int per = EPT > 0 ? EPT : (m + 16 * NT - 1) / (16 * NT) * 16, i0 = tid * per;
+  uint32_t key[N];
+  auto fetch = [&](int from) __attribute__((always_inline)) {      // scores from .. from + N - 1; 0 past the end
+    if constexpr (EPT == 1) {
+      key[0] = sc[min(from, m - 1)];
+    } else {
 #pragma unroll
-    for (int e = 0; e < EPT; ++e) {
-      const int i = e * NT + tid;
-      key[e] = i < m ? order_of(sc[i]) : 0;
+      for (int v = 0; v < N / 4; ++v) {
+        const uint4 k = *(const uint4*)(sc + min(from + 4 * v, (m - 1) & ~3));
+        key[4 * v] = k.x;
+        key[4 * v + 1] = k.y;
+        key[4 * v + 2] = k.z;
+        key[4 * v + 3] = k.w;
+      }
     }
-  }
-  // f(key) of every score of this thread
-  auto each = [&](auto f) __attribute__((always_inline)) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) key[e] = from + e < m ? key[e] : 0u;
+  };
+  if constexpr (EPT > 0) fetch(i0);
+  auto each = [&](auto f) __attribute__((always_inline)) {          // f(index, key)
     if constexpr (EPT > 0) {
 #pragma unroll
-      for (int e = 0; e < EPT; ++e) f(key[e]);
+      for (int e = 0; e < EPT; ++e) f(i0 + e, key[e]);
     } else {
-      for (int i0 = 0; i0 < m; i0 += NT) f(i0 + tid < m ? order_of(sc[i0 + tid]) : 0u);
+      for (int x = 0; x < per; x += 16) {
+        fetch(i0 + x);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) f(i0 + x + e, key[e]);
+      }
     }
   };
-  uint32_t hi = 0, lo = 0xffffffffu;
-  each([&](uint32_t k) {
+  for (int i = tid; i < 4 * 256; i += NT) (&s.hist[0][0])[i] = 0;
+  uint32_t lo, hi = 0, top = 0;                  // top: the greatest ~key
+  each([&](int, uint32_t k) {
     hi = max(hi, k);
-    lo = min(lo, k ? k : 0xffffffffu);
+    top = max(top, k ? ~k : 0u);
   });
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    hi = max(hi, (uint32_t)__shfl_xor((int)hi, o));
-    lo = min(lo, (uint32_t)__shfl_xor((int)lo, o));
-  }
+  hi = wave_max(hi);
+  top = wave_max(top);
+  if (lane == 0) s.total[w] = make_uint2(hi, top);
   __syncthreads();
-  if (lane == 0) {
-    atomicMax(&s_max, hi);
-    atomicMin(&s_min, lo);
+#pragma unroll
+  for (int x = 0; x < W; ++x) {
+    hi = max(hi, s.total[x].x);
+    top = max(top, s.total[x].y);
   }
+  hi = __builtin_amdgcn_readfirstlane(hi);
+  lo = __builtin_amdgcn_readfirstlane(~top);
+  uint32_t need = (uint32_t)want, t;             // chosen: above t, and the first `need` of those equal to it
+  for (int round = 0;; ++round) {
+    const uint32_t width = hi - lo;
+    const int shift = width < 256 ? 0 : 24 - __clz((int)width);
+    uint32_t* h = s.hist[round];
+    each([&](int, uint32_t k) {
+      if (k - lo <= width) atomicAdd(&h[(k - lo) >> shift], 1u);      // (0, for none, is below every lo)
+    });
+    __syncthreads();
+    // every wavefront for itself: lane l has steps 4 l .. 4 l + 3
+    const uint4 c = *(const uint4*)(h + 4 * lane);
+    const uint32_t own = c.x + c.y + c.z + c.w;
+    const uint32_t sum = suffix_sum(own);
+    const int at = 63 - __clzll((long long)__builtin_amdgcn_ballot_w64(sum >= need));      // the highest lane with enough from its steps on
+    uint32_t above = (uint32_t)__builtin_amdgcn_readlane((int)(sum - own), at);
+    const uint32_t cx = (uint32_t)__builtin_amdgcn_readlane((int)c.x, at), cy = (uint32_t)__builtin_amdgcn_readlane((int)c.y, at);
+    const uint32_t cz = (uint32_t)__builtin_amdgcn_readlane((int)c.z, at), cw = (uint32_t)__builtin_amdgcn_readlane((int)c.w, at);
+    uint32_t step = 4 * at + 3, count = cw;
+    if (above + count < need) above += count, --step, count = cz;
+    if (above + count < need) above += count, --step, count = cy;
+    if (above + count < need) above += count, --step, count = cx;
+    need -= above;
+    lo += step << shift;
+    if (need == count) {                         // the whole step
+      t = lo - 1;
+      need = 0;
+      break;
+    }
+    if (shift == 0) {                            // all of one value
+      t = lo;
+      break;
+    }
+    hi = min(hi, lo + ((1u << shift) - 1));
+  }
+  // Place of a chosen one: those above t before it, and at most `need` of the equal ones before it.
+  uint32_t gt = 0, eq = 0;
+  each([&](int, uint32_t k) {
+    gt += k > t ? 1 : 0;
+    eq += k == t ? 1 : 0;
+  });
+  const uint32_t g_to = prefix_sum(gt), q_to = prefix_sum(eq);
+  __syncthreads();                               // (s.total is read above)
+  if (lane == 63) s.total[w] = make_uint2(g_to, q_to);
   __syncthreads();
-  hi = s_max;
-  lo = s_min;
-  // keys of at least x
-  auto count = [&](uint32_t x, int at) __attribute__((always_inline)) {
-    uint32_t c = 0;
-    each([&](uint32_t k) { c += (uint32_t)__popcll(__builtin_amdgcn_ballot_w64(k >= x)); });
-    if (lane == 0) atomicAdd(&s_cnt[at], c);
-    __syncthreads();
-    return s_cnt[at];
-  };
-  // the largest t with at least `want` keys >= t: from the bits that all keys share, the next lower bit each time
-  uint32_t t = hi;
-  if (hi != lo) {
-    const int top = 31 - __clz((int)(hi ^ lo));
-    t = hi & ~((2u << top) - 1);
-    for (int b = top; b >= 0; --b)
-      if (count(t | (1u << b), b) >= (uint32_t)want) t |= 1u << b;
+  uint32_t g = g_to - gt, q = q_to - eq;
+#pragma unroll
+  for (int x = 0; x < W; ++x) {
+    g += x < w ? s.total[x].x : 0;
+    q += x < w ? s.total[x].y : 0;
   }
-  const uint32_t above = t == 0xffffffffu ? 0 : count(t + 1, 32);
-  const uint32_t need = (uint32_t)want - above;  // of those equal to t
-  // Place of a chosen page among the chosen: those above t before it, and of the equal ones before it at most `need`.
-  if constexpr (EPT > 0) {
-    static_assert(NT * EPT < 65536, "two counts of 16 bits in a word");
-    uint64_t gt[N], eq[N];
-#pragma unroll
-    for (int e = 0; e < EPT; ++e) {
-      gt[e] = __builtin_amdgcn_ballot_w64(key[e] > t);
-      eq[e] = __builtin_amdgcn_ballot_w64(key[e] == t);
-      if (lane == 0) s_pre[e * W + w] = (uint32_t)__popcll(gt[e]) | (uint32_t)__popcll(eq[e]) << 16;
-    }
-    __syncthreads();
-    if (w == 0) {                                // exclusive sums over the N * W words, a stretch to each lane
-      constexpr int PER = (N * W + 63) / 64;
-      uint32_t g = 0, q = 0;
-#pragma unroll
-      for (int i = 0; i < PER; ++i)
-        if (lane * PER + i < N * W) {
-          g += s_pre[lane * PER + i] & 0xffff;
-          q += s_pre[lane * PER + i] >> 16;
-        }
-      uint32_t gs = g, qs = q;
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const uint32_t x = (uint32_t)__shfl_up((int)gs, o), y = (uint32_t)__shfl_up((int)qs, o);
-        if (lane >= o) {
-          gs += x;
-          qs += y;
-        }
-      }
-      gs -= g;
-      qs -= q;
-#pragma unroll
-      for (int i = 0; i < PER; ++i)
-        if (lane * PER + i < N * W) {
-          const uint32_t c = s_pre[lane * PER + i];
-          s_pre[lane * PER + i] = gs | qs << 16;
-          gs += c & 0xffff;
-          qs += c >> 16;
-        }
-    }
-    __syncthreads();
-    const uint64_t below = (1ull << lane) - 1;
-#pragma unroll
-    for (int e = 0; e < EPT; ++e) {
-      const uint32_t pre = s_pre[e * W + w];
-      const uint32_t g = (pre & 0xffff) + (uint32_t)__popcll(gt[e] & below), q = (pre >> 16) + (uint32_t)__popcll(eq[e] & below);
-      if (key[e] > t || (key[e] == t && q < need)) put(a.first + (int)(g + min(q, need)), a.first + e * NT + tid);
-    }
-  } else {
-    uint32_t g0 = 0, q0 = 0;
-    const uint64_t below = (1ull << lane) - 1;
-    for (int i0 = 0; i0 < m; i0 += NT) {
-      const uint32_t k = i0 + tid < m ? order_of(sc[i0 + tid]) : 0u;
-      const uint64_t gt = __builtin_amdgcn_ballot_w64(k > t), eq = __builtin_amdgcn_ballot_w64(k == t);
-      if (lane == 0) s_pre[w] = (uint32_t)__popcll(gt) | (uint32_t)__popcll(eq) << 16;
-      __syncthreads();
-      uint32_t g = g0, q = q0;
-      for (int x = 0; x < W; ++x) {
-        const uint32_t c = s_pre[x];
-        if (x < w) {
-          g += c & 0xffff;
-          q += c >> 16;
-        }
-        g0 += c & 0xffff;
-        q0 += c >> 16;
-      }
-      __syncthreads();                           // before the next round's counts
-      g += (uint32_t)__popcll(gt & below);
-      q += (uint32_t)__popcll(eq & below);
-      if (k > t || (k == t && q < need)) put(a.first + (int)(g + min(q, need)), a.first + i0 + tid);
-    }
-  }
+  each([&](int i, uint32_t k) {
+    if (k < t || k == 0) return;
+    if (k > t || q < need) put((int)(g + min(q, need)), i);
+    g += k > t ? 1 : 0;
+    q += k == t ? 1 : 0;
+  });
 }
 
 // ---------------------------------------------------------------------------------------
-// Attention over the listed pages of a (new token, kv head): a workgroup of four wavefronts to each of `splits` equal parts of the list.
-// The list is read like a file's page table: only its last page may be partly filled.  One pass, with the running maximum and sum
-// of the softmax in fp32; the wavefronts' results are combined through LDS, those of several parts by the merge kernel.
-// Bound: HBM (8 KiB for 4 D 16 G flops).
+// Attention over the chosen pages of a (new token, kv head): a workgroup of four wavefronts to each of `splits` equal parts of their list.
+// Every workgroup chooses from the row's scores for itself and keeps its part of the list in LDS, where it reads like a
+// file's page table: only the last page may be partly filled.  One pass over the pages, with the running maximum and sum of the softmax in
+// fp32; the wavefronts' results are combined through LDS.  The workgroup that finishes last of a row's parts joins them, so that no
+// launch follows.  Bound: HBM (8 KiB for 4 D 16 G flops).
 // ---------------------------------------------------------------------------------------
+// What workgroups of one launch hand to each other goes past the caches that they do not share, in both directions, and a workgroup
+// counts itself done when its stores have arrived.  (A release fence instead writes back everything in the L2: with one from every
+// wavefront the choice among 5000 pages took 470 us instead of 40.)
+__device__ __forceinline__ void hand_over(float* p, float x) { __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ float take(const float* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+// Whether this workgroup is the last of `all` to come; every thread calls it, behind its stores.  The counter is 0 again for the next launch.
+__device__ __forceinline__ bool comes_last(int32_t* counter, const int all, int& shared) {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    shared = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == all - 1;
+    if (shared) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  __syncthreads();
+  return shared;
+}
+
 // bf16 storage: on the matrix cores, an fp32 weight cut into three bf16 numbers (8 bits each: exact), as in decode_bins_mx.  Where 3 G columns fit
 // into 16 each takes a column of one product.  With 8 heads per kv head there are two products to the same sums: the upper part halved in columns 0..7
 // of both (0 there would make an infinite V NaN), the middle and the lower part in columns 8..15.  (Weights cut to 16 bits in one
@@ -834,28 +851,69 @@ struct AttendF32 {
   }
 };
 
-constexpr int kAttendWaves = 4;
 template <typename AT, int G>
 __global__ __launch_bounds__(64 * kAttendWaves, 2) void sparse_attend_kernel(SparseArgs a) {
   constexpr int D = AT::D, NT = 64 * kAttendWaves;
-  __shared__ __align__(16) float s_acc[kAttendWaves][G * D];
+  // the choice's counts, then the wavefronts' results
+  constexpr int kResult = kAttendWaves * G * D * 4;
+  __shared__ __align__(16) uint8_t s_mem[kResult > (int)sizeof(ChooseLds) ? kResult : (int)sizeof(ChooseLds)];
   __shared__ __align__(16) float s_ml[kAttendWaves][2 * G];
+  __shared__ int32_t s_list[kPartPages];
+  __shared__ int s_last;
+  hold(a.rows, a.tables, a.scores, a.pool, a.page_bytes, a.q, a.out, a.picked, a.Hq, a.Hkv, a.budget, a.first, a.last, a.splits);
   const int unit = (int)blockIdx.x / a.splits, split = (int)blockIdx.x - unit * a.splits;
   const int row = a.row0 + unit / a.Hkv, head = unit % a.Hkv;
   const int32_t* rw = a.rows + (int64_t)row * SPARSE_ROW_WORDS;
-  const int vis = sload(rw + 1), kept = sload(rw + 2);
+  const int32_t* pt = a.tables + sload(rw);
+  const int vis = sload(rw + 1), n = (vis + kP - 1) / kP, kept = min(n, a.budget);
   const int tail = (vis - 1) % kP + 1;           // tokens of the last page
   const int wv = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-  const int parts = a.splits * kAttendWaves, mine = split * kAttendWaves + wv;
-  int p = (int)((int64_t)kept * mine / parts);
-  const int pe = (int)((int64_t)kept * (mine + 1) / parts);
-  const int32_t* list = a.lists + (int64_t)unit * a.list_stride;
-  const uint8_t* pool = a.pool + (int64_t)head * kSlab;
   AT at;
-  PageRegs A, B;
-  auto id = [&](int i) __attribute__((always_inline)) { return (int64_t)sload(list + min(i, kept - 1)); };      // past the part's end: read, not used
-  at.request(A, pool + id(p) * a.page_bytes);
   at.start((const uint8_t*)a.q + ((int64_t)row * a.Hq + head * G) * kRowBytes, a.scale_log2e);
+  // this workgroup's part of the list
+  const int lo = (int)((int64_t)kept * split / a.splits), hi = (int)((int64_t)kept * (split + 1) / a.splits);
+  int32_t* picked = a.picked ? a.picked + ((int64_t)row * a.Hkv + head) * a.budget : nullptr;
+  auto put = [&](int i, int p) __attribute__((always_inline)) {
+    if (i < lo || i >= hi) return;
+    s_list[i - lo] = pt[p];
+    if (picked) picked[i] = p;
+  };
+  if (n <= a.budget) {
+    for (int i = lo + threadIdx.x; i < hi; i += NT) put(i, i);
+    if (picked && split == 0)
+      for (int i = n + threadIdx.x; i < a.budget; i += NT) picked[i] = -1;
+  } else {
+    for (int i = threadIdx.x; i < a.first + a.last; i += NT) {
+      if (i < a.first) put(i, i);
+      else put(kept - a.last + i - a.first, n - a.last + i - a.first);
+    }
+    const int m = n - a.first - a.last, want = kept - a.first - a.last;
+    const uint32_t* sc = a.scores + (int64_t)unit * a.score_stride;
+    auto chosen = [&](int i, int p) __attribute__((always_inline)) { put(a.first + i, a.first + p); };
+    ChooseLds& s = *(ChooseLds*)s_mem;
+    if (want == 0) {
+    } else if (m <= NT) {
+      pick_highest<1>(sc, m, want, s, chosen);
+    } else if (m <= 4 * NT) {
+      pick_highest<4>(sc, m, want, s, chosen);
+    } else if (m <= 8 * NT) {
+      pick_highest<8>(sc, m, want, s, chosen);
+    } else if (m <= 16 * NT) {
+      pick_highest<16>(sc, m, want, s, chosen);
+    } else if (m <= 32 * NT) {
+      pick_highest<32>(sc, m, want, s, chosen);
+    } else {
+      pick_highest<0>(sc, m, want, s, chosen);
+    }
+  }
+  __syncthreads();
+  int p = lo + (int)((int64_t)(hi - lo) * wv / kAttendWaves);
+  const int pe = lo + (int)((int64_t)(hi - lo) * (wv + 1) / kAttendWaves);
+  const uint8_t* pool = a.pool + (int64_t)head * kSlab;
+  PageRegs A, B;
+  // (past the wavefront's pages: another page of the part, read and not used; a part has a page at least)
+  auto id = [&](int i) __attribute__((always_inline)) { return (int64_t)__builtin_amdgcn_readfirstlane(s_list[min(i, hi - 1) - lo]); };
+  at.request(A, pool + id(p) * a.page_bytes);
   while (p < pe) {
     at.request(B, pool + id(p + 1) * a.page_bytes);
     at.page(A, p == kept - 1 ? tail : kP);
@@ -864,6 +922,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void sparse_attend_kernel(Spa
     at.page(B, p == kept - 1 ? tail : kP);
     ++p;
   }
+  float (*s_acc)[G * D] = (float (*)[G * D])s_mem;
   at.finish(s_acc[wv], s_ml[wv]);
   __syncthreads();
   float* out = a.out + ((int64_t)row * a.Hq + head * G) * D;
@@ -882,9 +941,42 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void sparse_attend_kernel(Spa
     if (a.splits == 1) {
       out[x] = num / den;
     } else {
-      a.part_acc[slot * G * D + x] = num;
-      if (x % D == 0) *(float2*)(a.part_ml + (slot * G + h) * 2) = make_float2(M, den);
+      hand_over(a.part_acc + slot * G * D + x, num);
+      if (x % D == 0) {
+        hand_over(a.part_ml + (slot * G + h) * 2, M);
+        hand_over(a.part_ml + (slot * G + h) * 2 + 1, den);
+      }
     }
+  }
+  if (a.splits == 1 || !comes_last(a.counters + unit, a.splits, s_last)) return;
+  const int64_t first = (int64_t)unit * a.splits;
+  for (int x = threadIdx.x; x < G * D; x += NT) {      // the parts in their order, whoever came last
+    const int h = x / D;
+    float M = -1e30f, num = 0.f, den = 0.f;
+    for (int i0 = 0; i0 < a.splits; i0 += 8) {         // eight parts' loads in flight
+      float2 ml[8];
+      float v[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int64_t i = first + min(i0 + u, a.splits - 1);
+        ml[u] = make_float2(take(a.part_ml + (i * G + h) * 2), take(a.part_ml + (i * G + h) * 2 + 1));
+        v[u] = take(a.part_acc + i * G * D + x);
+      }
+      float mn = M;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) mn = fmaxf(mn, ml[u].x);
+      const float f0 = __builtin_amdgcn_exp2f(M - mn);
+      num *= f0;
+      den *= f0;
+      M = mn;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const float f = i0 + u < a.splits ? __builtin_amdgcn_exp2f(ml[u].x - M) : 0.f;
+        num = __builtin_fmaf(i0 + u < a.splits ? v[u] : 0.f, f, num);      // (0 * Inf is NaN)
+        den = __builtin_fmaf(ml[u].y, f, den);
+      }
+    }
+    out[x] = num / den;
   }
 }
 
@@ -925,7 +1017,8 @@ hipError_t launch_rope_rows(RopeRowsArgs a, const RopeTable& r, int dtype, hipSt
 hipError_t launch_append_rope(const AppendRopeArgs& a, const RopeTable& r, int dtype, hipStream_t st) {
   if (a.n_runs <= 0) return a.done ? hipEventRecord(a.done, st) : hipSuccess;
   if (a.n_layers < 1 || a.n_layers > 65535) return hipErrorInvalidValue;
-  const dim3 grid((unsigned)a.n_runs, (unsigned)a.n_layers), block(256);
+  const int64_t copy = std::min<int64_t>((a.copy_words / 4 + 255) / 256 + (a.copy_words > 0), 256);
+  const dim3 grid((unsigned)(a.n_runs + copy), (unsigned)a.n_layers), block(256);
   if (a.by_args) {
     if (a.n_runs > kArgRuns) return hipErrorInvalidValue;
     AppendRunsKernelArgs ka;
@@ -966,10 +1059,10 @@ hipError_t launch_bounds(const BoundsArgs& a, int dtype, hipStream_t st) {
 }
 
 hipError_t launch_sparse_scores(const SparseArgs& a, int dtype, hipStream_t st) {
-  if (a.n_groups <= 0 || a.most_scored <= 0) return hipSuccess;
+  if (a.n_groups <= 0) return hipSuccess;
   const int64_t waves = (int64_t)((a.most_scored + kScorePages - 1) / kScorePages) * a.Hkv;
-  const dim3 grid((unsigned)((waves + 3) / 4), (unsigned)a.n_groups), block(256);
   if (a.n_groups > 65535) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)((waves + 3) / 4), (unsigned)a.n_groups), block(256);
   if (dtype == 0) {
     if (a.group_rows == 1) hipLaunchKernelGGL((sparse_scores_kernel<ElemF32, 1>), grid, block, 0, st, a);
     else hipLaunchKernelGGL((sparse_scores_kernel<ElemF32, kGroupRows>), grid, block, 0, st, a);
@@ -977,20 +1070,6 @@ hipError_t launch_sparse_scores(const SparseArgs& a, int dtype, hipStream_t st) 
     if (a.group_rows == 1) hipLaunchKernelGGL((sparse_scores_kernel<ElemBF16, 1>), grid, block, 0, st, a);
     else hipLaunchKernelGGL((sparse_scores_kernel<ElemBF16, kGroupRows>), grid, block, 0, st, a);
   }
-  return hipGetLastError();
-}
-
-hipError_t launch_sparse_select(const SparseArgs& a, hipStream_t st) {
-  if (a.n_rows <= 0) return hipSuccess;
-  const dim3 grid((unsigned)a.n_rows * a.Hkv);
-  const int m = a.most_scored;
-#define SYM_SELECT(NT, EPT) hipLaunchKernelGGL((sparse_select_kernel<NT, EPT>), grid, dim3(NT), 0, st, a)
-  if (m <= 256) SYM_SELECT(256, 1);
-  else if (m <= 1024) SYM_SELECT(256, 4);
-  else if (m <= 4096) SYM_SELECT(512, 8);
-  else if (m <= 16384) SYM_SELECT(1024, 16);
-  else SYM_SELECT(1024, 0);
-#undef SYM_SELECT
   return hipGetLastError();
 }
 

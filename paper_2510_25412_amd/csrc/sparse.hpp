@@ -43,6 +43,9 @@ struct AppendRopeArgs {
   const int32_t* runs;      // host (at most kArgRuns), or pinned / device
   int32_t n_runs, Hq, Hkv, n_layers;
   int32_t by_args;          // the runs are host memory and travel with the arguments
+  const int32_t* host_words;   // lists to be copied along the way: pinned host memory, where to, how many words
+  int32_t* dev_words;
+  int64_t copy_words;
   hipEvent_t done;
 };
 
@@ -57,9 +60,11 @@ struct BoundsArgs {
   int32_t by_args;
 };
 
-constexpr int SPARSE_ROW_WORDS = 4;    // page table (offset into the tables), tokens seen, pages read, 0
-constexpr int SPARSE_GROUP_WORDS = 2;  // first row, rows: consecutive tokens of one file, scored together
+constexpr int SPARSE_ROW_WORDS = 2;    // page table (offset into the tables), tokens seen
+// Consecutive tokens of one file, scored together: first row, rows, page table (offset into the tables), end of the pages to score.
+constexpr int SPARSE_GROUP_WORDS = 4;
 constexpr int kGroupRows = 4;
+constexpr int kPartPages = 2048;       // most pages of a part of a row's list (one workgroup's)
 struct SparseArgs {
   const uint8_t* pool;
   int64_t page_bytes;
@@ -70,15 +75,15 @@ struct SparseArgs {
   const int32_t* rows;      // [rows][SPARSE_ROW_WORDS]
   const int32_t* groups;    // [n_groups][SPARSE_GROUP_WORDS]
   const int32_t* tables;
-  float* scores;            // [rows of the launch][Hkv][score_stride]
-  int32_t* lists;           // [rows of the launch][Hkv][list_stride]: pool pages that a row reads
+  uint32_t* scores;         // [rows of the launch][Hkv][score_stride]: in the order of the scores, from page `first` on
   float* part_acc;          // [rows of the launch][Hkv][splits][G][D]
   float* part_ml;           // [rows of the launch][Hkv][splits][G][2]
+  int32_t* counters;        // [rows of the launch][Hkv]: parts that are done (several parts); 0 between launches
   int32_t row0, n_rows;     // rows of this launch
-  int32_t group0, n_groups, group_rows;   // groups of this launch that need scores, and the most rows of one
+  int32_t group0, n_groups, group_rows;   // groups of this launch, which need scores, and the most rows of one
+  int32_t most_scored;      // pages of the group with most to score
   int32_t Hq, Hkv, budget, first, last;
-  int32_t score_stride, list_stride;
-  int32_t most_scored;      // pages of the row with most to score
+  int32_t score_stride;
   int32_t splits;
   float scale_log2e;
 };
@@ -89,7 +94,6 @@ SYMKV_LAUNCH hipError_t launch_rope_rows(RopeRowsArgs a, const RopeTable& r, int
 SYMKV_LAUNCH hipError_t launch_append_rope(const AppendRopeArgs& a, const RopeTable& r, int dtype, hipStream_t st);
 SYMKV_LAUNCH hipError_t launch_bounds(const BoundsArgs& a, int dtype, hipStream_t st);
 SYMKV_LAUNCH hipError_t launch_sparse_scores(const SparseArgs& a, int dtype, hipStream_t st);
-SYMKV_LAUNCH hipError_t launch_sparse_select(const SparseArgs& a, hipStream_t st);
 SYMKV_LAUNCH hipError_t launch_sparse_attend(const SparseArgs& a, int dtype, hipStream_t st);
 // Makes the device current and returns the one that was (-1: nothing to undo); the other way round.
 SYMKV_LAUNCH int enter_device(int device);
