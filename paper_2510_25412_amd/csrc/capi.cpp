@@ -997,7 +997,7 @@ int run_sparse_layer(sym_ctx* c, const SparsePlan& sp, uint8_t* ws, int64_t word
     a.most_scored = s.most_scored;
     hipError_t e = hipSuccess;
     {
-      Timed t(c, SYM_K_ATTN, st, false, true, 1 + (s.groups > 0));
+      Timed t(c, SYM_K_ATTN, st, false, true, 1 + (s.groups > 0 && !sparse_scores_itself(a)));
       if (s.groups > 0) e = launch_sparse_scores(a, c->cfg.dtype, st);
       if (e == hipSuccess) e = launch_sparse_attend(a, c->cfg.dtype, st);
     }

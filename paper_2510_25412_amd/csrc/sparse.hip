@@ -377,77 +377,96 @@ __device__ __forceinline__ uint32_t order_of(float x) {
   return (b & 0x80000000u) ? ~b : b | 0x80000000u;
 }
 
+// A wavefront's scores of 32 pages at a time, for one kv head and up to RT consecutive tokens.
+template <typename E, int RT>
+struct Scorer {
+  static constexpr int C = E::kDimsPerChunk;
+  double cf[RT][C];                              // coefficients of this lane's chunk: lanes 0..15 of a page hold lo, 16..31 hi
+  int id[kScorePages / 2];                       // pages 2 s + (upper half of the wavefront)
+
+  __device__ __forceinline__ void coefficients(const SparseArgs& a, const int r0, const int nr, const int head) {
+    const int hl = threadIdx.x & 31, part = hl >> 4, chunk = hl & 15, G = a.Hq / a.Hkv;
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+#pragma unroll
+      for (int e = 0; e < C; ++e) cf[t][e] = 0.0;
+      const uint8_t* q = (const uint8_t*)a.q + ((int64_t)(r0 + min(t, nr - 1)) * a.Hq + head * G) * kRowBytes + chunk * 16;
+      for (int h = 0; h < G; ++h) {
+        float x[C];
+        E::unpack(*(const uint4*)(q + h * kRowBytes), x);
+#pragma unroll
+        for (int e = 0; e < C; ++e) cf[t][e] += (double)(part ? (x[e] < 0.f ? 0.f : x[e]) : (x[e] > 0.f ? 0.f : x[e]));
+      }
+    }
+  }
+  __device__ __forceinline__ void ids(const int32_t* pt, const int p0, const int end) {
+#pragma unroll
+    for (int s = 0; s < kScorePages / 2; ++s) id[s] = pt[min(p0 + 2 * s + (int)((threadIdx.x & 63) >> 5), end - 1)];
+  }
+  // put(token, page, key) of the pages p0 .. of id, below end; next() runs when id has been used
+  template <typename N, typename P>
+  __device__ __forceinline__ void score(const SparseArgs& a, const int head, const int p0, const int end, const N& next, const P& put) {
+    const int lane = threadIdx.x & 63, sub = lane >> 5, hl = lane & 31;
+    const uint8_t* rec = a.bounds + head * (2 * kRowBytes) + hl * 16;
+    const int64_t page_rec = (int64_t)a.Hkv * (2 * kRowBytes);
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      uint4 x[8];
+#pragma unroll
+      for (int s = 0; s < 8; ++s) x[s] = *(const uint4*)(rec + (int64_t)id[b * 8 + s] * page_rec);
+      if (b == 1) next();
+#pragma unroll
+      for (int t = 0; t < RT; ++t) {
+        double v[8];
+#pragma unroll
+        for (int s = 0; s < 8; ++s) {
+          float f[C];
+          E::unpack(x[s], f);
+          v[s] = 0.0;
+#pragma unroll
+          for (int e = 0; e < C; ++e) v[s] = __builtin_fma(cf[t][e], (double)f[e], v[s]);
+        }
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {            // lane bit 4: even rows of 16 lanes keep pages 0..3, odd ones 4..7
+          const uint64_t p = __builtin_bit_cast(uint64_t, v[s]), q = __builtin_bit_cast(uint64_t, v[s + 4]);
+          const auto lo = __builtin_amdgcn_permlane16_swap((uint32_t)p, (uint32_t)q, false, false);
+          const auto hi = __builtin_amdgcn_permlane16_swap((uint32_t)(p >> 32), (uint32_t)(q >> 32), false, false);
+          v[s] = as_f64(lo[0], hi[0]) + as_f64(lo[1], hi[1]);
+        }
+        const bool b3 = (lane & 8) != 0;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {            // lane bit 3
+          const double keep = b3 ? v[s + 2] : v[s], send = b3 ? v[s] : v[s + 2];
+          v[s] = keep + dpp_f64<0x128>(send);    // row_ror:8
+          v[s] += dpp_f64<0xB1>(v[s]);           // the octet's sum
+          v[s] += dpp_f64<0x4E>(v[s]);
+          v[s] += dpp_f64<0x141>(v[s]);
+        }
+        // lane octet (bit 4, bit 3) holds steps 4 bit4 + 2 bit3 + {0, 1} of the eight
+        const int step = b * 8 + ((lane >> 4) & 1) * 4 + ((lane >> 3) & 1) * 2 + (lane & 1), p = p0 + 2 * step + sub;
+        if ((lane & 7) < 2 && p < end) put(t, p, order_of((float)((lane & 1) ? v[1] : v[0])));
+      }
+    }
+  }
+};
+
 template <typename E, int RT>
 __global__ __launch_bounds__(256) void sparse_scores_kernel(SparseArgs a) {
-  constexpr int C = E::kDimsPerChunk;
   hold(a.groups, a.tables, a.bounds, a.q, a.scores, a.Hq, a.Hkv, a.first, a.score_stride);
   const int32_t* grp = a.groups + (int64_t)(a.group0 + blockIdx.y) * SPARSE_GROUP_WORDS;
   const int r0 = sload(grp), nr = sload(grp + 1), tbl = sload(grp + 2), end = sload(grp + 3);
   const int wave = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6)));
   const int head = wave % a.Hkv, p0 = a.first + wave / a.Hkv * kScorePages;
   if (p0 >= end) return;
-  const int32_t* pt = a.tables + tbl;
   uint32_t* scores = a.scores + ((int64_t)(r0 - a.row0) * a.Hkv + head) * a.score_stride;
   const int64_t row_scores = (int64_t)a.Hkv * a.score_stride;
-  const int lane = threadIdx.x & 63, sub = lane >> 5, hl = lane & 31, part = hl >> 4, chunk = hl & 15;
-  const uint8_t* rec = a.bounds + head * (2 * kRowBytes) + hl * 16;
-  const int64_t page_rec = (int64_t)a.Hkv * (2 * kRowBytes);
-  int id[kScorePages / 2];
-#pragma unroll
-  for (int s = 0; s < kScorePages / 2; ++s) id[s] = pt[min(p0 + 2 * s + sub, end - 1)];
-  // coefficients of this lane's chunk: lanes 0..15 of a page hold lo, 16..31 hi
-  double cf[RT][C];
-  const int G = a.Hq / a.Hkv;
-#pragma unroll
-  for (int t = 0; t < RT; ++t) {
-#pragma unroll
-    for (int e = 0; e < C; ++e) cf[t][e] = 0.0;
-    const uint8_t* q = (const uint8_t*)a.q + ((int64_t)(r0 + min(t, nr - 1)) * a.Hq + head * G) * kRowBytes + chunk * 16;
-    for (int h = 0; h < G; ++h) {
-      float x[C];
-      E::unpack(*(const uint4*)(q + h * kRowBytes), x);
-#pragma unroll
-      for (int e = 0; e < C; ++e) cf[t][e] += (double)(part ? (x[e] < 0.f ? 0.f : x[e]) : (x[e] > 0.f ? 0.f : x[e]));
-    }
-  }
-#pragma unroll
-  for (int b = 0; b < 2; ++b) {
-    uint4 x[8];
-#pragma unroll
-    for (int s = 0; s < 8; ++s) x[s] = *(const uint4*)(rec + (int64_t)id[b * 8 + s] * page_rec);
-#pragma unroll
-    for (int t = 0; t < RT; ++t) {
-      double v[8];
-#pragma unroll
-      for (int s = 0; s < 8; ++s) {
-        float f[C];
-        E::unpack(x[s], f);
-        v[s] = 0.0;
-#pragma unroll
-        for (int e = 0; e < C; ++e) v[s] = __builtin_fma(cf[t][e], (double)f[e], v[s]);
-      }
-#pragma unroll
-      for (int s = 0; s < 4; ++s) {              // lane bit 4: even rows of 16 lanes keep pages 0..3, odd ones 4..7
-        const uint64_t p = __builtin_bit_cast(uint64_t, v[s]), q = __builtin_bit_cast(uint64_t, v[s + 4]);
-        const auto lo = __builtin_amdgcn_permlane16_swap((uint32_t)p, (uint32_t)q, false, false);
-        const auto hi = __builtin_amdgcn_permlane16_swap((uint32_t)(p >> 32), (uint32_t)(q >> 32), false, false);
-        v[s] = as_f64(lo[0], hi[0]) + as_f64(lo[1], hi[1]);
-      }
-      const bool b3 = (lane & 8) != 0;
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {              // lane bit 3
-        const double keep = b3 ? v[s + 2] : v[s], send = b3 ? v[s] : v[s + 2];
-        v[s] = keep + dpp_f64<0x128>(send);      // row_ror:8
-        v[s] += dpp_f64<0xB1>(v[s]);             // the octet's sum
-        v[s] += dpp_f64<0x4E>(v[s]);
-        v[s] += dpp_f64<0x141>(v[s]);
-      }
-      // lane octet (bit 4, bit 3) holds steps 4 bit4 + 2 bit3 + {0, 1} of the eight
-      const int step = b * 8 + ((lane >> 4) & 1) * 4 + ((lane >> 3) & 1) * 2 + (lane & 1), p = p0 + 2 * step + sub;
-      // (a row's last pages may be scored beyond its need: its stretch has room for the most pages of any row)
-      if (t < nr && (lane & 7) < 2 && p < end) scores[t * row_scores + (p - a.first)] = order_of((float)((lane & 1) ? v[1] : v[0]));
-    }
-  }
+  Scorer<E, RT> sc;
+  sc.ids(a.tables + tbl, p0, end);
+  sc.coefficients(a, r0, nr, head);
+  // (a row's last pages may be scored beyond its need: its stretch has room for the most pages of any row)
+  sc.score(a, head, p0, end, [] {}, [&](int t, int p, uint32_t key) {
+    if (t < nr) scores[t * row_scores + (p - a.first)] = key;
+  });
 }
 
 constexpr int kAttendWaves = 4;
@@ -630,6 +649,7 @@ __device__ __forceinline__ bool comes_last(int32_t* counter, const int all, int&
 // product: error against 64 bits 4.8e-6 instead of 2e-7.)
 template <int G>
 struct AttendMx {
+  typedef ElemBF16 Elem;
   static constexpr int D = 128;
   static constexpr bool TWICE = G == 8;
   bf16x8_t q[4];
@@ -746,6 +766,7 @@ struct AttendMx {
 // fp32 storage: on the vector units, lane (r, j) holds tokens r and 8 + r of a page and 8 dims; running maximum and sum are each lane's own.
 template <int G>
 struct AttendF32 {
+  typedef ElemF32 Elem;
   static constexpr int C = 4, DPL = 8, D = 64;
   uint4 q[G][2];
   float m[G], l[G], acc[G][DPL];
@@ -851,7 +872,8 @@ struct AttendF32 {
   }
 };
 
-template <typename AT, int G>
+// SCORES: the workgroup scores the row's pages itself, where they are few.
+template <typename AT, int G, bool SCORES>
 __global__ __launch_bounds__(64 * kAttendWaves, 2) void sparse_attend_kernel(SparseArgs a) {
   constexpr int D = AT::D, NT = 64 * kAttendWaves;
   // the choice's counts, then the wavefronts' results
@@ -860,6 +882,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void sparse_attend_kernel(Spa
   __shared__ __align__(16) float s_ml[kAttendWaves][2 * G];
   __shared__ int32_t s_list[kPartPages];
   __shared__ int s_last;
+  __shared__ __align__(16) uint32_t s_keys[SCORES ? kOwnScores : 4];
   hold(a.rows, a.tables, a.scores, a.pool, a.page_bytes, a.q, a.out, a.picked, a.Hq, a.Hkv, a.budget, a.first, a.last, a.splits);
   const int unit = (int)blockIdx.x / a.splits, split = (int)blockIdx.x - unit * a.splits;
   const int row = a.row0 + unit / a.Hkv, head = unit % a.Hkv;
@@ -888,10 +911,25 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void sparse_attend_kernel(Spa
       else put(kept - a.last + i - a.first, n - a.last + i - a.first);
     }
     const int m = n - a.first - a.last, want = kept - a.first - a.last;
-    const uint32_t* sc = a.scores + (int64_t)unit * a.score_stride;
     auto chosen = [&](int i, int p) __attribute__((always_inline)) { put(a.first + i, a.first + p); };
     ChooseLds& s = *(ChooseLds*)s_mem;
-    if (want == 0) {
+    const uint32_t* sc = a.scores + (int64_t)unit * a.score_stride;
+    if constexpr (SCORES) {
+      if (want > 0) {
+        int p0 = a.first + wv * kScorePages;
+        const int end = n - a.last;
+        Scorer<typename AT::Elem, 1> own;
+        if (p0 < end) {
+          own.ids(pt, p0, end);
+          own.coefficients(a, row, 1, head);
+        }
+        for (; p0 < end; p0 += kAttendWaves * kScorePages)
+          own.score(a, head, p0, end, [&] { own.ids(pt, p0 + kAttendWaves * kScorePages, end); }, [&](int, int p, uint32_t key) { s_keys[p - a.first] = key; });
+        __syncthreads();
+        if (m <= NT) pick_highest<1>(s_keys, m, want, s, chosen);
+        else pick_highest<kOwnScores / NT < 4 ? 4 : kOwnScores / NT>(s_keys, m, want, s, chosen);
+      }
+    } else if (want == 0) {
     } else if (m <= NT) {
       pick_highest<1>(sc, m, want, s, chosen);
     } else if (m <= 4 * NT) {
@@ -1059,7 +1097,7 @@ hipError_t launch_bounds(const BoundsArgs& a, int dtype, hipStream_t st) {
 }
 
 hipError_t launch_sparse_scores(const SparseArgs& a, int dtype, hipStream_t st) {
-  if (a.n_groups <= 0) return hipSuccess;
+  if (a.n_groups <= 0 || sparse_scores_itself(a)) return hipSuccess;
   const int64_t waves = (int64_t)((a.most_scored + kScorePages - 1) / kScorePages) * a.Hkv;
   if (a.n_groups > 65535) return hipErrorInvalidValue;
   const dim3 grid((unsigned)((waves + 3) / 4), (unsigned)a.n_groups), block(256);
@@ -1076,10 +1114,16 @@ hipError_t launch_sparse_scores(const SparseArgs& a, int dtype, hipStream_t st) 
 hipError_t launch_sparse_attend(const SparseArgs& a, int dtype, hipStream_t st) {
   if (a.n_rows <= 0) return hipSuccess;
   const dim3 grid((unsigned)(a.n_rows * a.Hkv * a.splits)), block(64 * kAttendWaves);
+  const bool own = sparse_scores_itself(a);
 #define SYM_ATTEND(GG) \
   case GG: \
-    if (dtype == 0) hipLaunchKernelGGL((sparse_attend_kernel<AttendF32<GG>, GG>), grid, block, 0, st, a); \
-    else hipLaunchKernelGGL((sparse_attend_kernel<AttendMx<GG>, GG>), grid, block, 0, st, a); \
+    if (dtype == 0) { \
+      if (own) hipLaunchKernelGGL((sparse_attend_kernel<AttendF32<GG>, GG, true>), grid, block, 0, st, a); \
+      else hipLaunchKernelGGL((sparse_attend_kernel<AttendF32<GG>, GG, false>), grid, block, 0, st, a); \
+    } else { \
+      if (own) hipLaunchKernelGGL((sparse_attend_kernel<AttendMx<GG>, GG, true>), grid, block, 0, st, a); \
+      else hipLaunchKernelGGL((sparse_attend_kernel<AttendMx<GG>, GG, false>), grid, block, 0, st, a); \
+    } \
     break;
   switch (a.Hq / a.Hkv) {
     SYM_ATTEND(1) SYM_ATTEND(2) SYM_ATTEND(4) SYM_ATTEND(8)

@@ -88,6 +88,10 @@ struct SparseArgs {
   float scale_log2e;
 };
 
+// Whether a workgroup of the attention scores its row's pages itself.
+constexpr int kOwnScores = 512;
+inline bool sparse_scores_itself(const SparseArgs& a) { return a.most_scored <= kOwnScores; }
+
 // Weak: the host code is also built without kernels (by tests of the host side, against stand-ins for the launches it made before these).
 #define SYMKV_LAUNCH __attribute__((weak))
 SYMKV_LAUNCH hipError_t launch_rope_rows(RopeRowsArgs a, const RopeTable& r, int dtype, hipStream_t st);
