@@ -181,17 +181,28 @@ def _ptr(t):
 
 
 def _batch(kv, n_tokens):
-    """Files and their new tokens as int32 arrays of one length."""
-    kv, n_tokens = np.ascontiguousarray(kv, np.int32), np.ascontiguousarray(n_tokens, np.int32)
+    """Files and their new tokens as int32 arrays of one length, and their addresses."""
+    (kv, kv_p), (n_tokens, nt_p) = _i32(kv), _i32(n_tokens)
     if kv.shape != n_tokens.shape or kv.ndim != 1:
         raise ValueError(f"{kv.shape} files, but {n_tokens.shape} numbers of tokens")
-    return kv, n_tokens
+    return kv, n_tokens, kv_p, nt_p
 
 
 def _positions(t):
     """Address of int32 positions."""
-    if t is not None and not isinstance(t, int) and str(t.dtype) != "torch.int32":
+    if t is None or isinstance(t, int):
+        return t
+    if t.element_size() != 4 or t.is_floating_point():
         raise TypeError(f"positions must be int32, got {t.dtype}")
+    return _ptr(t)
+
+
+def _rows(t, count):
+    """Address of `count` elements of rows."""
+    if t is None or isinstance(t, int):
+        return t
+    if t.numel() != count:
+        raise ValueError(f"rows of shape {tuple(t.shape)} for {count} elements")
     return _ptr(t)
 
 
@@ -294,6 +305,7 @@ class Context:
     def __init__(self, cfg):
         self.lib, self._fn = load(), _load_by_address()
         self.cfg = cfg
+        self._row_elements = cfg.n_q_heads * cfg.head_dim, cfg.n_kv_heads * cfg.head_dim      # of a token
         h = C.c_void_p()
         rc = self.lib.sym_init(C.byref(cfg), C.byref(h))
         if rc != SYM_OK:
@@ -413,14 +425,14 @@ class Context:
     def rope_rows(self, rope, positions, q, q_out, k, k_out, stream=None):
         """Rows of len(positions) tokens turned; q or k (and its output) may be None.  positions: int32 tensor on the device."""
         n = positions.numel()
-        for x, heads in ((q, self.cfg.n_q_heads), (q_out, self.cfg.n_q_heads), (k, self.cfg.n_kv_heads), (k_out, self.cfg.n_kv_heads)):
-            if x is not None and not isinstance(x, int) and x.numel() != n * heads * self.cfg.head_dim:
-                raise ValueError(f"{n} positions, but rows of shape {tuple(x.shape)}")
-        self._chk(self.lib.sym_rope_rows(self.h, C.byref(rope), n, _positions(positions), _ptr(q), _ptr(q_out), _ptr(k), _ptr(k_out), stream))
+        nq, nk = n * self._row_elements[0], n * self._row_elements[1]
+        rc = self.lib.sym_rope_rows(self.h, C.byref(rope), n, _positions(positions), _rows(q, nq), _rows(q_out, nq), _rows(k, nk), _rows(k_out, nk), stream)
+        if rc < 0:
+            self._chk(rc)
 
     def kv_append_rope(self, kv, n_tokens, rope, k, v, positions=None, stream=None):
-        kv_a, nt_a = _batch(kv, n_tokens)
-        self._chk(self._fn.sym_kv_append_rope(self.h, len(kv_a), kv_a.ctypes.data, nt_a.ctypes.data, None if rope is None else C.byref(rope), _positions(positions), _ptr(k), _ptr(v), stream))
+        kv_a, nt_a, kv_p, nt_p = _batch(kv, n_tokens)
+        self._chk(self._fn.sym_kv_append_rope(self.h, len(kv_a), kv_p, nt_p, None if rope is None else C.byref(rope), _positions(positions), _ptr(k), _ptr(v), stream))
 
     def bounds_attach(self, bounds):
         """bounds: device tensor of at least bounds_bytes(cfg) bytes, or None.  Kept alive by the context."""
@@ -435,12 +447,12 @@ class Context:
         return self._chk(self.lib.sym_kv_bounded(self.h, kv))
 
     def pred_sparse(self, kv, n_tokens, sparse, q, k_new, v_new, out, picked=None, stream=None):
-        kv_a, nt_a = _batch(kv, n_tokens)
-        self._chk(self._fn.sym_pred_sparse(self.h, len(kv_a), kv_a.ctypes.data, nt_a.ctypes.data, C.byref(sparse), _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(out), _ptr(picked), stream))
+        kv_a, nt_a, kv_p, nt_p = _batch(kv, n_tokens)
+        self._chk(self._fn.sym_pred_sparse(self.h, len(kv_a), kv_p, nt_p, C.byref(sparse), _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(out), _ptr(picked), stream))
 
     def pred_begin_sparse(self, kv, n_tokens, sparse, stream=None):
-        kv_a, nt_a = _batch(kv, n_tokens)
-        self._chk(self._fn.sym_pred_begin_sparse(self.h, len(kv_a), kv_a.ctypes.data, nt_a.ctypes.data, C.byref(sparse), stream))
+        kv_a, nt_a, kv_p, nt_p = _batch(kv, n_tokens)
+        self._chk(self._fn.sym_pred_begin_sparse(self.h, len(kv_a), kv_p, nt_p, C.byref(sparse), stream))
         self._sparse = sparse                    # its positions are read by every layer
 
     def pred_layer_sparse(self, layer, q, k_new, v_new, out, picked=None, stream=None):
@@ -455,7 +467,7 @@ class Context:
         kept alive by the object."""
         kv_a, nt_a = np.ascontiguousarray(kv, np.int32), np.ascontiguousarray(n_tokens, np.int32)
         keep = (kv_a, nt_a, q, k_new, v_new, out)
-        args = (len(kv_a), kv_a.ctypes.data, nt_a.ctypes.data, _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(out))
+        args = (len(kv_a), kv_p, nt_p, _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(out))
         return keep, args
 
     def pred_prepared(self, prepared, stream=None):

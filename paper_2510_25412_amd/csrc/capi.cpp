@@ -68,7 +68,7 @@ struct SparsePlan {
   int64_t off_rows = 0, off_tables = 0, off_groups = 0, off_runs = 0, off_pages = 0, off_counters = 0;   // word offsets in the blob
   int64_t entries = 0;                             // page ids in the tables
   int64_t n_counters = 0;
-  int32_t n_rows = 0, n_runs = 0;
+  int32_t n_rows = 0, n_runs = 0, run_tokens = 1;
   int32_t n_stale = 0, n_done = 0;                 // full pages without bounds: from before the batch, then those that it completes
   int32_t splits = 1, score_stride = 0, group_rows = 1;
   int64_t q_bytes = 0, row_bytes = 0;              // scratch: turned query rows of the batch; per row and slab
@@ -118,6 +118,9 @@ struct sym_ctx {
   AppendPlan plan;
   GatherPlan gplan;
   SwapPlan splan;
+  sym_rope rope_of = {};                           // the rope that `rope` is the table of: its 64 powers take longer than a small launch
+  RopeTable rope = {};
+  bool rope_set = false;
   uint8_t* bounds = nullptr;                       // caller's buffer for the bounds of the pages' keys (sym_bounds_attach)
   std::vector<int32_t> words;                      // scratch: runs of an append, page ids
   std::vector<uint8_t*> host_chunks;   // pinned memory of the host slots, kHostChunk pages each
@@ -690,11 +693,19 @@ int64_t row_bytes_of(int64_t tokens, int32_t heads) { return tokens * heads * 25
 int64_t page_bounds_bytes(const sym_config& cfg) { return (int64_t)cfg.n_kv_heads * 512; }
 int64_t layer_bounds(const sym_ctx* c) { return c->cfg.n_pages * page_bounds_bytes(c->cfg); }
 
-// The table of a rope for this context's heads; null: rows stay as they are.
-int rope_table(sym_ctx* c, const sym_rope* r, RopeTable* t) {
-  *t = RopeTable{};
-  t->path = ROPE_NONE;
-  if (!r) return SYM_OK;
+bool same_rope(const sym_rope& a, const sym_rope& b) {
+  return a.layout == b.layout && a.dims == b.dims && a.base == b.base && a.factor == b.factor && a.original_len == b.original_len && a.low_turns == b.low_turns &&
+         a.high_turns == b.high_turns && a.magnitude == b.magnitude;
+}
+// The table of a rope for this context's heads (in c->rope); null: rows stay as they are.
+int rope_table(sym_ctx* c, const sym_rope* r, const RopeTable** out) {
+  static const RopeTable none = {};
+  static_assert(ROPE_NONE == 0, "an empty table turns nothing");
+  *out = r ? &c->rope : &none;
+  if (!r || (c->rope_set && same_rope(*r, c->rope_of))) return SYM_OK;
+  c->rope_set = false;
+  RopeTable* t = &c->rope;
+  *t = none;
   const int32_t D = c->cfg.head_dim, dims = r->dims == 0 ? D : r->dims;
   if (r->layout != SYM_ROPE_HALVES && r->layout != SYM_ROPE_INTERLEAVED) return fail(c, SYM_EINVAL, "rope: unknown layout");
   if (dims < 2 || dims > D || dims % 2) return fail(c, SYM_EINVAL, "rope: dims must be even, 2 .. head_dim");
@@ -721,6 +732,8 @@ int rope_table(sym_ctx* c, const sym_rope* r, RopeTable* t) {
   t->path = r->layout == SYM_ROPE_INTERLEAVED ? ROPE_INTERLEAVED : (dims / 2) % chunk == 0 ? ROPE_HALVES : ROPE_HALVES_ANY;
   t->dims = dims;
   t->mag = mag;
+  c->rope_of = *r;
+  c->rope_set = true;
   return SYM_OK;
 }
 
@@ -829,7 +842,9 @@ int check_sparse(sym_ctx* c, const sym_sparse* s, SparsePlan* sp) {
     return fail(c, SYM_EINVAL, "sparse: budget >= first + last, first >= 0, last >= 1");
   if (s->positions && !s->rope) return fail(c, SYM_EINVAL, "sparse: positions without a rope");
   if (!aligned(s->positions, 4)) return fail(c, SYM_EINVAL, "sparse: positions must be 4-byte aligned");
-  if (int rc = rope_table(c, s->rope, &sp->rope)) return rc;
+  const RopeTable* table;
+  if (int rc = rope_table(c, s->rope, &table)) return rc;
+  sp->rope = *table;                               // (the context's changes with the next rope)
   if (!c->bounds) return fail(c, SYM_EINVAL, "sparse: no buffer for page bounds is attached (sym_bounds_attach)");
   sp->turns = s->rope != nullptr;
   sp->pos = s->positions;
@@ -849,6 +864,7 @@ int size_sparse(sym_ctx* c, SparsePlan* sp, int32_t n_lips, const sym_kv* kv, co
     const KvFile* f = c->fs->file_of(kv[b]);
     const int64_t after = f->len + n_tokens[b], pages = (after + P - 1) / P;
     entries += pages;
+    sp->run_tokens = std::max(sp->run_tokens, n_tokens[b]);
     stale += f->len / P - f->bounded;
     done += after / P - f->len / P;
     most_pages = std::max(most_pages, pages);
@@ -947,6 +963,7 @@ int run_sparse_layer(sym_ctx* c, const SparsePlan& sp, uint8_t* ws, int64_t word
     a.q_out = q_turned;
     a.runs = blob + sp.off_runs;
     a.n_runs = sp.n_runs;
+    a.run_tokens = sp.run_tokens;
     const StageDone done(c, stage);
     if (stage >= 0) {                              // the lists travel with this launch
       a.host_words = c->stage[stage];
@@ -1641,7 +1658,7 @@ int sym_rope_rows(sym_ctx* c, const sym_rope* rope, int32_t n, const int32_t* po
   std::lock_guard<std::mutex> lk(c->mu);
   return guarded(c, [&]() -> int {
     if (!rope) return fail(c, SYM_EINVAL, "rope_rows: no rope");
-    RopeTable t;
+    const RopeTable* t;
     if (int rc = rope_table(c, rope, &t)) return rc;
     if (!positions && n > 0) return fail(c, SYM_EINVAL, "rope_rows: no positions");
     if ((q == nullptr) != (q_out == nullptr) || (k == nullptr) != (k_out == nullptr)) return fail(c, SYM_EINVAL, "rope_rows: rows without an output, or the other way round");
@@ -1671,8 +1688,8 @@ int sym_rope_rows(sym_ctx* c, const sym_rope* rope, int32_t n, const int32_t* po
       a.n = (int32_t)std::min<int64_t>(kMostRopeRows, n - t0);
       a.Hq = c->cfg.n_q_heads;
       a.Hkv = c->cfg.n_kv_heads;
-      Timed timed(c, SYM_K_PROLOGUE, st, false, !stream_captures(st));      // (events of a recorded stream could not be read)
-      const hipError_t e = launch_rope_rows(a, t, c->cfg.dtype, st);
+      Timed timed(c, SYM_K_PROLOGUE, st, false, c->prof_mask == 0 || !stream_captures(st));      // (events of a recorded stream could not be read)
+      const hipError_t e = launch_rope_rows(a, *t, c->cfg.dtype, st);
       if (e != hipSuccess) return fail_hip(c, e, "rope launch");
     }
     return SYM_OK;
@@ -1688,7 +1705,7 @@ int sym_kv_append_rope(sym_ctx* c, int32_t n_files, const sym_kv* kv, const int3
   return guarded(c, [&]() -> int {
     int rc;
     if ((rc = refuse_if_open(c, "kv_append_rope"))) return rc;
-    RopeTable t;
+    const RopeTable* t;
     if ((rc = rope_table(c, rope, &t))) return rc;
     if (positions && !rope) return fail(c, SYM_EINVAL, "kv_append_rope: positions without a rope");
     if (!aligned(k, 16) || !aligned(v, 16) || !aligned(positions, 4)) return fail(c, SYM_EINVAL, "kv_append_rope: rows must be 16-byte aligned, positions 4-byte");
@@ -1722,7 +1739,7 @@ int sym_kv_append_rope(sym_ctx* c, int32_t n_files, const sym_kv* kv, const int3
     a.done = done.event();
     {
       Timed timed(c, SYM_K_PROLOGUE, st);
-      const hipError_t e = launch_append_rope(a, t, c->cfg.dtype, st);
+      const hipError_t e = launch_append_rope(a, *t, c->cfg.dtype, st);
       if (e != hipSuccess) return fail_hip(c, e, "append launch");
     }
     if ((rc = done.launched(st))) return rc;

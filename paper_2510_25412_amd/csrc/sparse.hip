@@ -281,6 +281,10 @@ struct AppendRunsKernelArgs {
 template <typename E, int PATH>
 __device__ __forceinline__ void append_run(SYM_AS4 AppendKernelArgs* ka, const int t0, const int slot, const int nf, const int pos0, double2 (*cs)[kPairs], uint8_t (*stage)[kRowBytes]) {
   const int n = nf & 0xff, Hkv = ka->a.Hkv, Hq = ka->a.q ? ka->a.Hq : 0, layer = blockIdx.y;
+  // this workgroup's rows of a token: keys and values, or a part of the query rows
+  const int part = (int)blockIdx.z - 1, parts = (int)gridDim.z - 1;
+  const int first = part < 0 ? 0 : 2 * Hkv + Hq * part / parts, rows = (part < 0 ? 2 * Hkv : 2 * Hkv + Hq * (part + 1) / parts) - first;
+  if (rows <= 0) return;
   uint8_t* page = ka->a.pool + layer * ka->a.layer_bytes + (int64_t)(slot / kP) * ka->a.page_bytes;
   const int ts = slot % kP;
   const uint8_t* k = (const uint8_t*)ka->a.k + layer * ka->a.layer_rows + (int64_t)t0 * Hkv * kRowBytes;
@@ -290,7 +294,8 @@ __device__ __forceinline__ void append_run(SYM_AS4 AppendKernelArgs* ka, const i
   const int32_t* pos = ka->a.pos ? ka->a.pos + t0 : nullptr;
   const int lg = n == 1 ? 8 : n == 2 ? 7 : n <= 4 ? 6 : n <= 8 ? 5 : 4;
   turn_rows<E, PATH, 4>(
-      [=](int tok, int row) __attribute__((always_inline)) {
+      [=](int tok, int x) __attribute__((always_inline)) {
+        const int row = first + x;
         // all three of everything, then the choice: under branches the compiler chooses between addresses of the captured variables,
         // and these go to memory
         const bool is_q = row >= 2 * Hkv, is_v = row >= Hkv;
@@ -300,13 +305,14 @@ __device__ __forceinline__ void append_run(SYM_AS4 AppendKernelArgs* ka, const i
         uint8_t *dq = qo + from_q, *dk = page + (int64_t)g * kSlab + (is_v ? kBlk : 0) + (ts + tok) * kHalfBytes;
         return RowAt{is_q ? sq : is_v ? sv : sk, is_q ? dq : dk, is_q ? kHalfBytes : kP * kHalfBytes, is_q || !is_v};
       },
-      [=]() __attribute__((always_inline)) { fill_angles<PATH>(&ka->r, pos, pos0, n, cs); }, 2 * Hkv + Hq, n, lg, ka->r.dims, cs, stage);
-  if ((nf >> 8) && ka->a.bounds) {
+      [=]() __attribute__((always_inline)) { fill_angles<PATH>(&ka->r, pos, pos0, n, cs); }, rows, n, lg, ka->r.dims, cs, stage);
+  if ((nf >> 8) && ka->a.bounds && part < 0) {
     __syncthreads();                             // the page's last keys are written; the others were there
     uint8_t* b = ka->a.bounds + layer * ka->a.layer_bounds + (int64_t)(slot / kP) * Hkv * (2 * kRowBytes);
     for (int g = threadIdx.x >> 6; g < Hkv; g += 4) page_bounds<E>(page + (int64_t)g * kSlab, b + g * (2 * kRowBytes));
   }
 }
+// Query rows of a batch are turned beside, in workgroups of their own.
 // The workgroups behind the runs' copy a batch's lists to the workspace for the launches that follow, 16 bytes per thread.
 __device__ __forceinline__ bool copy_lists(SYM_AS4 AppendKernelArgs* ka) {
   const int blk = (int)blockIdx.x - ka->a.n_runs;
@@ -314,7 +320,7 @@ __device__ __forceinline__ bool copy_lists(SYM_AS4 AppendKernelArgs* ka) {
   const uint4* src = (const uint4*)ka->a.host_words;
   uint4* dst = (uint4*)ka->a.dev_words;
   const int64_t n16 = (ka->a.copy_words + 3) / 4;      // the staging buffer is padded to 16 bytes
-  if (blockIdx.y == 0)
+  if (blockIdx.y == 0 && blockIdx.z == 0)
     for (int64_t i = (int64_t)blk * 256 + threadIdx.x; i < n16; i += (int64_t)(gridDim.x - ka->a.n_runs) * 256) dst[i] = src[i];
   return true;
 }
@@ -1056,7 +1062,9 @@ hipError_t launch_append_rope(const AppendRopeArgs& a, const RopeTable& r, int d
   if (a.n_runs <= 0) return a.done ? hipEventRecord(a.done, st) : hipSuccess;
   if (a.n_layers < 1 || a.n_layers > 65535) return hipErrorInvalidValue;
   const int64_t copy = std::min<int64_t>((a.copy_words / 4 + 255) / 256 + (a.copy_words > 0), 256);
-  const dim3 grid((unsigned)(a.n_runs + copy), (unsigned)a.n_layers), block(256);
+  // the query rows of a run in parts of about four passes of a workgroup
+  const int parts = a.q ? std::min(std::max(a.Hq * std::min(a.run_tokens, kRunTokens) / 128, 1), std::min(a.Hq, 16)) : 0;
+  const dim3 grid((unsigned)(a.n_runs + copy), (unsigned)a.n_layers, (unsigned)(1 + parts)), block(256);
   if (a.by_args) {
     if (a.n_runs > kArgRuns) return hipErrorInvalidValue;
     AppendRunsKernelArgs ka;

@@ -42,6 +42,7 @@ struct AppendRopeArgs {
   const int32_t* pos;       // device [T], or null: the position that the run says
   const int32_t* runs;      // host (at most kArgRuns), or pinned / device
   int32_t n_runs, Hq, Hkv, n_layers;
+  int32_t run_tokens;       // tokens of the longest run
   int32_t by_args;          // the runs are host memory and travel with the arguments
   const int32_t* host_words;   // lists to be copied along the way: pinned host memory, where to, how many words
   int32_t* dev_words;
