@@ -877,10 +877,10 @@ int size_sparse(sym_ctx* c, SparsePlan* sp, int32_t n_lips, const sym_kv* kv, co
   sp->n_done = (int32_t)done;
   sp->kv.assign(kv, kv + n_lips);
   sp->score_stride = most_pages > sp->budget ? (int32_t)align_up(most_pages - sp->first - sp->last, 32) : 0;
-  // Parts of a list: enough workgroups for the chip where rows are few, each wavefront with two pages at least; no more pages than a
+  // Parts of a list: where rows are few as many workgroups as fill the chip, each with eight pages at least; no more pages than a
   // workgroup's list holds.
-  const int64_t units = tokens * H;
-  sp->splits = (int32_t)std::max({(int64_t)1, std::min(512 / units, most_kept / 8), (most_kept + kPartPages - 1) / kPartPages});
+  const int64_t units = tokens * H, most_scored = most_pages > sp->budget ? most_pages - sp->first - sp->last : 0;
+  sp->splits = (int32_t)std::max({(int64_t)1, std::min(2048 / attend_waves(most_scored) / units, most_kept / 8), (most_kept + kPartPages - 1) / kPartPages});
   sp->q_bytes = sp->turns ? align_up(row_bytes_of(tokens, c->cfg.n_q_heads), 256) : 0;
   sp->n_counters = sp->splits > 1 ? H * std::max<int64_t>(1, std::min(tokens, kMostUnits / (H * sp->splits))) : 0;
   *words = sp->n_rows * (int64_t)(SPARSE_ROW_WORDS + SPARSE_GROUP_WORDS) + entries + runs * RUN_WORDS + stale + done + sp->n_counters + 16;
@@ -1014,7 +1014,7 @@ int run_sparse_layer(sym_ctx* c, const SparsePlan& sp, uint8_t* ws, int64_t word
     a.most_scored = s.most_scored;
     hipError_t e = hipSuccess;
     {
-      Timed t(c, SYM_K_ATTN, st, false, true, 1 + (s.groups > 0 && !sparse_scores_itself(a)));
+      Timed t(c, SYM_K_ATTN, st, false, true, 1 + (s.groups > 0 && !scores_itself(s.most_scored)));
       if (s.groups > 0) e = launch_sparse_scores(a, c->cfg.dtype, st);
       if (e == hipSuccess) e = launch_sparse_attend(a, c->cfg.dtype, st);
     }

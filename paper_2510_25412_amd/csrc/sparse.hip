@@ -475,10 +475,10 @@ __global__ __launch_bounds__(256) void sparse_scores_kernel(SparseArgs a) {
   });
 }
 
-constexpr int kAttendWaves = 4;
+constexpr int kMostWaves = 8;                   // of a workgroup that attends
 struct ChooseLds {
   __align__(16) uint32_t hist[4][256];                         // one for every round
-  uint2 total[kAttendWaves];                     // of every wavefront: greatest and least score, then how many are above and equal to the least chosen
+  uint2 total[kMostWaves];                       // of every wavefront: greatest and least score, then how many are above and equal to the least chosen
 };
 
 // Sum over this lane and the higher ones of the wavefront: four DPP adds inside rows of 16 lanes, then the rows' totals.
@@ -515,9 +515,9 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t x) {
 // The smallest chosen score is found in at most four rounds: a histogram of 256 equal steps between the least and the greatest that it can be,
 // and the step in which the wanted one lies.  Usually a step that is wanted whole ends it.  A thread holds EPT scores in a row, so that
 // places are counted thread by thread; EPT = 0: any number of scores, sixteen at a time, read again for every round.
-template <int EPT, typename P>
+template <int W, int EPT, typename P>
 __device__ __forceinline__ void pick_highest(const uint32_t* sc, const int m, const int want, ChooseLds& s, const P& put) {
-  constexpr int W = kAttendWaves, NT = 64 * W, N = EPT > 0 ? EPT : 16;
+  constexpr int NT = 64 * W, N = EPT > 0 ? EPT : 16;
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   const int per = EPT > 0 ? EPT : (m + 16 * NT - 1) / (16 * NT) * 16, i0 = tid * per;
   uint32_t key[N];
@@ -626,7 +626,7 @@ __device__ __forceinline__ void pick_highest(const uint32_t* sc, const int m, co
 }
 
 // ---------------------------------------------------------------------------------------
-// Attention over the chosen pages of a (new token, kv head): a workgroup of four wavefronts to each of `splits` equal parts of their list.
+// Attention over the chosen pages of a (new token, kv head): a workgroup of W wavefronts to each of `splits` equal parts of their list.
 // Every workgroup chooses from the row's scores for itself and keeps its part of the list in LDS, where it reads like a
 // file's page table: only the last page may be partly filled.  One pass over the pages, with the running maximum and sum of the softmax in
 // fp32; the wavefronts' results are combined through LDS.  The workgroup that finishes last of a row's parts joins them, so that no
@@ -879,13 +879,13 @@ struct AttendF32 {
 };
 
 // SCORES: the workgroup scores the row's pages itself, where they are few.
-template <typename AT, int G, bool SCORES>
-__global__ __launch_bounds__(64 * kAttendWaves, 2) void sparse_attend_kernel(SparseArgs a) {
-  constexpr int D = AT::D, NT = 64 * kAttendWaves;
+template <typename AT, int G, bool SCORES, int W>
+__global__ __launch_bounds__(64 * W, 8 / W) void sparse_attend_kernel(SparseArgs a) {
+  constexpr int D = AT::D, NT = 64 * W;
   // the choice's counts, then the wavefronts' results
-  constexpr int kResult = kAttendWaves * G * D * 4;
+  constexpr int kResult = W * G * D * 4;
   __shared__ __align__(16) uint8_t s_mem[kResult > (int)sizeof(ChooseLds) ? kResult : (int)sizeof(ChooseLds)];
-  __shared__ __align__(16) float s_ml[kAttendWaves][2 * G];
+  __shared__ __align__(16) float s_ml[W][2 * G];
   __shared__ int32_t s_list[kPartPages];
   __shared__ int s_last;
   __shared__ __align__(16) uint32_t s_keys[SCORES ? kOwnScores : 4];
@@ -929,30 +929,30 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void sparse_attend_kernel(Spa
           own.ids(pt, p0, end);
           own.coefficients(a, row, 1, head);
         }
-        for (; p0 < end; p0 += kAttendWaves * kScorePages)
-          own.score(a, head, p0, end, [&] { own.ids(pt, p0 + kAttendWaves * kScorePages, end); }, [&](int, int p, uint32_t key) { s_keys[p - a.first] = key; });
+        for (; p0 < end; p0 += W * kScorePages)
+          own.score(a, head, p0, end, [&] { own.ids(pt, p0 + W * kScorePages, end); }, [&](int, int p, uint32_t key) { s_keys[p - a.first] = key; });
         __syncthreads();
-        if (m <= NT) pick_highest<1>(s_keys, m, want, s, chosen);
-        else pick_highest<kOwnScores / NT < 4 ? 4 : kOwnScores / NT>(s_keys, m, want, s, chosen);
+        if (m <= NT) pick_highest<W, 1>(s_keys, m, want, s, chosen);
+        else pick_highest<W, kOwnScores / NT < 4 ? 4 : kOwnScores / NT>(s_keys, m, want, s, chosen);
       }
     } else if (want == 0) {
     } else if (m <= NT) {
-      pick_highest<1>(sc, m, want, s, chosen);
+      pick_highest<W, 1>(sc, m, want, s, chosen);
     } else if (m <= 4 * NT) {
-      pick_highest<4>(sc, m, want, s, chosen);
+      pick_highest<W, 4>(sc, m, want, s, chosen);
     } else if (m <= 8 * NT) {
-      pick_highest<8>(sc, m, want, s, chosen);
+      pick_highest<W, 8>(sc, m, want, s, chosen);
     } else if (m <= 16 * NT) {
-      pick_highest<16>(sc, m, want, s, chosen);
+      pick_highest<W, 16>(sc, m, want, s, chosen);
     } else if (m <= 32 * NT) {
-      pick_highest<32>(sc, m, want, s, chosen);
+      pick_highest<W, 32>(sc, m, want, s, chosen);
     } else {
-      pick_highest<0>(sc, m, want, s, chosen);
+      pick_highest<W, 0>(sc, m, want, s, chosen);
     }
   }
   __syncthreads();
-  int p = lo + (int)((int64_t)(hi - lo) * wv / kAttendWaves);
-  const int pe = lo + (int)((int64_t)(hi - lo) * (wv + 1) / kAttendWaves);
+  int p = lo + (int)((int64_t)(hi - lo) * wv / W);
+  const int pe = lo + (int)((int64_t)(hi - lo) * (wv + 1) / W);
   const uint8_t* pool = a.pool + (int64_t)head * kSlab;
   PageRegs A, B;
   // (past the wavefront's pages: another page of the part, read and not used; a part has a page at least)
@@ -975,9 +975,9 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void sparse_attend_kernel(Spa
     const int h = x / D;
     float M = s_ml[0][2 * h], num = 0.f, den = 0.f;
 #pragma unroll
-    for (int w = 1; w < kAttendWaves; ++w) M = fmaxf(M, s_ml[w][2 * h]);
+    for (int w = 1; w < W; ++w) M = fmaxf(M, s_ml[w][2 * h]);
 #pragma unroll
-    for (int w = 0; w < kAttendWaves; ++w) {     // (a wavefront without pages: maximum -1e30, sum 0, zeros)
+    for (int w = 0; w < W; ++w) {     // (a wavefront without pages: maximum -1e30, sum 0, zeros)
       const float f = __builtin_amdgcn_exp2f(s_ml[w][2 * h] - M);
       num = __builtin_fmaf(s_acc[w][x], f, num);
       den = __builtin_fmaf(s_ml[w][2 * h + 1], f, den);
@@ -1105,7 +1105,7 @@ hipError_t launch_bounds(const BoundsArgs& a, int dtype, hipStream_t st) {
 }
 
 hipError_t launch_sparse_scores(const SparseArgs& a, int dtype, hipStream_t st) {
-  if (a.n_groups <= 0 || sparse_scores_itself(a)) return hipSuccess;
+  if (a.n_groups <= 0 || scores_itself(a.most_scored)) return hipSuccess;
   const int64_t waves = (int64_t)((a.most_scored + kScorePages - 1) / kScorePages) * a.Hkv;
   if (a.n_groups > 65535) return hipErrorInvalidValue;
   const dim3 grid((unsigned)((waves + 3) / 4), (unsigned)a.n_groups), block(256);
@@ -1121,16 +1121,16 @@ hipError_t launch_sparse_scores(const SparseArgs& a, int dtype, hipStream_t st) 
 
 hipError_t launch_sparse_attend(const SparseArgs& a, int dtype, hipStream_t st) {
   if (a.n_rows <= 0) return hipSuccess;
-  const dim3 grid((unsigned)(a.n_rows * a.Hkv * a.splits)), block(64 * kAttendWaves);
-  const bool own = sparse_scores_itself(a);
+  const bool own = scores_itself(a.most_scored);
+  const dim3 grid((unsigned)(a.n_rows * a.Hkv * a.splits)), block(64 * attend_waves(a.most_scored));
 #define SYM_ATTEND(GG) \
   case GG: \
     if (dtype == 0) { \
-      if (own) hipLaunchKernelGGL((sparse_attend_kernel<AttendF32<GG>, GG, true>), grid, block, 0, st, a); \
-      else hipLaunchKernelGGL((sparse_attend_kernel<AttendF32<GG>, GG, false>), grid, block, 0, st, a); \
+      if (own) hipLaunchKernelGGL((sparse_attend_kernel<AttendF32<GG>, GG, true, 4>), grid, block, 0, st, a); \
+      else hipLaunchKernelGGL((sparse_attend_kernel<AttendF32<GG>, GG, false, 8>), grid, block, 0, st, a); \
     } else { \
-      if (own) hipLaunchKernelGGL((sparse_attend_kernel<AttendMx<GG>, GG, true>), grid, block, 0, st, a); \
-      else hipLaunchKernelGGL((sparse_attend_kernel<AttendMx<GG>, GG, false>), grid, block, 0, st, a); \
+      if (own) hipLaunchKernelGGL((sparse_attend_kernel<AttendMx<GG>, GG, true, 4>), grid, block, 0, st, a); \
+      else hipLaunchKernelGGL((sparse_attend_kernel<AttendMx<GG>, GG, false, 8>), grid, block, 0, st, a); \
     } \
     break;
   switch (a.Hq / a.Hkv) {

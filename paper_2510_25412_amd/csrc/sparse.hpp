@@ -91,7 +91,8 @@ struct SparseArgs {
 
 // Whether a workgroup of the attention scores its row's pages itself.
 constexpr int kOwnScores = 512;
-inline bool sparse_scores_itself(const SparseArgs& a) { return a.most_scored <= kOwnScores; }
+inline bool scores_itself(int64_t most_scored) { return most_scored <= kOwnScores; }
+inline int attend_waves(int64_t most_scored) { return scores_itself(most_scored) ? 4 : 8; }
 
 // Weak: the host code is also built without kernels (by tests of the host side, against stand-ins for the launches it made before these).
 #define SYMKV_LAUNCH __attribute__((weak))
