@@ -796,20 +796,22 @@ AppendRopeArgs append_args(const sym_ctx* c, int32_t layer, int32_t n_layers, in
   return a;
 }
 
-// Bounds of `n` pages, ids in device memory (or, at most kArgPages, on the host), in layers [layer, layer + n_layers).
-int run_bounds(sym_ctx* c, const int32_t* pages, int64_t n, bool by_args, int32_t layer, int32_t n_layers, hipStream_t st) {
+// Bounds of `n` pages, ids in device memory, in the staging buffer `si`, or (at most kArgPages) on the host, in layers [layer, layer + n_layers).
+int run_bounds(sym_ctx* c, const int32_t* pages, int64_t n, bool by_args, int32_t layer, int32_t n_layers, int si, hipStream_t st) {
   constexpr int64_t kChunk = 1 << 20;
   for (int64_t off = 0; off < n; off += kChunk) {
+    const StageDone done(c, off + kChunk >= n ? si : -1);
     BoundsArgs a{pool_of(c, layer), c->page_bytes, c->layer_bytes, c->bounds + layer * layer_bounds(c), layer_bounds(c), pages + off,
-                 (int32_t)std::min(kChunk, n - off), c->cfg.n_kv_heads, n_layers, by_args ? 1 : 0};
+                 (int32_t)std::min(kChunk, n - off), c->cfg.n_kv_heads, n_layers, by_args ? 1 : 0, done.event()};
     Timed t(c, SYM_K_PROLOGUE, st);
     const hipError_t e = launch_bounds(a, c->cfg.dtype, st);
     if (e != hipSuccess) return fail_hip(c, e, "bounds launch");
+    if (int rc = done.launched(st)) return rc;
   }
   return SYM_OK;
 }
 int batch_bounds(sym_ctx* c, const SparsePlan& sp, const int32_t* blob, int32_t layer, int32_t n, hipStream_t st) {
-  return n > 0 ? run_bounds(c, blob + sp.off_pages, n, false, layer, 1, st) : SYM_OK;
+  return n > 0 ? run_bounds(c, blob + sp.off_pages, n, false, layer, 1, -1, st) : SYM_OK;
 }
 
 void open_batch(sym_ctx* c, const PlannedBatch& pb) {
@@ -1614,39 +1616,23 @@ int sym_kv_bounds(sym_ctx* c, int32_t n, const sym_kv* kv, void* stream) {
     if (c->cfg.device >= 0) {
       if ((rc = refuse_capture(c, st, "kv_bounds"))) return rc;
       const OnDevice on(c);
+      // few ids travel with the launch; more are read from the staging buffer
+      int si = -1;
+      int32_t* ids;
       if (pages <= kArgPages) {
-        c->words.clear();
-        for (int32_t b = 0; b < n; ++b) {
-          const KvFile* f = c->fs->file_of(kv[b]);
-          c->words.insert(c->words.end(), f->pages.begin(), f->pages.begin() + f->len / P);
-        }
-        if (pages > 0 && (rc = run_bounds(c, c->words.data(), pages, true, 0, c->n_layers, st))) return rc;
+        c->words.resize((size_t)pages);
+        ids = c->words.data();
       } else {
-        // the ids go to the workspace, as many at a time as it holds
-        const int64_t room = std::min<int64_t>(pages, c->cfg.workspace_bytes / 4 - 16);
-        if ((rc = stage_reserve(c, room + 4))) return rc;
-        int si = -1;
-        int64_t have = 0;
-        auto flush = [&]() -> int {
-          if (have == 0) return SYM_OK;
-          int r = launch_prologue(c, si, have, nullptr, 0, nullptr, 0, nullptr, nullptr, st, si);
-          if (!r) r = run_bounds(c, (const int32_t*)c->cfg.workspace, have, false, 0, c->n_layers, st);
-          have = 0;
-          return r;
-        };
-        for (int32_t b = 0; b < n; ++b) {
-          const KvFile* f = c->fs->file_of(kv[b]);
-          for (int64_t p = 0, full = f->len / P; p < full;) {
-            if (have == 0 && (rc = stage_acquire(c, room, &si))) return rc;
-            const int64_t m = std::min(full - p, room - have);
-            std::memcpy(c->stage[si] + have, f->pages.data() + p, (size_t)m * 4);
-            p += m;
-            have += m;
-            if (have == room && (rc = flush())) return rc;
-          }
-        }
-        if ((rc = flush())) return rc;
+        if ((rc = stage_reserve(c, pages)) || (rc = stage_acquire(c, pages, &si))) return rc;
+        ids = c->stage[si];
       }
+      int32_t* at = ids;
+      for (int32_t b = 0; b < n; ++b) {
+        const KvFile* f = c->fs->file_of(kv[b]);
+        copy_bytes(at, f->pages.data(), (size_t)(f->len / P) * 4);
+        at += f->len / P;
+      }
+      if (pages > 0 && (rc = run_bounds(c, ids, pages, si < 0, 0, c->n_layers, si, st))) return rc;
     }
     for (int32_t b = 0; b < n; ++b) c->fs->set_bounded(kv[b], c->fs->len(kv[b]) / P);
     return SYM_OK;

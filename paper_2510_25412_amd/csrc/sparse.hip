@@ -217,13 +217,19 @@ __global__ __launch_bounds__(256) void rope_rows_kernel(RopeRowsKernelArgs) {
 // both halves of tokens r and 8 + r; the eight lanes of a chunk are combined by halving exchanges over the list [lo, -hi]
 // (the minimum of -x is -maximum), which leave lane r with entries r V/8 .. of it.  A NaN makes both bounds of its element NaN.
 __device__ __forceinline__ float least(float a, float b) { return __builtin_elementwise_minimum(a, b); }
+struct PageKeys {
+  uint4 k[4];                                    // index = row half * 2 + token half
+};
+template <bool STREAM>
+__device__ __forceinline__ void load_keys(PageKeys& R, const uint8_t* slab) {
+#pragma unroll
+  for (int x = 0; x < 4; ++x) R.k[x] = ld16<STREAM>(slab + x * 1024 + (threadIdx.x & 63) * 16);
+}
 template <typename E>
-__device__ __forceinline__ void page_bounds(const uint8_t* slab, uint8_t* out) {
+__device__ __forceinline__ void write_bounds(const PageKeys& R, uint8_t* out) {
   constexpr int C = E::kDimsPerChunk, V = 4 * C;
   const int lane = threadIdx.x & 63, r = lane >> 3, j = lane & 7;
-  uint4 k[4];
-#pragma unroll
-  for (int x = 0; x < 4; ++x) k[x] = *(const uint4*)(slab + x * 1024 + lane * 16);
+  const uint4* k = R.k;
   float v[V];
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
@@ -309,7 +315,11 @@ __device__ __forceinline__ void append_run(SYM_AS4 AppendKernelArgs* ka, const i
   if ((nf >> 8) && ka->a.bounds && part < 0) {
     __syncthreads();                             // the page's last keys are written; the others were there
     uint8_t* b = ka->a.bounds + layer * ka->a.layer_bounds + (int64_t)(slot / kP) * Hkv * (2 * kRowBytes);
-    for (int g = threadIdx.x >> 6; g < Hkv; g += 4) page_bounds<E>(page + (int64_t)g * kSlab, b + g * (2 * kRowBytes));
+    for (int g = threadIdx.x >> 6; g < Hkv; g += 4) {
+      PageKeys R;
+      load_keys<false>(R, page + (int64_t)g * kSlab);
+      write_bounds<E>(R, b + g * (2 * kRowBytes));
+    }
   }
 }
 // Query rows of a batch are turned beside, in workgroups of their own.
@@ -344,19 +354,39 @@ __global__ __launch_bounds__(256) void append_rope_runs_kernel(AppendRunsKernelA
 }
 
 // ---------------------------------------------------------------------------------------
-// Bounds of a list of pages: a workgroup to a page and layer, a wavefront to a kv head at a time.  Bound: HBM (4 KiB read for 512 bytes written).
+// Bounds of a list of pages.  A workgroup takes PB pages and a layer; its wavefronts take the (page, kv head) in turn, the next one's keys under
+// way while one is reduced.  PB = 1 for few pages, whose ids travel with the arguments or lie in device memory; 8 for many, whose list
+// may stay in pinned host memory: 32 bytes of it are one request over the host link for a workgroup.
+// Bound: HBM (4 KiB read for 512 bytes written).
 // ---------------------------------------------------------------------------------------
 struct BoundsKernelArgs {
   BoundsArgs a;
   int32_t ids[kArgPages];
 };
-template <typename E, bool ARGS>
-__global__ __launch_bounds__(256) void bounds_kernel(std::conditional_t<ARGS, BoundsKernelArgs, BoundsArgs>) {
+template <typename E, bool ARGS, int PB>
+__global__ __launch_bounds__(PB == 1 ? 256 : 512) void bounds_kernel(std::conditional_t<ARGS, BoundsKernelArgs, BoundsArgs>) {
+  constexpr int W = PB == 1 ? 4 : 8;
   auto ka = (SYM_AS4 BoundsKernelArgs*)__builtin_amdgcn_kernarg_segment_ptr();
-  const int page = ARGS ? ka->ids[blockIdx.x] : sload(ka->a.pages + blockIdx.x), Hkv = ka->a.Hkv;
-  const uint8_t* p = ka->a.pool + blockIdx.y * ka->a.layer_bytes + page * ka->a.page_bytes;
-  uint8_t* b = ka->a.bounds + blockIdx.y * ka->a.layer_bounds + (int64_t)page * Hkv * (2 * kRowBytes);
-  for (int g = threadIdx.x >> 6; g < Hkv; g += 4) page_bounds<E>(p + (int64_t)g * kSlab, b + g * (2 * kRowBytes));
+  const int Hkv = ka->a.Hkv, n = min(PB, ka->a.n_pages - (int)blockIdx.x * PB) * Hkv, lane = threadIdx.x & 63;
+  int ids;                                       // lane l: page l of the workgroup's
+  if constexpr (ARGS) ids = ka->ids[blockIdx.x];
+  else ids = ka->a.pages[min((int)blockIdx.x * PB + lane % PB, ka->a.n_pages - 1)];
+  const uint8_t* pool = ka->a.pool + blockIdx.y * ka->a.layer_bytes;
+  uint8_t* bounds = ka->a.bounds + blockIdx.y * ka->a.layer_bounds;
+  const int64_t page_bytes = ka->a.page_bytes;
+  const int w = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  auto page = [&](int u) __attribute__((always_inline)) { return (int64_t)__builtin_amdgcn_readlane(ids, u / Hkv); };
+  if (w >= n) return;
+  PageKeys A, B;
+  load_keys<true>(A, pool + page(w) * page_bytes + (w % Hkv) * kSlab);
+  for (int u = w; u < n; u += 2 * W) {
+    const int v = u + W, x = v + W, vv = min(v, n - 1), xx = min(x, n - 1);      // (past the end: the last one again, not used)
+    load_keys<true>(B, pool + page(vv) * page_bytes + (vv % Hkv) * kSlab);
+    write_bounds<E>(A, bounds + (page(u) * Hkv + u % Hkv) * (2 * kRowBytes));
+    if (v >= n) break;
+    load_keys<true>(A, pool + page(xx) * page_bytes + (xx % Hkv) * kSlab);
+    write_bounds<E>(B, bounds + (page(v) * Hkv + v % Hkv) * (2 * kRowBytes));
+  }
 }
 
 // ---------------------------------------------------------------------------------------
@@ -1088,20 +1118,24 @@ hipError_t launch_append_rope(const AppendRopeArgs& a, const RopeTable& r, int d
 hipError_t launch_bounds(const BoundsArgs& a, int dtype, hipStream_t st) {
   if (a.n_pages <= 0) return hipSuccess;
   if (a.n_layers < 1 || a.n_layers > 65535) return hipErrorInvalidValue;
-  const dim3 grid((unsigned)a.n_pages, (unsigned)a.n_layers), block(256);
   if (a.by_args) {
     if (a.n_pages > kArgPages) return hipErrorInvalidValue;
     BoundsKernelArgs ka;
     ka.a = a;
     std::copy_n(a.pages, a.n_pages, ka.ids);
     std::fill(ka.ids + a.n_pages, ka.ids + kArgPages, 0);
-    if (dtype == 0) hipLaunchKernelGGL((bounds_kernel<ElemF32, true>), grid, block, 0, st, ka);
-    else hipLaunchKernelGGL((bounds_kernel<ElemBF16, true>), grid, block, 0, st, ka);
-  } else {
-    if (dtype == 0) hipLaunchKernelGGL((bounds_kernel<ElemF32, false>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((bounds_kernel<ElemBF16, false>), grid, block, 0, st, a);
+    const dim3 grid((unsigned)a.n_pages, (unsigned)a.n_layers);
+    if (dtype == 0) return launch_done(bounds_kernel<ElemF32, true, 1>, grid, dim3(256), st, a.done, ka);
+    return launch_done(bounds_kernel<ElemBF16, true, 1>, grid, dim3(256), st, a.done, ka);
   }
-  return hipGetLastError();
+  if ((int64_t)a.n_pages * a.n_layers <= kArgPages) {
+    const dim3 grid((unsigned)a.n_pages, (unsigned)a.n_layers);
+    if (dtype == 0) return launch_done(bounds_kernel<ElemF32, false, 1>, grid, dim3(256), st, a.done, a);
+    return launch_done(bounds_kernel<ElemBF16, false, 1>, grid, dim3(256), st, a.done, a);
+  }
+  const dim3 grid((unsigned)((a.n_pages + 7) / 8), (unsigned)a.n_layers);
+  if (dtype == 0) return launch_done(bounds_kernel<ElemF32, false, 8>, grid, dim3(512), st, a.done, a);
+  return launch_done(bounds_kernel<ElemBF16, false, 8>, grid, dim3(512), st, a.done, a);
 }
 
 hipError_t launch_sparse_scores(const SparseArgs& a, int dtype, hipStream_t st) {

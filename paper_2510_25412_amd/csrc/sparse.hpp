@@ -56,9 +56,10 @@ struct BoundsArgs {
   int64_t page_bytes, layer_bytes;
   uint8_t* bounds;
   int64_t layer_bounds;
-  const int32_t* pages;     // host (at most kArgPages) or device
+  const int32_t* pages;     // host (at most kArgPages), or pinned / device
   int32_t n_pages, Hkv, n_layers;
   int32_t by_args;
+  hipEvent_t done;
 };
 
 constexpr int SPARSE_ROW_WORDS = 2;    // page table (offset into the tables), tokens seen
