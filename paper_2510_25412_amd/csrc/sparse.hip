@@ -354,23 +354,23 @@ __global__ __launch_bounds__(256) void append_rope_runs_kernel(AppendRunsKernelA
 }
 
 // ---------------------------------------------------------------------------------------
-// Bounds of a list of pages.  A workgroup takes PB pages and a layer; its wavefronts take the (page, kv head) in turn, the next one's keys under
-// way while one is reduced.  PB = 1 for few pages, whose ids travel with the arguments or lie in device memory; 8 for many, whose list
-// may stay in pinned host memory: 32 bytes of it are one request over the host link for a workgroup.
-// Bound: HBM (4 KiB read for 512 bytes written).
+// Bounds of a list of pages.  A workgroup of W wavefronts takes an equal share of the pages (at most 64, an id to each lane) in one layer; its
+// wavefronts take the (page, kv head) in turn, the next one's keys under way while one is reduced.  W = 4, a page to a workgroup, for few
+// pages, whose ids travel with the arguments; W = 8 for many, as many workgroups as the chip holds at once, whose list may stay in pinned
+// host memory: a share is one request over the host link.  Bound: HBM (4 KiB read for 512 bytes written).
 // ---------------------------------------------------------------------------------------
 struct BoundsKernelArgs {
   BoundsArgs a;
   int32_t ids[kArgPages];
 };
-template <typename E, bool ARGS, int PB>
-__global__ __launch_bounds__(PB == 1 ? 256 : 512) void bounds_kernel(std::conditional_t<ARGS, BoundsKernelArgs, BoundsArgs>) {
-  constexpr int W = PB == 1 ? 4 : 8;
+template <typename E, bool ARGS, int W>
+__global__ __launch_bounds__(64 * W) void bounds_kernel(std::conditional_t<ARGS, BoundsKernelArgs, BoundsArgs>) {
   auto ka = (SYM_AS4 BoundsKernelArgs*)__builtin_amdgcn_kernarg_segment_ptr();
-  const int Hkv = ka->a.Hkv, n = min(PB, ka->a.n_pages - (int)blockIdx.x * PB) * Hkv, lane = threadIdx.x & 63;
+  const int first = (int)((int64_t)ka->a.n_pages * blockIdx.x / gridDim.x), end = (int)((int64_t)ka->a.n_pages * (blockIdx.x + 1) / gridDim.x);
+  const int Hkv = ka->a.Hkv, n = (end - first) * Hkv, at = min(first + (int)(threadIdx.x & 63), end - 1);
   int ids;                                       // lane l: page l of the workgroup's
-  if constexpr (ARGS) ids = ka->ids[blockIdx.x];
-  else ids = ka->a.pages[min((int)blockIdx.x * PB + lane % PB, ka->a.n_pages - 1)];
+  if constexpr (ARGS) ids = ka->ids[at];
+  else ids = ka->a.pages[at];
   const uint8_t* pool = ka->a.pool + blockIdx.y * ka->a.layer_bytes;
   uint8_t* bounds = ka->a.bounds + blockIdx.y * ka->a.layer_bounds;
   const int64_t page_bytes = ka->a.page_bytes;
@@ -1125,15 +1125,12 @@ hipError_t launch_bounds(const BoundsArgs& a, int dtype, hipStream_t st) {
     std::copy_n(a.pages, a.n_pages, ka.ids);
     std::fill(ka.ids + a.n_pages, ka.ids + kArgPages, 0);
     const dim3 grid((unsigned)a.n_pages, (unsigned)a.n_layers);
-    if (dtype == 0) return launch_done(bounds_kernel<ElemF32, true, 1>, grid, dim3(256), st, a.done, ka);
-    return launch_done(bounds_kernel<ElemBF16, true, 1>, grid, dim3(256), st, a.done, ka);
+    if (dtype == 0) return launch_done(bounds_kernel<ElemF32, true, 4>, grid, dim3(256), st, a.done, ka);
+    return launch_done(bounds_kernel<ElemBF16, true, 4>, grid, dim3(256), st, a.done, ka);
   }
-  if ((int64_t)a.n_pages * a.n_layers <= kArgPages) {
-    const dim3 grid((unsigned)a.n_pages, (unsigned)a.n_layers);
-    if (dtype == 0) return launch_done(bounds_kernel<ElemF32, false, 1>, grid, dim3(256), st, a.done, a);
-    return launch_done(bounds_kernel<ElemBF16, false, 1>, grid, dim3(256), st, a.done, a);
-  }
-  const dim3 grid((unsigned)((a.n_pages + 7) / 8), (unsigned)a.n_layers);
+  // 1024 workgroups of 8 wavefronts are all that 256 compute units hold
+  const int blocks = std::min(a.n_pages, std::max(std::max(1024 / a.n_layers, 1), (a.n_pages + 63) / 64));
+  const dim3 grid((unsigned)blocks, (unsigned)a.n_layers);
   if (dtype == 0) return launch_done(bounds_kernel<ElemF32, false, 8>, grid, dim3(512), st, a.done, a);
   return launch_done(bounds_kernel<ElemBF16, false, 8>, grid, dim3(512), st, a.done, a);
 }
