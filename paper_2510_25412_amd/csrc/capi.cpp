@@ -69,6 +69,7 @@ struct SparsePlan {
   int64_t entries = 0;                             // page ids in the tables
   int64_t n_counters = 0;
   int32_t n_rows = 0, n_runs = 0, run_tokens = 1;
+  bool alone = true;                               // no file of the batch has several new tokens or a first page that another file has too
   int32_t n_stale = 0, n_done = 0;                 // full pages without bounds: from before the batch, then those that it completes
   int32_t splits = 1, score_stride = 0, group_rows = 1;
   int64_t q_bytes = 0, row_bytes = 0;              // scratch: turned query rows of the batch; per row and slab
@@ -867,6 +868,7 @@ int size_sparse(sym_ctx* c, SparsePlan* sp, int32_t n_lips, const sym_kv* kv, co
     const int64_t after = f->len + n_tokens[b], pages = (after + P - 1) / P;
     entries += pages;
     sp->run_tokens = std::max(sp->run_tokens, n_tokens[b]);
+    sp->alone = sp->alone && n_tokens[b] == 1 && (f->pages.empty() || c->fs->refcount(f->pages[0]) == 1);
     stale += f->len / P - f->bounded;
     done += after / P - f->len / P;
     most_pages = std::max(most_pages, pages);
@@ -1007,6 +1009,7 @@ int run_sparse_layer(sym_ctx* c, const SparsePlan& sp, uint8_t* ws, int64_t word
   a.last = sp.last;
   a.score_stride = sp.score_stride;
   a.splits = sp.splits;
+  a.stream = sp.alone ? 1 : 0;
   a.scale_log2e = c->scale_log2e;
   for (const SparsePlan::Slab& s : sp.slabs) {
     a.row0 = s.row0;

@@ -660,7 +660,9 @@ __device__ __forceinline__ void pick_highest(const uint32_t* sc, const int m, co
 // Every workgroup chooses from the row's scores for itself and keeps its part of the list in LDS, where it reads like a
 // file's page table: only the last page may be partly filled.  One pass over the pages, with the running maximum and sum of the softmax in
 // fp32; the wavefronts' results are combined through LDS.  The workgroup that finishes last of a row's parts joins them, so that no
-// launch follows.  Bound: HBM (8 KiB for 4 D 16 G flops).
+// launch follows.  STREAM: nontemporal loads, where no two rows read the same pages (64 files 62.4 -> 59.3 us a call); where they do (several
+// tokens of a file, forks) the next row finds them in a cache (chunks 72 us, with nontemporal loads 95).
+// Bound: HBM (8 KiB for 4 D 16 G flops).
 // ---------------------------------------------------------------------------------------
 // What workgroups of one launch hand to each other goes past the caches that they do not share, in both directions, and a workgroup
 // counts itself done when its stores have arrived.  (A release fence instead writes back everything in the L2: with one from every
@@ -683,7 +685,7 @@ __device__ __forceinline__ bool comes_last(int32_t* counter, const int all, int&
 // into 16 each takes a column of one product.  With 8 heads per kv head there are two products to the same sums: the upper part halved in columns 0..7
 // of both (0 there would make an infinite V NaN), the middle and the lower part in columns 8..15.  (Weights cut to 16 bits in one
 // product: error against 64 bits 4.8e-6 instead of 2e-7.)
-template <int G>
+template <int G, bool STREAM>
 struct AttendMx {
   typedef ElemBF16 Elem;
   static constexpr int D = 128;
@@ -717,9 +719,9 @@ struct AttendMx {
     const uint8_t* kb = slab + col * kHalfBytes + grp * 16;
     const uint8_t* vb = slab + kBlk + (col >> 3) * (kP * kHalfBytes) + (4 * grp) * kHalfBytes + (col & 7) * 16;
 #pragma unroll
-    for (int ks = 0; ks < 4; ++ks) R.k[ks] = *(const uint4*)(kb + (ks >> 1) * (kP * kHalfBytes) + (ks & 1) * 64);
+    for (int ks = 0; ks < 4; ++ks) R.k[ks] = ld16<STREAM>(kb + (ks >> 1) * (kP * kHalfBytes) + (ks & 1) * 64);
 #pragma unroll
-    for (int u = 0; u < 4; ++u) R.v[u] = *(const uint4*)(vb + u * kHalfBytes);
+    for (int u = 0; u < 4; ++u) R.v[u] = ld16<STREAM>(vb + u * kHalfBytes);
   }
   __device__ __forceinline__ void page(PageRegs& R, const int nvalid) {
     f32x4_t S = {0.f, 0.f, 0.f, 0.f}, S2 = {0.f, 0.f, 0.f, 0.f};
@@ -800,7 +802,7 @@ struct AttendMx {
 };
 
 // fp32 storage: on the vector units, lane (r, j) holds tokens r and 8 + r of a page and 8 dims; running maximum and sum are each lane's own.
-template <int G>
+template <int G, bool STREAM>
 struct AttendF32 {
   typedef ElemF32 Elem;
   static constexpr int C = 4, DPL = 8, D = 64;
@@ -827,9 +829,9 @@ struct AttendF32 {
   __device__ __forceinline__ void request(PageRegs& R, const uint8_t* slab) const {
     const uint8_t* b = slab + (threadIdx.x & 63) * 16;
 #pragma unroll
-    for (int x = 0; x < 4; ++x) R.k[x] = *(const uint4*)(b + x * 1024);
+    for (int x = 0; x < 4; ++x) R.k[x] = ld16<STREAM>(b + x * 1024);
 #pragma unroll
-    for (int x = 0; x < 4; ++x) R.v[x] = *(const uint4*)(b + kBlk + x * 1024);
+    for (int x = 0; x < 4; ++x) R.v[x] = ld16<STREAM>(b + kBlk + x * 1024);
   }
   __device__ __forceinline__ void page(PageRegs& R, const int nvalid) {
 #pragma unroll
@@ -1154,14 +1156,17 @@ hipError_t launch_sparse_attend(const SparseArgs& a, int dtype, hipStream_t st) 
   if (a.n_rows <= 0) return hipSuccess;
   const bool own = scores_itself(a.most_scored);
   const dim3 grid((unsigned)(a.n_rows * a.Hkv * a.splits)), block(64 * attend_waves(a.most_scored));
+#define SYM_ATTEND_ROWS(AT, GG, STREAM) \
+  if (own) hipLaunchKernelGGL((sparse_attend_kernel<AT<GG, STREAM>, GG, true, 4>), grid, block, 0, st, a); \
+  else hipLaunchKernelGGL((sparse_attend_kernel<AT<GG, STREAM>, GG, false, 8>), grid, block, 0, st, a)
 #define SYM_ATTEND(GG) \
   case GG: \
     if (dtype == 0) { \
-      if (own) hipLaunchKernelGGL((sparse_attend_kernel<AttendF32<GG>, GG, true, 4>), grid, block, 0, st, a); \
-      else hipLaunchKernelGGL((sparse_attend_kernel<AttendF32<GG>, GG, false, 8>), grid, block, 0, st, a); \
+      if (a.stream) SYM_ATTEND_ROWS(AttendF32, GG, true); \
+      else SYM_ATTEND_ROWS(AttendF32, GG, false); \
     } else { \
-      if (own) hipLaunchKernelGGL((sparse_attend_kernel<AttendMx<GG>, GG, true, 4>), grid, block, 0, st, a); \
-      else hipLaunchKernelGGL((sparse_attend_kernel<AttendMx<GG>, GG, false, 8>), grid, block, 0, st, a); \
+      if (a.stream) SYM_ATTEND_ROWS(AttendMx, GG, true); \
+      else SYM_ATTEND_ROWS(AttendMx, GG, false); \
     } \
     break;
   switch (a.Hq / a.Hkv) {
@@ -1169,6 +1174,7 @@ hipError_t launch_sparse_attend(const SparseArgs& a, int dtype, hipStream_t st) 
     default: return hipErrorInvalidValue;
   }
 #undef SYM_ATTEND
+#undef SYM_ATTEND_ROWS
   return hipGetLastError();
 }
 

@@ -87,6 +87,7 @@ struct SparseArgs {
   int32_t Hq, Hkv, budget, first, last;
   int32_t score_stride;
   int32_t splits;
+  int32_t stream;           // no two rows read the same pages, as far as the host looks
   float scale_log2e;
 };
 
