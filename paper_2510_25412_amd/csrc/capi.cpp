@@ -961,29 +961,6 @@ int run_sparse_layer(sym_ctx* c, const SparsePlan& sp, uint8_t* ws, int64_t word
   void* q_turned = at;
   at += sp.q_bytes;
   const int64_t H = c->cfg.n_kv_heads;
-  {
-    AppendRopeArgs a = append_args(c, layer, 1, sp.n_rows, k_new, v_new, sp.pos);
-    a.q = sp.turns ? q : nullptr;
-    a.q_out = q_turned;
-    a.runs = blob + sp.off_runs;
-    a.n_runs = sp.n_runs;
-    a.run_tokens = sp.run_tokens;
-    const StageDone done(c, stage);
-    if (stage >= 0) {                              // the lists travel with this launch
-      a.host_words = c->stage[stage];
-      a.dev_words = (int32_t*)ws;
-      a.copy_words = words;
-      a.by_args = sp.n_runs <= kArgRuns ? 1 : 0;
-      a.runs = c->stage[stage] + sp.off_runs;
-      a.done = done.event();
-    }
-    Timed t(c, SYM_K_PROLOGUE, st);
-    const hipError_t e = launch_append_rope(a, sp.rope, c->cfg.dtype, st);
-    if (e != hipSuccess) return fail_hip(c, e, "append launch");
-    if (stage >= 0)
-      if (int rc = done.launched(st)) return rc;
-  }
-  if (int rc = batch_bounds(c, sp, blob, layer, sp.n_stale, st)) return rc;
   SparseArgs a{};
   a.pool = pool_of(c, layer);
   a.page_bytes = c->page_bytes;
@@ -1011,18 +988,51 @@ int run_sparse_layer(sym_ctx* c, const SparsePlan& sp, uint8_t* ws, int64_t word
   a.splits = sp.splits;
   a.stream = sp.alone ? 1 : 0;
   a.scale_log2e = c->scale_log2e;
-  for (const SparsePlan::Slab& s : sp.slabs) {
+  auto slab_args = [&](const SparsePlan::Slab& s) {
     a.row0 = s.row0;
     a.n_rows = s.rows;
     a.group0 = s.group0;
     a.n_groups = s.groups;
     a.most_scored = s.most_scored;
-    hipError_t e = hipSuccess;
-    {
-      Timed t(c, SYM_K_ATTN, st, false, true, 1 + (s.groups > 0 && !scores_itself(s.most_scored)));
-      if (s.groups > 0) e = launch_sparse_scores(a, c->cfg.dtype, st);
-      if (e == hipSuccess) e = launch_sparse_attend(a, c->cfg.dtype, st);
+  };
+  AppendRopeArgs ap = append_args(c, layer, 1, sp.n_rows, k_new, v_new, sp.pos);
+  ap.q = sp.turns ? q : nullptr;
+  ap.q_out = q_turned;
+  ap.runs = blob + sp.off_runs;
+  ap.n_runs = sp.n_runs;
+  ap.run_tokens = sp.run_tokens;
+  slab_args(sp.slabs[0]);
+  // single tokens, no bounds missing, the lists on the device, few scores: append and scores in one launch
+  const bool together = stage < 0 && sp.run_tokens == 1 && sp.n_stale == 0 && sp.slabs.size() == 1 &&
+                        scores_with_append(sp.rope, sp.turns, a.Hkv, a.n_groups, a.most_scored);
+  if (together) {
+    Timed t(c, SYM_K_ATTN, st);
+    const hipError_t e = launch_sparse_first(ap, sp.rope, a, c->cfg.dtype, st);
+    if (e != hipSuccess) return fail_hip(c, e, "append and scores launch");
+  } else {
+    const StageDone done(c, stage);
+    if (stage >= 0) {                              // the lists travel with this launch
+      ap.host_words = c->stage[stage];
+      ap.dev_words = (int32_t*)ws;
+      ap.copy_words = words;
+      ap.by_args = sp.n_runs <= kArgRuns ? 1 : 0;
+      ap.runs = c->stage[stage] + sp.off_runs;
+      ap.done = done.event();
     }
+    Timed t(c, SYM_K_PROLOGUE, st);
+    const hipError_t e = launch_append_rope(ap, sp.rope, c->cfg.dtype, st);
+    if (e != hipSuccess) return fail_hip(c, e, "append launch");
+    if (stage >= 0)
+      if (int rc = done.launched(st)) return rc;
+  }
+  if (int rc = batch_bounds(c, sp, blob, layer, sp.n_stale, st)) return rc;
+  for (const SparsePlan::Slab& s : sp.slabs) {
+    slab_args(s);
+    const bool scores = s.groups > 0 && !scores_itself(s.most_scored) && !together;
+    Timed t(c, SYM_K_ATTN, st, false, true, 1 + scores);
+    hipError_t e = hipSuccess;
+    if (scores) e = launch_sparse_scores(a, c->cfg.dtype, st);
+    if (e == hipSuccess) e = launch_sparse_attend(a, c->cfg.dtype, st);
     if (e != hipSuccess) return fail_hip(c, e, "sparse attention launch");
   }
   return SYM_OK;

@@ -285,10 +285,10 @@ struct AppendRunsKernelArgs {
   ArgRuns runs;
 };
 template <typename E, int PATH>
-__device__ __forceinline__ void append_run(SYM_AS4 AppendKernelArgs* ka, const int t0, const int slot, const int nf, const int pos0, double2 (*cs)[kPairs], uint8_t (*stage)[kRowBytes]) {
-  const int n = nf & 0xff, Hkv = ka->a.Hkv, Hq = ka->a.q ? ka->a.Hq : 0, layer = blockIdx.y;
-  // this workgroup's rows of a token: keys and values, or a part of the query rows
-  const int part = (int)blockIdx.z - 1, parts = (int)gridDim.z - 1;
+__device__ __forceinline__ void append_run(SYM_AS4 AppendKernelArgs* ka, const int t0, const int slot, const int nf, const int pos0, const int layer, const int part, const int parts,
+                                           double2 (*cs)[kPairs], uint8_t (*stage)[kRowBytes]) {
+  const int n = nf & 0xff, Hkv = ka->a.Hkv, Hq = ka->a.q ? ka->a.Hq : 0;
+  // this workgroup's rows of a token: keys and values (part -1), or a part of the query rows
   const int first = part < 0 ? 0 : 2 * Hkv + Hq * part / parts, rows = (part < 0 ? 2 * Hkv : 2 * Hkv + Hq * (part + 1) / parts) - first;
   if (rows <= 0) return;
   uint8_t* page = ka->a.pool + layer * ka->a.layer_bytes + (int64_t)(slot / kP) * ka->a.page_bytes;
@@ -341,7 +341,7 @@ __global__ __launch_bounds__(256) void append_rope_kernel(AppendKernelArgs) {
   auto ka = (SYM_AS4 AppendKernelArgs*)__builtin_amdgcn_kernarg_segment_ptr();
   if (copy_lists(ka)) return;
   const int32_t* w = ka->a.runs + (int64_t)blockIdx.x * RUN_WORDS;
-  append_run<E, PATH>(ka, sload(w), sload(w + 1), sload(w + 2), sload(w + 3), cs, stage);
+  append_run<E, PATH>(ka, sload(w), sload(w + 1), sload(w + 2), sload(w + 3), blockIdx.y, (int)blockIdx.z - 1, (int)gridDim.z - 1, cs, stage);
 }
 template <typename E, int PATH>
 __global__ __launch_bounds__(256) void append_rope_runs_kernel(AppendRunsKernelArgs) {
@@ -350,7 +350,7 @@ __global__ __launch_bounds__(256) void append_rope_runs_kernel(AppendRunsKernelA
   auto ka = (SYM_AS4 AppendRunsKernelArgs*)__builtin_amdgcn_kernarg_segment_ptr();
   if (copy_lists(&ka->k)) return;
   const auto* w = ka->runs.w + blockIdx.x * RUN_WORDS;
-  append_run<E, PATH>(&ka->k, w[0], w[1], w[2], w[3], cs, stage);
+  append_run<E, PATH>(&ka->k, w[0], w[1], w[2], w[3], blockIdx.y, (int)blockIdx.z - 1, (int)gridDim.z - 1, cs, stage);
 }
 
 // ---------------------------------------------------------------------------------------
@@ -413,12 +413,12 @@ __device__ __forceinline__ uint32_t order_of(float x) {
   return (b & 0x80000000u) ? ~b : b | 0x80000000u;
 }
 
-// A wavefront's scores of 32 pages at a time, for one kv head and up to RT consecutive tokens.
-template <typename E, int RT>
+// A wavefront's scores of 2 STEPS pages at a time, for one kv head and up to RT consecutive tokens.
+template <typename E, int RT, int STEPS = kScorePages / 2>
 struct Scorer {
   static constexpr int C = E::kDimsPerChunk;
   double cf[RT][C];                              // coefficients of this lane's chunk: lanes 0..15 of a page hold lo, 16..31 hi
-  int id[kScorePages / 2];                       // pages 2 s + (upper half of the wavefront)
+  int id[STEPS];                                 // pages 2 s + (upper half of the wavefront)
 
   __device__ __forceinline__ void coefficients(const SparseArgs& a, const int r0, const int nr, const int head) {
     const int hl = threadIdx.x & 31, part = hl >> 4, chunk = hl & 15, G = a.Hq / a.Hkv;
@@ -427,17 +427,19 @@ struct Scorer {
 #pragma unroll
       for (int e = 0; e < C; ++e) cf[t][e] = 0.0;
       const uint8_t* q = (const uint8_t*)a.q + ((int64_t)(r0 + min(t, nr - 1)) * a.Hq + head * G) * kRowBytes + chunk * 16;
-      for (int h = 0; h < G; ++h) {
-        float x[C];
-        E::unpack(*(const uint4*)(q + h * kRowBytes), x);
-#pragma unroll
-        for (int e = 0; e < C; ++e) cf[t][e] += (double)(part ? (x[e] < 0.f ? 0.f : x[e]) : (x[e] > 0.f ? 0.f : x[e]));
-      }
+      for (int h = 0; h < G; ++h) add(t, part, *(const uint4*)(q + h * kRowBytes));
     }
+  }
+  // one query head's chunk
+  __device__ __forceinline__ void add(const int t, const int part, const uint4& row) {
+    float x[C];
+    E::unpack(row, x);
+#pragma unroll
+    for (int e = 0; e < C; ++e) cf[t][e] += (double)(part ? (x[e] < 0.f ? 0.f : x[e]) : (x[e] > 0.f ? 0.f : x[e]));
   }
   __device__ __forceinline__ void ids(const int32_t* pt, const int p0, const int end) {
 #pragma unroll
-    for (int s = 0; s < kScorePages / 2; ++s) id[s] = pt[min(p0 + 2 * s + (int)((threadIdx.x & 63) >> 5), end - 1)];
+    for (int s = 0; s < STEPS; ++s) id[s] = pt[min(p0 + 2 * s + (int)((threadIdx.x & 63) >> 5), end - 1)];
   }
   // put(token, page, key) of the pages p0 .. of id, below end; next() runs when id has been used
   template <typename N, typename P>
@@ -446,11 +448,11 @@ struct Scorer {
     const uint8_t* rec = a.bounds + head * (2 * kRowBytes) + hl * 16;
     const int64_t page_rec = (int64_t)a.Hkv * (2 * kRowBytes);
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
+    for (int b = 0; b < STEPS / 8; ++b) {
       uint4 x[8];
 #pragma unroll
       for (int s = 0; s < 8; ++s) x[s] = *(const uint4*)(rec + (int64_t)id[b * 8 + s] * page_rec);
-      if (b == 1) next();
+      if (b == STEPS / 8 - 1) next();
 #pragma unroll
       for (int t = 0; t < RT; ++t) {
         double v[8];
@@ -503,6 +505,94 @@ __global__ __launch_bounds__(256) void sparse_scores_kernel(SparseArgs a) {
   sc.score(a, head, p0, end, [] {}, [&](int t, int p, uint32_t key) {
     if (t < nr) scores[t * row_scores + (p - a.first)] = key;
   });
+}
+
+// ---------------------------------------------------------------------------------------
+// Append and scores of a small batch in one launch: single new tokens, few pages to score.  The first workgroups append as above; the
+// others score 16 pages to a wavefront and turn the query rows for themselves, because those that the others write are not there yet.
+// (The pages that the tokens complete are their rows' last ones, which nobody scores.)  What it saves is a launch's start and end: 8
+// layers of one file of 30000 tokens.
+// ---------------------------------------------------------------------------------------
+struct FirstKernelArgs {
+  AppendKernelArgs k;
+  SparseArgs s;
+  int32_t parts, append_blocks, group_blocks;      // workgroups of a run beside the first, of all runs, of a scored row
+};
+// Chunk `c` of a row, turned: its own 16 bytes and those that hold its pairs' other elements.
+template <typename E, int PATH>
+__device__ __forceinline__ uint4 turned_chunk(const uint4& own, const uint4& other, const int c, const int dims, const double2* cs) {
+  constexpr int C = E::kDimsPerChunk;
+  float a[C], b[C], y[C];
+  E::unpack(own, a);
+  E::unpack(other, b);
+  u32x4_t r = __builtin_bit_cast(u32x4_t, own);
+  if constexpr (PATH == ROPE_HALVES) {
+    const int hr = dims / 2 / C;
+    if (c >= 2 * hr) return own;
+    const bool upper = c >= hr;
+#pragma unroll
+    for (int e = 0; e < C; ++e) {
+      const double2 t = cs[(upper ? c - hr : c) * C + e];
+      y[e] = round_f32(upper ? (double)a[e] * t.x + (double)b[e] * t.y : (double)a[e] * t.x - (double)b[e] * t.y);
+    }
+    r = pack_chunk<E>(y);
+  } else if constexpr (PATH == ROPE_INTERLEAVED) {
+#pragma unroll
+    for (int p = 0; p < C / 2; ++p) {
+      const double2 t = cs[c * (C / 2) + p];
+      y[2 * p] = round_f32((double)a[2 * p] * t.x - (double)a[2 * p + 1] * t.y);
+      y[2 * p + 1] = round_f32((double)a[2 * p + 1] * t.x + (double)a[2 * p] * t.y);
+    }
+    const u32x4_t t = pack_chunk<E>(y);
+#pragma unroll
+    for (int w = 0; w < 4; ++w)
+      if (c * C + w * (C / 4) < dims) r[w] = t[w];
+  }
+  return __builtin_bit_cast(uint4, r);
+}
+template <typename E, int PATH>
+__global__ __launch_bounds__(256) void sparse_first_kernel(FirstKernelArgs) {
+  constexpr int C = E::kDimsPerChunk;
+  __shared__ double2 cs[1][kPairs];
+  auto ka = (SYM_AS4 FirstKernelArgs*)__builtin_amdgcn_kernarg_segment_ptr();
+  if ((int)blockIdx.x < ka->append_blocks) {
+    const int run = (int)blockIdx.x / (1 + ka->parts), part = (int)blockIdx.x % (1 + ka->parts) - 1;
+    const int32_t* w = ka->k.a.runs + (int64_t)run * RUN_WORDS;
+    append_run<E, PATH>(&ka->k, sload(w), sload(w + 1), sload(w + 2), sload(w + 3), 0, part, ka->parts, cs, nullptr);
+    return;
+  }
+  const int blk = (int)blockIdx.x - ka->append_blocks, grp_at = blk / ka->group_blocks, Hkv = ka->s.Hkv, first = ka->s.first;
+  const int32_t* grp = ka->s.groups + (int64_t)grp_at * SPARSE_GROUP_WORDS;
+  const int row = sload(grp), tbl = sload(grp + 2), end = sload(grp + 3);
+  const int wave = __builtin_amdgcn_readfirstlane(blk % ka->group_blocks * 4 + (int)(threadIdx.x >> 6));
+  const int head = wave % Hkv, p0 = first + wave / Hkv * kFirstPages, G = ka->s.Hq / Hkv;
+  const int chunk = threadIdx.x & 15, part = (threadIdx.x >> 4) & 1, hr = ka->k.r.dims / 2 / C;
+  const int other = PATH == ROPE_HALVES ? (chunk < hr ? chunk + hr : chunk < 2 * hr ? chunk - hr : chunk) : chunk;
+  SparseArgs a{};                                // (what score() reads of it)
+  a.bounds = ka->s.bounds;
+  a.Hkv = Hkv;
+  Scorer<E, 1, kFirstPages / 2> sc;
+  sc.ids(ka->s.tables + tbl, min(p0, end - 1), end);
+  const uint8_t* q = (const uint8_t*)ka->k.a.q + ((int64_t)row * ka->s.Hq + head * G) * kRowBytes;
+  uint4 x[8], y[8];                                // (G <= 8)
+#pragma unroll
+  for (int h = 0; h < 8; ++h) {
+    x[h] = *(const uint4*)(q + min(h, G - 1) * kRowBytes + chunk * 16);
+    if constexpr (PATH == ROPE_HALVES) y[h] = *(const uint4*)(q + min(h, G - 1) * kRowBytes + other * 16);
+    else y[h] = x[h];
+  }
+  const int32_t* pos = ka->k.a.pos;
+  const int at = pos ? pos[row] : sload(ka->s.rows + (int64_t)row * SPARSE_ROW_WORDS + 1) - 1;
+  if ((int)threadIdx.x < ka->k.r.dims / 2) cs[0][threadIdx.x] = angle_of(&ka->k.r, at, threadIdx.x);
+  __syncthreads();
+  if (p0 >= end) return;
+#pragma unroll
+  for (int e = 0; e < C; ++e) sc.cf[0][e] = 0.0;
+#pragma unroll
+  for (int h = 0; h < 8; ++h)
+    if (h < G) sc.add(0, part, turned_chunk<E, PATH>(x[h], y[h], chunk, ka->k.r.dims, cs[0]));
+  uint32_t* scores = ka->s.scores + ((int64_t)row * Hkv + head) * ka->s.score_stride;
+  sc.score(a, head, p0, end, [] {}, [&](int, int p, uint32_t key) { scores[p - first] = key; });
 }
 
 constexpr int kMostWaves = 8;                   // of a workgroup that attends
@@ -1137,8 +1227,25 @@ hipError_t launch_bounds(const BoundsArgs& a, int dtype, hipStream_t st) {
   return launch_done(bounds_kernel<ElemBF16, false, 8>, grid, dim3(512), st, a.done, a);
 }
 
+hipError_t launch_sparse_first(const AppendRopeArgs& a, const RopeTable& r, const SparseArgs& s, int dtype, hipStream_t st) {
+  FirstKernelArgs ka{{a, r}, s, std::max(a.Hq / 128, 1), 0, 0};
+  ka.append_blocks = a.n_runs * (1 + ka.parts);
+  ka.group_blocks = ((s.most_scored + kFirstPages - 1) / kFirstPages * s.Hkv + 3) / 4;
+  const dim3 grid((unsigned)(ka.append_blocks + ka.group_blocks * s.n_groups)), block(256);
+#define SYM_LAUNCH(E) \
+  if (r.path == ROPE_HALVES) hipLaunchKernelGGL((sparse_first_kernel<E, ROPE_HALVES>), grid, block, 0, st, ka); \
+  else hipLaunchKernelGGL((sparse_first_kernel<E, ROPE_INTERLEAVED>), grid, block, 0, st, ka)
+  if (dtype == 0) {
+    SYM_LAUNCH(ElemF32);
+  } else {
+    SYM_LAUNCH(ElemBF16);
+  }
+#undef SYM_LAUNCH
+  return hipGetLastError();
+}
+
 hipError_t launch_sparse_scores(const SparseArgs& a, int dtype, hipStream_t st) {
-  if (a.n_groups <= 0 || scores_itself(a.most_scored)) return hipSuccess;
+  if (a.n_groups <= 0) return hipSuccess;
   const int64_t waves = (int64_t)((a.most_scored + kScorePages - 1) / kScorePages) * a.Hkv;
   if (a.n_groups > 65535) return hipErrorInvalidValue;
   const dim3 grid((unsigned)((waves + 3) / 4), (unsigned)a.n_groups), block(256);

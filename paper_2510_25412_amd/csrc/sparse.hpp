@@ -96,11 +96,21 @@ constexpr int kOwnScores = 512;
 inline bool scores_itself(int64_t most_scored) { return most_scored <= kOwnScores; }
 inline int attend_waves(int64_t most_scored) { return scores_itself(most_scored) ? 4 : 8; }
 
+// Whether the append of a batch and its scores are one launch, for a batch of single tokens with no bounds missing: turned query rows
+// in pairs that a lane holds, and few wavefronts to score.
+constexpr int kFirstPages = 16;            // of a wavefront that scores there
+constexpr int64_t kFirstWaves = 2048;
+inline bool scores_with_append(const RopeTable& r, bool turns, int Hkv, int64_t n_groups, int64_t most_scored) {
+  return turns && (r.path == ROPE_HALVES || r.path == ROPE_INTERLEAVED) && n_groups > 0 && !scores_itself(most_scored) &&
+         (most_scored + kFirstPages - 1) / kFirstPages * Hkv * n_groups <= kFirstWaves;
+}
+
 // Weak: the host code is also built without kernels (by tests of the host side, against stand-ins for the launches it made before these).
 #define SYMKV_LAUNCH __attribute__((weak))
 SYMKV_LAUNCH hipError_t launch_rope_rows(RopeRowsArgs a, const RopeTable& r, int dtype, hipStream_t st);
 SYMKV_LAUNCH hipError_t launch_append_rope(const AppendRopeArgs& a, const RopeTable& r, int dtype, hipStream_t st);
 SYMKV_LAUNCH hipError_t launch_bounds(const BoundsArgs& a, int dtype, hipStream_t st);
+SYMKV_LAUNCH hipError_t launch_sparse_first(const AppendRopeArgs& a, const RopeTable& r, const SparseArgs& s, int dtype, hipStream_t st);
 SYMKV_LAUNCH hipError_t launch_sparse_scores(const SparseArgs& a, int dtype, hipStream_t st);
 SYMKV_LAUNCH hipError_t launch_sparse_attend(const SparseArgs& a, int dtype, hipStream_t st);
 // Makes the device current and returns the one that was (-1: nothing to undo); the other way round.

@@ -18,6 +18,7 @@ hipError_t launch_bounds(const BoundsArgs& a, int, hipStream_t) {
   if (!a.by_args) add(c, a.pages, (int64_t)a.n_pages * 4);
   return launch(c);
 }
+hipError_t launch_sparse_first(const AppendRopeArgs&, const RopeTable&, const SparseArgs&, int, hipStream_t) { return launch({}); }
 hipError_t launch_sparse_scores(const SparseArgs&, int, hipStream_t) { return launch({}); }
 hipError_t launch_sparse_attend(const SparseArgs&, int, hipStream_t) { return launch({}); }
 }  // namespace symkv

@@ -693,3 +693,20 @@ def test_forks_of_one_prompt():
     for new in ([1] * 8, [12] + [1] * 7, [1] * 8):
         run_sparse(sess, kids, new, binding.make_sparse(7, 1, 2, rope=rope), rope, lc.frequencies(128), g=g)
     sess.close()
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,layout,dims,lens", [("bf16", 8, 1, "halves", 0, [8991, 20, 8300]), ("bf16", 8, 4, "interleaved", 36, [8300]), ("f32", 4, 2, "halves", 16, [8815, 8400]),
+                                                           ("f32", 3, 3, "interleaved", 64, [8303]), ("bf16", 2, 2, "halves", 24, [8400]), ("bf16", 16, 8, "halves", 0, [8400] * 4)])
+@pytest.mark.parametrize("given", [False, True])
+def test_steps_over_layers_of_files_with_many_scores(dtype, hq, hkv, layout, dims, lens, given):
+    # later steps find all bounds there: their appends and scores may go together (files that complete a page, one with nothing to score;
+    # 24 elements are halves that a lane does not hold, and four files of eight heads have too many scores for that)
+    print(f"[case] layers, many scores {dtype} {hq}/{hkv} {layout} {dims} {lens} {given}", flush=True)
+    sess = session(dtype, hq, hkv, sum(-(-n // P) + 2 for n in lens), layers=2)
+    g = torch.Generator().manual_seed(len(lens))
+    files = make_files(sess, lens, g)
+    rope = binding.make_rope(layout, dims, base=50000.0, magnitude=1.25)
+    for _ in range(3):
+        pos = torch.tensor([n + 70001 for n in map(sess.ctx.kv_len, files)], dtype=torch.int32, device="cuda") if given else None
+        run_sparse(sess, files, [1] * len(files), binding.make_sparse(9, 1, 2, rope=rope, positions=pos), rope, lc.frequencies(dims or DIM[dtype], 50000.0), layout, g=g, pos=pos)
+    sess.close()
