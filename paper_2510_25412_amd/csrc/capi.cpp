@@ -65,16 +65,17 @@ struct SparsePlan {
   bool turns = false;                              // a rope is given
   RopeTable rope;
   const int32_t* pos = nullptr;
-  int64_t off_rows = 0, off_tables = 0, off_groups = 0, off_runs = 0, off_pages = 0, off_counters = 0;   // word offsets in the blob
+  int64_t off_rows = 0, off_tables = 0, off_scored = 0, off_runs = 0, off_pages = 0, off_counters = 0;   // word offsets in the blob
   int64_t entries = 0;                             // page ids in the tables
   int64_t n_counters = 0;
   int32_t n_rows = 0, n_runs = 0, run_tokens = 1;
   bool alone = true;                               // no file of the batch has several new tokens or a first page that another file has too
   int32_t n_stale = 0, n_done = 0;                 // full pages without bounds: from before the batch, then those that it completes
-  int32_t splits = 1, score_stride = 0, group_rows = 1;
+  int32_t splits = 1, waves = 4, score_stride = 0;
+  bool own = false;                                // the attention scores pages itself
   int64_t q_bytes = 0, row_bytes = 0;              // scratch: turned query rows of the batch; per row and slab
   struct Slab {
-    int32_t row0, rows, group0, groups, most_scored;
+    int32_t row0, rows, scored0, scored, most_scored;
   };
   int64_t slab_rows = 0;                           // rows that fit the scratch at a time
   std::vector<Slab> slabs;
@@ -884,10 +885,12 @@ int size_sparse(sym_ctx* c, SparsePlan* sp, int32_t n_lips, const sym_kv* kv, co
   // Parts of a list: where rows are few as many workgroups as fill the chip, each with eight pages at least; no more pages than a
   // workgroup's list holds.
   const int64_t units = tokens * H, most_scored = most_pages > sp->budget ? most_pages - sp->first - sp->last : 0;
-  sp->splits = (int32_t)std::max({(int64_t)1, std::min(2048 / attend_waves(most_scored) / units, most_kept / 8), (most_kept + kPartPages - 1) / kPartPages});
+  sp->own = scores_itself(units, most_scored);
+  sp->waves = attend_waves(sp->own, units);
+  sp->splits = (int32_t)std::max({(int64_t)1, std::min(2048 / sp->waves / units, most_kept / 8), (most_kept + kPartPages - 1) / kPartPages});
   sp->q_bytes = sp->turns ? align_up(row_bytes_of(tokens, c->cfg.n_q_heads), 256) : 0;
   sp->n_counters = sp->splits > 1 ? H * std::max<int64_t>(1, std::min(tokens, kMostUnits / (H * sp->splits))) : 0;
-  *words = sp->n_rows * (int64_t)(SPARSE_ROW_WORDS + SPARSE_GROUP_WORDS) + entries + runs * RUN_WORDS + stale + done + sp->n_counters + 16;
+  *words = sp->n_rows * (int64_t)(SPARSE_ROW_WORDS + SPARSE_SCORED_WORDS) + entries + runs * RUN_WORDS + stale + done + sp->n_counters + 16;
   return SYM_OK;
 }
 int fit_sparse(sym_ctx* c, SparsePlan* sp, int64_t ws_bytes, int64_t blob_words) {
@@ -899,52 +902,41 @@ int fit_sparse(sym_ctx* c, SparsePlan* sp, int64_t ws_bytes, int64_t blob_words)
   if (sp->slab_rows < 1) return fail(c, SYM_ENOSPC, "workspace too small for this sparse batch");
   return SYM_OK;
 }
-// Writes the sections at word `at` of `blob` (after the append): rows, groups, tables, runs, pages without bounds, counters.
+// Writes the sections at word `at` of `blob` (after the append): rows, scored rows, tables, runs, pages without bounds, counters.
 void fill_sparse(sym_ctx* c, SparsePlan* sp, int32_t n_lips, const sym_kv* kv, const int32_t* n_tokens, int32_t* blob, int64_t at) {
   const int32_t P = c->cfg.page_tokens;
   sp->off_rows = at;
-  sp->off_groups = sp->off_rows + (int64_t)sp->n_rows * SPARSE_ROW_WORDS;
-  sp->off_tables = sp->off_groups + (int64_t)sp->n_rows * SPARSE_GROUP_WORDS;
+  sp->off_scored = sp->off_rows + (int64_t)sp->n_rows * SPARSE_ROW_WORDS;
+  sp->off_tables = sp->off_scored + (int64_t)sp->n_rows * SPARSE_SCORED_WORDS;
   sp->off_runs = sp->off_tables + sp->entries;
   sp->off_pages = sp->off_runs + (int64_t)sp->n_runs * RUN_WORDS;
   sp->off_counters = sp->off_pages + sp->n_stale + sp->n_done;
-  int32_t *rows = blob + sp->off_rows, *groups = blob + sp->off_groups, *tables = blob + sp->off_tables;
+  int32_t *rows = blob + sp->off_rows, *scored = blob + sp->off_scored, *tables = blob + sp->off_tables;
   int32_t *stale = blob + sp->off_pages, *done = stale + sp->n_stale;
   append_runs(c, n_lips, kv, n_tokens, &c->words);
   copy_bytes(blob + sp->off_runs, c->words.data(), c->words.size() * 4);
   sp->slabs.clear();
-  sp->group_rows = 1;
-  int32_t row = 0, tbl = 0, n_groups = 0;
+  int32_t row = 0, tbl = 0, n_scored = 0;
   for (int32_t b = 0; b < n_lips; ++b) {
     const KvFile* f = c->fs->file_of(kv[b]);
     const int64_t before = f->len - n_tokens[b];
     copy_bytes(tables + tbl, f->pages.data(), f->pages.size() * 4);
     for (int64_t p = f->bounded; p < before / P; ++p) *stale++ = f->pages[(size_t)p];
     for (int64_t p = before / P; p < f->len / P; ++p) *done++ = f->pages[(size_t)p];
-    int32_t in_group = 0;                          // rows of the group that is being filled (0: none)
     for (int32_t i = 0; i < n_tokens[b]; ++i, ++row) {
       const int32_t vis = (int32_t)(before + i + 1), n = (vis + P - 1) / P;
       int32_t* r = rows + (int64_t)row * SPARSE_ROW_WORDS;
       r[0] = tbl;
       r[1] = vis;
-      if (row % sp->slab_rows == 0) {
-        sp->slabs.push_back({row, 0, n_groups, 0, 0});
-        in_group = 0;
-      }
+      if (row % sp->slab_rows == 0) sp->slabs.push_back({row, 0, n_scored, 0, 0});
       SparsePlan::Slab& slab = sp->slabs.back();
       ++slab.rows;
       if (n <= sp->budget) continue;               // every page is read
-      if (in_group == 0 || in_group == kGroupRows) {
-        groups[n_groups * SPARSE_GROUP_WORDS] = row;
-        ++n_groups;
-        ++slab.groups;
-        in_group = 0;
-      }
-      int32_t* g = groups + (int64_t)(n_groups - 1) * SPARSE_GROUP_WORDS;
-      g[1] = ++in_group;
-      g[2] = tbl;
-      g[3] = n - sp->last;                         // (of a group's tokens the last sees most)
-      sp->group_rows = std::max(sp->group_rows, in_group);
+      int32_t* w = scored + (int64_t)n_scored++ * SPARSE_SCORED_WORDS;
+      w[0] = row;
+      w[1] = tbl;
+      w[2] = n - sp->last;
+      ++slab.scored;
       slab.most_scored = std::max(slab.most_scored, n - sp->first - sp->last);
     }
     tbl += (int32_t)f->pages.size();
@@ -969,7 +961,7 @@ int run_sparse_layer(sym_ctx* c, const SparsePlan& sp, uint8_t* ws, int64_t word
   a.out = out;
   a.picked = picked;
   a.rows = blob + sp.off_rows;
-  a.groups = blob + sp.off_groups;
+  a.scored = blob + sp.off_scored;
   a.tables = blob + sp.off_tables;
   a.counters = (int32_t*)ws + sp.off_counters;
   const int64_t slab = std::min<int64_t>(sp.slab_rows, sp.n_rows);
@@ -978,7 +970,6 @@ int run_sparse_layer(sym_ctx* c, const SparsePlan& sp, uint8_t* ws, int64_t word
   a.part_ml = (float*)at;
   at += align_up(sp.splits > 1 ? slab * H * sp.splits * c->G * 2 * 4 : 0, 256);
   a.part_acc = (float*)at;
-  a.group_rows = sp.group_rows;
   a.Hq = c->cfg.n_q_heads;
   a.Hkv = c->cfg.n_kv_heads;
   a.budget = sp.budget;
@@ -986,13 +977,15 @@ int run_sparse_layer(sym_ctx* c, const SparsePlan& sp, uint8_t* ws, int64_t word
   a.last = sp.last;
   a.score_stride = sp.score_stride;
   a.splits = sp.splits;
+  a.waves = sp.waves;
+  a.own = sp.own ? 1 : 0;
   a.stream = sp.alone ? 1 : 0;
   a.scale_log2e = c->scale_log2e;
   auto slab_args = [&](const SparsePlan::Slab& s) {
     a.row0 = s.row0;
     a.n_rows = s.rows;
-    a.group0 = s.group0;
-    a.n_groups = s.groups;
+    a.scored0 = s.scored0;
+    a.n_scored = s.scored;
     a.most_scored = s.most_scored;
   };
   AppendRopeArgs ap = append_args(c, layer, 1, sp.n_rows, k_new, v_new, sp.pos);
@@ -1003,8 +996,8 @@ int run_sparse_layer(sym_ctx* c, const SparsePlan& sp, uint8_t* ws, int64_t word
   ap.run_tokens = sp.run_tokens;
   slab_args(sp.slabs[0]);
   // single tokens, no bounds missing, the lists on the device, few scores: append and scores in one launch
-  const bool together = stage < 0 && sp.run_tokens == 1 && sp.n_stale == 0 && sp.slabs.size() == 1 &&
-                        scores_with_append(sp.rope, sp.turns, a.Hkv, a.n_groups, a.most_scored);
+  const bool together = stage < 0 && sp.run_tokens == 1 && sp.n_stale == 0 && sp.slabs.size() == 1 && sp.turns && !sp.own &&
+                        scores_with_append(sp.rope, a.Hkv, a.n_scored, a.most_scored);
   if (together) {
     Timed t(c, SYM_K_ATTN, st);
     const hipError_t e = launch_sparse_first(ap, sp.rope, a, c->cfg.dtype, st);
@@ -1028,7 +1021,7 @@ int run_sparse_layer(sym_ctx* c, const SparsePlan& sp, uint8_t* ws, int64_t word
   if (int rc = batch_bounds(c, sp, blob, layer, sp.n_stale, st)) return rc;
   for (const SparsePlan::Slab& s : sp.slabs) {
     slab_args(s);
-    const bool scores = s.groups > 0 && !scores_itself(s.most_scored) && !together;
+    const bool scores = s.scored > 0 && !sp.own && !together;
     Timed t(c, SYM_K_ATTN, st, false, true, 1 + scores);
     hipError_t e = hipSuccess;
     if (scores) e = launch_sparse_scores(a, c->cfg.dtype, st);

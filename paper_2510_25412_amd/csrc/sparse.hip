@@ -356,7 +356,7 @@ __global__ __launch_bounds__(256) void append_rope_runs_kernel(AppendRunsKernelA
 // ---------------------------------------------------------------------------------------
 // Bounds of a list of pages.  A workgroup of W wavefronts takes an equal share of the pages (at most 64, an id to each lane) in one layer; its
 // wavefronts take the (page, kv head) in turn, the next one's keys under way while one is reduced.  W = 4, a page to a workgroup, for few
-// pages, whose ids travel with the arguments; W = 8 for many, as many workgroups as the chip holds at once, whose list may stay in pinned
+// pages, whose ids travel with the arguments; W = 8 for many, as many workgroups as compute units, whose list may stay in pinned
 // host memory: a share is one request over the host link.  Bound: HBM (4 KiB read for 512 bytes written).
 // ---------------------------------------------------------------------------------------
 struct BoundsKernelArgs {
@@ -395,8 +395,7 @@ __global__ __launch_bounds__(64 * W) void bounds_kernel(std::conditional_t<ARGS,
 // bits (the choice hangs on comparisons of scores that lie close together; with sums in 32 bits it would depend on their order),
 // rounded to 32 at the end and written down as whole numbers of the same order.
 // A wavefront takes one kv head and 32 pages; 32 lanes share a page's 512 bytes, a 16-byte chunk each, with the chunk's coefficients
-// in registers; eight pages a lane are then added up over the 32 lanes by halving exchanges.  Up to RT consecutive tokens of a file
-// share the pass.  Bound: HBM for one token, 64-bit arithmetic for four.
+// in registers; eight pages a lane are then added up over the 32 lanes by halving exchanges.
 // ---------------------------------------------------------------------------------------
 constexpr int kScorePages = 32;                  // of a wavefront
 __device__ __forceinline__ double as_f64(uint32_t lo, uint32_t hi) { return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo); }
@@ -413,35 +412,32 @@ __device__ __forceinline__ uint32_t order_of(float x) {
   return (b & 0x80000000u) ? ~b : b | 0x80000000u;
 }
 
-// A wavefront's scores of 2 STEPS pages at a time, for one kv head and up to RT consecutive tokens.
-template <typename E, int RT, int STEPS = kScorePages / 2>
+// A wavefront's scores of 2 STEPS pages at a time, for one kv head of a token.
+template <typename E, int STEPS = kScorePages / 2>
 struct Scorer {
   static constexpr int C = E::kDimsPerChunk;
-  double cf[RT][C];                              // coefficients of this lane's chunk: lanes 0..15 of a page hold lo, 16..31 hi
+  double cf[C];                                  // coefficients of this lane's chunk: lanes 0..15 of a page hold lo, 16..31 hi
   int id[STEPS];                                 // pages 2 s + (upper half of the wavefront)
 
-  __device__ __forceinline__ void coefficients(const SparseArgs& a, const int r0, const int nr, const int head) {
+  __device__ __forceinline__ void coefficients(const SparseArgs& a, const int row, const int head) {
     const int hl = threadIdx.x & 31, part = hl >> 4, chunk = hl & 15, G = a.Hq / a.Hkv;
+    const uint8_t* q = (const uint8_t*)a.q + ((int64_t)row * a.Hq + head * G) * kRowBytes + chunk * 16;
 #pragma unroll
-    for (int t = 0; t < RT; ++t) {
-#pragma unroll
-      for (int e = 0; e < C; ++e) cf[t][e] = 0.0;
-      const uint8_t* q = (const uint8_t*)a.q + ((int64_t)(r0 + min(t, nr - 1)) * a.Hq + head * G) * kRowBytes + chunk * 16;
-      for (int h = 0; h < G; ++h) add(t, part, *(const uint4*)(q + h * kRowBytes));
-    }
+    for (int e = 0; e < C; ++e) cf[e] = 0.0;
+    for (int h = 0; h < G; ++h) add(part, *(const uint4*)(q + h * kRowBytes));
   }
   // one query head's chunk
-  __device__ __forceinline__ void add(const int t, const int part, const uint4& row) {
+  __device__ __forceinline__ void add(const int part, const uint4& row) {
     float x[C];
     E::unpack(row, x);
 #pragma unroll
-    for (int e = 0; e < C; ++e) cf[t][e] += (double)(part ? (x[e] < 0.f ? 0.f : x[e]) : (x[e] > 0.f ? 0.f : x[e]));
+    for (int e = 0; e < C; ++e) cf[e] += (double)(part ? (x[e] < 0.f ? 0.f : x[e]) : (x[e] > 0.f ? 0.f : x[e]));
   }
   __device__ __forceinline__ void ids(const int32_t* pt, const int p0, const int end) {
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) id[s] = pt[min(p0 + 2 * s + (int)((threadIdx.x & 63) >> 5), end - 1)];
   }
-  // put(token, page, key) of the pages p0 .. of id, below end; next() runs when id has been used
+  // put(page, key) of the pages p0 .. of id, below end; next() runs when id has been used
   template <typename N, typename P>
   __device__ __forceinline__ void score(const SparseArgs& a, const int head, const int p0, const int end, const N& next, const P& put) {
     const int lane = threadIdx.x & 63, sub = lane >> 5, hl = lane & 31;
@@ -453,58 +449,51 @@ struct Scorer {
 #pragma unroll
       for (int s = 0; s < 8; ++s) x[s] = *(const uint4*)(rec + (int64_t)id[b * 8 + s] * page_rec);
       if (b == STEPS / 8 - 1) next();
+      double v[8];
 #pragma unroll
-      for (int t = 0; t < RT; ++t) {
-        double v[8];
+      for (int s = 0; s < 8; ++s) {
+        float f[C];
+        E::unpack(x[s], f);
+        v[s] = 0.0;
 #pragma unroll
-        for (int s = 0; s < 8; ++s) {
-          float f[C];
-          E::unpack(x[s], f);
-          v[s] = 0.0;
-#pragma unroll
-          for (int e = 0; e < C; ++e) v[s] = __builtin_fma(cf[t][e], (double)f[e], v[s]);
-        }
-#pragma unroll
-        for (int s = 0; s < 4; ++s) {            // lane bit 4: even rows of 16 lanes keep pages 0..3, odd ones 4..7
-          const uint64_t p = __builtin_bit_cast(uint64_t, v[s]), q = __builtin_bit_cast(uint64_t, v[s + 4]);
-          const auto lo = __builtin_amdgcn_permlane16_swap((uint32_t)p, (uint32_t)q, false, false);
-          const auto hi = __builtin_amdgcn_permlane16_swap((uint32_t)(p >> 32), (uint32_t)(q >> 32), false, false);
-          v[s] = as_f64(lo[0], hi[0]) + as_f64(lo[1], hi[1]);
-        }
-        const bool b3 = (lane & 8) != 0;
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {            // lane bit 3
-          const double keep = b3 ? v[s + 2] : v[s], send = b3 ? v[s] : v[s + 2];
-          v[s] = keep + dpp_f64<0x128>(send);    // row_ror:8
-          v[s] += dpp_f64<0xB1>(v[s]);           // the octet's sum
-          v[s] += dpp_f64<0x4E>(v[s]);
-          v[s] += dpp_f64<0x141>(v[s]);
-        }
-        // lane octet (bit 4, bit 3) holds steps 4 bit4 + 2 bit3 + {0, 1} of the eight
-        const int step = b * 8 + ((lane >> 4) & 1) * 4 + ((lane >> 3) & 1) * 2 + (lane & 1), p = p0 + 2 * step + sub;
-        if ((lane & 7) < 2 && p < end) put(t, p, order_of((float)((lane & 1) ? v[1] : v[0])));
+        for (int e = 0; e < C; ++e) v[s] = __builtin_fma(cf[e], (double)f[e], v[s]);
       }
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {              // lane bit 4: even rows of 16 lanes keep pages 0..3, odd ones 4..7
+        const uint64_t p = __builtin_bit_cast(uint64_t, v[s]), q = __builtin_bit_cast(uint64_t, v[s + 4]);
+        const auto lo = __builtin_amdgcn_permlane16_swap((uint32_t)p, (uint32_t)q, false, false);
+        const auto hi = __builtin_amdgcn_permlane16_swap((uint32_t)(p >> 32), (uint32_t)(q >> 32), false, false);
+        v[s] = as_f64(lo[0], hi[0]) + as_f64(lo[1], hi[1]);
+      }
+      const bool b3 = (lane & 8) != 0;
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {              // lane bit 3
+        const double keep = b3 ? v[s + 2] : v[s], send = b3 ? v[s] : v[s + 2];
+        v[s] = keep + dpp_f64<0x128>(send);      // row_ror:8
+        v[s] += dpp_f64<0xB1>(v[s]);             // the octet's sum
+        v[s] += dpp_f64<0x4E>(v[s]);
+        v[s] += dpp_f64<0x141>(v[s]);
+      }
+      // lane octet (bit 4, bit 3) holds steps 4 bit4 + 2 bit3 + {0, 1} of the eight
+      const int step = b * 8 + ((lane >> 4) & 1) * 4 + ((lane >> 3) & 1) * 2 + (lane & 1), p = p0 + 2 * step + sub;
+      if ((lane & 7) < 2 && p < end) put(p, order_of((float)((lane & 1) ? v[1] : v[0])));
     }
   }
 };
 
-template <typename E, int RT>
+template <typename E>
 __global__ __launch_bounds__(256) void sparse_scores_kernel(SparseArgs a) {
-  hold(a.groups, a.tables, a.bounds, a.q, a.scores, a.Hq, a.Hkv, a.first, a.score_stride);
-  const int32_t* grp = a.groups + (int64_t)(a.group0 + blockIdx.y) * SPARSE_GROUP_WORDS;
-  const int r0 = sload(grp), nr = sload(grp + 1), tbl = sload(grp + 2), end = sload(grp + 3);
+  hold(a.scored, a.tables, a.bounds, a.q, a.scores, a.Hq, a.Hkv, a.first, a.score_stride);
+  const int32_t* w = a.scored + (int64_t)(a.scored0 + blockIdx.y) * SPARSE_SCORED_WORDS;
+  const int row = sload(w), tbl = sload(w + 1), end = sload(w + 2);
   const int wave = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6)));
   const int head = wave % a.Hkv, p0 = a.first + wave / a.Hkv * kScorePages;
   if (p0 >= end) return;
-  uint32_t* scores = a.scores + ((int64_t)(r0 - a.row0) * a.Hkv + head) * a.score_stride;
-  const int64_t row_scores = (int64_t)a.Hkv * a.score_stride;
-  Scorer<E, RT> sc;
+  uint32_t* scores = a.scores + ((int64_t)(row - a.row0) * a.Hkv + head) * a.score_stride;
+  Scorer<E> sc;
   sc.ids(a.tables + tbl, p0, end);
-  sc.coefficients(a, r0, nr, head);
-  // (a row's last pages may be scored beyond its need: its stretch has room for the most pages of any row)
-  sc.score(a, head, p0, end, [] {}, [&](int t, int p, uint32_t key) {
-    if (t < nr) scores[t * row_scores + (p - a.first)] = key;
-  });
+  sc.coefficients(a, row, head);
+  sc.score(a, head, p0, end, [] {}, [&](int p, uint32_t key) { scores[p - a.first] = key; });
 }
 
 // ---------------------------------------------------------------------------------------
@@ -516,7 +505,7 @@ __global__ __launch_bounds__(256) void sparse_scores_kernel(SparseArgs a) {
 struct FirstKernelArgs {
   AppendKernelArgs k;
   SparseArgs s;
-  int32_t parts, append_blocks, group_blocks;      // workgroups of a run beside the first, of all runs, of a scored row
+  int32_t parts, append_blocks, row_blocks;      // workgroups of a run beside the first, of all runs, of a scored row
 };
 // Chunk `c` of a row, turned: its own 16 bytes and those that hold its pairs' other elements.
 template <typename E, int PATH>
@@ -561,17 +550,17 @@ __global__ __launch_bounds__(256) void sparse_first_kernel(FirstKernelArgs) {
     append_run<E, PATH>(&ka->k, sload(w), sload(w + 1), sload(w + 2), sload(w + 3), 0, part, ka->parts, cs, nullptr);
     return;
   }
-  const int blk = (int)blockIdx.x - ka->append_blocks, grp_at = blk / ka->group_blocks, Hkv = ka->s.Hkv, first = ka->s.first;
-  const int32_t* grp = ka->s.groups + (int64_t)grp_at * SPARSE_GROUP_WORDS;
-  const int row = sload(grp), tbl = sload(grp + 2), end = sload(grp + 3);
-  const int wave = __builtin_amdgcn_readfirstlane(blk % ka->group_blocks * 4 + (int)(threadIdx.x >> 6));
+  const int blk = (int)blockIdx.x - ka->append_blocks, at_row = blk / ka->row_blocks, Hkv = ka->s.Hkv, first = ka->s.first;
+  const int32_t* w = ka->s.scored + (int64_t)at_row * SPARSE_SCORED_WORDS;
+  const int row = sload(w), tbl = sload(w + 1), end = sload(w + 2);
+  const int wave = __builtin_amdgcn_readfirstlane(blk % ka->row_blocks * 4 + (int)(threadIdx.x >> 6));
   const int head = wave % Hkv, p0 = first + wave / Hkv * kFirstPages, G = ka->s.Hq / Hkv;
   const int chunk = threadIdx.x & 15, part = (threadIdx.x >> 4) & 1, hr = ka->k.r.dims / 2 / C;
   const int other = PATH == ROPE_HALVES ? (chunk < hr ? chunk + hr : chunk < 2 * hr ? chunk - hr : chunk) : chunk;
   SparseArgs a{};                                // (what score() reads of it)
   a.bounds = ka->s.bounds;
   a.Hkv = Hkv;
-  Scorer<E, 1, kFirstPages / 2> sc;
+  Scorer<E, kFirstPages / 2> sc;
   sc.ids(ka->s.tables + tbl, min(p0, end - 1), end);
   const uint8_t* q = (const uint8_t*)ka->k.a.q + ((int64_t)row * ka->s.Hq + head * G) * kRowBytes;
   uint4 x[8], y[8];                                // (G <= 8)
@@ -587,12 +576,12 @@ __global__ __launch_bounds__(256) void sparse_first_kernel(FirstKernelArgs) {
   __syncthreads();
   if (p0 >= end) return;
 #pragma unroll
-  for (int e = 0; e < C; ++e) sc.cf[0][e] = 0.0;
+  for (int e = 0; e < C; ++e) sc.cf[e] = 0.0;
 #pragma unroll
   for (int h = 0; h < 8; ++h)
-    if (h < G) sc.add(0, part, turned_chunk<E, PATH>(x[h], y[h], chunk, ka->k.r.dims, cs[0]));
+    if (h < G) sc.add(part, turned_chunk<E, PATH>(x[h], y[h], chunk, ka->k.r.dims, cs[0]));
   uint32_t* scores = ka->s.scores + ((int64_t)row * Hkv + head) * ka->s.score_stride;
-  sc.score(a, head, p0, end, [] {}, [&](int, int p, uint32_t key) { scores[p - first] = key; });
+  sc.score(a, head, p0, end, [] {}, [&](int p, uint32_t key) { scores[p - first] = key; });
 }
 
 constexpr int kMostWaves = 8;                   // of a workgroup that attends
@@ -1046,13 +1035,13 @@ __global__ __launch_bounds__(64 * W, 8 / W) void sparse_attend_kernel(SparseArgs
       if (want > 0) {
         int p0 = a.first + wv * kScorePages;
         const int end = n - a.last;
-        Scorer<typename AT::Elem, 1> own;
+        Scorer<typename AT::Elem> own;
         if (p0 < end) {
           own.ids(pt, p0, end);
-          own.coefficients(a, row, 1, head);
+          own.coefficients(a, row, head);
         }
         for (; p0 < end; p0 += W * kScorePages)
-          own.score(a, head, p0, end, [&] { own.ids(pt, p0 + W * kScorePages, end); }, [&](int, int p, uint32_t key) { s_keys[p - a.first] = key; });
+          own.score(a, head, p0, end, [&] { own.ids(pt, p0 + W * kScorePages, end); }, [&](int p, uint32_t key) { s_keys[p - a.first] = key; });
         __syncthreads();
         if (m <= NT) pick_highest<W, 1>(s_keys, m, want, s, chosen);
         else pick_highest<W, kOwnScores / NT < 4 ? 4 : kOwnScores / NT>(s_keys, m, want, s, chosen);
@@ -1171,7 +1160,8 @@ __global__ __launch_bounds__(64 * W, 8 / W) void sparse_attend_kernel(SparseArgs
 hipError_t launch_rope_rows(RopeRowsArgs a, const RopeTable& r, int dtype, hipStream_t st) {
   if (a.n <= 0) return hipSuccess;
   if (a.n > kMostRopeRows) return hipErrorInvalidValue;
-  a.tokens = a.n >= 2048 ? 4 : 1;
+  // enough rows for every compute unit: 1024 bf16 rows of 32 + 8 heads 7.0 us a call (7.8 with one token), 2048 10.4 (12.5), 16384 65 (75)
+  a.tokens = a.n >= 1024 ? 4 : 1;
   const RopeRowsKernelArgs ka{a, r};
   const dim3 grid((unsigned)((a.n + a.tokens - 1) / a.tokens)), block(256);
 #define SYM_LAUNCH(E, PATH) hipLaunchKernelGGL((rope_rows_kernel<E, PATH>), grid, block, 0, st, ka)
@@ -1220,8 +1210,9 @@ hipError_t launch_bounds(const BoundsArgs& a, int dtype, hipStream_t st) {
     if (dtype == 0) return launch_done(bounds_kernel<ElemF32, true, 4>, grid, dim3(256), st, a.done, ka);
     return launch_done(bounds_kernel<ElemBF16, true, 4>, grid, dim3(256), st, a.done, ka);
   }
-  // 1024 workgroups of 8 wavefronts are all that 256 compute units hold
-  const int blocks = std::min(a.n_pages, std::max(std::max(1024 / a.n_layers, 1), (a.n_pages + 63) / 64));
+  // a workgroup to a compute unit: files of 10000, 20000, 120000 tokens of 8 heads 7.3, 10.8, 53.2 us a call, with four 8.0, 11.9, 54.9;
+  // 64 files of 512..4096 tokens 58.7 and 60.0 (71 with half as many, 68 with 320)
+  const int blocks = std::min(a.n_pages, std::max(std::max(256 / a.n_layers, 1), (a.n_pages + 63) / 64));
   const dim3 grid((unsigned)blocks, (unsigned)a.n_layers);
   if (dtype == 0) return launch_done(bounds_kernel<ElemF32, false, 8>, grid, dim3(512), st, a.done, a);
   return launch_done(bounds_kernel<ElemBF16, false, 8>, grid, dim3(512), st, a.done, a);
@@ -1230,8 +1221,8 @@ hipError_t launch_bounds(const BoundsArgs& a, int dtype, hipStream_t st) {
 hipError_t launch_sparse_first(const AppendRopeArgs& a, const RopeTable& r, const SparseArgs& s, int dtype, hipStream_t st) {
   FirstKernelArgs ka{{a, r}, s, std::max(a.Hq / 128, 1), 0, 0};
   ka.append_blocks = a.n_runs * (1 + ka.parts);
-  ka.group_blocks = ((s.most_scored + kFirstPages - 1) / kFirstPages * s.Hkv + 3) / 4;
-  const dim3 grid((unsigned)(ka.append_blocks + ka.group_blocks * s.n_groups)), block(256);
+  ka.row_blocks = ((s.most_scored + kFirstPages - 1) / kFirstPages * s.Hkv + 3) / 4;
+  const dim3 grid((unsigned)(ka.append_blocks + ka.row_blocks * s.n_scored)), block(256);
 #define SYM_LAUNCH(E) \
   if (r.path == ROPE_HALVES) hipLaunchKernelGGL((sparse_first_kernel<E, ROPE_HALVES>), grid, block, 0, st, ka); \
   else hipLaunchKernelGGL((sparse_first_kernel<E, ROPE_INTERLEAVED>), grid, block, 0, st, ka)
@@ -1245,26 +1236,21 @@ hipError_t launch_sparse_first(const AppendRopeArgs& a, const RopeTable& r, cons
 }
 
 hipError_t launch_sparse_scores(const SparseArgs& a, int dtype, hipStream_t st) {
-  if (a.n_groups <= 0) return hipSuccess;
+  if (a.n_scored <= 0) return hipSuccess;
   const int64_t waves = (int64_t)((a.most_scored + kScorePages - 1) / kScorePages) * a.Hkv;
-  if (a.n_groups > 65535) return hipErrorInvalidValue;
-  const dim3 grid((unsigned)((waves + 3) / 4), (unsigned)a.n_groups), block(256);
-  if (dtype == 0) {
-    if (a.group_rows == 1) hipLaunchKernelGGL((sparse_scores_kernel<ElemF32, 1>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((sparse_scores_kernel<ElemF32, kGroupRows>), grid, block, 0, st, a);
-  } else {
-    if (a.group_rows == 1) hipLaunchKernelGGL((sparse_scores_kernel<ElemBF16, 1>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((sparse_scores_kernel<ElemBF16, kGroupRows>), grid, block, 0, st, a);
-  }
+  if (a.n_scored > 65535) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)((waves + 3) / 4), (unsigned)a.n_scored), block(256);
+  if (dtype == 0) hipLaunchKernelGGL((sparse_scores_kernel<ElemF32>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((sparse_scores_kernel<ElemBF16>), grid, block, 0, st, a);
   return hipGetLastError();
 }
 
 hipError_t launch_sparse_attend(const SparseArgs& a, int dtype, hipStream_t st) {
   if (a.n_rows <= 0) return hipSuccess;
-  const bool own = scores_itself(a.most_scored);
-  const dim3 grid((unsigned)(a.n_rows * a.Hkv * a.splits)), block(64 * attend_waves(a.most_scored));
+  const dim3 grid((unsigned)(a.n_rows * a.Hkv * a.splits)), block(64 * a.waves);
 #define SYM_ATTEND_ROWS(AT, GG, STREAM) \
-  if (own) hipLaunchKernelGGL((sparse_attend_kernel<AT<GG, STREAM>, GG, true, 4>), grid, block, 0, st, a); \
+  if (a.own) hipLaunchKernelGGL((sparse_attend_kernel<AT<GG, STREAM>, GG, true, 4>), grid, block, 0, st, a); \
+  else if (a.waves == 4) hipLaunchKernelGGL((sparse_attend_kernel<AT<GG, STREAM>, GG, false, 4>), grid, block, 0, st, a); \
   else hipLaunchKernelGGL((sparse_attend_kernel<AT<GG, STREAM>, GG, false, 8>), grid, block, 0, st, a)
 #define SYM_ATTEND(GG) \
   case GG: \

@@ -63,9 +63,8 @@ struct BoundsArgs {
 };
 
 constexpr int SPARSE_ROW_WORDS = 2;    // page table (offset into the tables), tokens seen
-// Consecutive tokens of one file, scored together: first row, rows, page table (offset into the tables), end of the pages to score.
-constexpr int SPARSE_GROUP_WORDS = 4;
-constexpr int kGroupRows = 4;
+// A row with pages to score: row, page table (offset into the tables), end of the pages to score.
+constexpr int SPARSE_SCORED_WORDS = 3;
 constexpr int kPartPages = 2048;       // most pages of a part of a row's list (one workgroup's)
 struct SparseArgs {
   const uint8_t* pool;
@@ -75,34 +74,44 @@ struct SparseArgs {
   float* out;               // [rows][Hq][D]
   int32_t* picked;          // [rows][Hkv][budget] or null: index of the pages read, -1 past the last
   const int32_t* rows;      // [rows][SPARSE_ROW_WORDS]
-  const int32_t* groups;    // [n_groups][SPARSE_GROUP_WORDS]
+  const int32_t* scored;    // [n_scored][SPARSE_SCORED_WORDS]
   const int32_t* tables;
   uint32_t* scores;         // [rows of the launch][Hkv][score_stride]: in the order of the scores, from page `first` on
   float* part_acc;          // [rows of the launch][Hkv][splits][G][D]
   float* part_ml;           // [rows of the launch][Hkv][splits][G][2]
   int32_t* counters;        // [rows of the launch][Hkv]: parts that are done (several parts); 0 between launches
   int32_t row0, n_rows;     // rows of this launch
-  int32_t group0, n_groups, group_rows;   // groups of this launch, which need scores, and the most rows of one
-  int32_t most_scored;      // pages of the group with most to score
+  int32_t scored0, n_scored;              // scored rows of this launch
+  int32_t most_scored;      // pages of the one with most of them
   int32_t Hq, Hkv, budget, first, last;
   int32_t score_stride;
-  int32_t splits;
+  int32_t splits, waves;    // parts of a row's list; wavefronts of a workgroup that attends
+  int32_t own;              // the workgroups that attend score their row's pages themselves
   int32_t stream;           // no two rows read the same pages, as far as the host looks
   float scale_log2e;
 };
 
-// Whether a workgroup of the attention scores its row's pages itself.
-constexpr int kOwnScores = 512;
-inline bool scores_itself(int64_t most_scored) { return most_scored <= kOwnScores; }
-inline int attend_waves(int64_t most_scored) { return scores_itself(most_scored) ? 4 : 8; }
+// Whether the workgroups that attend score their row's pages themselves, for `units` rows and heads of which the longest scores `most`
+// pages.  That saves a launch and the scores' way through memory.  Beyond a workgroup for every compute unit nothing is lost by it: 64
+// files of 256, 512, 1024 and 2000 pages, 8 heads: 65, 81, 106 and 152 us a call, 78, 96, 125 and 175 with a launch of its own.  With
+// fewer rows a wavefront has more to score (and every part of a row's list does it again): one file of 128, 256, 512 pages 17.7, 19.9,
+// 25.1 us, and 20.8, 21.5, 21.8 with the launch; 4 files of 256 pages 23.2 and 24.8, 8 files 31.1 and 28.1; 16 and 32 files of 128 pages
+// 32.6 and 43.5, and 32.8 and 42.8.
+constexpr int kOwnScores = 2048;
+inline bool scores_itself(int64_t units, int64_t most) { return most <= (units > 256 ? kOwnScores : units <= 32 ? 256 : 128); }
+// Wavefronts of a workgroup that attends.  Eight share the choice of a long row, where there are no more rows than compute units: 8 files
+// of 32k..131k tokens 84 us a call (89 with four), 32 files of 36000 tokens 102 (107), 8 layers of one file 186 (192).  Otherwise four, of
+// which more fit: 64 files of 512..4096 tokens 61 us (70 with eight), 64 files of 36000 tokens 184 (192).
+inline int attend_waves(bool own, int64_t units) { return !own && units <= 256 ? 8 : 4; }
 
 // Whether the append of a batch and its scores are one launch, for a batch of single tokens with no bounds missing: turned query rows
-// in pairs that a lane holds, and few wavefronts to score.
+// in pairs that a lane holds, and no more wavefronts to score than run at once: each turns query rows again.  8 layers of 1, 2, 4 and 8
+// files of 30000 tokens: 173, 202, 242 and 354 us a step, and 203, 237, 267 and 357 with two launches a layer; 4 layers of 1, 2 and 4
+// files of 60000 tokens with 64 query heads: 118, 146 and 201, and 129, 150 and 179.
 constexpr int kFirstPages = 16;            // of a wavefront that scores there
-constexpr int64_t kFirstWaves = 2048;
-inline bool scores_with_append(const RopeTable& r, bool turns, int Hkv, int64_t n_groups, int64_t most_scored) {
-  return turns && (r.path == ROPE_HALVES || r.path == ROPE_INTERLEAVED) && n_groups > 0 && !scores_itself(most_scored) &&
-         (most_scored + kFirstPages - 1) / kFirstPages * Hkv * n_groups <= kFirstWaves;
+constexpr int64_t kFirstWaves = 4096;
+inline bool scores_with_append(const RopeTable& r, int Hkv, int64_t n_scored, int64_t most_scored) {
+  return (r.path == ROPE_HALVES || r.path == ROPE_INTERLEAVED) && n_scored > 0 && (most_scored + kFirstPages - 1) / kFirstPages * Hkv * n_scored <= kFirstWaves;
 }
 
 // Weak: the host code is also built without kernels (by tests of the host side, against stand-ins for the launches it made before these).

@@ -710,3 +710,14 @@ def test_steps_over_layers_of_files_with_many_scores(dtype, hq, hkv, layout, dim
         pos = torch.tensor([n + 70001 for n in map(sess.ctx.kv_len, files)], dtype=torch.int32, device="cuda") if given else None
         run_sparse(sess, files, [1] * len(files), binding.make_sparse(9, 1, 2, rope=rope, positions=pos), rope, lc.frequencies(dims or DIM[dtype], 50000.0), layout, g=g, pos=pos)
     sess.close()
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,lens,new", [("bf16", 8, 8, [16 * 130, 16 * 700, 16 * 1500 + 7], [11, 12, 13]), ("bf16", 8, 4, [16 * 2045], [66]), ("bf16", 4, 2, [16 * 2049], [130]),
+                                                   ("f32", 4, 4, [16 * 300, 16 * 1030], [40, 30]), ("f32", 16, 2, [16 * 2300, 50], [100, 40])])
+def test_many_rows_with_many_scores(dtype, hq, hkv, lens, new):
+    # more rows and heads than compute units: the attention scores up to 2048 pages itself, beyond them not
+    print(f"[case] many rows, many scores {dtype} {hq}/{hkv} {lens} {new}", flush=True)
+    sess = session(dtype, hq, hkv, sum(-(-(n + m) // P) + 2 for n, m in zip(lens, new)))
+    files = make_files(sess, lens, torch.Generator().manual_seed(len(lens)))
+    run_sparse(sess, files, new, binding.make_sparse(7, 1, 2))
+    sess.close()
