@@ -358,8 +358,9 @@ int64_t sym_kv_bounded(sym_ctx* ctx, sym_kv kv);
  * sym_pred_begin_sparse / sym_pred_layer_sparse: the same over layers, like sym_pred_begin / sym_pred_layer and under the same rules; with
  *   dense_layers each layer is run by either sym_pred_layer_sparse or sym_pred_layer (rows as they are: it knows no rope).
  * Rows and outputs 16-byte aligned.  A buffer for bounds has to be attached.  SYM_ENOSPC if the workspace does not hold the batch:
- * beside the page tables about T * Hq * 256 bytes with a rope, and for one token Hkv * 4 bytes per page of the longest file and
- * per page read.                                                                          */
+ * beside the page tables T * Hq * 256 bytes with a rope, Hkv * 4 bytes per page of the longest file for one token (a batch goes
+ * through what is left some tokens at a time), and Hq * (D + 2) * 4 bytes for each part of eight pages or more in which a
+ * token's list is read when tokens are few.                                               */
 typedef struct sym_sparse {
   int32_t budget, first, last;     /* first >= 0, last >= 1, first + last <= budget      */
   int32_t dense_layers;
@@ -523,7 +524,8 @@ int     sym_sched_state(sym_sched* s, double* rate_per_us, double* target_batch,
 /* sym_profile_enable(mask): bit k (k < 8) of mask set = launches of kernel id k are bracketed by
  * HIP events on the launch stream (at most 4096 timed launches are kept per kernel id, later
  * ones are not timed).  For SYM_K_ATTN the two events are attached to the dispatches themselves
- * (start of the first kernel of the attention launch, end of its last): kernel time only; bits 8..23 of mask = stride s (0 or 1: every launch; s > 1: every s-th
+ * (start of the first kernel of the attention launch, end of its last): kernel time only (those of a
+ * sparse pred stand around them on the stream); bits 8..23 of mask = stride s (0 or 1: every launch; s > 1: every s-th
  * launch of each kernel id, so that the two event records do not stretch every step); mask 0 = off.
  * sym_profile_read synchronises on the recorded events and returns the summed duration in
  * milliseconds and the number of timed launches of one kernel id, then forgets them.     */

@@ -863,7 +863,7 @@ int check_sparse(sym_ctx* c, const sym_sparse* s, SparsePlan* sp) {
 // `ws_bytes` bytes behind `blob_words` words.
 int size_sparse(sym_ctx* c, SparsePlan* sp, int32_t n_lips, const sym_kv* kv, const int32_t* n_tokens, int64_t tokens, int64_t runs, int64_t* words) {
   const int64_t P = c->cfg.page_tokens, H = c->cfg.n_kv_heads;
-  int64_t entries = 0, stale = 0, done = 0, most_pages = 0, most_kept = 0;
+  int64_t entries = 0, stale = 0, done = 0, most_pages = 0, most_kept = 0, scored = 0;
   for (int32_t b = 0; b < n_lips; ++b) {
     const KvFile* f = c->fs->file_of(kv[b]);
     const int64_t after = f->len + n_tokens[b], pages = (after + P - 1) / P;
@@ -873,6 +873,7 @@ int size_sparse(sym_ctx* c, SparsePlan* sp, int32_t n_lips, const sym_kv* kv, co
     stale += f->len / P - f->bounded;
     done += after / P - f->len / P;
     most_pages = std::max(most_pages, pages);
+    if (pages > sp->budget) scored += n_tokens[b];
     most_kept = std::max(most_kept, std::min<int64_t>(pages, sp->budget));
   }
   sp->n_rows = (int32_t)tokens;
@@ -883,9 +884,10 @@ int size_sparse(sym_ctx* c, SparsePlan* sp, int32_t n_lips, const sym_kv* kv, co
   sp->kv.assign(kv, kv + n_lips);
   sp->score_stride = most_pages > sp->budget ? (int32_t)align_up(most_pages - sp->first - sp->last, 32) : 0;
   // Parts of a list: where rows are few as many workgroups as fill the chip, each with eight pages at least; no more pages than a
-  // workgroup's list holds.
+  // workgroup's list holds.  8 files of 32k..131k tokens with 2048, 1024, 512 wavefronts: 82, 95, 119 us a call (4096: 95), 8 layers of one
+  // file 183, 183, 193; with 8, 16, 32 pages at least 185, 192, 220, and one fp32 file 13.9, 14.3, 15.3 (4 pages: 14.1).
   const int64_t units = tokens * H, most_scored = most_pages > sp->budget ? most_pages - sp->first - sp->last : 0;
-  sp->own = scores_itself(units, most_scored);
+  sp->own = scores_itself(scored * H, most_scored);
   sp->waves = attend_waves(sp->own, units);
   sp->splits = (int32_t)std::max({(int64_t)1, std::min(2048 / sp->waves / units, most_kept / 8), (most_kept + kPartPages - 1) / kPartPages});
   sp->q_bytes = sp->turns ? align_up(row_bytes_of(tokens, c->cfg.n_q_heads), 256) : 0;

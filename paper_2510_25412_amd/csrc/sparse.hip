@@ -42,6 +42,8 @@ __device__ __forceinline__ u32x4_t pack_chunk(const float* y) {
 // (it takes an error of 2^-25 in a cosine) shows in the outputs of attention as 1e-5.  The angle is reduced to p t - round(p t) turns, so that
 // sincospi's argument is exact.  A workgroup computes the angles of its tokens once, into LDS, for all heads; a thread then keeps
 // those of its two 16-byte chunks in registers and walks the token's rows with them.
+// Bound: HBM, read + write: 16384 rows of 32 + 8 bf16 heads in 65 us, 336 MB at 5.2 TB/s (a copy of that size reaches 4.8).  64 rows
+// take 4.3 us, a launch and one angle's arithmetic.
 // ---------------------------------------------------------------------------------------
 constexpr int kPairs = 64;                       // pairs of a head at most
 constexpr int kRunTokens = kP;                   // most tokens of a workgroup
@@ -271,7 +273,9 @@ __device__ __forceinline__ void write_bounds(const PageKeys& R, uint8_t* out) {
 // ---------------------------------------------------------------------------------------
 // Append with the keys turned on the way.  A workgroup takes a run: the new tokens of a file that go to consecutive slots of one page,
 // one layer.  Few runs travel with the kernel's arguments, so that no request over the host link stands before the first load.  When the
-// run completes its page, the workgroup writes the page's bounds behind its own stores.  Bound: HBM, read + write; few tokens: the launch.
+// run completes its page, the workgroup writes the page's bounds behind its own stores.  Bound: HBM, read + write: 7500 tokens of 8 bf16
+// heads in 17 us, 63 MB at 3.7 TB/s (470 workgroups, two to a compute unit, so that starts and ends show); 64 files of one token 4.8 us: the
+// launch and a chain of two loads, an angle and a store.
 // ---------------------------------------------------------------------------------------
 struct ArgRuns {
   int32_t w[kArgRuns * RUN_WORDS];
@@ -357,7 +361,8 @@ __global__ __launch_bounds__(256) void append_rope_runs_kernel(AppendRunsKernelA
 // Bounds of a list of pages.  A workgroup of W wavefronts takes an equal share of the pages (at most 64, an id to each lane) in one layer; its
 // wavefronts take the (page, kv head) in turn, the next one's keys under way while one is reduced.  W = 4, a page to a workgroup, for few
 // pages, whose ids travel with the arguments; W = 8 for many, as many workgroups as compute units, whose list may stay in pinned
-// host memory: a share is one request over the host link.  Bound: HBM (4 KiB read for 512 bytes written).
+// host memory: a share is one request over the host link.  Bound: HBM (4 KiB read for 512 bytes written): 64 files of 512..4096
+// tokens in 57 us, 297 MB at 5.2 TB/s (pieces of 4 KiB at a stride of 8 KiB are read at 6.0 to 6.6 TB/s when nothing is written).
 // ---------------------------------------------------------------------------------------
 struct BoundsKernelArgs {
   BoundsArgs a;
@@ -395,7 +400,10 @@ __global__ __launch_bounds__(64 * W) void bounds_kernel(std::conditional_t<ARGS,
 // bits (the choice hangs on comparisons of scores that lie close together; with sums in 32 bits it would depend on their order),
 // rounded to 32 at the end and written down as whole numbers of the same order.
 // A wavefront takes one kv head and 32 pages; 32 lanes share a page's 512 bytes, a 16-byte chunk each, with the chunk's coefficients
-// in registers; eight pages a lane are then added up over the 32 lanes by halving exchanges.
+// in registers; eight pages a lane are then added up over the 32 lanes by halving exchanges.  A wavefront's coefficients could serve
+// more of a row's pages, but fewer wavefronts then hide less: 8 files of 32k..131k tokens, 8 heads, 41, 40, 45 and 44 us with 32, 64,
+// 128 and 256 pages to a wavefront, one file 9, 12, 17 and 27.  Bound: between HBM (161 MB in 39.5 us, 4.1 TB/s) and the vector units (busy
+// for 57 % of it: conversions and products in 64 bits).
 // ---------------------------------------------------------------------------------------
 constexpr int kScorePages = 32;                  // of a wavefront
 __device__ __forceinline__ double as_f64(uint32_t lo, uint32_t hi) { return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo); }
@@ -499,8 +507,8 @@ __global__ __launch_bounds__(256) void sparse_scores_kernel(SparseArgs a) {
 // ---------------------------------------------------------------------------------------
 // Append and scores of a small batch in one launch: single new tokens, few pages to score.  The first workgroups append as above; the
 // others score 16 pages to a wavefront and turn the query rows for themselves, because those that the others write are not there yet.
-// (The pages that the tokens complete are their rows' last ones, which nobody scores.)  What it saves is a launch's start and end: 8
-// layers of one file of 30000 tokens.
+// (The pages that the tokens complete are their rows' last ones, which nobody scores.)  What it saves is a launch's start and end: one
+// file of 30000 tokens, 8 heads, 9.0 us instead of 4.1 and 8.7.  Bound: latency (arguments, lists, query rows, an angle, records).
 // ---------------------------------------------------------------------------------------
 struct FirstKernelArgs {
   AppendKernelArgs k;
@@ -741,7 +749,9 @@ __device__ __forceinline__ void pick_highest(const uint32_t* sc, const int m, co
 // fp32; the wavefronts' results are combined through LDS.  The workgroup that finishes last of a row's parts joins them, so that no
 // launch follows.  STREAM: nontemporal loads, where no two rows read the same pages (64 files 62.4 -> 59.3 us a call); where they do (several
 // tokens of a file, forks) the next row finds them in a cache (chunks 72 us, with nontemporal loads 95).
-// Bound: HBM (8 KiB for 4 D 16 G flops).
+// Bound: HBM (8 KiB for 4 D 16 G flops): 64 files of 512..4096 tokens, 1024 tokens read of each, in 53 us, 306 MB at 5.8 TB/s, the scoring
+// of bounds with it; 138 rows of 8 files in 66 us, 440 MB of which the caches serve the most.  One row of one file is latency: 14 us, of
+// which the choice 3.8, pages 1.9, combining 2.1, handing over 2.4.
 // ---------------------------------------------------------------------------------------
 // What workgroups of one launch hand to each other goes past the caches that they do not share, in both directions, and a workgroup
 // counts itself done when its stores have arrived.  (A release fence instead writes back everything in the L2: with one from every
@@ -1174,7 +1184,7 @@ hipError_t launch_append_rope(const AppendRopeArgs& a, const RopeTable& r, int d
   if (a.n_runs <= 0) return a.done ? hipEventRecord(a.done, st) : hipSuccess;
   if (a.n_layers < 1 || a.n_layers > 65535) return hipErrorInvalidValue;
   const int64_t copy = std::min<int64_t>((a.copy_words / 4 + 255) / 256 + (a.copy_words > 0), 256);
-  // the query rows of a run in parts of about four passes of a workgroup
+  // the query rows of a run in parts of about four passes of a workgroup (8 files of up to 33 new tokens 72.5 us a pred; one part to a run 75.3)
   const int parts = a.q ? std::min(std::max(a.Hq * std::min(a.run_tokens, kRunTokens) / 128, 1), std::min(a.Hq, 16)) : 0;
   const dim3 grid((unsigned)(a.n_runs + copy), (unsigned)a.n_layers, (unsigned)(1 + parts)), block(256);
   if (a.by_args) {

@@ -721,3 +721,14 @@ def test_many_rows_with_many_scores(dtype, hq, hkv, lens, new):
     files = make_files(sess, lens, torch.Generator().manual_seed(len(lens)))
     run_sparse(sess, files, new, binding.make_sparse(7, 1, 2))
     sess.close()
+
+
+@pytest.mark.parametrize("pages", [400, 1900])
+def test_one_long_file_among_many_short_ones(pages):
+    # many rows, of which few have pages to score
+    sess = session("bf16", 16, 8, pages + 200)
+    g = torch.Generator().manual_seed(pages)
+    files = make_files(sess, [16 * pages - 3] + list(range(1, 80, 2)), g)
+    for _ in range(2):
+        run_sparse(sess, files, [1] * len(files), binding.make_sparse(20, 1, 2), g=g)
+    sess.close()
