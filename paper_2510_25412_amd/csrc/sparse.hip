@@ -271,10 +271,10 @@ __device__ __forceinline__ void write_bounds(const PageKeys& R, uint8_t* out) {
 }
 
 // ---------------------------------------------------------------------------------------
-// Append with the keys turned on the way.  A workgroup takes a run: the new tokens of a file that go to consecutive slots of one page,
-// one layer.  Few runs travel with the kernel's arguments, so that no request over the host link stands before the first load.  When the
-// run completes its page, the workgroup writes the page's bounds behind its own stores.  Bound: HBM, read + write: 7500 tokens of 8 bf16
-// heads in 17 us, 63 MB at 3.7 TB/s (470 workgroups, two to a compute unit, so that starts and ends show); 64 files of one token 4.8 us: the
+// Append with the keys turned on the way.  A workgroup takes the keys or the values of a run: the new tokens of a file that go to consecutive
+// slots of one page, one layer.  (Both in one, values wait for angles: 7500 tokens 17.4 us a call, 16.6 apart.)  Few runs travel with the kernel's arguments, so that no request over the host link stands before the first load.  When the
+// run completes its page, the workgroup of the keys writes the page's bounds behind its own stores.  Bound: HBM, read + write: 7500 tokens of 8 bf16
+// heads in 16 us, 63 MB at 3.9 TB/s (940 workgroups that all run at once: start, list, rows, angles and bounds show); 64 files of one token 4.8 us: the
 // launch and a chain of two loads, an angle and a store.
 // ---------------------------------------------------------------------------------------
 struct ArgRuns {
@@ -292,8 +292,8 @@ template <typename E, int PATH>
 __device__ __forceinline__ void append_run(SYM_AS4 AppendKernelArgs* ka, const int t0, const int slot, const int nf, const int pos0, const int layer, const int part, const int parts,
                                            double2 (*cs)[kPairs], uint8_t (*stage)[kRowBytes]) {
   const int n = nf & 0xff, Hkv = ka->a.Hkv, Hq = ka->a.q ? ka->a.Hq : 0;
-  // this workgroup's rows of a token: keys and values (part -1), or a part of the query rows
-  const int first = part < 0 ? 0 : 2 * Hkv + Hq * part / parts, rows = (part < 0 ? 2 * Hkv : 2 * Hkv + Hq * (part + 1) / parts) - first;
+  // this workgroup's rows of a token: keys (part -2), values (part -1), or a part of the query rows
+  const int first = part < 0 ? (part + 2) * Hkv : 2 * Hkv + Hq * part / parts, rows = (part < 0 ? first + Hkv : 2 * Hkv + Hq * (part + 1) / parts) - first;
   if (rows <= 0) return;
   uint8_t* page = ka->a.pool + layer * ka->a.layer_bytes + (int64_t)(slot / kP) * ka->a.page_bytes;
   const int ts = slot % kP;
@@ -315,8 +315,10 @@ __device__ __forceinline__ void append_run(SYM_AS4 AppendKernelArgs* ka, const i
         uint8_t *dq = qo + from_q, *dk = page + (int64_t)g * kSlab + (is_v ? kBlk : 0) + (ts + tok) * kHalfBytes;
         return RowAt{is_q ? sq : is_v ? sv : sk, is_q ? dq : dk, is_q ? kHalfBytes : kP * kHalfBytes, is_q || !is_v};
       },
-      [=]() __attribute__((always_inline)) { fill_angles<PATH>(&ka->r, pos, pos0, n, cs); }, rows, n, lg, ka->r.dims, cs, stage);
-  if ((nf >> 8) && ka->a.bounds && part < 0) {
+      [=]() __attribute__((always_inline)) {
+        if (part != -1) fill_angles<PATH>(&ka->r, pos, pos0, n, cs);      // (values do not turn: what is read of cs is not used)
+      }, rows, n, lg, ka->r.dims, cs, stage);
+  if ((nf >> 8) && ka->a.bounds && part == -2) {
     __syncthreads();                             // the page's last keys are written; the others were there
     uint8_t* b = ka->a.bounds + layer * ka->a.layer_bounds + (int64_t)(slot / kP) * Hkv * (2 * kRowBytes);
     for (int g = threadIdx.x >> 6; g < Hkv; g += 4) {
@@ -345,7 +347,7 @@ __global__ __launch_bounds__(256) void append_rope_kernel(AppendKernelArgs) {
   auto ka = (SYM_AS4 AppendKernelArgs*)__builtin_amdgcn_kernarg_segment_ptr();
   if (copy_lists(ka)) return;
   const int32_t* w = ka->a.runs + (int64_t)blockIdx.x * RUN_WORDS;
-  append_run<E, PATH>(ka, sload(w), sload(w + 1), sload(w + 2), sload(w + 3), blockIdx.y, (int)blockIdx.z - 1, (int)gridDim.z - 1, cs, stage);
+  append_run<E, PATH>(ka, sload(w), sload(w + 1), sload(w + 2), sload(w + 3), blockIdx.y, (int)blockIdx.z - 2, (int)gridDim.z - 2, cs, stage);
 }
 template <typename E, int PATH>
 __global__ __launch_bounds__(256) void append_rope_runs_kernel(AppendRunsKernelArgs) {
@@ -354,7 +356,7 @@ __global__ __launch_bounds__(256) void append_rope_runs_kernel(AppendRunsKernelA
   auto ka = (SYM_AS4 AppendRunsKernelArgs*)__builtin_amdgcn_kernarg_segment_ptr();
   if (copy_lists(&ka->k)) return;
   const auto* w = ka->runs.w + blockIdx.x * RUN_WORDS;
-  append_run<E, PATH>(&ka->k, w[0], w[1], w[2], w[3], blockIdx.y, (int)blockIdx.z - 1, (int)gridDim.z - 1, cs, stage);
+  append_run<E, PATH>(&ka->k, w[0], w[1], w[2], w[3], blockIdx.y, (int)blockIdx.z - 2, (int)gridDim.z - 2, cs, stage);
 }
 
 // ---------------------------------------------------------------------------------------
@@ -513,7 +515,7 @@ __global__ __launch_bounds__(256) void sparse_scores_kernel(SparseArgs a) {
 struct FirstKernelArgs {
   AppendKernelArgs k;
   SparseArgs s;
-  int32_t parts, append_blocks, row_blocks;      // workgroups of a run beside the first, of all runs, of a scored row
+  int32_t parts, append_blocks, row_blocks;        // workgroups of a run's query rows, of all runs, of a scored row
 };
 // Chunk `c` of a row, turned: its own 16 bytes and those that hold its pairs' other elements.
 template <typename E, int PATH>
@@ -553,7 +555,7 @@ __global__ __launch_bounds__(256) void sparse_first_kernel(FirstKernelArgs) {
   __shared__ double2 cs[1][kPairs];
   auto ka = (SYM_AS4 FirstKernelArgs*)__builtin_amdgcn_kernarg_segment_ptr();
   if ((int)blockIdx.x < ka->append_blocks) {
-    const int run = (int)blockIdx.x / (1 + ka->parts), part = (int)blockIdx.x % (1 + ka->parts) - 1;
+    const int run = (int)blockIdx.x / (2 + ka->parts), part = (int)blockIdx.x % (2 + ka->parts) - 2;
     const int32_t* w = ka->k.a.runs + (int64_t)run * RUN_WORDS;
     append_run<E, PATH>(&ka->k, sload(w), sload(w + 1), sload(w + 2), sload(w + 3), 0, part, ka->parts, cs, nullptr);
     return;
@@ -1186,7 +1188,7 @@ hipError_t launch_append_rope(const AppendRopeArgs& a, const RopeTable& r, int d
   const int64_t copy = std::min<int64_t>((a.copy_words / 4 + 255) / 256 + (a.copy_words > 0), 256);
   // the query rows of a run in parts of about four passes of a workgroup (8 files of up to 33 new tokens 72.5 us a pred; one part to a run 75.3)
   const int parts = a.q ? std::min(std::max(a.Hq * std::min(a.run_tokens, kRunTokens) / 128, 1), std::min(a.Hq, 16)) : 0;
-  const dim3 grid((unsigned)(a.n_runs + copy), (unsigned)a.n_layers, (unsigned)(1 + parts)), block(256);
+  const dim3 grid((unsigned)(a.n_runs + copy), (unsigned)a.n_layers, (unsigned)(2 + parts)), block(256);
   if (a.by_args) {
     if (a.n_runs > kArgRuns) return hipErrorInvalidValue;
     AppendRunsKernelArgs ka;
@@ -1230,7 +1232,7 @@ hipError_t launch_bounds(const BoundsArgs& a, int dtype, hipStream_t st) {
 
 hipError_t launch_sparse_first(const AppendRopeArgs& a, const RopeTable& r, const SparseArgs& s, int dtype, hipStream_t st) {
   FirstKernelArgs ka{{a, r}, s, std::max(a.Hq / 128, 1), 0, 0};
-  ka.append_blocks = a.n_runs * (1 + ka.parts);
+  ka.append_blocks = a.n_runs * (2 + ka.parts);
   ka.row_blocks = ((s.most_scored + kFirstPages - 1) / kFirstPages * s.Hkv + 3) / 4;
   const dim3 grid((unsigned)(ka.append_blocks + ka.row_blocks * s.n_scored)), block(256);
 #define SYM_LAUNCH(E) \
