@@ -1729,6 +1729,7 @@ int sym_kv_append_rope(sym_ctx* c, int32_t n_files, const sym_kv* kv, const int3
     a.by_args = by_args ? 1 : 0;
     a.runs = by_args ? c->words.data() : c->stage[si] + c->plan.cow.size();
     a.n_runs = (int32_t)runs;
+    a.run_tokens = *std::max_element(n_tokens, n_tokens + n_files);
     const StageDone done(c, by_args ? -1 : si);
     a.done = done.event();
     {

@@ -271,11 +271,11 @@ __device__ __forceinline__ void write_bounds(const PageKeys& R, uint8_t* out) {
 }
 
 // ---------------------------------------------------------------------------------------
-// Append with the keys turned on the way.  A workgroup takes the keys or the values of a run: the new tokens of a file that go to consecutive
-// slots of one page, one layer.  (Both in one, values wait for angles: 7500 tokens 17.4 us a call, 16.6 apart.)  Few runs travel with the kernel's arguments, so that no request over the host link stands before the first load.  When the
-// run completes its page, the workgroup of the keys writes the page's bounds behind its own stores.  Bound: HBM, read + write: 7500 tokens of 8 bf16
-// heads in 16 us, 63 MB at 3.9 TB/s (940 workgroups that all run at once: start, list, rows, angles and bounds show); 64 files of one token 4.8 us: the
-// launch and a chain of two loads, an angle and a store.
+// Append with the keys turned on the way.  A workgroup takes a run, the new tokens of a file that go to consecutive slots of one page, one
+// layer: its keys and values, or one of them where runs are long.  Few runs travel with the kernel's arguments, so that no request over
+// the host link stands before the first load.  When the run completes its page, the workgroup of the keys writes the page's bounds
+// behind its own stores.  Bound: HBM, read + write: 7500 tokens of 8 bf16 heads in 16 us, 63 MB at 3.9 TB/s (940 workgroups that all run at
+// once: start, list, rows, angles and bounds show); 64 files of one token 4.8 us: the launch and a chain of two loads, an angle and a store.
 // ---------------------------------------------------------------------------------------
 struct ArgRuns {
   int32_t w[kArgRuns * RUN_WORDS];
@@ -289,11 +289,12 @@ struct AppendRunsKernelArgs {
   ArgRuns runs;
 };
 template <typename E, int PATH>
-__device__ __forceinline__ void append_run(SYM_AS4 AppendKernelArgs* ka, const int t0, const int slot, const int nf, const int pos0, const int layer, const int part, const int parts,
+__device__ __forceinline__ void append_run(SYM_AS4 AppendKernelArgs* ka, const int t0, const int slot, const int nf, const int pos0, const int layer, const int part, const int parts, const bool apart,
                                            double2 (*cs)[kPairs], uint8_t (*stage)[kRowBytes]) {
   const int n = nf & 0xff, Hkv = ka->a.Hkv, Hq = ka->a.q ? ka->a.Hq : 0;
-  // this workgroup's rows of a token: keys (part -2), values (part -1), or a part of the query rows
-  const int first = part < 0 ? (part + 2) * Hkv : 2 * Hkv + Hq * part / parts, rows = (part < 0 ? first + Hkv : 2 * Hkv + Hq * (part + 1) / parts) - first;
+  // this workgroup's rows of a token: keys and values (part -1) or, where they are apart, keys (-2) or values (-1); or a part of the query rows
+  const int first = part >= 0 ? 2 * Hkv + Hq * part / parts : apart && part == -1 ? Hkv : 0;
+  const int rows = (part >= 0 ? 2 * Hkv + Hq * (part + 1) / parts : part == -2 ? Hkv : 2 * Hkv) - first;
   if (rows <= 0) return;
   uint8_t* page = ka->a.pool + layer * ka->a.layer_bytes + (int64_t)(slot / kP) * ka->a.page_bytes;
   const int ts = slot % kP;
@@ -316,9 +317,9 @@ __device__ __forceinline__ void append_run(SYM_AS4 AppendKernelArgs* ka, const i
         return RowAt{is_q ? sq : is_v ? sv : sk, is_q ? dq : dk, is_q ? kHalfBytes : kP * kHalfBytes, is_q || !is_v};
       },
       [=]() __attribute__((always_inline)) {
-        if (part != -1) fill_angles<PATH>(&ka->r, pos, pos0, n, cs);      // (values do not turn: what is read of cs is not used)
+        if (!apart || part != -1) fill_angles<PATH>(&ka->r, pos, pos0, n, cs);      // (values do not turn: what is read of cs is not used)
       }, rows, n, lg, ka->r.dims, cs, stage);
-  if ((nf >> 8) && ka->a.bounds && part == -2) {
+  if ((nf >> 8) && ka->a.bounds && part == (apart ? -2 : -1)) {
     __syncthreads();                             // the page's last keys are written; the others were there
     uint8_t* b = ka->a.bounds + layer * ka->a.layer_bounds + (int64_t)(slot / kP) * Hkv * (2 * kRowBytes);
     for (int g = threadIdx.x >> 6; g < Hkv; g += 4) {
@@ -347,7 +348,7 @@ __global__ __launch_bounds__(256) void append_rope_kernel(AppendKernelArgs) {
   auto ka = (SYM_AS4 AppendKernelArgs*)__builtin_amdgcn_kernarg_segment_ptr();
   if (copy_lists(ka)) return;
   const int32_t* w = ka->a.runs + (int64_t)blockIdx.x * RUN_WORDS;
-  append_run<E, PATH>(ka, sload(w), sload(w + 1), sload(w + 2), sload(w + 3), blockIdx.y, (int)blockIdx.z - 2, (int)gridDim.z - 2, cs, stage);
+  append_run<E, PATH>(ka, sload(w), sload(w + 1), sload(w + 2), sload(w + 3), blockIdx.y, (int)blockIdx.z - 1 - ka->a.apart, (int)gridDim.z - 1 - ka->a.apart, ka->a.apart, cs, stage);
 }
 template <typename E, int PATH>
 __global__ __launch_bounds__(256) void append_rope_runs_kernel(AppendRunsKernelArgs) {
@@ -356,7 +357,7 @@ __global__ __launch_bounds__(256) void append_rope_runs_kernel(AppendRunsKernelA
   auto ka = (SYM_AS4 AppendRunsKernelArgs*)__builtin_amdgcn_kernarg_segment_ptr();
   if (copy_lists(&ka->k)) return;
   const auto* w = ka->runs.w + blockIdx.x * RUN_WORDS;
-  append_run<E, PATH>(&ka->k, w[0], w[1], w[2], w[3], blockIdx.y, (int)blockIdx.z - 2, (int)gridDim.z - 2, cs, stage);
+  append_run<E, PATH>(&ka->k, w[0], w[1], w[2], w[3], blockIdx.y, (int)blockIdx.z - 1 - ka->k.a.apart, (int)gridDim.z - 1 - ka->k.a.apart, ka->k.a.apart, cs, stage);
 }
 
 // ---------------------------------------------------------------------------------------
@@ -555,9 +556,9 @@ __global__ __launch_bounds__(256) void sparse_first_kernel(FirstKernelArgs) {
   __shared__ double2 cs[1][kPairs];
   auto ka = (SYM_AS4 FirstKernelArgs*)__builtin_amdgcn_kernarg_segment_ptr();
   if ((int)blockIdx.x < ka->append_blocks) {
-    const int run = (int)blockIdx.x / (2 + ka->parts), part = (int)blockIdx.x % (2 + ka->parts) - 2;
+    const int run = (int)blockIdx.x / (1 + ka->parts), part = (int)blockIdx.x % (1 + ka->parts) - 1;
     const int32_t* w = ka->k.a.runs + (int64_t)run * RUN_WORDS;
-    append_run<E, PATH>(&ka->k, sload(w), sload(w + 1), sload(w + 2), sload(w + 3), 0, part, ka->parts, cs, nullptr);
+    append_run<E, PATH>(&ka->k, sload(w), sload(w + 1), sload(w + 2), sload(w + 3), 0, part, ka->parts, false, cs, nullptr);
     return;
   }
   const int blk = (int)blockIdx.x - ka->append_blocks, at_row = blk / ka->row_blocks, Hkv = ka->s.Hkv, first = ka->s.first;
@@ -1182,13 +1183,16 @@ hipError_t launch_rope_rows(RopeRowsArgs a, const RopeTable& r, int dtype, hipSt
   return hipGetLastError();
 }
 
-hipError_t launch_append_rope(const AppendRopeArgs& a, const RopeTable& r, int dtype, hipStream_t st) {
+hipError_t launch_append_rope(AppendRopeArgs a, const RopeTable& r, int dtype, hipStream_t st) {
   if (a.n_runs <= 0) return a.done ? hipEventRecord(a.done, st) : hipSuccess;
   if (a.n_layers < 1 || a.n_layers > 65535) return hipErrorInvalidValue;
   const int64_t copy = std::min<int64_t>((a.copy_words / 4 + 255) / 256 + (a.copy_words > 0), 256);
   // the query rows of a run in parts of about four passes of a workgroup (8 files of up to 33 new tokens 72.5 us a pred; one part to a run 75.3)
   const int parts = a.q ? std::min(std::max(a.Hq * std::min(a.run_tokens, kRunTokens) / 128, 1), std::min(a.Hq, 16)) : 0;
-  const dim3 grid((unsigned)(a.n_runs + copy), (unsigned)a.n_layers, (unsigned)(2 + parts)), block(256);
+  // keys and values of long runs apart: values need not wait for angles (8000 tokens of a file 16.9 us a call, 17.8 in one; 8 files of 2..33 tokens
+  // 70.6 and 71.9; 2 tokens of 8 files 29.5 and 28.8, one of 64 files 62.1 and 61.6)
+  a.apart = a.run_tokens > 8;
+  const dim3 grid((unsigned)(a.n_runs + copy), (unsigned)a.n_layers, (unsigned)(1 + a.apart + parts)), block(256);
   if (a.by_args) {
     if (a.n_runs > kArgRuns) return hipErrorInvalidValue;
     AppendRunsKernelArgs ka;
@@ -1232,7 +1236,7 @@ hipError_t launch_bounds(const BoundsArgs& a, int dtype, hipStream_t st) {
 
 hipError_t launch_sparse_first(const AppendRopeArgs& a, const RopeTable& r, const SparseArgs& s, int dtype, hipStream_t st) {
   FirstKernelArgs ka{{a, r}, s, std::max(a.Hq / 128, 1), 0, 0};
-  ka.append_blocks = a.n_runs * (2 + ka.parts);
+  ka.append_blocks = a.n_runs * (1 + ka.parts);
   ka.row_blocks = ((s.most_scored + kFirstPages - 1) / kFirstPages * s.Hkv + 3) / 4;
   const dim3 grid((unsigned)(ka.append_blocks + ka.row_blocks * s.n_scored)), block(256);
 #define SYM_LAUNCH(E) \

@@ -45,6 +45,7 @@ struct AppendRopeArgs {
   int32_t n_runs, Hq, Hkv, n_layers;
   int32_t run_tokens;       // tokens of the longest run
   int32_t by_args;          // the runs are host memory and travel with the arguments
+  int32_t apart;            // keys and values in workgroups of their own (set by the launch function)
   const int32_t* host_words;   // lists to be copied along the way: pinned host memory, where to, how many words
   int32_t* dev_words;
   int64_t copy_words;
@@ -118,7 +119,7 @@ inline bool scores_with_append(const RopeTable& r, int Hkv, int64_t n_scored, in
 // Weak: the host code is also built without kernels (by tests of the host side, against stand-ins for the launches it made before these).
 #define SYMKV_LAUNCH __attribute__((weak))
 SYMKV_LAUNCH hipError_t launch_rope_rows(RopeRowsArgs a, const RopeTable& r, int dtype, hipStream_t st);
-SYMKV_LAUNCH hipError_t launch_append_rope(const AppendRopeArgs& a, const RopeTable& r, int dtype, hipStream_t st);
+SYMKV_LAUNCH hipError_t launch_append_rope(AppendRopeArgs a, const RopeTable& r, int dtype, hipStream_t st);
 SYMKV_LAUNCH hipError_t launch_bounds(const BoundsArgs& a, int dtype, hipStream_t st);
 SYMKV_LAUNCH hipError_t launch_sparse_first(const AppendRopeArgs& a, const RopeTable& r, const SparseArgs& s, int dtype, hipStream_t st);
 SYMKV_LAUNCH hipError_t launch_sparse_scores(const SparseArgs& a, int dtype, hipStream_t st);

@@ -7,7 +7,7 @@ int enter_device(int) { return -1; }
 void leave_device(int) {}
 bool stream_captures(hipStream_t) { return false; }
 hipError_t launch_rope_rows(RopeRowsArgs, const RopeTable&, int, hipStream_t) { return launch({}); }
-hipError_t launch_append_rope(const AppendRopeArgs& a, const RopeTable&, int, hipStream_t) {
+hipError_t launch_append_rope(AppendRopeArgs a, const RopeTable&, int, hipStream_t) {
   Command c{{}, a.done};
   if (!a.by_args) add(c, a.runs, (int64_t)a.n_runs * RUN_WORDS * 4);
   add(c, a.host_words, a.copy_words * 4);
