@@ -1074,13 +1074,14 @@ __global__ __launch_bounds__(64 * W, 8 / W) void sparse_attend_kernel(SparseArgs
       pick_highest<W, 0>(sc, m, want, s, chosen);
     }
   }
+  if (lo >= hi && threadIdx.x == 0) s_list[0] = pt[0];      // a part without pages (a short file among long ones)
   __syncthreads();
   int p = lo + (int)((int64_t)(hi - lo) * wv / W);
   const int pe = lo + (int)((int64_t)(hi - lo) * (wv + 1) / W);
   const uint8_t* pool = a.pool + (int64_t)head * kSlab;
   PageRegs A, B;
-  // (past the wavefront's pages: another page of the part, read and not used; a part has a page at least)
-  auto id = [&](int i) __attribute__((always_inline)) { return (int64_t)__builtin_amdgcn_readfirstlane(s_list[min(i, hi - 1) - lo]); };
+  // (past the wavefront's pages, and without any: another page, read and not used)
+  auto id = [&](int i) __attribute__((always_inline)) { return (int64_t)__builtin_amdgcn_readfirstlane(s_list[max(min(i, hi - 1) - lo, 0)]); };
   at.request(A, pool + id(p) * a.page_bytes);
   while (p < pe) {
     at.request(B, pool + id(p + 1) * a.page_bytes);

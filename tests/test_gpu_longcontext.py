@@ -732,3 +732,17 @@ def test_one_long_file_among_many_short_ones(pages):
     for _ in range(2):
         run_sparse(sess, files, [1] * len(files), binding.make_sparse(20, 1, 2), g=g)
     sess.close()
+
+
+@pytest.mark.parametrize("dtype,hq,hkv", [("bf16", 1, 1), ("bf16", 8, 1), ("bf16", 2, 2), ("f32", 1, 1), ("f32", 4, 1)])
+@pytest.mark.parametrize("budget", [70, 300])
+def test_short_files_beside_long_ones(dtype, hq, hkv, budget):
+    # the list of a long file goes in parts, of which a short file's row has pages for a few or for one
+    print(f"[case] short beside long {dtype} {hq}/{hkv} {budget}", flush=True)
+    lens = [0, 5, 16, 40, 16 * 420 + 1, 16 * 64]
+    sess = session(dtype, hq, hkv, sum(-(-n // P) + 2 for n in lens), order=np.arange(sum(-(-n // P) + 2 for n in lens), dtype=np.int32)[::-1].copy())
+    g = torch.Generator().manual_seed(budget)
+    files = make_files(sess, lens, g)
+    for _ in range(2):
+        run_sparse(sess, files, [1] * len(files), binding.make_sparse(budget, 1, 2), g=g)
+    sess.close()
