@@ -597,7 +597,7 @@ __global__ __launch_bounds__(256) void sparse_first_kernel(FirstKernelArgs) {
 
 constexpr int kMostWaves = 8;                   // of a workgroup that attends
 struct ChooseLds {
-  __align__(16) uint32_t hist[4][256];                         // one for every round
+  __align__(16) uint32_t hist[kChoiceRounds][256];                // one for every round
   uint2 total[kMostWaves];                       // of every wavefront: greatest and least score, then how many are above and equal to the least chosen
 };
 
@@ -632,8 +632,8 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t x) {
 }
 
 // The `want` highest of the m scores (want < m), by the whole workgroup: put(i-th chosen, its index), in order of the index.
-// The smallest chosen score is found in at most four rounds: a histogram of 256 equal steps between the least and the greatest that it can be,
-// and the step in which the wanted one lies.  Usually a step that is wanted whole ends it.  A thread holds EPT scores in a row, so that
+// The smallest chosen score is found in at most four rounds (ScoreRange): a histogram of 256 equal steps between the least and the greatest
+// that it can be, and the step in which the wanted one lies.  Usually a step that is wanted whole ends it.  A thread holds EPT scores in a row, so that
 // places are counted thread by thread; EPT = 0: any number of scores, sixteen at a time, read again for every round.
 template <int W, int EPT, typename P>
 __device__ __forceinline__ void pick_highest(const uint32_t* sc, const int m, const int want, ChooseLds& s, const P& put) {
@@ -670,8 +670,8 @@ __device__ __forceinline__ void pick_highest(const uint32_t* sc, const int m, co
       }
     }
   };
-  for (int i = tid; i < 4 * 256; i += NT) (&s.hist[0][0])[i] = 0;
-  uint32_t lo, hi = 0, top = 0;                  // top: the greatest ~key
+  for (int i = tid; i < kChoiceRounds * 256; i += NT) (&s.hist[0][0])[i] = 0;
+  uint32_t hi = 0, top = 0;                      // top: the greatest ~key
   each([&](int, uint32_t k) {
     hi = max(hi, k);
     top = max(top, k ? ~k : 0u);
@@ -685,15 +685,14 @@ __device__ __forceinline__ void pick_highest(const uint32_t* sc, const int m, co
     hi = max(hi, s.total[x].x);
     top = max(top, s.total[x].y);
   }
-  hi = __builtin_amdgcn_readfirstlane(hi);
-  lo = __builtin_amdgcn_readfirstlane(~top);
-  uint32_t need = (uint32_t)want, t;             // chosen: above t, and the first `need` of those equal to it
-  for (int round = 0;; ++round) {
-    const uint32_t width = hi - lo;
-    const int shift = width < 256 ? 0 : 24 - __clz((int)width);
+  ScoreRange r{(uint32_t)__builtin_amdgcn_readfirstlane(~top), (uint32_t)__builtin_amdgcn_readfirstlane(hi)};
+  uint32_t need = (uint32_t)want, t = 0;         // chosen: above t, and the first `need` of those equal to it
+#pragma unroll 1
+  for (int round = 0; round < kChoiceRounds; ++round) {
+    const int shift = r.shift();
     uint32_t* h = s.hist[round];
     each([&](int, uint32_t k) {
-      if (k - lo <= width) atomicAdd(&h[(k - lo) >> shift], 1u);      // (0, for none, is below every lo)
+      if (r.holds(k)) atomicAdd(&h[r.step(k, shift)], 1u);      // (0, for none, is below every lo)
     });
     __syncthreads();
     // every wavefront for itself: lane l has steps 4 l .. 4 l + 3
@@ -709,17 +708,14 @@ __device__ __forceinline__ void pick_highest(const uint32_t* sc, const int m, co
     if (above + count < need) above += count, --step, count = cy;
     if (above + count < need) above += count, --step, count = cx;
     need -= above;
-    lo += step << shift;
+    r.narrow(step, shift);
     if (need == count) {                         // the whole step
-      t = lo - 1;
+      t = r.lo - 1;
       need = 0;
       break;
     }
-    if (shift == 0) {                            // all of one value
-      t = lo;
-      break;
-    }
-    hi = min(hi, lo + ((1u << shift) - 1));
+    t = r.lo;
+    if (shift == 0) break;                       // all of one value
   }
   // Place of a chosen one: those above t before it, and at most `need` of the equal ones before it.
   uint32_t gt = 0, eq = 0;
@@ -1041,6 +1037,8 @@ __global__ __launch_bounds__(64 * W, 8 / W) void sparse_attend_kernel(SparseArgs
       else put(kept - a.last + i - a.first, n - a.last + i - a.first);
     }
     const int m = n - a.first - a.last, want = kept - a.first - a.last;
+    // places that the choice fills: a page of the pool in each until then (the choice has barriers before it fills them)
+    for (int i = max(lo, a.first) + threadIdx.x; i < min(hi, kept - a.last); i += NT) s_list[i - lo] = 0;
     auto chosen = [&](int i, int p) __attribute__((always_inline)) { put(a.first + i, a.first + p); };
     ChooseLds& s = *(ChooseLds*)s_mem;
     const uint32_t* sc = a.scores + (int64_t)unit * a.score_stride;

@@ -116,6 +116,23 @@ inline bool scores_with_append(const RopeTable& r, int Hkv, int64_t n_scored, in
   return (r.path == ROPE_HALVES || r.path == ROPE_INTERLEAVED) && n_scored > 0 && (most_scored + kFirstPages - 1) / kFirstPages * Hkv * n_scored <= kFirstWaves;
 }
 
+// The scores that the least chosen one can still be, lo <= it <= hi, in rounds: 256 equal steps (a power of two each), of which the one with
+// the wanted score becomes the range.  Scores are whole numbers from 1 on (0: none) up to 2^32 - 1, and a range may end at
+// the last of them: its end is found by subtracting, since lo + a step's width may not fit 32 bits.
+constexpr int kChoiceRounds = 4;           // a range of less than 2^32, 2^24, 2^16, 2^8: the last one's steps are single values
+struct ScoreRange {
+  uint32_t lo, hi;
+  __host__ __device__ int shift() const { return hi - lo < 256 ? 0 : 24 - __builtin_clz(hi - lo); }
+  __host__ __device__ bool holds(uint32_t k) const { return k - lo <= hi - lo; }
+  __host__ __device__ uint32_t step(uint32_t k, int by) const { return (k - lo) >> by; }
+  // to its step s, steps of 1 << by
+  __host__ __device__ void narrow(uint32_t s, int by) {
+    lo += s << by;
+    const uint32_t most = (1u << by) - 1;
+    hi = hi - lo < most ? hi : lo + most;
+  }
+};
+
 // Weak: the host code is also built without kernels (by tests of the host side, against stand-ins for the launches it made before these).
 #define SYMKV_LAUNCH __attribute__((weak))
 SYMKV_LAUNCH hipError_t launch_rope_rows(RopeRowsArgs a, const RopeTable& r, int dtype, hipStream_t st);
