@@ -465,7 +465,8 @@ class Context:
         """Marshals the arguments of pred_batch once, for callers that issue the same batch many
         times (a decode loop): returns an object for pred_prepared.  The arrays and tensors are
         kept alive by the object."""
-        kv_a, nt_a = np.ascontiguousarray(kv, np.int32), np.ascontiguousarray(n_tokens, np.int32)
+        kv_a, kv_p = _i32(kv)
+        nt_a, nt_p = _i32(n_tokens)
         keep = (kv_a, nt_a, q, k_new, v_new, out)
         args = (len(kv_a), kv_p, nt_p, _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(out))
         return keep, args
