@@ -882,12 +882,12 @@ int size_sparse(sym_ctx* c, SparsePlan* sp, int32_t n_lips, const sym_kv* kv, co
   sp->n_stale = (int32_t)stale;
   sp->n_done = (int32_t)done;
   sp->kv.assign(kv, kv + n_lips);
-  sp->score_stride = most_pages > sp->budget ? (int32_t)align_up(most_pages - sp->first - sp->last, 32) : 0;
   // Parts of a list: where rows are few as many workgroups as fill the chip, each with eight pages at least; no more pages than a
   // workgroup's list holds.  8 files of 32k..131k tokens with 2048, 1024, 512 wavefronts: 82, 95, 119 us a call (4096: 95), 8 layers of one
   // file 183, 183, 193; with 8, 16, 32 pages at least 185, 192, 220, and one fp32 file 13.9, 14.3, 15.3 (4 pages: 14.1).
   const int64_t units = tokens * H, most_scored = most_pages > sp->budget ? most_pages - sp->first - sp->last : 0;
   sp->own = scores_itself(scored * H, most_scored);
+  sp->score_stride = sp->own ? 0 : (int32_t)align_up(most_scored, 32);      // (the attention keeps its own in LDS)
   sp->waves = attend_waves(sp->own, units);
   sp->splits = (int32_t)std::max({(int64_t)1, std::min(2048 / sp->waves / units, most_kept / 8), (most_kept + kPartPages - 1) / kPartPages});
   sp->q_bytes = sp->turns ? align_up(row_bytes_of(tokens, c->cfg.n_q_heads), 256) : 0;
