@@ -359,8 +359,8 @@ int64_t sym_kv_bounded(sym_ctx* ctx, sym_kv kv);
  *   dense_layers each layer is run by either sym_pred_layer_sparse or sym_pred_layer (rows as they are: it knows no rope).
  * Rows and outputs 16-byte aligned.  A buffer for bounds has to be attached.  SYM_ENOSPC if the workspace does not hold the batch:
  * beside the page tables T * Hq * 256 bytes with a rope, Hkv * 4 bytes per page of the longest file for one token (a batch goes
- * through what is left some tokens at a time), and Hq * (D + 2) * 4 bytes for each part of eight pages or more in which a
- * token's list is read when tokens are few.                                               */
+ * through what is left some tokens at a time), and Hq * (D + 2) * 4 bytes for each part in which a token's list is read: of 2048
+ * pages at most, and as long as there is room of eight or more when tokens are few.       */
 typedef struct sym_sparse {
   int32_t budget, first, last;     /* first >= 0, last >= 1, first + last <= budget      */
   int32_t dense_layers;

@@ -71,7 +71,7 @@ struct SparsePlan {
   int32_t n_rows = 0, n_runs = 0, run_tokens = 1;
   bool alone = true;                               // no file of the batch has several new tokens or a first page that another file has too
   int32_t n_stale = 0, n_done = 0;                 // full pages without bounds: from before the batch, then those that it completes
-  int32_t splits = 1, waves = 4, score_stride = 0;
+  int32_t splits = 1, least_splits = 1, waves = 4, score_stride = 0;
   bool own = false;                                // the attention scores pages itself
   int64_t q_bytes = 0, row_bytes = 0;              // scratch: turned query rows of the batch; per row and slab
   struct Slab {
@@ -889,19 +889,22 @@ int size_sparse(sym_ctx* c, SparsePlan* sp, int32_t n_lips, const sym_kv* kv, co
   sp->own = scores_itself(scored * H, most_scored);
   sp->score_stride = sp->own ? 0 : (int32_t)align_up(most_scored, 32);      // (the attention keeps its own in LDS)
   sp->waves = attend_waves(sp->own, units);
-  sp->splits = (int32_t)std::max({(int64_t)1, std::min(2048 / sp->waves / units, most_kept / 8), (most_kept + kPartPages - 1) / kPartPages});
+  sp->least_splits = (int32_t)std::max<int64_t>(1, (most_kept + kPartPages - 1) / kPartPages);
+  sp->splits = (int32_t)std::max<int64_t>(sp->least_splits, std::min(2048 / sp->waves / units, most_kept / 8));
   sp->q_bytes = sp->turns ? align_up(row_bytes_of(tokens, c->cfg.n_q_heads), 256) : 0;
   sp->n_counters = sp->splits > 1 ? H * std::max<int64_t>(1, std::min(tokens, kMostUnits / (H * sp->splits))) : 0;
   *words = sp->n_rows * (int64_t)(SPARSE_ROW_WORDS + SPARSE_SCORED_WORDS) + entries + runs * RUN_WORDS + stale + done + sp->n_counters + 16;
   return SYM_OK;
 }
 int fit_sparse(sym_ctx* c, SparsePlan* sp, int64_t ws_bytes, int64_t blob_words) {
-  const int64_t H = c->cfg.n_kv_heads;
-  const int64_t slot = sp->splits > 1 ? (int64_t)sp->splits * c->G * (2 + c->cfg.head_dim) * 4 : 0;
-  sp->row_bytes = H * ((int64_t)sp->score_stride * 4 + slot);
+  const int64_t H = c->cfg.n_kv_heads, scores = (int64_t)sp->score_stride * 4, part = (int64_t)c->G * (2 + c->cfg.head_dim) * 4;
   const int64_t room = ws_bytes - align_up(blob_words * 4, 256) - sp->q_bytes - 4 * 256;
-  sp->slab_rows = std::min({room / std::max<int64_t>(sp->row_bytes, 1), std::max<int64_t>(1, kMostUnits / (H * sp->splits)), (int64_t)65535, (int64_t)sp->n_rows});
-  if (sp->slab_rows < 1) return fail(c, SYM_ENOSPC, "workspace too small for this sparse batch");
+  const int64_t most_rows = std::min({std::max<int64_t>(1, kMostUnits / (H * sp->splits)), (int64_t)65535, (int64_t)sp->n_rows});
+  if (H * (scores + sp->splits * part) > room)       // fewer parts rather than no room for a row
+    sp->splits = (int32_t)std::max<int64_t>(sp->least_splits, std::min<int64_t>(sp->splits, (room / H - scores) / part));
+  sp->row_bytes = H * (scores + (sp->splits > 1 ? sp->splits * part : 0));
+  if (sp->row_bytes > room || room < 0) return fail(c, SYM_ENOSPC, "workspace too small for this sparse batch");
+  sp->slab_rows = sp->row_bytes > 0 ? std::min(most_rows, room / sp->row_bytes) : most_rows;
   return SYM_OK;
 }
 // Writes the sections at word `at` of `blob` (after the append): rows, scored rows, tables, runs, pages without bounds, counters.

@@ -1,5 +1,5 @@
-"""The scratch of sparse preds (CPU only): a device that computes nothing looks at what its launches are given.  Every
-section lies in the workspace, apart from the others; what a batch does not use takes no room."""
+"""The scratch of sparse preds (CPU only): a device that computes nothing looks at what its launches are given.  A batch is taken as long as its lists, its
+turned query rows and one token in the fewest parts fit the workspace; what a batch does not use takes no room."""
 import os
 import shutil
 import subprocess
@@ -46,6 +46,43 @@ def run(tmp_path_factory):
         p = subprocess.run([sys.executable, "-c", PRELUDE + code], cwd=ROOT, env=dict(os.environ, SYMPHONY_KV_LIB=out), stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, timeout=300)
         assert p.returncode == 0, p.stdout[-4000:]
     return child
+
+
+def test_a_batch_that_fits_with_fewer_parts_is_taken(run):
+    # one token, 2 kv heads of 2 query heads, 300 of 700 pages: 5.6 KB of scores, lists of 3 KB, and 2 * 2 * 130 * 4 bytes for each of up to 37 parts
+    run("""
+want = {}
+for kb in (256, 64, 48, 40):
+    ctx = context(4, 2, "bf16", 720, kb << 10)
+    f = ctx.kv_open(None)
+    ctx.plan_append([f], [11195])
+    ctx.pred_sparse([f], [1], binding.make_sparse(300, 1, 1), rows, rows, rows, rows, None, None)
+    want[kb] = seen()
+    assert want[kb][0] == 0 and want[kb][1] == 1 and ctx.kv_len(f) == 11196
+assert want[256][2:] == [37, 37] and 20 <= want[64][2] < 37 and 10 <= want[48][2] < want[64][2] and 5 <= want[40][2] < want[48][2]
+ctx = context(4, 2, "bf16", 9000, 40 << 10)      # 8700 pages: 70 KB of scores
+f = ctx.kv_open(None)
+ctx.plan_append([f], [139195])
+try:
+    ctx.pred_sparse([f], [1], binding.make_sparse(300, 1, 1), rows, rows, rows, rows, None, None)
+    raise AssertionError("taken without room for the scores")
+except binding.SymError as e:
+    assert e.code == binding.SYM_ENOSPC and ctx.kv_len(f) == 139195 and seen()[1] == 0
+""")
+
+
+def test_lists_longer_than_a_workgroup_holds_keep_their_parts(run):
+    run("""
+for kb, taken in ((4096, True), (64, True), (46, False)):      # 5000 pages read whole: three parts at least, 6.5 KB each, and lists of 20 KB
+    ctx = context(8, 1, "f32", 5100, kb << 10)
+    f = ctx.kv_open(None)
+    ctx.plan_append([f], [79990])
+    try:
+        ctx.pred_sparse([f], [1], binding.make_sparse(6000, 1, 1), rows, rows, rows, rows, None, None)
+        assert taken and seen()[0] == 0 and seen()[2] >= 3, (kb, seen())
+    except binding.SymError as e:
+        assert not taken and e.code == binding.SYM_ENOSPC, (kb, e)
+""")
 
 
 def test_scores_that_stay_in_a_workgroup_take_no_room(run):
