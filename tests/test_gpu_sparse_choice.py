@@ -102,3 +102,17 @@ def test_many_rows_with_extreme_scores(values):
     for budget in (6, 40):
         files.check(budget, 1, 1)
     files.close()
+
+
+@pytest.mark.parametrize("dtype,hq", [("bf16", 16), ("f32", 8)])
+def test_many_rows_of_very_different_lengths(dtype, hq):
+    # four wavefronts to a workgroup, one file each of the numbers of scores that a thread of them holds: 1, 4, 8, 16, 32, and read again
+    pages = [200, 900, 1500, 3000, 4500, 8500] + list(range(1, 61, 2))
+    files = Files(dtype, hq, 8, pages, 11)
+    for budget, first, last in ((9, 1, 2), (333, 0, 1), (2500, 3, 4)):
+        files.check(budget, first, last)
+    for i in range(6):
+        files.plant(i, 120, [INF, NAN])
+    files.ctx.bounds_attach(files.bounds)                        # (the bounds of the planted pages are computed again)
+    files.check(60, 1, 1)
+    files.close()
