@@ -920,7 +920,6 @@ void fill_sparse(sym_ctx* c, SparsePlan* sp, int32_t n_lips, const sym_kv* kv, c
   int32_t *stale = blob + sp->off_pages, *done = stale + sp->n_stale;
   append_runs(c, n_lips, kv, n_tokens, &c->words);
   copy_bytes(blob + sp->off_runs, c->words.data(), c->words.size() * 4);
-  sp->slabs.clear();
   int32_t row = 0, tbl = 0, n_scored = 0;
   for (int32_t b = 0; b < n_lips; ++b) {
     const KvFile* f = c->fs->file_of(kv[b]);
@@ -1047,14 +1046,16 @@ int begin_sparse_locked(sym_ctx* c, int32_t n_lips, const sym_kv* kv, const int3
   if ((rc = refuse_capture(c, st, "pred_sparse"))) return rc;
   if ((rc = size_sparse(c, &sp, n_lips, kv, n_tokens, tokens, runs, &extra))) return rc;
   PlannedBatch pb;
+  const int64_t bound = (sp.dense ? blob_words_bound(c, n_lips, tokens, sp.entries) : 3ll * n_lips) + extra;
+  if ((rc = fit_sparse(c, &sp, c->cfg.workspace_bytes, bound))) return rc;
+  // what is filled behind the append, while memory may still run out
+  c->words.reserve((size_t)runs * RUN_WORDS);
+  sp.slabs.reserve((size_t)((sp.n_rows + sp.slab_rows - 1) / sp.slab_rows));
+  c->pred.done.reserve((size_t)c->n_layers);
   if (sp.dense) {
-    int64_t entries = 0;
-    for (int32_t b = 0; b < n_lips; ++b) entries += (c->fs->len(kv[b]) + n_tokens[b] + c->cfg.page_tokens - 1) / c->cfg.page_tokens;
-    if ((rc = fit_sparse(c, &sp, c->cfg.workspace_bytes, blob_words_bound(c, n_lips, tokens, entries) + extra))) return rc;
     if ((rc = pred_plan_locked(c, n_lips, kv, n_tokens, workspace_of(c), false, &pb, extra))) return rc;
   } else {
-    const int64_t bound = 3ll * n_lips + extra;
-    if ((rc = fit_sparse(c, &sp, c->cfg.workspace_bytes, bound)) || (rc = stage_reserve(c, bound))) return rc;
+    if ((rc = stage_reserve(c, bound))) return rc;
     c->plan.clear();
     if ((rc = c->fs->append(n_lips, kv, n_tokens, &c->plan, &c->err))) return rc;
     if ((rc = stage_acquire(c, bound, &pb.si))) return rc;
