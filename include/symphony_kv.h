@@ -53,6 +53,7 @@ extern "C" {
 
 #define SYM_F32  0
 #define SYM_BF16 1
+#define SYM_F16  2       /* logits of sym_beam_select only                              */
 
 typedef struct sym_ctx sym_ctx;   /* opaque; owns host metadata and pinned staging only */
 typedef int32_t sym_kv;           /* file handle >= 0; the lowest free slot is reused   */
@@ -374,6 +375,76 @@ int sym_pred_begin_sparse(sym_ctx* ctx, int32_t n_lips, const sym_kv* kv, const 
 int sym_pred_layer_sparse(sym_ctx* ctx, int32_t layer, const void* q, const void* k_new, const void* v_new,
                           float* out, int32_t* picked, void* stream);
 
+/* ---- beams: choices, state rows, files ------------------------------------------------ */
+/* One step of beam search over the next-token distributions of a batch of requests ("groups").  Group g has beams[g] consecutive rows;
+ * the score of token v after beam b is
+ *   score_b + x_bv - log sum_u exp(x_bu),
+ * u over the tokens that the row allows: a token that it does not allow counts as -inf, whatever its logit holds.  Each group gets the
+ * n_best (beam, token) pairs of largest score, best first; of equal ones the lower beam, then the lower token.  A pair of a score that is
+ * not finite is never chosen: rows whose running score is not finite (-inf: a beam that does not live; its logits are not read),
+ * rows that allow nothing, and rows with a NaN or +inf among what they allow have none.  Places that nothing fills
+ * hold -inf, -1, -1.  Compared in 64 bits, returned in 32; exponentials in 32 bits, summed in 32 within 512 logits' stride and in 64 beyond.
+ * All pointers are device memory of the caller but `beams` (host, read before the call returns); scratch is written and read by the call alone:
+ * two calls that may run at one time (graphs among them) need one each.  An output that overlaps anything else is refused.  Touches
+ * neither files nor workspace: allowed while a batch is open, and may be recorded into a graph.              */
+#define SYM_BEAMS_MOST 64       /* rows of a group   */
+#define SYM_BEST_MOST  128      /* choices of a group */
+typedef struct sym_beam_step {
+  int32_t n_groups, n_best;
+  const int32_t* beams;            /* [n_groups], 1 .. SYM_BEAMS_MOST each                */
+  int32_t vocab, dtype;            /* 1 .. 2^24; SYM_F32, SYM_BF16 or SYM_F16             */
+  const void* logits;              /* [rows][logits_stride], aligned to an element        */
+  int64_t logits_stride;           /* elements from row to row, >= vocab (0: vocab)       */
+  const float* scores;             /* [rows]                                              */
+  const uint32_t* allowed;         /* NULL, or [rows][allowed_stride]: bit v % 32 of word v / 32 */
+  int64_t allowed_stride;          /* words from row to row, >= (vocab + 31) / 32 (0: that) */
+  float* best_scores;              /* [n_groups][n_best]                                  */
+  int32_t* best_beams;             /* [n_groups][n_best]: row within the group            */
+  int32_t* best_tokens;            /* [n_groups][n_best]                                  */
+  void* scratch;                   /* sym_beam_scratch_bytes(), 16-byte aligned           */
+  int64_t scratch_bytes;
+} sym_beam_step;
+int64_t sym_beam_scratch_bytes(int32_t n_groups, const int32_t* beams, int32_t vocab, int32_t n_best);   /* or a negative status */
+int     sym_beam_select(sym_ctx* ctx, const sym_beam_step* step, void* stream);
+
+/* Rows of per-beam state (token histories, recurrent states) after the beams: in each of n_states arrays [outer][rows][row_bytes], row r
+ * of group g receives row parents[r] of the group (device int32 [rows], index within the group).  A parent outside the group, -1 above
+ * all, leaves the row as it is.  dst may be src (in place) or apart from it, then every row is written; nothing else may overlap.  Rows
+ * of any alignment; 16-byte aligned ones move fastest.  Like sym_beam_select allowed while a batch is open and in graphs.  */
+#define SYM_STATES_MOST 64
+typedef struct sym_beam_state {
+  void* dst;
+  const void* src;
+  int64_t outer, outer_stride;     /* bytes from one [rows][row_bytes] to the next        */
+  int64_t row_stride, row_bytes;   /* bytes from row to row, >= row_bytes; bytes that move */
+} sym_beam_state;
+int     sym_beam_states(sym_ctx* ctx, int32_t n_groups, const int32_t* beams, const int32_t* parents,
+                        int32_t n_states, const sym_beam_state* states, void* stream);
+
+/* The files of beams.  All on the host but the copies, one launch for all of them and all layers, on `stream`:
+ *   sym_kv_fork_batch: out[i] = a fork of parents[i] (a file may be named often).
+ *   sym_kv_reorder: file kv[i] takes over the tokens that file kv[from[i]] holds before the call (from[i] = i or -1: it keeps its own); kv
+ *     distinct files (else SYM_EBUSY).  Handles and names stay; what no file has any more is freed, and may hold the copies.
+ *   own_last: a partly filled last page that is shared is copied now (every new or taking file in order, then every keeping one, while
+ *     others have the page too), as the file's next append would: the preds behind the call then copy nothing.  0: it stays shared.
+ *   sym_kv_remove_batch: sym_kv_remove of n distinct files (else SYM_EBUSY).
+ * kv, parents, from, out: host.  All or nothing.  With own_last not to be recorded into a graph (SYM_EINVAL).      */
+int     sym_kv_fork_batch(sym_ctx* ctx, int32_t n, const sym_kv* parents, int32_t own_last, sym_kv* out, void* stream);
+int     sym_kv_reorder(sym_ctx* ctx, int32_t n, const sym_kv* kv, const int32_t* from, int32_t own_last, void* stream);
+int     sym_kv_remove_batch(sym_ctx* ctx, int32_t n, const sym_kv* kv);
+
+/* Pages [first, first + n) are emptied and leave the allocator, so that the caller may use their memory (in every layer) once the stream
+ * has passed the call: each one in use moves, lowest id first, to the free page of lowest rank outside (its filled slots, and its
+ * bounds where a file has them), and every file's table with it, of waiting files too.  SYM_ENOSPC, nothing changed, if there is no
+ * room; SYM_EINVAL if a page is withdrawn already.  sym_pool_return gives pages back, all of them withdrawn before (else SYM_EINVAL);
+ * withdrawn pages are not among the free ones.  Not to be recorded into a graph.                                 */
+int     sym_pool_withdraw(sym_ctx* ctx, int64_t first, int64_t n, void* stream);
+int     sym_pool_return(sym_ctx* ctx, int64_t first, int64_t n);
+int64_t sym_pool_withdrawn(sym_ctx* ctx);
+/* The page copies of the last of these calls, (source page, destination page, filled slots) triples in order.  Returns the
+ * number of copies; writes at most cap of them (out may be NULL).                                              */
+int64_t sym_last_copies(sym_ctx* ctx, int32_t* out, int64_t cap);
+
 /* Kernel-level entry without the allocator: attention only, over page tables the caller
  * supplies.  K/V of every token (new ones included) must already be in the pool.
  * page_table_flat: host int32, LIP b's page ids at [pt_offsets[b], pt_offsets[b+1]);
@@ -515,10 +586,12 @@ int     sym_sched_state(sym_sched* s, double* rate_per_us, double* target_batch,
 
 /* ---- measurement ------------------------------------------------------------------- */
 /* Kernel ids for sym_profile_read. */
-#define SYM_K_PROLOGUE 0   /* descriptor copy + copy-on-write copies + KV append, one launch; rope, rotated appends, bounds */
+#define SYM_K_PROLOGUE 0   /* descriptor copy + copy-on-write copies + KV append, one launch; rope, rotated appends, bounds;
+                              both launches of sym_beam_select                                */
 #define SYM_K_ATTN     1   /* attention over the page tables: decode ranges + MFMA tiles; scores, choice and attention of a sparse pred */
 #define SYM_K_MERGE    2   /* merge of the partial results of ranges that were cut           */
-#define SYM_K_MOVE     3   /* token copies of sym_kv_extract / sym_kv_merge                  */
+#define SYM_K_MOVE     3   /* token copies of sym_kv_extract / sym_kv_merge; page copies of sym_kv_fork_batch,
+                              sym_kv_reorder and sym_pool_withdraw; rows of sym_beam_states   */
 #define SYM_K_SWAP     4   /* page copies of sym_kv_offload / sym_kv_restore                 */
 #define SYM_K_COUNT    5
 /* sym_profile_enable(mask): bit k (k < 8) of mask set = launches of kernel id k are bracketed by

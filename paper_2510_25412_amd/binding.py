@@ -12,7 +12,8 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("SYMPHONY_KV_LIB") or os.path.join(_HERE, "libsymphony_kv.so")
 
 SYM_OK, SYM_EINVAL, SYM_EBADF, SYM_ENOSPC, SYM_ENOENT, SYM_EEXIST, SYM_EBUSY, SYM_EHIP = 0, -1, -2, -3, -4, -5, -6, -7
-SYM_F32, SYM_BF16 = 0, 1
+SYM_F32, SYM_BF16, SYM_F16 = 0, 1, 2
+LOGIT_TYPES = {"torch.float32": SYM_F32, "torch.bfloat16": SYM_BF16, "torch.float16": SYM_F16}
 ROPE_LAYOUTS = {"halves": 0, "interleaved": 1}
 K_PROLOGUE, K_ATTN, K_MERGE, K_MOVE, K_SWAP = 0, 1, 2, 3, 4
 
@@ -50,6 +51,16 @@ class SymRope(C.Structure):
 class SymSparse(C.Structure):
     _fields_ = [("budget", C.c_int32), ("first", C.c_int32), ("last", C.c_int32), ("dense_layers", C.c_int32),
                 ("rope", C.POINTER(SymRope)), ("positions", C.c_void_p)]
+
+
+class SymBeamStep(C.Structure):
+    _fields_ = [("n_groups", C.c_int32), ("n_best", C.c_int32), ("beams", C.c_void_p), ("vocab", C.c_int32), ("dtype", C.c_int32),
+                ("logits", C.c_void_p), ("logits_stride", C.c_int64), ("scores", C.c_void_p), ("allowed", C.c_void_p), ("allowed_stride", C.c_int64),
+                ("best_scores", C.c_void_p), ("best_beams", C.c_void_p), ("best_tokens", C.c_void_p), ("scratch", C.c_void_p), ("scratch_bytes", C.c_int64)]
+
+
+class SymBeamState(C.Structure):
+    _fields_ = [("dst", C.c_void_p), ("src", C.c_void_p), ("outer", C.c_int64), ("outer_stride", C.c_int64), ("row_stride", C.c_int64), ("row_bytes", C.c_int64)]
 
 
 class SymError(RuntimeError):
@@ -100,6 +111,16 @@ _SIGNATURES = {
     "sym_pred_sparse": (C.c_int, [C.c_void_p, C.c_int32, _I32P, _I32P, C.POINTER(SymSparse)] + [C.c_void_p] * 6),
     "sym_pred_begin_sparse": (C.c_int, [C.c_void_p, C.c_int32, _I32P, _I32P, C.POINTER(SymSparse), C.c_void_p]),
     "sym_pred_layer_sparse": (C.c_int, [C.c_void_p, C.c_int32] + [C.c_void_p] * 6),
+    "sym_beam_scratch_bytes": (C.c_int64, [C.c_int32, _I32P, C.c_int32, C.c_int32]),
+    "sym_beam_select": (C.c_int, [C.c_void_p, C.POINTER(SymBeamStep), C.c_void_p]),
+    "sym_beam_states": (C.c_int, [C.c_void_p, C.c_int32, _I32P, C.c_void_p, C.c_int32, C.POINTER(SymBeamState), C.c_void_p]),
+    "sym_kv_fork_batch": (C.c_int, [C.c_void_p, C.c_int32, _I32P, C.c_int32, _I32P, C.c_void_p]),
+    "sym_kv_reorder": (C.c_int, [C.c_void_p, C.c_int32, _I32P, _I32P, C.c_int32, C.c_void_p]),
+    "sym_kv_remove_batch": (C.c_int, [C.c_void_p, C.c_int32, _I32P]),
+    "sym_pool_withdraw": (C.c_int, [C.c_void_p, C.c_int64, C.c_int64, C.c_void_p]),
+    "sym_pool_return": (C.c_int, [C.c_void_p, C.c_int64, C.c_int64]),
+    "sym_pool_withdrawn": (C.c_int64, [C.c_void_p]),
+    "sym_last_copies": (C.c_int64, [C.c_void_p, _I32P, C.c_int64]),
     "sym_kv_pages": (C.c_int64, [C.c_void_p, C.c_int32, _I32P, C.c_int64]),
     "sym_page_refcount": (C.c_int32, [C.c_void_p, C.c_int32]),
     "sym_free_pages": (C.c_int64, [C.c_void_p]),
@@ -243,6 +264,42 @@ def make_sparse(budget, first=1, last=1, rope=None, positions=None, dense_layers
     s = SymSparse(budget, first, last, 1 if dense_layers else 0, C.pointer(rope) if rope is not None else None, _positions(positions))
     s._keep = (rope, positions)
     return s
+
+
+def beam_scratch_bytes(beams, vocab, n_best):
+    """Scratch of beam_select for requests of beams[i] rows each."""
+    b_a, b_p = _i32(beams)
+    n = _load_by_address().sym_beam_scratch_bytes(len(b_a), b_p, vocab, n_best)
+    if n < 0:
+        raise SymError(n, "sym_beam_scratch_bytes: bad argument")
+    return n
+
+
+def make_states(arrays):
+    """Arrays whose rows follow the beams (struct sym_beam_state of the header): (destination, source, dimension of the rows) each, the
+    same tensor twice to move in place.  Kept alive by the plan."""
+    plan = (SymBeamState * max(len(arrays), 1))()
+    for s, (dst, src, dim) in zip(plan, arrays):
+        if dst.shape != src.shape or dst.stride() != src.stride() or dst.dtype != src.dtype:
+            raise ValueError(f"states of shapes {tuple(dst.shape)} and {tuple(src.shape)}, or of different strides or types")
+        es, shape, stride = dst.element_size(), list(dst.shape), list(dst.stride())
+        inner = 1
+        for n, step in zip(shape[:dim:-1], stride[:dim:-1]):
+            if n > 1 and step != inner:
+                raise ValueError("what lies behind the rows' dimension must be contiguous")
+            inner *= n
+        outer, outer_stride = 1, 0
+        for n, step in zip(shape[:dim][::-1], stride[:dim][::-1]):      # the dimensions before it, as one
+            if n > 1 and outer > 1 and step != outer * outer_stride:
+                raise ValueError("the dimensions before the rows' must be one stretch")
+            outer_stride = step if outer == 1 else outer_stride
+            outer *= n
+        s.dst, s.src, s.outer, s.outer_stride, s.row_stride, s.row_bytes = dst.data_ptr(), src.data_ptr(), outer, outer_stride * es, stride[dim] * es, inner * es
+    rows = {a[0].shape[a[2]] for a in arrays}
+    if len(rows) > 1:
+        raise ValueError(f"states of {sorted(rows)} rows")
+    plan._n, plan._rows, plan._keep = len(arrays), rows.pop() if rows else None, list(arrays)
+    return plan
 
 
 def bounds_bytes(cfg):
@@ -457,6 +514,75 @@ class Context:
 
     def pred_layer_sparse(self, layer, q, k_new, v_new, out, picked=None, stream=None):
         self._chk(self.lib.sym_pred_layer_sparse(self.h, layer, _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(out), _ptr(picked), stream))
+
+    # ---- beams ----
+    def beam_select(self, beams, n_best, logits, scores, best_scores, best_beams, best_tokens, scratch, allowed=None, stream=None):
+        """beams: rows of each request.  logits [rows, vocab] (rows may lie apart), scores [rows] float32, allowed: int32 words [rows, ...] of bits or
+        None; best_*: [requests, n_best]; scratch: a tensor of beam_scratch_bytes().  All on the device but beams."""
+        b_a, b_p = _i32(beams)
+        (rows, vocab), groups = logits.shape, len(b_a)
+        if int(b_a.sum()) != rows or vocab > 1 and logits.stride(1) != 1:
+            raise ValueError(f"logits of shape {tuple(logits.shape)} for {int(b_a.sum())} beams, each row contiguous")
+        for t, n, size in ((scores, rows, 4), (best_scores, groups * n_best, 4), (best_beams, groups * n_best, 4), (best_tokens, groups * n_best, 4)):
+            if t.numel() != n or t.element_size() != size:
+                raise ValueError(f"{tuple(t.shape)} of {t.dtype} for {n} values of 4 bytes")
+        if not (scores.is_floating_point() and best_scores.is_floating_point()) or best_beams.is_floating_point() or best_tokens.is_floating_point():
+            raise TypeError("scores are float32, beams and tokens int32")
+        kind = LOGIT_TYPES.get(str(logits.dtype))
+        if kind is None:
+            raise TypeError(f"logits of {logits.dtype}")
+        a_ptr, a_stride = None, 0
+        if allowed is not None:
+            if allowed.element_size() != 4 or allowed.is_floating_point() or allowed.dim() != 2 or allowed.shape[0] != rows or allowed.shape[1] * 32 < vocab or \
+                    allowed.shape[1] > 1 and allowed.stride(1) != 1:
+                raise ValueError(f"allowed tokens: int32 words [{rows}, {(vocab + 31) // 32}], got {tuple(allowed.shape)} of {allowed.dtype}")
+            a_ptr, a_stride = allowed.data_ptr(), allowed.stride(0) if rows > 1 else 0
+        step = SymBeamStep(groups, n_best, b_p, vocab, kind, logits.data_ptr(), logits.stride(0) if rows > 1 else 0, _ptr(scores), a_ptr, a_stride,
+                           _ptr(best_scores), _ptr(best_beams), _ptr(best_tokens), _ptr(scratch), scratch.numel() * scratch.element_size())
+        rc = self.lib.sym_beam_select(self.h, C.byref(step), stream)
+        if rc < 0:
+            self._chk(rc)
+
+    def beam_states(self, beams, parents, states, stream=None):
+        """Rows of the arrays of make_states() after their beams.  parents: int32 [rows] on the device, index within the request; -1: the row stays."""
+        b_a, b_p = _i32(beams)
+        rows = int(b_a.sum())
+        if states._rows is not None and states._rows != rows or parents.numel() != rows:
+            raise ValueError(f"{rows} beams, states of {states._rows} rows, {parents.numel()} parents")
+        rc = self._fn.sym_beam_states(self.h, len(b_a), b_p, _positions(parents), states._n, states, stream)
+        if rc < 0:
+            self._chk(rc)
+
+    def kv_fork_batch(self, parents, own_last=False, stream=None):
+        """Forks of the files `parents` (each may be named often): int32 array of new handles."""
+        p_a, p_p = _i32(parents)
+        out = np.empty(len(p_a), np.int32)
+        self._chk(self._fn.sym_kv_fork_batch(self.h, len(p_a), p_p, 1 if own_last else 0, out.ctypes.data, stream))
+        return out
+
+    def kv_reorder(self, kv, sources, own_last=False, stream=None):
+        """File kv[i] takes over what file kv[sources[i]] holds."""
+        kv_a, s_a, kv_p, s_p = _batch(kv, sources)
+        self._chk(self._fn.sym_kv_reorder(self.h, len(kv_a), kv_p, s_p, 1 if own_last else 0, stream))
+
+    def kv_remove_batch(self, kv):
+        kv_a, kv_p = _i32(kv)
+        self._chk(self._fn.sym_kv_remove_batch(self.h, len(kv_a), kv_p))
+
+    def pool_withdraw(self, first, n, stream=None):
+        self._chk(self.lib.sym_pool_withdraw(self.h, first, n, stream))
+
+    def pool_return(self, first, n):
+        self._chk(self.lib.sym_pool_return(self.h, first, n))
+
+    def pool_withdrawn(self):
+        return self._chk(self.lib.sym_pool_withdrawn(self.h))
+
+    def last_copies(self):
+        n = self._chk(self._fn.sym_last_copies(self.h, None, 0))
+        out = np.empty((n, 3), np.int32)
+        self._chk(self._fn.sym_last_copies(self.h, out.ctypes.data, n))
+        return out
 
     def test_fail_staging(self, count):
         self._chk(self.lib.sym_test_fail_staging(self.h, count))

@@ -1,0 +1,87 @@
+// Argument blocks and launch functions of the kernels for beams: choices, state rows (beam.hip) and page copies (pages.hip).
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cstdint>
+
+namespace symkv {
+
+constexpr int kBeamsMost = 64;         // rows of a group
+constexpr int kBestMost = 128;         // choices of a group
+constexpr int kGroupsAtOnce = 512;     // groups of a launch: their first rows travel with its arguments (1 KB)
+struct GroupRows {
+  int32_t base;                        // row of the launch's first group
+  uint16_t first[kGroupsAtOnce + 1];   // rows before each group, from there on
+};
+
+constexpr int kOctet = 8;              // logits that a lane takes at a time
+constexpr int kMostLists = 256;        // lists of a group that its choice starts from: a thread each
+struct SelectArgs {
+  const void* logits;
+  int64_t stride;                      // elements from row to row
+  const float* scores;
+  const uint8_t* allowed;              // or null
+  int64_t allowed_stride;              // bytes from row to row
+  float* best_scores;
+  int32_t* best_beams;
+  int32_t* best_tokens;
+  // [rows][parts]: largest logit of a part (or one not far below), sum of exponentials from there, [n_best] best logits and their tokens
+  double* sums;
+  float* refs;
+  float* values;
+  int32_t* tokens;
+  int32_t rows, vocab, n_best;
+  int32_t parts, part_octets;          // wavefronts of a row, octets of each
+};
+
+// How a row is cut: parts, octets of a part.
+struct SelectCut {
+  int32_t parts, part_octets;
+};
+constexpr int kSelectWaves = 4096;
+inline SelectCut select_cut(int64_t rows, int32_t most_beams, int32_t vocab) {
+  const int64_t octets = (vocab + kOctet - 1) / kOctet;
+  int64_t parts = std::min<int64_t>((kSelectWaves + rows - 1) / rows, kMostLists / most_beams);
+  parts = std::max<int64_t>(1, std::min<int64_t>(parts, (octets + 255) / 256));
+  const int64_t per = ((octets + parts - 1) / parts + 63) / 64 * 64;
+  return SelectCut{(int32_t)((octets + per - 1) / per), (int32_t)per};
+}
+
+constexpr int kStatesAtOnce = 8;       // arrays of a launch
+struct StateArray {
+  uint8_t* dst;
+  const uint8_t* src;
+  int64_t outer_stride, row_stride, row_bytes;
+  uint32_t chunks;                     // workgroups of a group's rows
+  uint32_t end;                        // workgroups of this array and those before it
+};
+struct StatesArgs {
+  StateArray array[kStatesAtOnce];
+  const int32_t* parents;
+  int32_t n_arrays, n_groups;
+};
+constexpr int kStateUnit = 16;         // bytes of each row that a thread moves
+constexpr int kStateThreads = 256;
+
+constexpr int kArgCopies = 256;        // copies that travel with the arguments (3 KB of the 4 KB that a launch may have)
+struct CopyArgs {
+  uint8_t* pool;
+  int64_t page_bytes, layer_bytes;
+  uint8_t* bounds;                     // or null
+  int64_t layer_bounds;
+  const int32_t* list;                 // (source, destination, slots | 1 << 8: bounds too): host (by_args), or pinned
+  int32_t n_copies, n_layers, Hkv;
+  int32_t by_args;
+  hipEvent_t done;
+};
+
+// Weak: see sparse.hpp.
+#define SYMKV_LAUNCH __attribute__((weak))
+SYMKV_LAUNCH hipError_t launch_select_rows(const SelectArgs& a, int dtype, hipStream_t st);
+SYMKV_LAUNCH hipError_t launch_select_best(const SelectArgs& a, const GroupRows& g, int32_t group0, int32_t n_groups, hipStream_t st);
+SYMKV_LAUNCH hipError_t launch_states(const StatesArgs& a, const GroupRows& g, int32_t most_beams, hipStream_t st);
+SYMKV_LAUNCH hipError_t launch_copies(const CopyArgs& a, hipStream_t st);
+#undef SYMKV_LAUNCH
+
+}  // namespace symkv

@@ -13,6 +13,7 @@
 #include <vector>
 
 #include "../../include/symphony_kv.h"
+#include "beam.hpp"
 #include "desc.hpp"
 #include "kernels.hpp"
 #include "kvfs.hpp"
@@ -120,6 +121,7 @@ struct sym_ctx {
   AppendPlan plan;
   GatherPlan gplan;
   SwapPlan splan;
+  CopyPlan cplan;
   sym_rope rope_of = {};                           // the rope that `rope` is the table of: its 64 powers take longer than a small launch
   RopeTable rope = {};
   bool rope_set = false;
@@ -666,6 +668,32 @@ int pred_batch_locked(sym_ctx* c, int32_t n_lips, const sym_kv* kv, const int32_
   c->host_ns_plan += ns(t_planned - t_begin) - pb.wait_ns;
   c->host_ns_pred += ns(t_end - t_begin) - pb.wait_ns;
   return rc;
+}
+
+// Carries out c->cplan in every layer.
+constexpr int64_t kCopyChunk = 32768;                                 // copies per launch
+int64_t copy_stage_words(int64_t copies) { return copies > kArgCopies ? 3 * std::min(copies, kCopyChunk) : 0; }
+int64_t layer_bounds(const sym_ctx* c);
+int run_copies(sym_ctx* c, hipStream_t st) {
+  const int64_t n = (int64_t)c->cplan.copies.size() / 3;
+  for (int64_t off = 0; off < n; off += kCopyChunk) {
+    const int64_t cnt = std::min(kCopyChunk, n - off);
+    const int32_t* list = c->cplan.copies.data() + 3 * off;
+    const bool by_args = cnt <= kArgCopies;
+    int si = -1, rc;
+    if (!by_args) {
+      if ((rc = stage_acquire(c, 3 * cnt, &si))) return rc;
+      copy_bytes(c->stage[si], list, (size_t)cnt * 12);
+      list = c->stage[si];
+    }
+    const StageDone done(c, si);
+    const CopyArgs a{(uint8_t*)c->cfg.pool, c->page_bytes, c->layer_bytes, c->bounds, layer_bounds(c), list, (int32_t)cnt, c->n_layers, c->cfg.n_kv_heads, by_args ? 1 : 0, done.event()};
+    Timed t(c, SYM_K_MOVE, st);
+    const hipError_t e = launch_copies(a, st);
+    if (e != hipSuccess) return fail_hip(c, e, "copy launch");
+    if ((rc = done.launched(st))) return rc;
+  }
+  return SYM_OK;
 }
 
 // ---- rotary positions, page bounds, sparse preds ------------------------------------------------------------------------------
@@ -1797,6 +1825,289 @@ int sym_pred_sparse(sym_ctx* c, int32_t n_lips, const sym_kv* kv, const int32_t*
     if (rc) c->pred.open = c->pred.sparse.on = false;
     return rc;
   });
+}
+
+// ---- beams ----------------------------------------------------------------------------------------------------------------------
+
+namespace {
+constexpr int32_t kGroupsMost = 1 << 16;
+// Rows of all groups and of the largest, or a negative status.
+int64_t count_rows(int32_t n_groups, const int32_t* beams, int32_t* most) {
+  if (n_groups < 0 || n_groups > kGroupsMost || (n_groups > 0 && !beams)) return SYM_EINVAL;
+  int64_t rows = 0;
+  *most = 0;
+  for (int32_t i = 0; i < n_groups; ++i) {
+    if (beams[i] < 1 || beams[i] > kBeamsMost) return SYM_EINVAL;
+    rows += beams[i];
+    *most = std::max(*most, beams[i]);
+  }
+  return rows;
+}
+// The first rows of the groups from g0 on, as many as go into a launch.
+int32_t group_rows(int32_t n_groups, const int32_t* beams, int32_t g0, int32_t row0, GroupRows* g) {
+  const int32_t n = std::min(kGroupsAtOnce, n_groups - g0);
+  g->base = row0;
+  g->first[0] = 0;
+  for (int32_t i = 0; i < n; ++i) g->first[i + 1] = (uint16_t)(g->first[i] + beams[g0 + i]);
+  return n;
+}
+int64_t select_scratch(int64_t rows, int32_t most, int32_t vocab, int32_t n_best) {
+  const int64_t lists = rows * select_cut(rows, most, vocab).parts;
+  return align_up(lists * 8, 16) + align_up(lists * 4, 16) + 2 * align_up(lists * n_best * 4, 16);
+}
+static_assert(kBeamsMost == SYM_BEAMS_MOST && kBestMost == SYM_BEST_MOST, "the header's limits");
+constexpr int64_t kStateBlocks = 1 << 22;              // workgroups of a launch
+}  // namespace
+
+int64_t sym_beam_scratch_bytes(int32_t n_groups, const int32_t* beams, int32_t vocab, int32_t n_best) {
+  int32_t most;
+  const int64_t rows = count_rows(n_groups, beams, &most);
+  if (rows < 0 || vocab < 1 || vocab > (1 << 24) || n_best < 1 || n_best > kBestMost) return SYM_EINVAL;
+  return rows == 0 ? 0 : select_scratch(rows, most, vocab, n_best);
+}
+
+int sym_beam_select(sym_ctx* c, const sym_beam_step* b, void* stream) {
+  if (!c || !b) return SYM_EINVAL;
+  std::lock_guard<std::mutex> lk(c->mu);
+  return guarded(c, [&]() -> int {
+    int32_t most;
+    const int64_t rows = count_rows(b->n_groups, b->beams, &most);
+    if (rows < 0) return fail(c, SYM_EINVAL, "beam_select: groups of 1 .. 64 beams, 65536 of them at most");
+    if (b->n_best < 1 || b->n_best > kBestMost) return fail(c, SYM_EINVAL, "beam_select: n_best must be 1 .. 128");
+    if (b->vocab < 1 || b->vocab > (1 << 24)) return fail(c, SYM_EINVAL, "beam_select: vocab must be 1 .. 2^24");
+    if (b->dtype != SYM_F32 && b->dtype != SYM_BF16 && b->dtype != SYM_F16) return fail(c, SYM_EINVAL, "beam_select: unknown type of logits");
+    const int64_t words = (b->vocab + 31) / 32, stride = b->logits_stride ? b->logits_stride : b->vocab, bit_stride = b->allowed_stride ? b->allowed_stride : words;
+    if (stride < b->vocab || stride > (int64_t)1 << 40) return fail(c, SYM_EINVAL, "beam_select: rows of logits overlap, or lie too far apart");
+    if (b->allowed && (bit_stride < words || bit_stride > (int64_t)1 << 40)) return fail(c, SYM_EINVAL, "beam_select: rows of allowed tokens overlap, or lie too far apart");
+    if (rows == 0) return SYM_OK;
+    const int64_t es = b->dtype == SYM_F32 ? 4 : 2, scratch = select_scratch(rows, most, b->vocab, b->n_best), out = (int64_t)b->n_groups * b->n_best * 4;
+    if (!b->logits || !b->scores || !b->best_scores || !b->best_beams || !b->best_tokens || !b->scratch) return fail(c, SYM_EINVAL, "beam_select: a pointer is missing");
+    if (!aligned(b->logits, (uintptr_t)es) || !aligned(b->scores, 4) || !aligned(b->allowed, 4) || !aligned(b->best_scores, 4) || !aligned(b->best_beams, 4) ||
+        !aligned(b->best_tokens, 4) || !aligned(b->scratch, 16))
+      return fail(c, SYM_EINVAL, "beam_select: an array is not aligned to its elements, or the scratch to 16 bytes");
+    if (b->scratch_bytes < scratch) return fail(c, SYM_ENOSPC, "beam_select: scratch too small (sym_beam_scratch_bytes)");
+    const struct {
+      const void* p;
+      int64_t n;
+      bool written;
+    } area[] = {{b->logits, ((rows - 1) * stride + b->vocab) * es, false}, {b->scores, rows * 4, false}, {b->allowed, b->allowed ? ((rows - 1) * bit_stride + words) * 4 : 0, false},
+                {b->best_scores, out, true}, {b->best_beams, out, true}, {b->best_tokens, out, true}, {b->scratch, scratch, true}};
+    for (const auto& x : area)
+      for (const auto& y : area)
+        if (&x != &y && x.written && x.n && y.n && overlap(x.p, x.n, y.p, y.n)) return fail(c, SYM_EINVAL, "beam_select: an output or the scratch overlaps something else");
+    if (c->cfg.device < 0) return fail(c, SYM_EINVAL, "host-only context");
+    if (!launch_select_rows || !stream_captures) return fail(c, SYM_EHIP, "beam_select: this build has no kernels");
+    const OnDevice on(c);
+    hipStream_t st = (hipStream_t)stream;
+    const SelectCut cut = select_cut(rows, most, b->vocab);
+    const int64_t lists = rows * cut.parts;
+    uint8_t* at = (uint8_t*)b->scratch;
+    const auto take = [&](int64_t bytes) {
+      uint8_t* p = at;
+      at += align_up(bytes, 16);
+      return p;
+    };
+    SelectArgs a{};
+    a.logits = b->logits;
+    a.stride = stride;
+    a.scores = b->scores;
+    a.allowed = (const uint8_t*)b->allowed;
+    a.allowed_stride = bit_stride * 4;
+    a.best_scores = b->best_scores;
+    a.best_beams = b->best_beams;
+    a.best_tokens = b->best_tokens;
+    a.sums = (double*)take(lists * 8);
+    a.refs = (float*)take(lists * 4);
+    a.values = (float*)take(lists * b->n_best * 4);
+    a.tokens = (int32_t*)take(lists * b->n_best * 4);
+    a.rows = (int32_t)rows;
+    a.vocab = b->vocab;
+    a.n_best = b->n_best;
+    a.parts = cut.parts;
+    a.part_octets = cut.part_octets;
+    const bool timed = c->prof_mask == 0 || !stream_captures(st);
+    {
+      Timed t(c, SYM_K_PROLOGUE, st, false, timed);
+      const hipError_t e = launch_select_rows(a, b->dtype, st);
+      if (e != hipSuccess) return fail_hip(c, e, "beam rows launch");
+    }
+    GroupRows g;
+    for (int32_t g0 = 0, row = 0; g0 < b->n_groups;) {
+      const int32_t n = group_rows(b->n_groups, b->beams, g0, row, &g);
+      Timed t(c, SYM_K_PROLOGUE, st, false, timed);
+      const hipError_t e = launch_select_best(a, g, g0, n, st);
+      if (e != hipSuccess) return fail_hip(c, e, "beam choice launch");
+      row += g.first[n];
+      g0 += n;
+    }
+    return SYM_OK;
+  });
+}
+
+int sym_beam_states(sym_ctx* c, int32_t n_groups, const int32_t* beams, const int32_t* parents, int32_t n_states, const sym_beam_state* states, void* stream) {
+  if (!c || n_states < 0 || n_states > SYM_STATES_MOST || (n_states > 0 && !states)) return SYM_EINVAL;
+  std::lock_guard<std::mutex> lk(c->mu);
+  return guarded(c, [&]() -> int {
+    int32_t most;
+    const int64_t rows = count_rows(n_groups, beams, &most);
+    if (rows < 0) return fail(c, SYM_EINVAL, "beam_states: groups of 1 .. 64 beams, 65536 of them at most");
+    struct Area {
+      const void* p;
+      int64_t n;
+      int32_t state;
+      bool written;
+    };
+    std::vector<Area> area;
+    area.reserve(2 * (size_t)n_states + 1);
+    if (rows > 0) area.push_back({parents, rows * 4, -1, false});
+    constexpr int64_t kFar = (int64_t)1 << 46;             // bytes of an array at most
+    for (int32_t i = 0; i < n_states; ++i) {
+      const sym_beam_state& s = states[i];
+      if (s.outer < 0 || s.row_bytes < 0 || (s.row_bytes > 0 && s.row_stride < s.row_bytes) || s.row_stride > kFar || s.outer > kFar)
+        return fail(c, SYM_EINVAL, "beam_states: rows overlap, or a size is negative");
+      if (rows == 0 || s.outer == 0 || s.row_bytes == 0) continue;
+      if (!s.dst || !s.src) return fail(c, SYM_EINVAL, "beam_states: a pointer is missing");
+      if (s.row_stride > kFar / rows) return fail(c, SYM_EINVAL, "beam_states: an array is too large");
+      const int64_t one = (rows - 1) * s.row_stride + s.row_bytes;
+      if (s.outer > 1 && (s.outer_stride < one || s.outer_stride > kFar / s.outer)) return fail(c, SYM_EINVAL, "beam_states: parts of an array overlap, or it is too large");
+      const int64_t bytes = s.outer > 1 ? (s.outer - 1) * s.outer_stride + one : one;
+      area.push_back({s.dst, bytes, i, true});
+      if (s.src != s.dst) area.push_back({s.src, bytes, i, false});
+    }
+    if (rows == 0 || area.size() == 1) return SYM_OK;
+    if (!parents || !aligned(parents, 4)) return fail(c, SYM_EINVAL, "beam_states: parents are missing or not aligned");
+    for (const Area& x : area)
+      for (const Area& y : area)
+        if (&x != &y && x.written && overlap(x.p, x.n, y.p, y.n)) return fail(c, SYM_EINVAL, "beam_states: an array that is written overlaps another one");
+    if (c->cfg.device < 0) return fail(c, SYM_EINVAL, "host-only context");
+    if (!launch_states || !stream_captures) return fail(c, SYM_EHIP, "beam_states: this build has no kernels");
+    const OnDevice on(c);
+    hipStream_t st = (hipStream_t)stream;
+    const bool timed = c->prof_mask == 0 || !stream_captures(st);
+    GroupRows g;
+    for (int32_t g0 = 0, row = 0; g0 < n_groups;) {
+      const int32_t n = group_rows(n_groups, beams, g0, row, &g);
+      StatesArgs a{};
+      a.parents = parents;
+      a.n_groups = n;
+      const auto launch = [&]() -> int {
+        if (a.n_arrays == 0) return SYM_OK;
+        Timed t(c, SYM_K_MOVE, st, false, timed);
+        const hipError_t e = launch_states(a, g, most, st);
+        a.n_arrays = 0;
+        return e == hipSuccess ? SYM_OK : fail_hip(c, e, "state rows launch");
+      };
+      int rc;
+      for (int32_t i = 0; i < n_states; ++i) {
+        const sym_beam_state& s = states[i];
+        if (s.outer == 0 || s.row_bytes == 0) continue;
+        // stretches of columns, then of the outer dimension, so that a launch has no more workgroups than it may
+        constexpr int64_t kSlice = kStateBlocks / kGroupsAtOnce * kStateThreads * kStateUnit - kStateThreads * kStateUnit;
+        for (int64_t col = 0; col < s.row_bytes; col += kSlice) {
+          const int64_t bytes = std::min(kSlice, s.row_bytes - col);
+          const int64_t chunks = (bytes / kStateUnit + bytes % kStateUnit + kStateThreads - 1) / kStateThreads;
+          const int64_t step = std::max<int64_t>(1, kStateBlocks / (chunks * n));
+          for (int64_t o = 0; o < s.outer; o += step) {
+            const int64_t blocks = std::min(step, s.outer - o) * chunks * n, before = a.n_arrays ? a.array[a.n_arrays - 1].end : 0;
+            if (a.n_arrays == kStatesAtOnce || before + blocks > 2 * kStateBlocks) {
+              if ((rc = launch())) return rc;
+            }
+            const int64_t first = a.n_arrays ? before : 0, off = o * s.outer_stride + col;
+            a.array[a.n_arrays++] = StateArray{(uint8_t*)s.dst + off, (const uint8_t*)s.src + off, s.outer_stride, s.row_stride, bytes, (uint32_t)chunks, (uint32_t)(first + blocks)};
+          }
+        }
+      }
+      if ((rc = launch())) return rc;
+      row += g.first[n];
+      g0 += n;
+    }
+    return SYM_OK;
+  });
+}
+
+int sym_kv_fork_batch(sym_ctx* c, int32_t n, const sym_kv* parents, int32_t own_last, sym_kv* out, void* stream) {
+  if (!c || n < 0 || (n > 0 && (!parents || !out))) return SYM_EINVAL;
+  std::lock_guard<std::mutex> lk(c->mu);
+  return guarded(c, [&]() -> int {
+    if (int busy = refuse_if_open(c, "kv_fork_batch")) return busy;
+    hipStream_t st = (hipStream_t)stream;
+    const bool copies = own_last && c->cfg.device >= 0;
+    int rc;
+    if (copies && (!launch_copies || (rc = refuse_capture(c, st, "kv_fork_batch")))) return launch_copies ? rc : fail(c, SYM_EHIP, "kv_fork_batch: this build has no kernels");
+    if (own_last && (rc = stage_reserve(c, copy_stage_words(n)))) return rc;      // before any state change
+    if ((rc = c->fs->fork_batch(n, parents, own_last != 0, out, &c->cplan, &c->err)) || !copies) return rc;
+    const OnDevice on(c);
+    return run_copies(c, st);
+  });
+}
+
+int sym_kv_reorder(sym_ctx* c, int32_t n, const sym_kv* kv, const int32_t* from, int32_t own_last, void* stream) {
+  if (!c || n < 0 || (n > 0 && (!kv || !from))) return SYM_EINVAL;
+  std::lock_guard<std::mutex> lk(c->mu);
+  return guarded(c, [&]() -> int {
+    if (int busy = refuse_if_open(c, "kv_reorder")) return busy;
+    hipStream_t st = (hipStream_t)stream;
+    const bool copies = own_last && c->cfg.device >= 0;
+    int rc;
+    if (copies && (!launch_copies || (rc = refuse_capture(c, st, "kv_reorder")))) return launch_copies ? rc : fail(c, SYM_EHIP, "kv_reorder: this build has no kernels");
+    if (own_last && (rc = stage_reserve(c, copy_stage_words(n)))) return rc;      // before any state change
+    if ((rc = c->fs->reorder(n, kv, from, own_last != 0, &c->cplan, &c->err)) || !copies) return rc;
+    const OnDevice on(c);
+    return run_copies(c, st);
+  });
+}
+
+int sym_kv_remove_batch(sym_ctx* c, int32_t n, const sym_kv* kv) {
+  if (!c || n < 0 || (n > 0 && !kv)) return SYM_EINVAL;
+  std::lock_guard<std::mutex> lk(c->mu);
+  return guarded(c, [&]() -> int {
+    if (int busy = refuse_if_open(c, "kv_remove_batch")) return busy;
+    return c->fs->remove_batch(n, kv, &c->err);
+  });
+}
+
+int sym_pool_withdraw(sym_ctx* c, int64_t first, int64_t n, void* stream) {
+  if (!c) return SYM_EINVAL;
+  std::lock_guard<std::mutex> lk(c->mu);
+  return guarded(c, [&]() -> int {
+    if (int busy = refuse_if_open(c, "pool_withdraw")) return busy;
+    hipStream_t st = (hipStream_t)stream;
+    const bool copies = c->cfg.device >= 0;
+    int rc;
+    if (copies && (!launch_copies || (rc = refuse_capture(c, st, "pool_withdraw")))) return launch_copies ? rc : fail(c, SYM_EHIP, "pool_withdraw: this build has no kernels");
+    const int64_t in_use = c->fs->n_pages() - c->fs->free_pages() - c->fs->withdrawn();
+    if ((rc = stage_reserve(c, copy_stage_words(std::max<int64_t>(0, std::min(n, in_use)))))) return rc;      // before any state change
+    if ((rc = c->fs->withdraw(first, n, &c->cplan, &c->err)) || !copies) return rc;
+    const OnDevice on(c);
+    return run_copies(c, st);
+  });
+}
+
+int sym_pool_return(sym_ctx* c, int64_t first, int64_t n) {
+  if (!c) return SYM_EINVAL;
+  std::lock_guard<std::mutex> lk(c->mu);
+  return guarded(c, [&]() -> int {
+    if (int busy = refuse_if_open(c, "pool_return")) return busy;
+    return c->fs->give_back(first, n, &c->err);
+  });
+}
+
+int64_t sym_pool_withdrawn(sym_ctx* c) {
+  if (!c) return SYM_EINVAL;
+  std::lock_guard<std::mutex> lk(c->mu);
+  return c->fs->withdrawn();
+}
+
+int64_t sym_last_copies(sym_ctx* c, int32_t* out, int64_t cap) {
+  if (!c || cap < 0) return SYM_EINVAL;
+  std::lock_guard<std::mutex> lk(c->mu);
+  const int64_t n = (int64_t)c->cplan.copies.size() / 3;
+  for (int64_t i = 0; out && i < std::min(n, cap); ++i) {
+    out[3 * i] = c->cplan.copies[(size_t)(3 * i)];
+    out[3 * i + 1] = c->cplan.copies[(size_t)(3 * i + 1)];
+    out[3 * i + 2] = c->cplan.copies[(size_t)(3 * i + 2)] & ~CopyPlan::kBounds;
+  }
+  return n;
 }
 
 int sym_test_fail_staging(sym_ctx* c, int32_t count) {

@@ -505,6 +505,217 @@ int Kvfs::restore(int32_t n, const int32_t* handles, SwapPlan* plan, std::string
   return SYM_OK;
 }
 
+// The file's partly filled last page, if others have it too, becomes a page of its own, to be copied.
+bool Kvfs::copy_last(int32_t id, CopyPlan* plan) {
+  KvFile& f = files_[id];
+  const int32_t r = (int32_t)(f.len % P_);
+  if (r == 0 || refcount_[f.pages.back()] < 2) return false;
+  const int32_t src = f.pages.back(), dst = alloc_page();
+  --refcount_[src];
+  f.pages.back() = dst;
+  ++cow_copies;
+  plan->copies.insert(plan->copies.end(), {src, dst, r});
+  return true;
+}
+
+int Kvfs::fork_batch(int32_t n, const int32_t* parents, bool own_last, int32_t* out, CopyPlan* plan, std::string* err) {
+  plan->copies.clear();
+  int64_t need = 0;
+  for (int32_t i = 0; i < n; ++i) {
+    const KvFile* f = file_of(parents[i]);
+    if (!f || f->waiting) {
+      if (err) *err = f ? "kv_fork_batch: file is offloaded" : "kv_fork_batch: bad file handle";
+      return f ? SYM_EBUSY : SYM_EBADF;
+    }
+    need += own_last && f->len % P_ != 0;       // the parent keeps the page, so every fork copies it
+  }
+  if (need > free_pages()) {
+    if (err) *err = "page pool exhausted";
+    return SYM_ENOSPC;
+  }
+  plan->copies.reserve(3 * (size_t)need);
+  for (int32_t i = 0; i < n; ++i) {
+    out[i] = fork(parents[i]);
+    if (own_last) copy_last(handle_file_[out[i]], plan);
+  }
+  return SYM_OK;
+}
+
+int Kvfs::reorder(int32_t n, const int32_t* handles, const int32_t* from, bool own_last, CopyPlan* plan, std::string* err) {
+  plan->copies.clear();
+  begin_marks();
+  for (int32_t i = 0; i < n; ++i) {
+    const KvFile* f = file_of(handles[i]);
+    if (!f || f->waiting) {
+      if (err) *err = f ? "kv_reorder: file is offloaded" : "kv_reorder: bad file handle";
+      return f ? SYM_EBUSY : SYM_EBADF;
+    }
+    if (from[i] < -1 || from[i] >= n) {
+      if (err) *err = "kv_reorder: a source outside the list";
+      return SYM_EINVAL;
+    }
+    if (!mark(handles[i])) {
+      if (err) *err = "kv_reorder: same file twice";
+      return SYM_EBUSY;
+    }
+  }
+  // What each taking file gets: the entries that it has already (beams share their prompt) stay, the others are kept aside, since the
+  // source may take something itself.
+  struct Take {
+    int32_t file;
+    int64_t len, bounded;
+    size_t same, tail, tail_n;
+  };
+  std::vector<Take> takes;
+  std::vector<int32_t> tails, freed;
+  size_t dropped = 0;
+  for (int32_t i = 0; i < n; ++i) {
+    if (from[i] < 0 || from[i] == i) continue;
+    KvFile& f = files_[handle_file_[handles[i]]];
+    const KvFile& s = files_[handle_file_[handles[from[i]]]];
+    const size_t both = std::min(f.pages.size(), s.pages.size());
+    const size_t same = (size_t)(std::mismatch(f.pages.begin(), f.pages.begin() + (ptrdiff_t)both, s.pages.begin()).first - f.pages.begin());
+    takes.push_back({handle_file_[handles[i]], s.len, s.bounded, same, tails.size(), s.pages.size() - same});
+    tails.insert(tails.end(), s.pages.begin() + (ptrdiff_t)same, s.pages.end());
+    f.pages.reserve(s.pages.size());
+    dropped += f.pages.size() - same;
+  }
+  freed.reserve(dropped);
+  plan->copies.reserve(3 * (size_t)n);
+  for (int32_t p : tails) ++refcount_[p];
+  for (const Take& t : takes) {
+    const std::vector<int32_t>& pages = files_[t.file].pages;
+    for (size_t k = t.same; k < pages.size(); ++k)
+      if (--refcount_[pages[k]] == 0) freed.push_back(pages[k]);
+  }
+  // The copies: of a page that several have, the last that is asked keeps it.
+  int64_t need = 0;
+  if (own_last) {
+    pending_.clear();
+    const auto ask = [&](int32_t last, int64_t len) {
+      if (len % P_ == 0) return;
+      int32_t& gone = pending_[last];
+      if ((int64_t)refcount_[last] - gone > 1) {
+        ++need;
+        ++gone;
+      }
+    };
+    for (const Take& t : takes) ask(t.tail_n ? tails[t.tail + t.tail_n - 1] : t.same ? files_[t.file].pages[t.same - 1] : -1, t.len);
+    for (int32_t i = 0; i < n; ++i) {
+      const KvFile& f = files_[handle_file_[handles[i]]];
+      if (from[i] < 0 || from[i] == i) ask(f.pages.empty() ? -1 : f.pages.back(), f.len);
+    }
+  }
+  if (need > free_pages() + (int64_t)freed.size()) {
+    for (const Take& t : takes)
+      for (size_t k = t.same; k < files_[t.file].pages.size(); ++k) ++refcount_[files_[t.file].pages[k]];
+    for (int32_t p : tails) --refcount_[p];
+    if (err) *err = "page pool exhausted";
+    return SYM_ENOSPC;
+  }
+  for (int32_t p : freed) free_ranks_.insert(rank_[p]);
+  for (const Take& t : takes) {
+    KvFile& f = files_[t.file];
+    f.pages.resize(t.same);
+    f.pages.insert(f.pages.end(), tails.begin() + (ptrdiff_t)t.tail, tails.begin() + (ptrdiff_t)(t.tail + t.tail_n));
+    f.len = t.len;
+    f.bounded = t.bounded;
+  }
+  if (own_last) {
+    for (const Take& t : takes) copy_last(t.file, plan);
+    for (int32_t i = 0; i < n; ++i)
+      if (from[i] < 0 || from[i] == i) copy_last(handle_file_[handles[i]], plan);
+  }
+  return SYM_OK;
+}
+
+int Kvfs::remove_batch(int32_t n, const int32_t* handles, std::string* err) {
+  begin_marks();
+  for (int32_t i = 0; i < n; ++i) {
+    if (!file_of(handles[i])) {
+      if (err) *err = "kv_remove_batch: bad file handle";
+      return SYM_EBADF;
+    }
+    if (!mark(handles[i])) {
+      if (err) *err = "kv_remove_batch: same file twice";
+      return SYM_EBUSY;
+    }
+  }
+  for (int32_t i = 0; i < n; ++i) drop_file(handle_file_[handles[i]]);
+  return SYM_OK;
+}
+
+int Kvfs::withdraw(int64_t first, int64_t n, CopyPlan* plan, std::string* err) {
+  plan->copies.clear();
+  if (first < 0 || n < 0 || first > n_pages_ || n > n_pages_ - first) {
+    if (err) *err = "pool_withdraw: pages outside the pool";
+    return SYM_EINVAL;
+  }
+  if (withdrawn_.empty()) withdrawn_.resize((size_t)n_pages_, 0);
+  int64_t used = 0;
+  for (int64_t p = first; p < first + n; ++p) {
+    if (withdrawn_[(size_t)p]) {
+      if (err) *err = "pool_withdraw: a page is withdrawn already";
+      return SYM_EINVAL;
+    }
+    used += refcount_[(size_t)p] > 0;
+  }
+  if (used > free_pages() - (n - used)) {
+    if (err) *err = "page pool exhausted";
+    return SYM_ENOSPC;
+  }
+  std::vector<int32_t> at((size_t)n, -1);        // place in the plan of every page that moves
+  plan->copies.reserve(3 * (size_t)used);
+  for (int64_t p = first; p < first + n; ++p) {
+    withdrawn_[(size_t)p] = 1;
+    if (!refcount_[(size_t)p]) free_ranks_.erase(rank_[(size_t)p]);
+  }
+  n_withdrawn_ += n;
+  for (int64_t p = first; p < first + n; ++p) {
+    if (!refcount_[(size_t)p]) continue;
+    const int32_t q = alloc_page();
+    refcount_[q] = refcount_[(size_t)p];
+    refcount_[(size_t)p] = 0;
+    at[(size_t)(p - first)] = (int32_t)plan->copies.size();
+    plan->copies.insert(plan->copies.end(), {(int32_t)p, q, 0});
+    const auto w = waiters_.find((int32_t)p);     // (entries of waiting files that reference it)
+    if (w != waiters_.end()) {
+      auto node = waiters_.extract(w);
+      node.key() = q;
+      waiters_.insert(std::move(node));
+    }
+  }
+  if (used == 0) return SYM_OK;
+  for (KvFile& f : files_)
+    for (size_t i = 0; i < f.pages.size(); ++i) {
+      const int64_t k = f.pages[i] - first;
+      if (k < 0 || k >= n) continue;
+      int32_t* c = plan->copies.data() + at[(size_t)k];
+      f.pages[i] = c[1];
+      const int32_t slots = (int32_t)std::min<int64_t>(P_, f.len - (int64_t)i * P_);      // the most that any file sees of the page
+      c[2] = std::max(c[2] & ~CopyPlan::kBounds, slots) | (c[2] & CopyPlan::kBounds) | ((int64_t)i < f.bounded ? CopyPlan::kBounds : 0);
+    }
+  return SYM_OK;
+}
+
+int Kvfs::give_back(int64_t first, int64_t n, std::string* err) {
+  if (first < 0 || n < 0 || first > n_pages_ || n > n_pages_ - first) {
+    if (err) *err = "pool_return: pages outside the pool";
+    return SYM_EINVAL;
+  }
+  for (int64_t p = first; p < first + n; ++p)
+    if (withdrawn_.empty() || !withdrawn_[(size_t)p]) {
+      if (err) *err = "pool_return: a page is not withdrawn";
+      return SYM_EINVAL;
+    }
+  for (int64_t p = first; p < first + n; ++p) {
+    withdrawn_[(size_t)p] = 0;
+    free_ranks_.insert(rank_[(size_t)p]);
+  }
+  n_withdrawn_ -= n;
+  return SYM_OK;
+}
+
 int64_t Kvfs::count_shared() const {
   int64_t c = 0;
   for (uint32_t r : refcount_) c += r > 1;

@@ -60,6 +60,12 @@ class RankSet {
     if ((w >> 6) < hint_) hint_ = w >> 6;
     ++count_;
   }
+  void erase(int32_t r) {                     // a rank that is in the set
+    const size_t w = (size_t)r >> 6;
+    l0_[w] &= ~(1ull << (r & 63));
+    if (!l0_[w]) l1_[w >> 6] &= ~(1ull << (w & 63));
+    --count_;
+  }
 
  private:
   std::vector<uint64_t> l0_, l1_;
@@ -118,6 +124,12 @@ struct SwapPlan {
   std::vector<int32_t> pairs;
 };
 
+// Page copies: (source page, destination page, filled slots) triples, destinations fresh pages.
+struct CopyPlan {
+  static constexpr int32_t kBounds = 1 << 8;   // beside the slots: the page's key bounds go with it
+  std::vector<int32_t> copies;
+};
+
 class Kvfs {
  public:
   Kvfs(int64_t n_pages, int32_t page_tokens, const int32_t* free_order);
@@ -165,6 +177,20 @@ class Kvfs {
   int offload(int32_t n, const int32_t* handles, SwapPlan* plan, std::string* err);
   int restore(int32_t n, const int32_t* handles, SwapPlan* plan, std::string* err);
   int waiting(int32_t h) const;                 // 1, 0 or a negative status
+
+  // fork_batch: out[i] = a fork of parents[i] (which may repeat).  reorder: file i takes over what file from[i] of the list holds before the call
+  // (-1 or i: it keeps its own); files distinct.  With `own_last`, every new or taking file (then every keeping one) whose
+  // partly filled last page is shared copies it now, in order, as its next append would; the copies go into the plan.
+  // remove_batch: several distinct files.  All or nothing.
+  int fork_batch(int32_t n, const int32_t* parents, bool own_last, int32_t* out, CopyPlan* plan, std::string* err);
+  int reorder(int32_t n, const int32_t* handles, const int32_t* from, bool own_last, CopyPlan* plan, std::string* err);
+  int remove_batch(int32_t n, const int32_t* handles, std::string* err);
+
+  // Pages [first, first + n) leave the allocator: those in use move, lowest id first, to the free pages of lowest rank elsewhere, every
+  // table entry with them.  give_back ends that for pages that were withdrawn.  All or nothing.
+  int withdraw(int64_t first, int64_t n, CopyPlan* plan, std::string* err);
+  int give_back(int64_t first, int64_t n, std::string* err);
+  int64_t withdrawn() const { return n_withdrawn_; }
   int64_t host_slots() const { return n_slots_; }   // host slots ever created (ids 0 .. n - 1)
   int64_t host_slots_in_use() const { return (int64_t)host_refs_.size(); }
 
@@ -180,6 +206,7 @@ class Kvfs {
 
  private:
   int32_t alloc_page();
+  bool copy_last(int32_t file_id, CopyPlan* plan);
   void release_entries(int32_t file_id, size_t keep);
   void drop_ref(int32_t page);
   int check_swap_args(int32_t n, const int32_t* handles, bool want_waiting, std::string* err);
@@ -207,6 +234,8 @@ class Kvfs {
   std::vector<int32_t> seen_files_;                 // scratch of check_swap_args
   std::vector<uint32_t> seen_in_;                   // file id -> the last list of handles that named it (mark)
   uint32_t batch_no_ = 0;
+  std::vector<uint8_t> withdrawn_;                  // per page, once any was
+  int64_t n_withdrawn_ = 0;
 };
 
 }  // namespace symkv

@@ -1,0 +1,70 @@
+// Page copies: forked and reordered files' last pages, pages that leave a range of the pool.
+#include "beam.hpp"
+#include "device.hpp"
+
+namespace symkv {
+
+namespace {
+
+template <int N>
+struct CopyList {
+  int32_t word[3 * N];
+};
+
+// The filled slots of pages, bit for bit.  A page is 4 * Hkv pieces (kv head, K or V, row half) of 16 slots of 128 bytes; the first r
+// slots of a piece lie together, so the 16-byte chunks of a copy are counted through, r * 8 to a piece.  Sources and destinations are
+// different pages.  Bound: HBM, read + write.
+constexpr int kCopyChunks = 8;         // chunks of a thread, all in flight
+template <bool BY_ARGS, int N>
+__global__ __launch_bounds__(256) void copy_kernel(CopyArgs a, CopyList<N> l) {
+  const int e = 3 * (int)blockIdx.y;
+  int src, dst, what;
+  if constexpr (BY_ARGS) {
+    src = l.word[e], dst = l.word[e + 1], what = l.word[e + 2];
+  } else {
+    src = sload(a.list + e), dst = sload(a.list + e + 1), what = sload(a.list + e + 2);
+  }
+  const uint32_t per = (uint32_t)(what & 0xff) * 8, total = per * (uint32_t)a.Hkv * 4;      // chunks of a piece, of the copy
+  uint8_t* pool = a.pool + (int64_t)blockIdx.z * a.layer_bytes;
+  const uint8_t* s = pool + (int64_t)src * a.page_bytes;
+  uint8_t* d = pool + (int64_t)dst * a.page_bytes;
+  const uint32_t first = blockIdx.x * (256 * kCopyChunks) + threadIdx.x;
+  const float inv = 1.0f / (float)per;
+  u32x4_t v[kCopyChunks];
+  uint32_t at[kCopyChunks];
+#pragma unroll
+  for (int u = 0; u < kCopyChunks; ++u) {
+    const uint32_t i = first + u * 256;
+    // i / per: with a half added, no quotient of an i below 2^21 is within its roundings of a whole number
+    const uint32_t piece = (uint32_t)(((float)i + 0.5f) * inv);
+    at[u] = piece * (kP * kHalfBytes) + (i - piece * per) * 16;
+    if (i < total) v[u] = *(const u32x4_t*)(s + at[u]);
+  }
+#pragma unroll
+  for (int u = 0; u < kCopyChunks; ++u)
+    if (first + u * 256 < total) *(u32x4_t*)(d + at[u]) = v[u];
+  if (blockIdx.x == 0 && (what >> 8) && a.bounds) {
+    uint8_t* b = a.bounds + (int64_t)blockIdx.z * a.layer_bounds;
+    const int64_t n = (int64_t)a.Hkv * 512;
+    for (int64_t i = threadIdx.x * 16; i < n; i += 256 * 16) *(u32x4_t*)(b + dst * n + i) = *(const u32x4_t*)(b + src * n + i);
+  }
+}
+
+}  // namespace
+
+template <int N>
+static hipError_t launch_listed(const CopyArgs& a, dim3 grid, hipStream_t st) {
+  CopyList<N> l = {};
+  std::copy(a.list, a.list + 3 * a.n_copies, l.word);
+  return launch_done(copy_kernel<true, N>, grid, dim3(256), st, a.done, a, l);
+}
+
+hipError_t launch_copies(const CopyArgs& a, hipStream_t st) {
+  if (a.n_copies <= 0) return hipSuccess;
+  if (a.page_bytes / 16 > (1 << 21) || (a.by_args && a.n_copies > kArgCopies)) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)((a.page_bytes / 16 + 256 * kCopyChunks - 1) / (256 * kCopyChunks)), (unsigned)a.n_copies, (unsigned)a.n_layers);
+  if (a.by_args) return a.n_copies <= 32 ? launch_listed<32>(a, grid, st) : launch_listed<kArgCopies>(a, grid, st);
+  return launch_done(copy_kernel<false, 1>, grid, dim3(256), st, a.done, a, CopyList<1>{});
+}
+
+}  // namespace symkv

@@ -1,0 +1,326 @@
+"""Host half of the beams' calls (CPU only): batched forks, reordered files, batched removal and withdrawn pages against the state model over
+random programs, with a shadow of what every slot of the pool holds; refusals that change nothing; arguments of the calls on device arrays."""
+import ctypes as C
+import random
+
+import numpy as np
+import pytest
+
+from oracle.beams import BeamFiles
+from oracle.kvfs_model import KVError
+from paper_2510_25412_amd import binding
+
+EINVAL, EBADF, ENOSPC, EBUSY, EHIP = binding.SYM_EINVAL, binding.SYM_EBADF, binding.SYM_ENOSPC, binding.SYM_EBUSY, binding.SYM_EHIP
+P = 16
+
+
+def host_ctx(n_pages=64, free_order=None, n_layers=1):
+    return binding.Context(binding.make_config(32, 8, 128, P, "bf16", n_pages, device=-1, free_order=free_order, n_layers=n_layers))
+
+
+def refused(code, fn, *args, **kw):
+    with pytest.raises(binding.SymError) as e:
+        fn(*args, **kw)
+    assert e.value.code == code, e.value
+
+
+def state(ctx, files):
+    return [(ctx.kv_len(f), ctx.kv_pages(f)) for f in files], ctx.free_pages(), [ctx.page_refcount(p) for p in range(ctx.cfg.n_pages)], ctx.pool_withdrawn()
+
+
+class Both:
+    """The library and the model side by side, with what every slot of the pool holds and every file should hold."""
+
+    def __init__(self, pages, seed):
+        self.r = random.Random(seed)
+        order = list(range(pages))
+        if seed % 2:
+            self.r.shuffle(order)
+        self.ctx, self.model = host_ctx(pages, order), BeamFiles(pages, P, order)
+        self.pages, self.slot, self.host, self.holds, self.token = pages, {}, {}, {}, 0
+
+    def both(self, lib, model):
+        """Runs both; returns what they return, or None where both refuse with the same code."""
+        try:
+            want, code = model(), 0
+        except KVError as e:
+            want, code = None, e.code
+        try:
+            got = lib()
+            assert code == 0, code
+        except binding.SymError as e:
+            assert e.code == code, (e, code)
+            return None
+        return got, want
+
+    def copy(self, copies):
+        got = [tuple(int(v) for v in c) for c in self.ctx.last_copies()]
+        assert got == copies
+        for s, d, n in copies:                       # one after the other, as a destination is never another one's source
+            for k in range(n):
+                self.slot[d, k] = self.slot.get((s, k))
+        assert not {d for _, d, _ in copies} & {s for s, _, _ in copies} and len({d for _, d, _ in copies}) == len(copies)
+
+    def check(self):
+        assert self.ctx.free_pages() == self.model.free_pages() and self.ctx.pool_withdrawn() == len(self.model.gone)
+        for h in self.holds:
+            pages = self.ctx.kv_pages(h)
+            assert pages == self.model.kv_pages(h) and self.ctx.kv_len(h) == self.model.kv_len(h) == len(self.holds[h])
+            assert not set(pages) & self.model.gone
+            at = [self.slot.get((pages[i // P], i % P)) if pages[i // P] >= 0 else self.host[-pages[i // P] - 1, i % P] for i in range(len(self.holds[h]))]
+            assert at == self.holds[h]
+        for p in range(self.pages):
+            assert self.ctx.page_refcount(p) == self.model.refcount[p]
+
+    def step(self):
+        r, live = self.r, list(self.holds)
+        awake = [h for h in live if not self.ctx.kv_waiting(h)]
+        some = r.sample(awake, min(len(awake), r.randint(1, 5)))
+        op = r.choice(["open", "append", "append", "fork", "fork_batch", "reorder", "reorder", "reorder", "remove", "truncate", "withdraw", "withdraw", "return", "offload", "restore"])
+        if op == "open" or not some:
+            h, g = self.both(lambda: self.ctx.kv_open(None), lambda: self.model.kv_open(None))
+            assert h == g
+            self.holds[h] = []
+        elif op == "append":
+            n = [r.choice([1, 1, 3, 16, 21]) for _ in some]
+            got = self.both(lambda: self.ctx.plan_append(some, n), lambda: self.model.append(list(zip(some, n))))
+            if got:
+                (cow, _), (cow_m, slots) = got
+                assert cow == cow_m
+                for s, d, k in cow:
+                    for i in range(k):
+                        self.slot[d, i] = self.slot.get((s, i))
+                for h, at in zip(some, slots):
+                    for page, k in at:
+                        self.token += 1
+                        self.slot[page, k] = self.token
+                        self.holds[h].append(self.token)
+        elif op in ("fork", "fork_batch"):
+            own, parents = r.random() < 0.6, [r.choice(some) for _ in range(r.randint(1, 6))]
+            got = self.both(lambda: self.ctx.kv_fork_batch(parents, own), lambda: self.model.kv_fork_batch(parents, own))
+            if got:
+                assert list(got[0]) == got[1][0]
+                for h, p in zip(got[0], parents):
+                    self.holds[int(h)] = list(self.holds[p])
+                self.copy(got[1][1])
+                if own:
+                    assert all(self.ctx.kv_len(h) % P == 0 or self.ctx.page_refcount(self.ctx.kv_pages(h)[-1]) == 1 for h in got[0])
+        elif op == "reorder":
+            own, src = r.random() < 0.6, [r.randint(-1, len(some) - 1) for _ in some]
+            got = self.both(lambda: self.ctx.kv_reorder(some, src, own), lambda: self.model.kv_reorder(some, src, own))
+            if got:
+                old = {h: self.holds[h] for h in some}
+                for h, s in zip(some, src):
+                    self.holds[h] = list(old[some[s]] if s >= 0 else old[h])
+                self.copy(got[1])
+                if own:
+                    assert all(self.ctx.kv_len(h) % P == 0 or self.ctx.page_refcount(self.ctx.kv_pages(h)[-1]) == 1 for h in some)
+        elif op == "remove" and len(live) > 8:
+            gone = r.sample(live, r.randint(1, 4))
+            self.both(lambda: self.ctx.kv_remove_batch(gone), lambda: self.model.kv_remove_batch(gone))
+            for h in gone:
+                del self.holds[h]
+        elif op == "truncate":
+            n = [r.randint(0, len(self.holds[h])) for h in some]
+            self.ctx.kv_truncate(some, n)
+            for h, k in zip(some, n):
+                self.model.kv_truncate(h, k)
+                del self.holds[h][k:]
+        elif op == "withdraw":
+            first = r.randint(0, self.pages - 1)
+            n = r.randint(0, min(self.pages - first, self.pages // 3))
+            got = self.both(lambda: self.ctx.pool_withdraw(first, n), lambda: self.model.pool_withdraw(first, n))
+            if got:
+                self.copy(got[1])
+                self.ranges = getattr(self, "ranges", []) + [(first, n)]
+        elif op == "return":
+            ranges = getattr(self, "ranges", [])
+            first, n = ranges.pop(r.randrange(len(ranges))) if ranges and r.random() < 0.8 else (r.randint(0, self.pages), r.randint(1, 5))
+            if self.both(lambda: self.ctx.pool_return(first, n), lambda: self.model.pool_return(first, n)) is None:
+                return
+            if (first, n) in ranges:
+                ranges.remove((first, n))
+            self.ranges = [x for x in ranges if all(p in self.model.gone for p in range(x[0], x[0] + x[1]))]
+        elif op == "offload":
+            self.ctx.kv_offload(some)
+            for p, s in self.model.kv_offload(some):
+                for k in range(P):
+                    self.host[s, k] = self.slot.get((p, k))
+        elif op == "restore":
+            wait = [h for h in live if self.ctx.kv_waiting(h)]
+            if wait:
+                got = self.both(lambda: self.ctx.kv_restore(wait), lambda: self.model.kv_restore(wait))
+                if got:
+                    for s, p in got[1]:
+                        for k in range(P):
+                            self.slot[p, k] = self.host[s, k]
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_random_programs_match_the_model(seed):
+    b = Both([24, 60, 200][seed % 3], seed)
+    for _ in range(250):
+        b.step()
+        b.check()
+
+
+def test_reorder_by_hand():
+    ctx = host_ctx(20)
+    f = [ctx.kv_open(None) for _ in range(4)]
+    ctx.plan_append(f, [20, 21, 22, 32])                      # pages 0 1, 2 3, 4 5, 6 7
+    ctx.kv_reorder(f, [1, 1, 0, 1], True)
+    # file 0 takes 1's, copied (page 3 goes on to be file 1's); file 2 takes 0's alone: no copy; file 3 takes 1's, copied
+    assert [ctx.kv_len(x) for x in f] == [21, 21, 20, 21]
+    assert ctx.last_copies().tolist() == [[3, 4, 5], [3, 5, 5]]      # pages 4 and 5 were file 2's and are free now
+    assert [ctx.kv_pages(x) for x in f] == [[2, 4], [2, 3], [0, 1], [2, 5]]
+    assert ctx.free_pages() == 20 - 6
+    ctx.kv_reorder(f, [-1, 1, 2, -1], True)
+    assert len(ctx.last_copies()) == 0
+
+
+def test_reorder_swaps_and_shares():
+    ctx = host_ctx(20)
+    a, b = ctx.kv_open("a"), ctx.kv_open(None)
+    ctx.plan_append([a, b], [5, 40])
+    ctx.kv_reorder([a, b], [1, 0])
+    assert ctx.kv_pages(a) == [1, 2, 3] and ctx.kv_pages(b) == [0] and ctx.kv_open("a") >= 0
+    c = ctx.kv_fork(b)                                        # page 0 shared with a file outside the list: the file that keeps it copies too
+    ctx.kv_reorder([b], [-1], True)
+    assert ctx.last_copies().tolist() == [[0, 4, 5]] and ctx.kv_pages(b) == [4] and ctx.kv_pages(c) == [0]
+
+
+def test_a_freed_page_may_hold_a_copy_where_nothing_else_is_free():
+    ctx = host_ctx(3)
+    f = [ctx.kv_open(None) for _ in range(3)]
+    ctx.plan_append(f, [5, 6, 7])
+    assert ctx.free_pages() == 0
+    ctx.kv_reorder(f, [2, 2, 2], True)
+    assert ctx.last_copies().tolist() == [[2, 0, 7], [2, 1, 7]]
+    # and not where the copies need more than is freed
+    ctx = host_ctx(4)
+    f = [ctx.kv_open(None) for _ in range(3)]
+    ctx.plan_append(f, [5, 32, 16])                           # page 0; 1, 2; 3
+    g = ctx.kv_fork(f[2])
+    before = state(ctx, f + [g])
+    refused(ENOSPC, ctx.kv_reorder, f, [-1, 1, 0], True)      # file 2's page stays with g: nowhere to copy page 0 to
+    assert state(ctx, f + [g]) == before
+    ctx.kv_reorder(f, [-1, 1, 0], False)
+    assert ctx.kv_pages(f[2]) == [0] and ctx.page_refcount(0) == 2
+
+
+def test_refusals_change_nothing():
+    ctx = host_ctx(12)
+    f = [ctx.kv_open(None) for _ in range(4)]
+    ctx.plan_append(f[:3], [20, 33, 16])
+    other = ctx.kv_open("named")
+    again = ctx.kv_open("named")
+    ctx.kv_offload([f[2]])
+    before = state(ctx, f)
+    for code, fn, args in [(EBADF, ctx.kv_reorder, ([f[0], 99], [0, 0], True)), (EBUSY, ctx.kv_reorder, ([f[0], f[2]], [0, 0], True)), (EBUSY, ctx.kv_reorder, ([f[0], f[0]], [0, 0], False)),
+                           (EBUSY, ctx.kv_reorder, ([other, again], [0, 0], False)), (EINVAL, ctx.kv_reorder, ([f[0], f[1]], [0, 2], True)), (EINVAL, ctx.kv_reorder, ([f[0], f[1]], [-2, 0], True)),
+                           (EBADF, ctx.kv_fork_batch, ([f[0], -1], False)), (EBUSY, ctx.kv_fork_batch, ([f[0], f[2]], True)), (ENOSPC, ctx.kv_fork_batch, ([f[0]] * 8, True)),
+                           (EBADF, ctx.kv_remove_batch, ([f[0], 99],)), (EBUSY, ctx.kv_remove_batch, ([f[0], f[1], f[0]],)), (EBUSY, ctx.kv_remove_batch, ([other, again],)),
+                           (EINVAL, ctx.pool_withdraw, (-1, 2)), (EINVAL, ctx.pool_withdraw, (0, -1)), (EINVAL, ctx.pool_withdraw, (0, 13)), (EINVAL, ctx.pool_withdraw, (13, 0)),
+                           (EINVAL, ctx.pool_withdraw, (1 << 62, 1 << 62)), (ENOSPC, ctx.pool_withdraw, (0, 12)), (EINVAL, ctx.pool_return, (0, 1)), (EINVAL, ctx.pool_return, (-1, 1)),
+                           (EINVAL, ctx.pool_return, (5, 1 << 62))]:
+        refused(code, fn, *args)
+        assert state(ctx, f) == before, (fn, args)
+    ctx.kv_reorder([], [], True)
+    ctx.kv_remove_batch([])
+    assert len(ctx.kv_fork_batch([], True)) == 0
+    ctx.pool_withdraw(12, 0)
+    ctx.pool_withdraw(10, 2)
+    refused(EINVAL, ctx.pool_withdraw, 9, 2)
+    refused(EINVAL, ctx.pool_return, 9, 2)
+    assert ctx.pool_withdrawn() == 2 and ctx.get_stats()["pages_free"] == ctx.free_pages()
+    ctx.pool_return(10, 1)
+    ctx.pool_return(11, 1)
+    assert state(ctx, f) == before
+    with pytest.raises(ValueError):
+        ctx.kv_reorder([f[0], f[1]], [0], True)
+
+
+@pytest.mark.parametrize("call", ["fork", "reorder", "withdraw"])
+def test_a_failed_reservation_changes_nothing(call):
+    ctx = host_ctx(40)
+    f = [ctx.kv_open(None) for _ in range(3)]
+    ctx.plan_append(f, [20, 21, 22])
+    before = state(ctx, f)
+    go = {"fork": lambda: ctx.kv_fork_batch(f, True), "reorder": lambda: ctx.kv_reorder(f, [1, 1, 1], True), "withdraw": lambda: ctx.pool_withdraw(0, 6)}[call]
+    ctx.test_fail_staging(1)
+    refused(EHIP, go)
+    assert state(ctx, f) == before
+    go()
+    assert state(ctx, f) != before
+
+
+def test_bounds_follow_a_withdrawn_page():
+    ctx = host_ctx(40)
+    ctx.lib.sym_bounds_attach(ctx.h, 1 << 20, binding.bounds_bytes(ctx.cfg))
+    f = ctx.kv_open(None)
+    ctx.plan_append([f], [40])
+    ctx.kv_bounds([f])
+    ctx.pool_withdraw(0, 20)
+    assert ctx.kv_pages(f) == [20, 21, 22] and ctx.kv_bounded(f) == 2 and ctx.last_copies().tolist() == [[0, 20, 16], [1, 21, 16], [2, 22, 8]]
+    g = ctx.kv_open(None)
+    ctx.kv_reorder([f, g], [-1, 0])
+    assert ctx.kv_bounded(g) == 2
+    ctx.kv_reorder([f, g], [-1, -1], True)
+    ctx.plan_append([g], [30])
+    ctx.kv_reorder([f, g], [-1, 0])
+    assert ctx.kv_bounded(g) == 2 and ctx.kv_len(g) == 40
+
+
+def test_scratch_of_a_choice():
+    assert binding.beam_scratch_bytes([], 100, 4) == 0
+    assert binding.beam_scratch_bytes([4], 32768, 8) > binding.beam_scratch_bytes([4], 100, 8) > 0
+    for beams, vocab, best in [([0], 10, 1), ([65], 10, 1), ([-1], 10, 1), ([4], 0, 1), ([4], (1 << 24) + 1, 1), ([4], 10, 0), ([4], 10, 129)]:
+        with pytest.raises(binding.SymError):
+            binding.beam_scratch_bytes(beams, vocab, best)
+
+
+def step_of(**kw):
+    """A well-formed step on addresses that a host-only context never follows."""
+    beams = np.array(kw.pop("beams", [4, 3]), np.int32)
+    d = dict(n_groups=len(beams), n_best=8, beams=beams.ctypes.data, vocab=1000, dtype=binding.SYM_BF16, logits=1 << 30, logits_stride=0, scores=1 << 28, allowed=1 << 27, allowed_stride=0,
+             best_scores=1 << 20, best_beams=1 << 21, best_tokens=1 << 22, scratch=1 << 40, scratch_bytes=1 << 30)
+    d.update(kw)
+    s = binding.SymBeamStep(**d)
+    s._keep = beams
+    return s
+
+
+def test_choice_arguments():
+    ctx = host_ctx()
+    call = lambda **kw: (ctx.lib.sym_beam_select(ctx.h, C.byref(step_of(**kw)), None), ctx.lib.sym_strerror(ctx.h).decode())  # noqa: E731
+    assert call() == (EINVAL, "host-only context")            # everything else was well-formed
+    assert call(allowed=None) == (EINVAL, "host-only context")
+    for kw in [dict(beams=[0, 1]), dict(beams=[65]), dict(n_groups=-1), dict(n_best=0), dict(n_best=129), dict(vocab=0), dict(vocab=(1 << 24) + 1), dict(dtype=3), dict(logits_stride=999),
+               dict(logits_stride=-1), dict(allowed_stride=31), dict(logits=None), dict(scores=None), dict(best_scores=None), dict(best_beams=None), dict(best_tokens=None), dict(scratch=None),
+               dict(logits=(1 << 30) + 1), dict(dtype=0, logits=(1 << 30) + 2), dict(scores=(1 << 28) + 2), dict(allowed=(1 << 27) + 1), dict(best_scores=(1 << 20) + 2),
+               dict(scratch=(1 << 40) + 8), dict(best_beams=(1 << 20) + 60), dict(best_tokens=1 << 28), dict(best_tokens=(1 << 30) + 7 * 2000 - 4), dict(scratch=(1 << 30) + 13984),
+               dict(best_scores=1 << 40), dict(best_scores=(1 << 27) + 7 * 128 - 4)]:
+        code, what = call(**kw)
+        assert code == EINVAL and what != "host-only context", (kw, what)
+    assert call(scratch_bytes=100)[0] == ENOSPC
+    assert call(best_tokens=(1 << 30) + 7 * 2000) == (EINVAL, "host-only context")      # right behind the logits
+    assert call(beams=[]) [0] == 0
+
+
+def test_state_arguments():
+    ctx = host_ctx()
+    beams = np.array([4, 3], np.int32)
+    good = dict(dst=1 << 30, src=1 << 30, outer=2, outer_stride=7000, row_stride=1000, row_bytes=1000)
+
+    def call(*states, parents=1 << 20, n=2):
+        plan = (binding.SymBeamState * max(len(states), 1))(*[binding.SymBeamState(**dict(good, **s)) for s in states])
+        return ctx.lib.sym_beam_states(ctx.h, n, beams.ctypes.data_as(C.POINTER(C.c_int32)), parents, len(states), plan, None), ctx.lib.sym_strerror(ctx.h).decode()
+
+    host_only = (EINVAL, "host-only context")
+    assert call({}) == host_only and call({}, dict(dst=1 << 31, src=(1 << 31) + 14000)) == host_only
+    for states, kw in [(({}, {}), {}), (({}, dict(dst=(1 << 30) + 13999, src=1 << 32)), {}), ((dict(src=(1 << 30) + 1),), {}), ((dict(row_bytes=1001),), {}), ((dict(outer_stride=6999),), {}),
+                       ((dict(outer=-1),), {}), ((dict(row_bytes=-1),), {}), ((dict(dst=None),), {}), ((dict(src=None),), {}), (({},), dict(parents=None)), (({},), dict(parents=(1 << 20) + 2)),
+                       (({},), dict(parents=(1 << 30) + 400)), ((dict(row_stride=1 << 50),), {}), ((dict(outer=1 << 40, outer_stride=1 << 40),), {})]:
+        code, what = call(*states, **kw)
+        assert code == EINVAL and what != "host-only context", (states, kw, what)
+    assert call(dict(row_bytes=0))[0] == 0 and call(dict(outer=0))[0] == 0 and call({}, n=0)[0] == 0 and call()[0] == 0
