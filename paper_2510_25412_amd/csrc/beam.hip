@@ -40,12 +40,27 @@ struct Larger {
 struct Smaller {
   __device__ __forceinline__ float operator()(float a, float b) const { return fminf(a, b); }
 };
+// The sum over the wavefront, in every lane: the same steps on both halves of a double.
+template <int CTRL>
+__device__ __forceinline__ double dpp(double x) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, x);
+  const uint32_t lo = __builtin_amdgcn_update_dpp((uint32_t)u, (uint32_t)u, CTRL, 0xf, 0xf, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp((uint32_t)(u >> 32), (uint32_t)(u >> 32), CTRL, 0xf, 0xf, false);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
 __device__ __forceinline__ double wave_sum(double x) {
-  for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d);
-  return x;
+  x += dpp<0xB1>(x);
+  x += dpp<0x4E>(x);
+  x += dpp<0x141>(x);
+  x += dpp<0x140>(x);
+  uint64_t u = __builtin_bit_cast(uint64_t, x);
+  const auto a = __builtin_amdgcn_permlane16_swap((uint32_t)u, (uint32_t)u, false, false), b = __builtin_amdgcn_permlane16_swap((uint32_t)(u >> 32), (uint32_t)(u >> 32), false, false);
+  x = __builtin_bit_cast(double, (uint64_t)b[0] << 32 | a[0]) + __builtin_bit_cast(double, (uint64_t)b[1] << 32 | a[1]);
+  u = __builtin_bit_cast(uint64_t, x);
+  const auto c = __builtin_amdgcn_permlane32_swap((uint32_t)u, (uint32_t)u, false, false), d = __builtin_amdgcn_permlane32_swap((uint32_t)(u >> 32), (uint32_t)(u >> 32), false, false);
+  return __builtin_bit_cast(double, (uint64_t)d[0] << 32 | c[0]) + __builtin_bit_cast(double, (uint64_t)d[1] << 32 | c[1]);
 }
 __device__ __forceinline__ int lanes_of(uint64_t b) { return __builtin_popcountll(b); }
-__device__ __forceinline__ int lanes_below(uint64_t b) { return __builtin_amdgcn_mbcnt_hi((uint32_t)(b >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)b, 0)); }
 
 // Floats as whole numbers of the same order, and back.
 __device__ __forceinline__ uint32_t key_of(float x) {
@@ -72,7 +87,7 @@ __device__ __forceinline__ float reached_by(const float (&x)[4], int K, int limi
   };
   if (!(low >= -FLT_MAX)) {
     low = -FLT_MAX;
-    if (count(low) <= limit) return low;
+    if (count(low) < K) return low;
   }
   uint32_t lo = __builtin_amdgcn_readfirstlane(key_of(low)), hi = __builtin_amdgcn_readfirstlane(key_of(top));
   while (hi > lo + 1 && count(of_key(lo)) > limit) {
@@ -149,9 +164,6 @@ struct LogitF32 {
 };
 
 constexpr int kAhead = 4;              // octets of a lane under way; a part's maxima are kept apart by their place among these
-constexpr int kFound = 256;            // logits that a wavefront sorts
-constexpr int kLists = 4 * 64;         // maxima of a part
-
 // One wavefront: a part of a row, 8 logits (an octet) to a lane at a time.  What it reads is counted from the row's start,
 // whatever the address, so equal rows give equal results.  TINY: rows of less than an octet, read one by one.
 template <typename E, bool MASKED, bool TINY>
@@ -191,101 +203,41 @@ struct Part {
   }
 };
 
-struct Found {
-  float value;
-  int token;
-};
-__device__ __forceinline__ bool before(float v, int t, float w, int u) { return v > w || (v == w && t < u); }
-
-// The K best of a part, where more than kFound logits reach the value that should have left about K: exactly the K-th largest is
-// found by halves over the whole part, then what is above it and of its equals the first.  Returns how many there are, in f.
-template <typename P>
-__device__ __attribute__((noinline)) int equals_too(const P& p, int K, float low, float top, Found* f) {
-  const int lane = threadIdx.x & 63;
-  const auto count = [&](auto reaches) {
-    int n = 0;
-    for (int o = p.first + lane; o - lane < p.end; o += 64) {
-      float x[8];
-      p.read(o, x);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) n += reaches(x[j]);
-    }
-    for (int d = 32; d; d >>= 1) n += __shfl_xor(n, d);
-    return n;
-  };
-  uint32_t lo = __builtin_amdgcn_readfirstlane(key_of(low)), hi = __builtin_amdgcn_readfirstlane(key_of(top)) + 1;
-  while (hi > lo + 1) {
-    const uint32_t mid = lo + (hi - lo) / 2;
-    const float t = of_key(mid);
-    if (__builtin_amdgcn_readfirstlane(count([t](float v) { return v >= t; })) >= K) lo = mid;
-    else hi = mid;
-  }
-  const float t = of_key(lo);
-  const int above = __builtin_amdgcn_readfirstlane(count([t](float v) { return v > t; }));
-  int n_above = 0, n_equal = 0;
-  for (int o = p.first + lane; o - lane < p.end; o += 64) {
-    float x[8];
-    p.read(o, x);
-    int equal_before = 0, above_before = 0, equal_all = 0, above_all = 0;      // of lower lanes, of the wavefront
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const uint64_t e = __ballot(x[j] == t), g = __ballot(x[j] > t);
-      equal_before += lanes_below(e);
-      equal_all += lanes_of(e);
-      above_before += lanes_below(g);
-      above_all += lanes_of(g);
-    }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      if (x[j] > t) f[n_above + above_before++] = Found{x[j], p.token(o, j)};
-      if (x[j] == t) {
-        const int at = above + n_equal + equal_before++;
-        if (at < K) f[at] = Found{t, p.token(o, j)};
-      }
-    }
-    n_above += above_all;
-    n_equal += equal_all;
-  }
-  return min(K, above + n_equal);
-}
-
+// The part of row `row` that begins at octet `first`.
 template <typename E, bool MASKED, bool TINY>
-__global__ __launch_bounds__(64) void select_rows_kernel(SelectArgs a) {
-  __shared__ Found found[kFound];
-  __shared__ uint16_t lists[kLists];
-  const int lane = threadIdx.x & 63, K = a.n_best;
-  const int row = (int)(blockIdx.x / (uint32_t)a.parts), part = (int)(blockIdx.x % (uint32_t)a.parts);
-  const int64_t list = blockIdx.x;
-  float* values = a.values + list * K;
-  int32_t* tokens = a.tokens + list * K;
-  const auto nothing = [&](int from) {
-    for (int k = from + lane; k < K; k += 64) {
-      values[k] = -INFINITY;
-      tokens[k] = -1;
-    }
-  };
-  const float score = a.scores[row];
-  if (!(fabsf(score) < INFINITY)) {                        // no beam lives here
-    if (lane == 0) {
-      a.sums[list] = 0.0;
-      a.refs[list] = -FLT_MAX;
-    }
-    nothing(0);
-    return;
-  }
+__device__ __forceinline__ Part<E, MASKED, TINY> part_of(const SelectArgs& a, int row, int first) {
   Part<E, MASKED, TINY> p;
   p.row = (const uint8_t*)a.logits + (int64_t)row * a.stride * E::kBytes;
   p.bits = MASKED ? a.allowed + (int64_t)row * a.allowed_stride : nullptr;
   p.vocab = a.vocab;
-  p.first = part * a.part_octets;
-  p.end = min(p.first + a.part_octets, (a.vocab + kOctet - 1) / kOctet);
+  p.first = first;
+  p.end = min(first + a.part_octets, (a.vocab + kOctet - 1) / kOctet);
+  return p;
+}
+
+// One pass over the logits.  Of every part: its normaliser's share, and for each lane (a list: octets 64 apart) the largest logit and the
+// octet where it is found first; the choice needs no more to know where it has to look again.
+template <typename E, bool MASKED, bool TINY>
+__global__ __launch_bounds__(64) void select_rows_kernel(SelectArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int row = (int)(blockIdx.x / (uint32_t)a.parts), part = (int)(blockIdx.x % (uint32_t)a.parts);
+  const int64_t at = blockIdx.x;
+  const float score = a.scores[row];
+  const auto p = part_of<E, MASKED, TINY>(a, row, part * a.part_octets);
+  if (p.first >= p.end || !(fabsf(score) < INFINITY)) {    // behind the row's end, or no beam lives here
+    a.most[at * 64 + lane] = -INFINITY;
+    if (lane == 0) {
+      a.sums[at] = 0.0;
+      a.refs[at] = -FLT_MAX;
+    }
+    return;
+  }
   const int whole = min(p.end, a.vocab / kOctet);          // octets that need no look at the row's end
 
-  // One pass: sums of exp(x - c), eight to a lane, and the maxima.  c is a lane's largest logit so far, so that no exponent is positive: a
-  // rounding of (x - c) log2 e then weighs at most 2^-24 of the sum, where with c some way below the largest it would weigh that many times as much.
-  float c = -FLT_MAX, s[8] = {}, most[kAhead];
-#pragma unroll
-  for (int d = 0; d < kAhead; ++d) most[d] = -INFINITY;
+  // Sums of exp(x - c), eight to a lane.  c is a lane's largest logit so far, so that no exponent is positive: a rounding of (x - c)
+  // log2 e then weighs at most 2^-24 of the sum, where with c some way below the largest it would weigh that many times as much.
+  float c = -FLT_MAX, s[8] = {}, most = -INFINITY;
+  int most_at = p.first + lane;
   const int batches = (p.end - p.first + 64 * kAhead - 1) / (64 * kAhead);
   typename E::Raw cur[kAhead], next[kAhead];
   uint32_t m[kAhead], m_next[kAhead], m_later[kAhead];
@@ -309,9 +261,10 @@ __global__ __launch_bounds__(64) void select_rows_kernel(SelectArgs a) {
       E::unpack(cur[d], x[d]);
       if (!plain) p.mask(x[d], octet(i, d), m[d]);
       const float top = fmaxf(fmaxf(fmaxf(x[d][0], x[d][1]), fmaxf(x[d][2], x[d][3])), fmaxf(fmaxf(x[d][4], x[d][5]), fmaxf(x[d][6], x[d][7])));
-      most[d] = fmaxf(most[d], top);
-      to = fmaxf(to, top);
+      most_at = top > most ? octet(i, d) : most_at;
+      most = fmaxf(most, top);
     }
+    to = fmaxf(to, most);
     const float by = __builtin_amdgcn_exp2f((c - to) * kLog2e);
     c = to;
 #pragma unroll
@@ -327,165 +280,171 @@ __global__ __launch_bounds__(64) void select_rows_kernel(SelectArgs a) {
       m_next[d] = m_later[d];
     }
   }
+  a.most[at * 64 + lane] = most;
+  a.most_at[at * 64 + lane] = most_at;
   const float ref = across<6>(c, Larger());
   const double sum = wave_sum((double)(((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]))) * (double)__builtin_amdgcn_exp2f((c - ref) * kLog2e));
   if (lane == 0) {
-    a.sums[list] = sum;
-    a.refs[list] = ref;
+    a.sums[at] = sum;
+    a.refs[at] = ref;
   }
-  if (!(sum > 0.0)) return nothing(0);                     // nothing allowed, or no distribution
-
-  // The K best: only lists (a lane, a place among those ahead) whose maximum is among the K largest can hold one.  These are read
-  // again, and what reaches the K-th largest maximum is sorted by counting what comes before it.
-  const float top = across<6>(fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])), Larger());
-  const float low = reached_by(most, K, K + 4);
-  int n_lists = 0;
-#pragma unroll
-  for (int d = 0; d < kAhead; ++d) {
-    const bool in = most[d] >= low;
-    const uint64_t b = __ballot(in);
-    if (in) lists[n_lists + lanes_below(b)] = (uint16_t)(d * 64 + lane);
-    n_lists += lanes_of(b);
-  }
-  __syncthreads();
-  int n = 0;
-  const int work = n_lists * batches;
-  for (int w = lane; w - lane < work; w += 64) {
-    float x[8];
-    const int at = w < work ? w / batches : 0;
-    const int l = lists[at], o = w < work ? p.first + (w - at * batches) * (kAhead * 64) + l : p.end;
-    p.read(o, x);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const bool in = x[j] >= low;
-      const uint64_t b = __ballot(in);
-      const int to = n + lanes_below(b);
-      if (in && to < kFound) found[to] = Found{x[j], p.token(o, j)};
-      n += lanes_of(b);
-    }
-  }
-  if (n > kFound) n = equals_too(p, K, low, top, found);
-  __syncthreads();
-  for (int k0 = 0; k0 < n; k0 += 64) {
-    const Found mine = found[min(k0 + lane, n - 1)];
-    int rank = k0 + lane < n ? 0 : K;
-    for (int k = 0; k < n; ++k) {
-      const Found other = found[k];
-      rank += before(other.value, other.token, mine.value, mine.token);
-    }
-    if (rank < K) {
-      values[rank] = mine.value;
-      tokens[rank] = mine.token;
-    }
-  }
-  nothing(n);
 }
 
-// ---- a group's choice among its rows' parts --------------------------------------------------------
+// ---- a group's choice --------------------------------------------------------------------------
 
+// A logit, or a list by its largest, in the order of choices: by score, then row, logit (scores of one row are in the order of its logits even
+// where 64 bits cannot tell them apart), token or octet.  rest: row, logit from the largest down, token (24 bits).
 struct Choice {
   double score;
-  float value;
-  int row, token;
+  uint64_t rest;
 };
-// Scores of one row are in the order of its logits even where 64 bits cannot tell them apart.
-__device__ __forceinline__ bool before(const Choice& a, const Choice& b) {
-  if (a.score != b.score) return a.score > b.score;
-  if (a.row != b.row) return a.row < b.row;
-  return before(a.value, a.token, b.value, b.token);
+__device__ __forceinline__ uint64_t rest_of(int row, float value, int token) { return (uint64_t)row << 56 | (uint64_t)~key_of(value + 0.0f) << 24 | (uint32_t)token; }
+__device__ __forceinline__ bool before(const Choice& a, const Choice& b) { return a.score > b.score || (a.score == b.score && a.rest < b.rest); }
+constexpr uint64_t kNone = ~0ull;
+
+constexpr int kFound = 1024;           // choices that are sorted by counting what comes before each
+constexpr int kFoundLists = 512;
+constexpr int kBestThreads = 256;
+
+// The best choice of what `each` shows to `see` in every thread, behind `last` (k > 0): the threads' best in `best`, then one of them.
+template <typename F>
+__device__ __forceinline__ Choice next_best(Choice* best, int k, const Choice& last, F each) {
+  const int tid = threadIdx.x;
+  Choice b = {0.0, kNone};
+  each([&](const Choice& x) __attribute__((always_inline)) {
+    if ((k == 0 || before(last, x)) && (b.rest == kNone || before(x, b))) b = x;
+  });
+  __syncthreads();                                         // the last one has been read
+  best[tid] = b;
+  __syncthreads();
+  for (int d = kBestThreads / 2; d; d >>= 1) {
+    if (tid < d && best[tid + d].rest != kNone && (best[tid].rest == kNone || before(best[tid + d], best[tid]))) best[tid] = best[tid + d];
+    __syncthreads();
+  }
+  return best[0];
 }
 
-constexpr int kChoices = 512;
-__global__ __launch_bounds__(256) void select_best_kernel(SelectArgs a, GroupRows g, int group0) {
-  __shared__ double base[kBeamsMost], sums[kMostLists];
-  __shared__ float refs[kMostLists], heads[kMostLists], from[kBeamsMost], least;
-  __shared__ Choice choice[kChoices];
-  __shared__ int count;
-  const int tid = threadIdx.x, K = a.n_best, parts = a.parts;
-  const int row0 = g.base + g.first[blockIdx.x], beams = g.first[blockIdx.x + 1] - g.first[blockIdx.x], lists = beams * parts;
-  const int64_t list0 = (int64_t)row0 * parts;
-  float head = -INFINITY;
-  if (tid < lists) {
-    refs[tid] = a.refs[list0 + tid];
-    sums[tid] = a.sums[list0 + tid];
-    head = a.values[(list0 + tid) * K];
-  }
-  if (tid == 0) count = 0;
-  __syncthreads();
+// One workgroup for a group.  A value that the K best reach comes from 256 disjoint subsets' largest, each thread's lists: of every row some,
+// since the best may all be one row's.  Lists that reach it are read again, and what reaches it in them is sorted.
+template <typename E, bool MASKED, bool TINY>
+__global__ __launch_bounds__(kBestThreads) void select_best_kernel(SelectArgs a, GroupRows g, int group0) {
+  __shared__ double base[kBeamsMost];
+  __shared__ float from[kBeamsMost], subset[kBestThreads];
+  __shared__ Choice list[kFoundLists], found[kFound];
+  __shared__ int n_list, n_found;
+  const int tid = threadIdx.x, K = a.n_best, bits = a.parts_bits, parts = 1 << bits;
+  const int row0 = g.base + g.first[blockIdx.x], beams = g.first[blockIdx.x + 1] - g.first[blockIdx.x], all = beams << bits;
+  const int64_t at0 = (int64_t)row0 << bits;
+  if (tid == 0) n_list = n_found = 0;
   // Of each row the score less the logarithm of its sum, and where its exponents are counted from: a logit is taken from there first,
-  // which is exact where it is large, and rows of the type's lowest value alone keep their sum.
-  if (tid < beams) {
-    float c = -FLT_MAX;
-    for (int p = 0; p < parts; ++p) c = fmaxf(c, refs[tid * parts + p]);
-    double s = 0.0;
-    for (int p = 0; p < parts; ++p) s += sums[tid * parts + p] * (double)__builtin_amdgcn_exp2f((refs[tid * parts + p] - c) * kLog2e);
-    const double b = (double)a.scores[row0 + tid] - log(s);
-    base[tid] = s > 0.0 && fabs(b) < (double)INFINITY ? b : -(double)INFINITY;
-    from[tid] = c;
+  // which is exact where it is large, and rows of the type's lowest value alone keep their sum.  A row's parts are neighbouring threads'.
+  const int mine = min(tid, all - 1);
+  const float ref = a.refs[at0 + mine];
+  const float score = a.scores[row0 + (mine >> bits)];
+  double sum = a.sums[at0 + mine];
+  float c = ref;
+  for (int d = 1; d < parts; d <<= 1) c = fmaxf(c, __shfl_xor(c, d));
+  sum *= (double)__builtin_amdgcn_exp2f((ref - c) * kLog2e);
+  for (int d = 1; d < parts; d <<= 1) sum += __shfl_xor(sum, d);
+  double b = (double)score - log(sum);
+  b = sum > 0.0 && fabs(b) < (double)INFINITY ? b : -(double)INFINITY;
+  if (tid < all && (tid & (parts - 1)) == 0) {
+    base[tid >> bits] = b;
+    from[tid >> bits] = c;
   }
+  // scores as 32 bits round them, which keeps their order: at most K - 1 are above one that is below the K-th of any K
+  const auto scored = [&](int row, float value) __attribute__((always_inline)) { return ((double)value - (double)from[row]) + base[row]; };
   __syncthreads();
-  // No choice is below the K-th largest of the lists' best, as 32 bits round them.
-  heads[tid] = tid < lists ? (float)(((double)head - (double)from[tid / parts]) + base[tid / parts]) : -INFINITY;
-  __syncthreads();
-  if (tid < 64) {
-    const float x[4] = {heads[tid], heads[64 + tid], heads[128 + tid], heads[192 + tid]};
-    const float l = reached_by(x, K, K + 16);
-    if (tid == 0) least = l;
+  // Four neighbouring lists at a time: their row is one.
+  const int quads = all * 16;
+  const f32x4_t* most = (const f32x4_t*)(a.most + at0 * 64);
+  float top = -INFINITY;
+#pragma unroll 4
+  for (int q = tid; q < quads; q += kBestThreads) {
+    const f32x4_t v = most[q];
+    top = fmaxf(top, (float)scored(q >> (4 + bits), fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3]))));
   }
+  subset[tid] = top;
   __syncthreads();
-  const float low = least;
-  const int entries = lists * K;
-  const auto entry = [&](int e) {
-    Choice x;
-    x.row = e / K / parts;
-    x.value = a.values[list0 * K + e];
-    x.token = a.tokens[list0 * K + e];
-    x.score = ((double)x.value - (double)from[x.row]) + base[x.row];
-    return x;
-  };
-  for (int e = tid; e < entries; e += 256) {
-    const Choice x = entry(e);
-    if ((float)x.score >= low) {
-      const int at = atomicAdd(&count, 1);
-      if (at < kChoices) choice[at] = x;
+  const int lane = tid & 63;
+  const float four[4] = {subset[lane], subset[64 + lane], subset[128 + lane], subset[192 + lane]};
+  const float low = reached_by(four, K, K + K / 8);
+
+  const auto see_lists = [&](auto see) __attribute__((always_inline)) {
+    if (!(top >= low)) return;
+#pragma unroll 4
+    for (int q = tid; q < quads; q += kBestThreads) {
+      const f32x4_t v = most[q];
+      const int row = q >> (4 + bits);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const double s = scored(row, v[j]);
+        if ((float)s >= low) see(Choice{s, rest_of(row, v[j], a.most_at[at0 * 64 + 4 * q + j])});
+      }
     }
+  };
+  see_lists([&](const Choice& x) __attribute__((always_inline)) {
+    const int to = atomicAdd(&n_list, 1);
+    if (to < kFoundLists) list[to] = x;
+  });
+  __syncthreads();
+  int lists = n_list;
+  if (lists > kFoundLists) {                               // many equals: exactly the K best lists, which hold the K best
+    lists = min(K, lists);
+    Choice last = {};
+    for (int k = 0; k < lists; ++k) {
+      last = next_best(found, k, last, see_lists);
+      if (tid == 0) list[k] = last;
+    }
+    __syncthreads();
   }
+
+  const int deep = (a.part_octets + 63) / 64, work = lists * deep;
+  const auto see_octets = [&](auto see) __attribute__((always_inline)) {
+    for (int w = tid; w < work; w += kBestThreads) {
+      const int l = w / deep;
+      const uint64_t rest = list[l].rest;
+      const int row = (int)(rest >> 56), best_at = (int)(rest & 0xffffff), first = best_at / a.part_octets * a.part_octets;
+      const int o = first + (best_at - first & 63) + (w - l * deep) * 64;
+      const auto p = part_of<E, MASKED, TINY>(a, row0 + row, first);
+      if (o >= p.end) continue;
+      float x[8];
+      p.read(o, x);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const double s = scored(row, x[j]);
+        if ((float)s >= low) see(Choice{s, rest_of(row, x[j], p.token(o, j))});
+      }
+    }
+  };
+  see_octets([&](const Choice& x) __attribute__((always_inline)) {
+    const int to = atomicAdd(&n_found, 1);
+    if (to < kFound) found[to] = x;
+  });
   __syncthreads();
   const int64_t out = (int64_t)(group0 + blockIdx.x) * K;
-  const auto write = [&](int k, const Choice& x) {
+  const auto write = [&](int k, const Choice& x) __attribute__((always_inline)) {
     a.best_scores[out + k] = (float)x.score;
-    a.best_beams[out + k] = x.row;
-    a.best_tokens[out + k] = x.token;
+    a.best_beams[out + k] = (int)(x.rest >> 56);
+    a.best_tokens[out + k] = (int)(x.rest & 0xffffff);
   };
-  int n = count;
-  if (n <= kChoices) {
-    for (int i = tid; i < n; i += 256) {
-      const Choice mine = choice[i];
+  int n = n_found;
+  if (n <= kFound) {
+    for (int i = tid; i < n; i += kBestThreads) {
+      const Choice x = found[i];
       int rank = 0;
-      for (int k = 0; k < n; ++k) rank += before(choice[k], mine);
-      if (rank < K) write(rank, mine);
+      for (int k = 0; k < n; ++k) rank += before(found[k], x);
+      if (rank < K) write(rank, x);
     }
-  } else {                                                 // many equals: one choice after the other
+  } else {                                                 // many large ones in few lists: one after the other
     n = K;
-    Choice last;
+    Choice last = {};
     for (int k = 0; k < K; ++k) {
-      Choice best = {-(double)INFINITY, 0.f, -1, -1};
-      for (int e = tid; e < entries; e += 256) {
-        const Choice x = entry(e);
-        if ((float)x.score >= low && (k == 0 || before(last, x)) && (best.row < 0 || before(x, best))) best = x;
-      }
-      choice[tid] = best;
-      __syncthreads();
-      for (int d = 128; d; d >>= 1) {
-        if (tid < d && choice[tid + d].row >= 0 && (choice[tid].row < 0 || before(choice[tid + d], choice[tid]))) choice[tid] = choice[tid + d];
-        __syncthreads();
-      }
-      last = choice[0];
+      last = next_best(found, k, last, see_octets);
       if (tid == 0) write(k, last);
-      __syncthreads();
     }
   }
-  for (int k = n + tid; k < K; k += 256) {
+  for (int k = n + tid; k < K; k += kBestThreads) {
     a.best_scores[out + k] = -INFINITY;
     a.best_beams[out + k] = a.best_tokens[out + k] = -1;
   }
@@ -540,32 +499,35 @@ __global__ __launch_bounds__(kStateThreads) void states_kernel(StatesArgs a, Gro
   }
 }
 
-template <typename E>
+template <typename E, bool MASKED, bool TINY>
 void launch_rows(const SelectArgs& a, hipStream_t st) {
-  const dim3 grid((unsigned)(a.rows * a.parts)), block(64);
-  if (a.vocab < kOctet) {
-    if (a.allowed) select_rows_kernel<E, true, true><<<grid, block, 0, st>>>(a);
-    else select_rows_kernel<E, false, true><<<grid, block, 0, st>>>(a);
-  } else if (a.allowed) {
-    select_rows_kernel<E, true, false><<<grid, block, 0, st>>>(a);
-  } else {
-    select_rows_kernel<E, false, false><<<grid, block, 0, st>>>(a);
-  }
+  select_rows_kernel<E, MASKED, TINY><<<dim3((unsigned)(a.rows * a.parts)), dim3(64), 0, st>>>(a);
 }
+template <typename E, bool MASKED, bool TINY>
+void launch_best(const SelectArgs& a, const GroupRows& g, int32_t group0, int32_t n_groups, hipStream_t st) {
+  select_best_kernel<E, MASKED, TINY><<<dim3((unsigned)n_groups), dim3(kBestThreads), 0, st>>>(a, g, group0);
+}
+#define SYM_OF_TYPE(launch, E, ...)                                                     \
+  (a.vocab < kOctet ? (a.allowed ? launch<E, true, true>(__VA_ARGS__) : launch<E, false, true>(__VA_ARGS__)) \
+                    : (a.allowed ? launch<E, true, false>(__VA_ARGS__) : launch<E, false, false>(__VA_ARGS__)))
+#define SYM_OF_STEP(launch, ...)                                        \
+  (dtype == SYM_F32    ? SYM_OF_TYPE(launch, LogitF32, __VA_ARGS__)     \
+   : dtype == SYM_BF16 ? SYM_OF_TYPE(launch, LogitBF16, __VA_ARGS__)    \
+                       : SYM_OF_TYPE(launch, LogitF16, __VA_ARGS__))
 
 }  // namespace
 
 hipError_t launch_select_rows(const SelectArgs& a, int dtype, hipStream_t st) {
-  if (dtype == SYM_F32) launch_rows<LogitF32>(a, st);
-  else if (dtype == SYM_BF16) launch_rows<LogitBF16>(a, st);
-  else launch_rows<LogitF16>(a, st);
+  SYM_OF_STEP(launch_rows, a, st);
   return hipGetLastError();
 }
 
-hipError_t launch_select_best(const SelectArgs& a, const GroupRows& g, int32_t group0, int32_t n_groups, hipStream_t st) {
-  select_best_kernel<<<dim3((unsigned)n_groups), dim3(256), 0, st>>>(a, g, group0);
+hipError_t launch_select_best(const SelectArgs& a, const GroupRows& g, int32_t group0, int32_t n_groups, int dtype, hipStream_t st) {
+  SYM_OF_STEP(launch_best, a, g, group0, n_groups, st);
   return hipGetLastError();
 }
+#undef SYM_OF_STEP
+#undef SYM_OF_TYPE
 
 hipError_t launch_states(const StatesArgs& a, const GroupRows& g, int32_t most_beams, hipStream_t st) {
   const dim3 grid(a.array[a.n_arrays - 1].end), block(kStateThreads);

@@ -16,7 +16,7 @@ struct GroupRows {
 };
 
 constexpr int kOctet = 8;              // logits that a lane takes at a time
-constexpr int kMostLists = 256;        // lists of a group that its choice starts from: a thread each
+constexpr int kMostLists = 256;        // parts of a group that its choice starts from: a thread each
 struct SelectArgs {
   const void* logits;
   int64_t stride;                      // elements from row to row
@@ -26,26 +26,26 @@ struct SelectArgs {
   float* best_scores;
   int32_t* best_beams;
   int32_t* best_tokens;
-  // [rows][parts]: largest logit of a part (or one not far below), sum of exponentials from there, [n_best] best logits and their tokens
+  // scratch, [rows][parts]: the logit that exponents are counted from, their sum; [rows][parts][64]: the largest logit of each lane, and the
+  // octet that holds it first
   double* sums;
   float* refs;
-  float* values;
-  int32_t* tokens;
+  float* most;
+  int32_t* most_at;
   int32_t rows, vocab, n_best;
-  int32_t parts, part_octets;          // wavefronts of a row, octets of each
+  int32_t parts, parts_bits, part_octets;      // wavefronts of a row (a power of two), octets of each
 };
 
-// How a row is cut: parts, octets of a part.
+// How a row is cut: a power of two of parts, octets of a part.
 struct SelectCut {
-  int32_t parts, part_octets;
+  int32_t bits, part_octets;
 };
 constexpr int kSelectWaves = 4096;
 inline SelectCut select_cut(int64_t rows, int32_t most_beams, int32_t vocab) {
-  const int64_t octets = (vocab + kOctet - 1) / kOctet;
-  int64_t parts = std::min<int64_t>((kSelectWaves + rows - 1) / rows, kMostLists / most_beams);
-  parts = std::max<int64_t>(1, std::min<int64_t>(parts, (octets + 255) / 256));
-  const int64_t per = ((octets + parts - 1) / parts + 63) / 64 * 64;
-  return SelectCut{(int32_t)((octets + per - 1) / per), (int32_t)per};
+  const int64_t octets = (vocab + kOctet - 1) / kOctet, want = (kSelectWaves + rows - 1) / rows, most = std::min<int64_t>(kMostLists / most_beams, 64);
+  int32_t bits = 0;
+  while ((2ll << bits) <= most && (1ll << bits) < want && (octets >> bits) > 256) ++bits;
+  return SelectCut{bits, (int32_t)((((octets + (1ll << bits) - 1) >> bits) + 63) / 64 * 64)};
 }
 
 constexpr int kStatesAtOnce = 8;       // arrays of a launch
@@ -79,7 +79,7 @@ struct CopyArgs {
 // Weak: see sparse.hpp.
 #define SYMKV_LAUNCH __attribute__((weak))
 SYMKV_LAUNCH hipError_t launch_select_rows(const SelectArgs& a, int dtype, hipStream_t st);
-SYMKV_LAUNCH hipError_t launch_select_best(const SelectArgs& a, const GroupRows& g, int32_t group0, int32_t n_groups, hipStream_t st);
+SYMKV_LAUNCH hipError_t launch_select_best(const SelectArgs& a, const GroupRows& g, int32_t group0, int32_t n_groups, int dtype, hipStream_t st);
 SYMKV_LAUNCH hipError_t launch_states(const StatesArgs& a, const GroupRows& g, int32_t most_beams, hipStream_t st);
 SYMKV_LAUNCH hipError_t launch_copies(const CopyArgs& a, hipStream_t st);
 #undef SYMKV_LAUNCH

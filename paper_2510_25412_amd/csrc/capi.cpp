@@ -1851,9 +1851,9 @@ int32_t group_rows(int32_t n_groups, const int32_t* beams, int32_t g0, int32_t r
   for (int32_t i = 0; i < n; ++i) g->first[i + 1] = (uint16_t)(g->first[i] + beams[g0 + i]);
   return n;
 }
-int64_t select_scratch(int64_t rows, int32_t most, int32_t vocab, int32_t n_best) {
-  const int64_t lists = rows * select_cut(rows, most, vocab).parts;
-  return align_up(lists * 8, 16) + align_up(lists * 4, 16) + 2 * align_up(lists * n_best * 4, 16);
+int64_t select_scratch(int64_t rows, int32_t most, int32_t vocab) {
+  const int64_t parts = rows << select_cut(rows, most, vocab).bits;
+  return align_up(parts * 8, 16) + align_up(parts * 4, 16) + 2 * parts * 64 * 4;
 }
 static_assert(kBeamsMost == SYM_BEAMS_MOST && kBestMost == SYM_BEST_MOST, "the header's limits");
 constexpr int64_t kStateBlocks = 1 << 22;              // workgroups of a launch
@@ -1863,7 +1863,7 @@ int64_t sym_beam_scratch_bytes(int32_t n_groups, const int32_t* beams, int32_t v
   int32_t most;
   const int64_t rows = count_rows(n_groups, beams, &most);
   if (rows < 0 || vocab < 1 || vocab > (1 << 24) || n_best < 1 || n_best > kBestMost) return SYM_EINVAL;
-  return rows == 0 ? 0 : select_scratch(rows, most, vocab, n_best);
+  return rows == 0 ? 0 : select_scratch(rows, most, vocab);
 }
 
 int sym_beam_select(sym_ctx* c, const sym_beam_step* b, void* stream) {
@@ -1880,7 +1880,7 @@ int sym_beam_select(sym_ctx* c, const sym_beam_step* b, void* stream) {
     if (stride < b->vocab || stride > (int64_t)1 << 40) return fail(c, SYM_EINVAL, "beam_select: rows of logits overlap, or lie too far apart");
     if (b->allowed && (bit_stride < words || bit_stride > (int64_t)1 << 40)) return fail(c, SYM_EINVAL, "beam_select: rows of allowed tokens overlap, or lie too far apart");
     if (rows == 0) return SYM_OK;
-    const int64_t es = b->dtype == SYM_F32 ? 4 : 2, scratch = select_scratch(rows, most, b->vocab, b->n_best), out = (int64_t)b->n_groups * b->n_best * 4;
+    const int64_t es = b->dtype == SYM_F32 ? 4 : 2, scratch = select_scratch(rows, most, b->vocab), out = (int64_t)b->n_groups * b->n_best * 4;
     if (!b->logits || !b->scores || !b->best_scores || !b->best_beams || !b->best_tokens || !b->scratch) return fail(c, SYM_EINVAL, "beam_select: a pointer is missing");
     if (!aligned(b->logits, (uintptr_t)es) || !aligned(b->scores, 4) || !aligned(b->allowed, 4) || !aligned(b->best_scores, 4) || !aligned(b->best_beams, 4) ||
         !aligned(b->best_tokens, 4) || !aligned(b->scratch, 16))
@@ -1900,7 +1900,7 @@ int sym_beam_select(sym_ctx* c, const sym_beam_step* b, void* stream) {
     const OnDevice on(c);
     hipStream_t st = (hipStream_t)stream;
     const SelectCut cut = select_cut(rows, most, b->vocab);
-    const int64_t lists = rows * cut.parts;
+    const int64_t parts = rows << cut.bits;
     uint8_t* at = (uint8_t*)b->scratch;
     const auto take = [&](int64_t bytes) {
       uint8_t* p = at;
@@ -1916,14 +1916,15 @@ int sym_beam_select(sym_ctx* c, const sym_beam_step* b, void* stream) {
     a.best_scores = b->best_scores;
     a.best_beams = b->best_beams;
     a.best_tokens = b->best_tokens;
-    a.sums = (double*)take(lists * 8);
-    a.refs = (float*)take(lists * 4);
-    a.values = (float*)take(lists * b->n_best * 4);
-    a.tokens = (int32_t*)take(lists * b->n_best * 4);
+    a.sums = (double*)take(parts * 8);
+    a.refs = (float*)take(parts * 4);
+    a.most = (float*)take(parts * 64 * 4);
+    a.most_at = (int32_t*)take(parts * 64 * 4);
     a.rows = (int32_t)rows;
     a.vocab = b->vocab;
     a.n_best = b->n_best;
-    a.parts = cut.parts;
+    a.parts = 1 << cut.bits;
+    a.parts_bits = cut.bits;
     a.part_octets = cut.part_octets;
     const bool timed = c->prof_mask == 0 || !stream_captures(st);
     {
@@ -1935,7 +1936,7 @@ int sym_beam_select(sym_ctx* c, const sym_beam_step* b, void* stream) {
     for (int32_t g0 = 0, row = 0; g0 < b->n_groups;) {
       const int32_t n = group_rows(b->n_groups, b->beams, g0, row, &g);
       Timed t(c, SYM_K_PROLOGUE, st, false, timed);
-      const hipError_t e = launch_select_best(a, g, g0, n, st);
+      const hipError_t e = launch_select_best(a, g, g0, n, b->dtype, st);
       if (e != hipSuccess) return fail_hip(c, e, "beam choice launch");
       row += g.first[n];
       g0 += n;
