@@ -304,10 +304,10 @@ constexpr uint64_t kNone = ~0ull;
 
 constexpr int kFound = 1024;           // choices that are sorted by counting what comes before each
 constexpr int kFoundLists = 512;
-constexpr int kBestThreads = 256;
+constexpr int kQuads = 4;              // times four lists that a thread holds
 
 // The best choice of what `each` shows to `see` in every thread, behind `last` (k > 0): the threads' best in `best`, then one of them.
-template <typename F>
+template <int THREADS, typename F>
 __device__ __forceinline__ Choice next_best(Choice* best, int k, const Choice& last, F each) {
   const int tid = threadIdx.x;
   Choice b = {0.0, kNone};
@@ -317,54 +317,66 @@ __device__ __forceinline__ Choice next_best(Choice* best, int k, const Choice& l
   __syncthreads();                                         // the last one has been read
   best[tid] = b;
   __syncthreads();
-  for (int d = kBestThreads / 2; d; d >>= 1) {
+  for (int d = THREADS / 2; d; d >>= 1) {
     if (tid < d && best[tid + d].rest != kNone && (best[tid].rest == kNone || before(best[tid + d], best[tid]))) best[tid] = best[tid + d];
     __syncthreads();
   }
   return best[0];
 }
 
-// One workgroup for a group.  A value that the K best reach comes from 256 disjoint subsets' largest, each thread's lists: of every row some,
-// since the best may all be one row's.  Lists that reach it are read again, and what reaches it in them is sorted.
-template <typename E, bool MASKED, bool TINY>
-__global__ __launch_bounds__(kBestThreads) void select_best_kernel(SelectArgs a, GroupRows g, int group0) {
+// One workgroup for a group.  A value that the K best reach comes from 256 disjoint subsets' largest: of every row some lists, since the best
+// may all be one row's.  Lists that reach it are read again, and what reaches it in them is sorted.  What is read of the rows' pass is
+// requested at once and kept, so that a choice is three round trips: where the group's rows are, their lists, the logits looked at again.
+template <typename E, bool MASKED, bool TINY, int THREADS>
+__global__ __launch_bounds__(THREADS) void select_best_kernel(SelectArgs a, GroupRows g, int group0) {
+  static_assert(THREADS * kQuads * 4 >= 64 * kMostLists || THREADS == 256, "a thread holds its share of the lists");
   __shared__ double base[kBeamsMost];
-  __shared__ float from[kBeamsMost], subset[kBestThreads];
+  __shared__ float from[kBeamsMost], subset[256];
   __shared__ Choice list[kFoundLists], found[kFound];
   __shared__ int n_list, n_found;
   const int tid = threadIdx.x, K = a.n_best, bits = a.parts_bits, parts = 1 << bits;
   const int row0 = g.base + g.first[blockIdx.x], beams = g.first[blockIdx.x + 1] - g.first[blockIdx.x], all = beams << bits;
   const int64_t at0 = (int64_t)row0 << bits;
+  // Four neighbouring lists at a time: their row is one.
+  const int quads = all * 16, mine = min(tid, all - 1);
+  f32x4_t most[kQuads];
+  u32x4_t most_at[kQuads];
+#pragma unroll
+  for (int i = 0; i < kQuads; ++i) {
+    const int q = min(tid + i * THREADS, quads - 1);
+    most[i] = ((const f32x4_t*)(a.most + at0 * 64))[q];
+    most_at[i] = ((const u32x4_t*)(a.most_at + at0 * 64))[q];
+  }
+  const float ref = a.refs[at0 + mine], score = a.scores[row0 + (mine >> bits)];
+  double sum = a.sums[at0 + mine];
   if (tid == 0) n_list = n_found = 0;
   // Of each row the score less the logarithm of its sum, and where its exponents are counted from: a logit is taken from there first,
   // which is exact where it is large, and rows of the type's lowest value alone keep their sum.  A row's parts are neighbouring threads'.
-  const int mine = min(tid, all - 1);
-  const float ref = a.refs[at0 + mine];
-  const float score = a.scores[row0 + (mine >> bits)];
-  double sum = a.sums[at0 + mine];
-  float c = ref;
-  for (int d = 1; d < parts; d <<= 1) c = fmaxf(c, __shfl_xor(c, d));
-  sum *= (double)__builtin_amdgcn_exp2f((ref - c) * kLog2e);
-  for (int d = 1; d < parts; d <<= 1) sum += __shfl_xor(sum, d);
-  double b = (double)score - log(sum);
-  b = sum > 0.0 && fabs(b) < (double)INFINITY ? b : -(double)INFINITY;
-  if (tid < all && (tid & (parts - 1)) == 0) {
-    base[tid >> bits] = b;
-    from[tid >> bits] = c;
+  if (tid < (all + 63 & ~63)) {
+    float c = ref;
+    for (int d = 1; d < parts; d <<= 1) c = fmaxf(c, __shfl_xor(c, d));
+    sum *= (double)__builtin_amdgcn_exp2f((ref - c) * kLog2e);
+    for (int d = 1; d < parts; d <<= 1) sum += __shfl_xor(sum, d);
+    const double b = (double)score - log(sum);
+    if (tid < all && (tid & (parts - 1)) == 0) {
+      base[tid >> bits] = sum > 0.0 && fabs(b) < (double)INFINITY ? b : -(double)INFINITY;
+      from[tid >> bits] = c;
+    }
   }
+  __syncthreads();
   // scores as 32 bits round them, which keeps their order: at most K - 1 are above one that is below the K-th of any K
   const auto scored = [&](int row, float value) __attribute__((always_inline)) { return ((double)value - (double)from[row]) + base[row]; };
-  __syncthreads();
-  // Four neighbouring lists at a time: their row is one.
-  const int quads = all * 16;
-  const f32x4_t* most = (const f32x4_t*)(a.most + at0 * 64);
   float top = -INFINITY;
-#pragma unroll 4
-  for (int q = tid; q < quads; q += kBestThreads) {
-    const f32x4_t v = most[q];
-    top = fmaxf(top, (float)scored(q >> (4 + bits), fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3]))));
+#pragma unroll
+  for (int i = 0; i < kQuads; ++i)
+    if (tid + i * THREADS < quads)
+      top = fmaxf(top, (float)scored((tid + i * THREADS) >> (4 + bits), fmaxf(fmaxf(most[i][0], most[i][1]), fmaxf(most[i][2], most[i][3]))));
+  if constexpr (THREADS == 256) {
+    subset[tid] = top;
+  } else {
+    const float of_four = across<2>(top, Larger());
+    if ((tid & 3) == 0) subset[tid >> 2] = of_four;
   }
-  subset[tid] = top;
   __syncthreads();
   const int lane = tid & 63;
   const float four[4] = {subset[lane], subset[64 + lane], subset[128 + lane], subset[192 + lane]};
@@ -372,14 +384,14 @@ __global__ __launch_bounds__(kBestThreads) void select_best_kernel(SelectArgs a,
 
   const auto see_lists = [&](auto see) __attribute__((always_inline)) {
     if (!(top >= low)) return;
-#pragma unroll 4
-    for (int q = tid; q < quads; q += kBestThreads) {
-      const f32x4_t v = most[q];
-      const int row = q >> (4 + bits);
+#pragma unroll
+    for (int i = 0; i < kQuads; ++i) {
+      const int q = tid + i * THREADS, row = q >> (4 + bits);
+      if (q >= quads) return;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const double s = scored(row, v[j]);
-        if ((float)s >= low) see(Choice{s, rest_of(row, v[j], a.most_at[at0 * 64 + 4 * q + j])});
+        const double s = scored(row, most[i][j]);
+        if ((float)s >= low) see(Choice{s, rest_of(row, most[i][j], (int)most_at[i][j])});
       }
     }
   };
@@ -393,7 +405,7 @@ __global__ __launch_bounds__(kBestThreads) void select_best_kernel(SelectArgs a,
     lists = min(K, lists);
     Choice last = {};
     for (int k = 0; k < lists; ++k) {
-      last = next_best(found, k, last, see_lists);
+      last = next_best<THREADS>(found, k, last, see_lists);
       if (tid == 0) list[k] = last;
     }
     __syncthreads();
@@ -401,11 +413,11 @@ __global__ __launch_bounds__(kBestThreads) void select_best_kernel(SelectArgs a,
 
   const int deep = (a.part_octets + 63) / 64, work = lists * deep;
   const auto see_octets = [&](auto see) __attribute__((always_inline)) {
-    for (int w = tid; w < work; w += kBestThreads) {
+    for (int w = tid; w < work; w += THREADS) {
       const int l = w / deep;
       const uint64_t rest = list[l].rest;
       const int row = (int)(rest >> 56), best_at = (int)(rest & 0xffffff), first = best_at / a.part_octets * a.part_octets;
-      const int o = first + (best_at - first & 63) + (w - l * deep) * 64;
+      const int o = first + ((best_at - first) & 63) + (w - l * deep) * 64;
       const auto p = part_of<E, MASKED, TINY>(a, row0 + row, first);
       if (o >= p.end) continue;
       float x[8];
@@ -430,7 +442,7 @@ __global__ __launch_bounds__(kBestThreads) void select_best_kernel(SelectArgs a,
   };
   int n = n_found;
   if (n <= kFound) {
-    for (int i = tid; i < n; i += kBestThreads) {
+    for (int i = tid; i < n; i += THREADS) {
       const Choice x = found[i];
       int rank = 0;
       for (int k = 0; k < n; ++k) rank += before(found[k], x);
@@ -440,11 +452,11 @@ __global__ __launch_bounds__(kBestThreads) void select_best_kernel(SelectArgs a,
     n = K;
     Choice last = {};
     for (int k = 0; k < K; ++k) {
-      last = next_best(found, k, last, see_octets);
+      last = next_best<THREADS>(found, k, last, see_octets);
       if (tid == 0) write(k, last);
     }
   }
-  for (int k = n + tid; k < K; k += kBestThreads) {
+  for (int k = n + tid; k < K; k += THREADS) {
     a.best_scores[out + k] = -INFINITY;
     a.best_beams[out + k] = a.best_tokens[out + k] = -1;
   }
@@ -505,7 +517,10 @@ void launch_rows(const SelectArgs& a, hipStream_t st) {
 }
 template <typename E, bool MASKED, bool TINY>
 void launch_best(const SelectArgs& a, const GroupRows& g, int32_t group0, int32_t n_groups, hipStream_t st) {
-  select_best_kernel<E, MASKED, TINY><<<dim3((unsigned)n_groups), dim3(kBestThreads), 0, st>>>(a, g, group0);
+  int most = 0;                                            // parts of the largest group
+  for (int32_t i = 0; i < n_groups; ++i) most = std::max(most, (g.first[i + 1] - g.first[i]) * a.parts);
+  if (most * 64 <= 256 * kQuads * 4) select_best_kernel<E, MASKED, TINY, 256><<<dim3((unsigned)n_groups), dim3(256), 0, st>>>(a, g, group0);
+  else select_best_kernel<E, MASKED, TINY, 1024><<<dim3((unsigned)n_groups), dim3(1024), 0, st>>>(a, g, group0);
 }
 #define SYM_OF_TYPE(launch, E, ...)                                                     \
   (a.vocab < kOctet ? (a.allowed ? launch<E, true, true>(__VA_ARGS__) : launch<E, false, true>(__VA_ARGS__)) \

@@ -9,14 +9,14 @@ namespace symkv {
 
 constexpr int kBeamsMost = 64;         // rows of a group
 constexpr int kBestMost = 128;         // choices of a group
-constexpr int kGroupsAtOnce = 512;     // groups of a launch: their first rows travel with its arguments (1 KB)
+constexpr int kGroupsAtOnce = 256;     // groups of a launch: their first rows travel with its arguments (1 KB)
 struct GroupRows {
   int32_t base;                        // row of the launch's first group
-  uint16_t first[kGroupsAtOnce + 1];   // rows before each group, from there on
+  int32_t first[kGroupsAtOnce + 1];    // rows before each group, from there on
 };
 
 constexpr int kOctet = 8;              // logits that a lane takes at a time
-constexpr int kMostLists = 256;        // parts of a group that its choice starts from: a thread each
+constexpr int kMostLists = 256;        // parts of a group that its choice starts from
 struct SelectArgs {
   const void* logits;
   int64_t stride;                      // elements from row to row

@@ -1848,7 +1848,7 @@ int32_t group_rows(int32_t n_groups, const int32_t* beams, int32_t g0, int32_t r
   const int32_t n = std::min(kGroupsAtOnce, n_groups - g0);
   g->base = row0;
   g->first[0] = 0;
-  for (int32_t i = 0; i < n; ++i) g->first[i + 1] = (uint16_t)(g->first[i] + beams[g0 + i]);
+  for (int32_t i = 0; i < n; ++i) g->first[i + 1] = g->first[i] + beams[g0 + i];
   return n;
 }
 int64_t select_scratch(int64_t rows, int32_t most, int32_t vocab) {
