@@ -17,6 +17,12 @@ template <int CTRL>
 __device__ __forceinline__ float dpp(float x) {
   return as_f32(__builtin_amdgcn_update_dpp(as_u32(x), as_u32(x), CTRL, 0xf, 0xf, false));
 }
+// The largest of three: an instruction, where fmaxf makes quiet values of its operands first.  NaN only where all are.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "v"(c));
+  return d;
+}
 // x of every lane combined over aligned subsets of 2^BITS lanes, in every lane
 template <int BITS, typename F>
 __device__ __forceinline__ float across(float x, F f) {
@@ -112,7 +118,7 @@ __device__ __forceinline__ R few16(const uint8_t* p, int n) {
   return r;
 }
 struct LogitBF16 {
-  static constexpr int kBytes = 2;
+  static constexpr int kBytes = 2, kGroup = 8;
   struct Raw {
     u32x4_t w;
   };
@@ -127,7 +133,7 @@ struct LogitBF16 {
   static __device__ __forceinline__ Raw few(const uint8_t* p, int n) { return few16<Raw>(p, n); }
 };
 struct LogitF16 {
-  static constexpr int kBytes = 2;
+  static constexpr int kBytes = 2, kGroup = 8;
   struct Raw {
     u32x4_t w;
   };
@@ -142,68 +148,75 @@ struct LogitF16 {
   static __device__ __forceinline__ Raw few(const uint8_t* p, int n) { return few16<Raw>(p, n); }
 };
 struct LogitF32 {
-  static constexpr int kBytes = 4;
+  static constexpr int kBytes = 4, kGroup = 4;
   struct Raw {
-    u32x4_t w, v;
+    u32x4_t w;
   };
-  static __device__ __forceinline__ Raw load(const uint8_t* p) { return Raw{*(const u32x4_a4*)p, *(const u32x4_a4*)(p + 16)}; }
-  static __device__ __forceinline__ void unpack(const Raw& r, float (&x)[8]) {
+  static __device__ __forceinline__ Raw load(const uint8_t* p) { return Raw{*(const u32x4_a4*)p}; }
+  static __device__ __forceinline__ void unpack(const Raw& r, float (&x)[4]) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[i] = as_f32(r.w[i]);
-      x[4 + i] = as_f32(r.v[i]);
-    }
+    for (int i = 0; i < 4; ++i) x[i] = as_f32(r.w[i]);
   }
   static __device__ __forceinline__ Raw few(const uint8_t* p, int n) {
     Raw r = {};
 #pragma unroll
-    for (int j = 0; j < 7; ++j)
-      if (j < n) (j < 4 ? r.w : r.v)[j & 3] = ((const uint32_t*)p)[j];
+    for (int j = 0; j < 3; ++j)
+      if (j < n) r.w[j] = ((const uint32_t*)p)[j];
     return r;
   }
 };
 
-constexpr int kAhead = 4;              // octets of a lane under way; a part's maxima are kept apart by their place among these
-// One wavefront: a part of a row, 8 logits (an octet) to a lane at a time.  What it reads is counted from the row's start,
-// whatever the address, so equal rows give equal results.  TINY: rows of less than an octet, read one by one.
+// One wavefront: a part of a row, a group of logits (16 bytes) to a lane at a time, so that neighbouring lanes read neighbouring
+// addresses.  What is read is counted from the row's start, whatever the address, so equal rows give equal results.  TINY: rows of less
+// than a group, read one by one.
 template <typename E, bool MASKED, bool TINY>
 struct Part {
+  static constexpr int N = E::kGroup;
   const uint8_t* row;
   const uint8_t* bits;
-  int vocab, first, end;               // octets of this part
+  int vocab, first, end;               // groups of this part
+  uint32_t last;                       // where the last of them is read, in bytes
 
-  // Octet o.  The last one of a row that does not end with it: the row's last 8 logits.  What is not wanted comes from where others read.
+  // Group o.  The last one of a row that does not end with it: the row's last N logits.  What is not wanted comes from where others read.
   __device__ __forceinline__ typename E::Raw raw(int o, bool want) const {
     if constexpr (TINY) return E::few(row, vocab);
-    const int at = min((want ? o : first) * kOctet, vocab - kOctet);
-    return E::load(row + (int64_t)at * E::kBytes);
+    const uint32_t at = min((uint32_t)o * 16, last);
+    return E::load(row + (MASKED && !want ? last : at));
   }
   __device__ __forceinline__ uint32_t allowed(int o) const {
+    constexpr uint32_t all = (1u << N) - 1;
     const bool in = o < end;
-    const uint32_t m = MASKED ? bits[in ? o : first] : 0xffu;
+    uint32_t m = all;
+    if constexpr (MASKED) {
+      const int at = (in ? o : first) * N;
+      m = (uint32_t)bits[at >> 3] >> (at & 7) & all;
+    }
     return in ? m : 0;
   }
-  // -inf in the place of what does not count.  m: the octet's allowed bits
-  __device__ __forceinline__ void mask(float (&x)[8], int o, uint32_t m) const {
-    const int over = (o + 1) * kOctet - vocab;             // more than a row's last octet holds
-    if constexpr (TINY) m = over > 0 ? m & (0xffu >> over) : m;
+  // -inf in the place of what does not count.  m: the group's allowed bits
+  __device__ __forceinline__ void mask(float (&x)[N], int o, uint32_t m) const {
+    const int over = (o + 1) * N - vocab;                  // more than a row's last group holds
+    if constexpr (TINY) m = over > 0 ? m & (((1u << N) - 1) >> over) : m;
     else m = over > 0 ? m << over : m;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
+    for (int j = 0; j < N; ++j) {
       const uint32_t keep = (uint32_t)((int32_t)(m << (31 - j)) >> 31);
       x[j] = as_f32((as_u32(x[j]) & keep) | (0xff800000u & ~keep));
     }
   }
-  __device__ __forceinline__ int token(int o, int j) const { return (TINY ? 0 : min(o * kOctet, vocab - kOctet)) + j; }
-  // Octet o's logits, masked
-  __device__ __forceinline__ void read(int o, float (&x)[8]) const {
+  __device__ __forceinline__ int token(int o, int j) const { return (TINY ? 0 : min(o * N, vocab - N)) + j; }
+  // Group o's logits, masked
+  __device__ __forceinline__ void read(int o, float (&x)[N]) const {
     const uint32_t m = allowed(o);
     E::unpack(raw(o, m != 0), x);
     mask(x, o, m);
   }
 };
 
-// The part of row `row` that begins at octet `first`.
+// Groups of a part.
+template <typename E>
+__device__ __forceinline__ int part_groups(const SelectArgs& a) { return a.part_octets * (kOctet / E::kGroup); }
+// The part of row `row` that begins at group `first`.
 template <typename E, bool MASKED, bool TINY>
 __device__ __forceinline__ Part<E, MASKED, TINY> part_of(const SelectArgs& a, int row, int first) {
   Part<E, MASKED, TINY> p;
@@ -211,19 +224,20 @@ __device__ __forceinline__ Part<E, MASKED, TINY> part_of(const SelectArgs& a, in
   p.bits = MASKED ? a.allowed + (int64_t)row * a.allowed_stride : nullptr;
   p.vocab = a.vocab;
   p.first = first;
-  p.end = min(first + a.part_octets, (a.vocab + kOctet - 1) / kOctet);
+  p.end = min(first + part_groups<E>(a), (a.vocab + E::kGroup - 1) / E::kGroup);
+  p.last = TINY ? 0 : (uint32_t)min((p.end - 1) * E::kGroup, a.vocab - E::kGroup) * E::kBytes;
   return p;
 }
 
-// One pass over the logits.  Of every part: its normaliser's share, and for each lane (a list: octets 64 apart) the largest logit and the
-// octet where it is found first; the choice needs no more to know where it has to look again.
+// One pass over the logits.  Of every part: its normaliser's share, and for each lane (a list: groups 64 apart) the largest logit and the
+// group where it is found first; the choice needs no more to know where it has to look again.
 template <typename E, bool MASKED, bool TINY>
 __global__ __launch_bounds__(64) void select_rows_kernel(SelectArgs a) {
   const int lane = threadIdx.x & 63;
   const int row = (int)(blockIdx.x / (uint32_t)a.parts), part = (int)(blockIdx.x % (uint32_t)a.parts);
   const int64_t at = blockIdx.x;
   const float score = a.scores[row];
-  const auto p = part_of<E, MASKED, TINY>(a, row, part * a.part_octets);
+  const auto p = part_of<E, MASKED, TINY>(a, row, part * part_groups<E>(a));
   if (p.first >= p.end || !(fabsf(score) < INFINITY)) {    // behind the row's end, or no beam lives here
     a.most[at * 64 + lane] = -INFINITY;
     if (lane == 0) {
@@ -232,58 +246,75 @@ __global__ __launch_bounds__(64) void select_rows_kernel(SelectArgs a) {
     }
     return;
   }
-  const int whole = min(p.end, a.vocab / kOctet);          // octets that need no look at the row's end
+  constexpr int N = E::kGroup, kAhead = 32 / N;            // groups of a lane that are added at a time
+  const int whole = min(p.end, a.vocab / N);               // groups that need no look at the row's end
 
-  // Sums of exp(x - c), eight to a lane.  c is a lane's largest logit so far, so that no exponent is positive: a rounding of (x - c)
-  // log2 e then weighs at most 2^-24 of the sum, where with c some way below the largest it would weigh that many times as much.
-  float c = -FLT_MAX, s[8] = {}, most = -INFINITY;
+  // Sums of exp(x - c), eight to a lane (four of fp32).  c is a lane's largest logit so far, so that no exponent is positive: a rounding of (x - c)
+  // log2 e then weighs at most 2^-24 of the sum, where with c some way below the largest it would weigh that many times as much.  The first
+  // c is the wavefront's: rows short enough for one group to a lane then sum the same numbers whatever their order, and in 64 bits, so
+  // that rows of the same logits in another order have equal scores.
+  float c = -FLT_MAX, s[N] = {}, most = -INFINITY;
   int most_at = p.first + lane;
   const int batches = (p.end - p.first + 64 * kAhead - 1) / (64 * kAhead);
-  typename E::Raw cur[kAhead], next[kAhead];
-  uint32_t m[kAhead], m_next[kAhead], m_later[kAhead];
-  const auto octet = [&](int i, int d) __attribute__((always_inline)) { return p.first + (i * kAhead + d) * 64 + lane; };
-#pragma unroll
-  for (int d = 0; d < kAhead; ++d) m[d] = p.allowed(octet(0, d));
-#pragma unroll
-  for (int d = 0; d < kAhead; ++d) m_next[d] = p.allowed(octet(1, d));
-#pragma unroll
-  for (int d = 0; d < kAhead; ++d) cur[d] = p.raw(octet(0, d), m[d] != 0);
-  for (int i = 0; i < batches; ++i) {
+  const auto group = [&](int i, int d) __attribute__((always_inline)) { return p.first + (i * kAhead + d) * 64 + lane; };
+  struct Batch {
+    typename E::Raw raw[kAhead];
+    uint32_t m[kAhead];
+  };
+  uint32_t m_next[kAhead];                                 // allowed bits are known a batch before the logits that they ask for
+  const auto load = [&](Batch& b, int i) __attribute__((always_inline)) {
 #pragma unroll
     for (int d = 0; d < kAhead; ++d) {
-      m_later[d] = p.allowed(octet(i + 2, d));
-      next[d] = p.raw(octet(i + 1, d), m_next[d] != 0);
+      b.m[d] = m_next[d];
+      b.raw[d] = p.raw(group(i, d), b.m[d] != 0);
     }
-    const bool plain = !MASKED && !TINY && p.first + (i + 1) * kAhead * 64 <= whole;
-    float x[kAhead][8], to = c;
+#pragma unroll
+    for (int d = 0; d < kAhead; ++d) m_next[d] = p.allowed(group(i + 1, d));
+  };
+  const auto add = [&](const Batch& b, int i) __attribute__((always_inline)) {
+    float x[kAhead][N];
+#pragma unroll
+    for (int d = 0; d < kAhead; ++d) E::unpack(b.raw[d], x[d]);
+    if (MASKED || TINY || p.first + (i + 1) * kAhead * 64 > whole) {
+#pragma unroll
+      for (int d = 0; d < kAhead; ++d) p.mask(x[d], group(i, d), b.m[d]);
+    }
 #pragma unroll
     for (int d = 0; d < kAhead; ++d) {
-      E::unpack(cur[d], x[d]);
-      if (!plain) p.mask(x[d], octet(i, d), m[d]);
-      const float top = fmaxf(fmaxf(fmaxf(x[d][0], x[d][1]), fmaxf(x[d][2], x[d][3])), fmaxf(fmaxf(x[d][4], x[d][5]), fmaxf(x[d][6], x[d][7])));
-      most_at = top > most ? octet(i, d) : most_at;
-      most = fmaxf(most, top);
+      float top = max3(x[d][0], x[d][1], x[d][2]);
+      if constexpr (N == 8) top = max3(max3(top, x[d][3], x[d][4]), max3(x[d][5], x[d][6], x[d][7]), -INFINITY);
+      else top = max3(top, x[d][3], x[d][3]);
+      most_at = top > most ? group(i, d) : most_at;
+      most = max3(most, top, top);
     }
-    to = fmaxf(to, most);
+    float to = max3(c, most, most);
+    if (i == 0) to = across<6>(to, Larger());
     const float by = __builtin_amdgcn_exp2f((c - to) * kLog2e);
     c = to;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) s[j] *= by;
+    for (int j = 0; j < N; ++j) s[j] *= by;
 #pragma unroll
     for (int d = 0; d < kAhead; ++d)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) s[j] += __builtin_amdgcn_exp2f((x[d][j] - c) * kLog2e);
+      for (int j = 0; j < N; ++j) s[j] += __builtin_amdgcn_exp2f((x[d][j] - c) * kLog2e);
+  };
+  Batch even, odd;                                         // the next one is under way while one is added; behind the last nothing counts
 #pragma unroll
-    for (int d = 0; d < kAhead; ++d) {
-      cur[d] = next[d];
-      m[d] = m_next[d];
-      m_next[d] = m_later[d];
-    }
+  for (int d = 0; d < kAhead; ++d) m_next[d] = p.allowed(group(0, d));
+  load(even, 0);
+  for (int i = 0; i < batches; i += 2) {
+    load(odd, i + 1);
+    add(even, i);
+    load(even, i + 2);
+    add(odd, i + 1);
   }
   a.most[at * 64 + lane] = most;
   a.most_at[at * 64 + lane] = most_at;
   const float ref = across<6>(c, Larger());
-  const double sum = wave_sum((double)(((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]))) * (double)__builtin_amdgcn_exp2f((c - ref) * kLog2e));
+  double of_lane = 0.0;
+#pragma unroll
+  for (int j = 0; j < N; ++j) of_lane += (double)s[j];
+  const double sum = wave_sum(of_lane * (double)__builtin_amdgcn_exp2f((c - ref) * kLog2e));
   if (lane == 0) {
     a.sums[at] = sum;
     a.refs[at] = ref;
@@ -293,7 +324,7 @@ __global__ __launch_bounds__(64) void select_rows_kernel(SelectArgs a) {
 // ---- a group's choice --------------------------------------------------------------------------
 
 // A logit, or a list by its largest, in the order of choices: by score, then row, logit (scores of one row are in the order of its logits even
-// where 64 bits cannot tell them apart), token or octet.  rest: row, logit from the largest down, token (24 bits).
+// where 64 bits cannot tell them apart), token or group.  rest: row, logit from the largest down, token (24 bits).
 struct Choice {
   double score;
   uint64_t rest;
@@ -304,7 +335,7 @@ constexpr uint64_t kNone = ~0ull;
 
 constexpr int kFound = 1024;           // choices that are sorted by counting what comes before each
 constexpr int kFoundLists = 512;
-constexpr int kQuads = 4;              // times four lists that a thread holds
+constexpr int kHeld = 16;              // lists that a thread holds
 
 // The best choice of what `each` shows to `see` in every thread, behind `last` (k > 0): the threads' best in `best`, then one of them.
 template <int THREADS, typename F>
@@ -329,23 +360,22 @@ __device__ __forceinline__ Choice next_best(Choice* best, int k, const Choice& l
 // requested at once and kept, so that a choice is three round trips: where the group's rows are, their lists, the logits looked at again.
 template <typename E, bool MASKED, bool TINY, int THREADS>
 __global__ __launch_bounds__(THREADS) void select_best_kernel(SelectArgs a, GroupRows g, int group0) {
-  static_assert(THREADS * kQuads * 4 >= 64 * kMostLists || THREADS == 256, "a thread holds its share of the lists");
+  static_assert(THREADS * kHeld >= 64 * kMostParts || THREADS == 256, "a thread holds its share of the lists");
   __shared__ double base[kBeamsMost];
-  __shared__ float from[kBeamsMost], subset[256];
+  __shared__ float from[kBeamsMost], subset[THREADS];
   __shared__ Choice list[kFoundLists], found[kFound];
   __shared__ int n_list, n_found;
   const int tid = threadIdx.x, K = a.n_best, bits = a.parts_bits, parts = 1 << bits;
   const int row0 = g.base + g.first[blockIdx.x], beams = g.first[blockIdx.x + 1] - g.first[blockIdx.x], all = beams << bits;
   const int64_t at0 = (int64_t)row0 << bits;
-  // Four neighbouring lists at a time: their row is one.
-  const int quads = all * 16, mine = min(tid, all - 1);
-  f32x4_t most[kQuads];
-  u32x4_t most_at[kQuads];
+  const int of_group = all * 64, mine = min(tid, all - 1);
+  float most[kHeld];
+  int most_at[kHeld];
 #pragma unroll
-  for (int i = 0; i < kQuads; ++i) {
-    const int q = min(tid + i * THREADS, quads - 1);
-    most[i] = ((const f32x4_t*)(a.most + at0 * 64))[q];
-    most_at[i] = ((const u32x4_t*)(a.most_at + at0 * 64))[q];
+  for (int i = 0; i < kHeld; ++i) {
+    const int l = min(tid + i * THREADS, of_group - 1);
+    most[i] = a.most[at0 * 64 + l];
+    most_at[i] = a.most_at[at0 * 64 + l];
   }
   const float ref = a.refs[at0 + mine], score = a.scores[row0 + (mine >> bits)];
   double sum = a.sums[at0 + mine];
@@ -366,33 +396,34 @@ __global__ __launch_bounds__(THREADS) void select_best_kernel(SelectArgs a, Grou
   __syncthreads();
   // scores as 32 bits round them, which keeps their order: at most K - 1 are above one that is below the K-th of any K
   const auto scored = [&](int row, float value) __attribute__((always_inline)) { return ((double)value - (double)from[row]) + base[row]; };
+  // The K-th largest of the 256 threads' values, or of as many subsets of four threads', or a little less.
+  const auto reached = [&](float top) __attribute__((always_inline)) {
+    subset[tid] = top;
+    __syncthreads();
+    float of[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int at = j * 64 + (tid & 63);
+      of[j] = subset[at];
+#pragma unroll
+      for (int more = 256; more < THREADS; more += 256) of[j] = fmaxf(of[j], subset[more + at]);
+    }
+    return reached_by(of, K, K + K / 8);
+  };
   float top = -INFINITY;
 #pragma unroll
-  for (int i = 0; i < kQuads; ++i)
-    if (tid + i * THREADS < quads)
-      top = fmaxf(top, (float)scored((tid + i * THREADS) >> (4 + bits), fmaxf(fmaxf(most[i][0], most[i][1]), fmaxf(most[i][2], most[i][3]))));
-  if constexpr (THREADS == 256) {
-    subset[tid] = top;
-  } else {
-    const float of_four = across<2>(top, Larger());
-    if ((tid & 3) == 0) subset[tid >> 2] = of_four;
-  }
-  __syncthreads();
-  const int lane = tid & 63;
-  const float four[4] = {subset[lane], subset[64 + lane], subset[128 + lane], subset[192 + lane]};
-  const float low = reached_by(four, K, K + K / 8);
+  for (int i = 0; i < kHeld; ++i)
+    if (tid + i * THREADS < of_group) top = fmaxf(top, (float)scored((tid + i * THREADS) >> (6 + bits), most[i]));
+  float low = reached(top);
 
   const auto see_lists = [&](auto see) __attribute__((always_inline)) {
     if (!(top >= low)) return;
 #pragma unroll
-    for (int i = 0; i < kQuads; ++i) {
-      const int q = tid + i * THREADS, row = q >> (4 + bits);
-      if (q >= quads) return;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const double s = scored(row, most[i][j]);
-        if ((float)s >= low) see(Choice{s, rest_of(row, most[i][j], (int)most_at[i][j])});
-      }
+    for (int i = 0; i < kHeld; ++i) {
+      const int l = tid + i * THREADS, row = l >> (6 + bits);
+      if (l >= of_group) return;
+      const double s = scored(row, most[i]);
+      if ((float)s >= low) see(Choice{s, rest_of(row, most[i], most_at[i])});
     }
   };
   see_lists([&](const Choice& x) __attribute__((always_inline)) {
@@ -411,40 +442,56 @@ __global__ __launch_bounds__(THREADS) void select_best_kernel(SelectArgs a, Grou
     __syncthreads();
   }
 
-  const int deep = (a.part_octets + 63) / 64, work = lists * deep;
-  const auto see_octets = [&](auto see) __attribute__((always_inline)) {
-    for (int w = tid; w < work; w += THREADS) {
-      const int l = w / deep;
+  // Lanes for a list: as many as it has groups, up to a wavefront.
+  constexpr int N = E::kGroup;
+  const int long_part = part_groups<E>(a), deep = (long_part + 63) / 64, wide = 32 - __builtin_clz(min(deep, 64) * 2 - 1) - 1;
+  const auto see_groups = [&](auto see) __attribute__((always_inline)) {
+    for (int l = tid >> wide; l < lists; l += THREADS >> wide) {
       const uint64_t rest = list[l].rest;
-      const int row = (int)(rest >> 56), best_at = (int)(rest & 0xffffff), first = best_at / a.part_octets * a.part_octets;
-      const int o = first + ((best_at - first) & 63) + (w - l * deep) * 64;
+      const int row = (int)(rest >> 56), best_at = (int)(rest & 0xffffff), first = best_at / long_part * long_part;
       const auto p = part_of<E, MASKED, TINY>(a, row0 + row, first);
-      if (o >= p.end) continue;
-      float x[8];
-      p.read(o, x);
+#pragma unroll 2
+      for (int o = first + ((best_at - first) & 63) + (tid & ((1 << wide) - 1)) * 64; o < p.end; o += 64 << wide) {
+        float x[N];
+        p.read(o, x);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const double s = scored(row, x[j]);
-        if ((float)s >= low) see(Choice{s, rest_of(row, x[j], p.token(o, j))});
+        for (int j = 0; j < N; ++j) {
+          const double s = scored(row, x[j]);
+          if ((float)s >= low) see(Choice{s, rest_of(row, x[j], p.token(o, j))});
+        }
       }
     }
   };
-  see_octets([&](const Choice& x) __attribute__((always_inline)) {
-    const int to = atomicAdd(&n_found, 1);
-    if (to < kFound) found[to] = x;
-  });
-  __syncthreads();
+  // What reaches it, or, where that is too much, the K-th largest of what the threads see of it.
+  int n;
+  for (int turn = 0;; ++turn) {
+    float seen = -INFINITY;
+    see_groups([&](const Choice& x) __attribute__((always_inline)) {
+      const int to = atomicAdd(&n_found, 1);
+      if (to < kFound) found[to] = x;
+      seen = fmaxf(seen, (float)x.score);
+    });
+    __syncthreads();
+    n = n_found;
+    if (n <= kFound || turn == 3) break;
+    const float higher = reached(seen);
+    if (!(higher > low)) break;
+    low = higher;
+    __syncthreads();                                       // everyone has read the subsets, and what was found
+    if (tid == 0) n_found = 0;
+    __syncthreads();
+  }
   const int64_t out = (int64_t)(group0 + blockIdx.x) * K;
   const auto write = [&](int k, const Choice& x) __attribute__((always_inline)) {
     a.best_scores[out + k] = (float)x.score;
     a.best_beams[out + k] = (int)(x.rest >> 56);
     a.best_tokens[out + k] = (int)(x.rest & 0xffffff);
   };
-  int n = n_found;
   if (n <= kFound) {
     for (int i = tid; i < n; i += THREADS) {
       const Choice x = found[i];
       int rank = 0;
+#pragma unroll 8
       for (int k = 0; k < n; ++k) rank += before(found[k], x);
       if (rank < K) write(rank, x);
     }
@@ -452,7 +499,7 @@ __global__ __launch_bounds__(THREADS) void select_best_kernel(SelectArgs a, Grou
     n = K;
     Choice last = {};
     for (int k = 0; k < K; ++k) {
-      last = next_best<THREADS>(found, k, last, see_octets);
+      last = next_best<THREADS>(found, k, last, see_groups);
       if (tid == 0) write(k, last);
     }
   }
@@ -519,11 +566,11 @@ template <typename E, bool MASKED, bool TINY>
 void launch_best(const SelectArgs& a, const GroupRows& g, int32_t group0, int32_t n_groups, hipStream_t st) {
   int most = 0;                                            // parts of the largest group
   for (int32_t i = 0; i < n_groups; ++i) most = std::max(most, (g.first[i + 1] - g.first[i]) * a.parts);
-  if (most * 64 <= 256 * kQuads * 4) select_best_kernel<E, MASKED, TINY, 256><<<dim3((unsigned)n_groups), dim3(256), 0, st>>>(a, g, group0);
+  if (most * 64 <= 256 * kHeld) select_best_kernel<E, MASKED, TINY, 256><<<dim3((unsigned)n_groups), dim3(256), 0, st>>>(a, g, group0);
   else select_best_kernel<E, MASKED, TINY, 1024><<<dim3((unsigned)n_groups), dim3(1024), 0, st>>>(a, g, group0);
 }
 #define SYM_OF_TYPE(launch, E, ...)                                                     \
-  (a.vocab < kOctet ? (a.allowed ? launch<E, true, true>(__VA_ARGS__) : launch<E, false, true>(__VA_ARGS__)) \
+  (a.vocab < E::kGroup ? (a.allowed ? launch<E, true, true>(__VA_ARGS__) : launch<E, false, true>(__VA_ARGS__)) \
                     : (a.allowed ? launch<E, true, false>(__VA_ARGS__) : launch<E, false, false>(__VA_ARGS__)))
 #define SYM_OF_STEP(launch, ...)                                        \
   (dtype == SYM_F32    ? SYM_OF_TYPE(launch, LogitF32, __VA_ARGS__)     \

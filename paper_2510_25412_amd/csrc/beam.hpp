@@ -15,8 +15,8 @@ struct GroupRows {
   int32_t first[kGroupsAtOnce + 1];    // rows before each group, from there on
 };
 
-constexpr int kOctet = 8;              // logits that a lane takes at a time
-constexpr int kMostLists = 256;        // parts of a group that its choice starts from
+constexpr int kOctet = 8;              // what a row is cut by, in logits
+constexpr int kMostParts = 256;        // parts of a group that its choice starts from
 struct SelectArgs {
   const void* logits;
   int64_t stride;                      // elements from row to row
@@ -27,13 +27,13 @@ struct SelectArgs {
   int32_t* best_beams;
   int32_t* best_tokens;
   // scratch, [rows][parts]: the logit that exponents are counted from, their sum; [rows][parts][64]: the largest logit of each lane, and the
-  // octet that holds it first
+  // group of 16 bytes that holds it first
   double* sums;
   float* refs;
   float* most;
   int32_t* most_at;
   int32_t rows, vocab, n_best;
-  int32_t parts, parts_bits, part_octets;      // wavefronts of a row (a power of two), octets of each
+  int32_t parts, parts_bits, part_octets;      // wavefronts of a row (a power of two), octets of logits of each
 };
 
 // How a row is cut: a power of two of parts, octets of a part.
@@ -41,10 +41,11 @@ struct SelectCut {
   int32_t bits, part_octets;
 };
 constexpr int kSelectWaves = 4096;
-inline SelectCut select_cut(int64_t rows, int32_t most_beams, int32_t vocab) {
-  const int64_t octets = (vocab + kOctet - 1) / kOctet, want = (kSelectWaves + rows - 1) / rows, most = std::min<int64_t>(kMostLists / most_beams, 64);
+inline SelectCut select_cut(int64_t rows, int32_t most_beams, int32_t vocab, int32_t n_best) {
+  const int64_t octets = (vocab + kOctet - 1) / kOctet, want = (kSelectWaves + rows - 1) / rows, most = std::min<int64_t>(kMostParts / most_beams, 64);
   int32_t bits = 0;
-  while ((2ll << bits) <= most && (1ll << bits) < want && (octets >> bits) > 256) ++bits;
+  // enough lists that the best of one row's are a choice's, then wavefronts, but none of less than 2048 logits
+  while ((2ll << bits) <= most && ((32ll << bits) < n_best || ((1ll << bits) < want && (octets >> bits) > 256))) ++bits;
   return SelectCut{bits, (int32_t)((((octets + (1ll << bits) - 1) >> bits) + 63) / 64 * 64)};
 }
 

@@ -1851,8 +1851,8 @@ int32_t group_rows(int32_t n_groups, const int32_t* beams, int32_t g0, int32_t r
   for (int32_t i = 0; i < n; ++i) g->first[i + 1] = g->first[i] + beams[g0 + i];
   return n;
 }
-int64_t select_scratch(int64_t rows, int32_t most, int32_t vocab) {
-  const int64_t parts = rows << select_cut(rows, most, vocab).bits;
+int64_t select_scratch(int64_t rows, int32_t most, int32_t vocab, int32_t n_best) {
+  const int64_t parts = rows << select_cut(rows, most, vocab, n_best).bits;
   return align_up(parts * 8, 16) + align_up(parts * 4, 16) + 2 * parts * 64 * 4;
 }
 static_assert(kBeamsMost == SYM_BEAMS_MOST && kBestMost == SYM_BEST_MOST, "the header's limits");
@@ -1863,7 +1863,7 @@ int64_t sym_beam_scratch_bytes(int32_t n_groups, const int32_t* beams, int32_t v
   int32_t most;
   const int64_t rows = count_rows(n_groups, beams, &most);
   if (rows < 0 || vocab < 1 || vocab > (1 << 24) || n_best < 1 || n_best > kBestMost) return SYM_EINVAL;
-  return rows == 0 ? 0 : select_scratch(rows, most, vocab);
+  return rows == 0 ? 0 : select_scratch(rows, most, vocab, n_best);
 }
 
 int sym_beam_select(sym_ctx* c, const sym_beam_step* b, void* stream) {
@@ -1880,7 +1880,7 @@ int sym_beam_select(sym_ctx* c, const sym_beam_step* b, void* stream) {
     if (stride < b->vocab || stride > (int64_t)1 << 40) return fail(c, SYM_EINVAL, "beam_select: rows of logits overlap, or lie too far apart");
     if (b->allowed && (bit_stride < words || bit_stride > (int64_t)1 << 40)) return fail(c, SYM_EINVAL, "beam_select: rows of allowed tokens overlap, or lie too far apart");
     if (rows == 0) return SYM_OK;
-    const int64_t es = b->dtype == SYM_F32 ? 4 : 2, scratch = select_scratch(rows, most, b->vocab), out = (int64_t)b->n_groups * b->n_best * 4;
+    const int64_t es = b->dtype == SYM_F32 ? 4 : 2, scratch = select_scratch(rows, most, b->vocab, b->n_best), out = (int64_t)b->n_groups * b->n_best * 4;
     if (!b->logits || !b->scores || !b->best_scores || !b->best_beams || !b->best_tokens || !b->scratch) return fail(c, SYM_EINVAL, "beam_select: a pointer is missing");
     if (!aligned(b->logits, (uintptr_t)es) || !aligned(b->scores, 4) || !aligned(b->allowed, 4) || !aligned(b->best_scores, 4) || !aligned(b->best_beams, 4) ||
         !aligned(b->best_tokens, 4) || !aligned(b->scratch, 16))
@@ -1899,7 +1899,7 @@ int sym_beam_select(sym_ctx* c, const sym_beam_step* b, void* stream) {
     if (!launch_select_rows || !stream_captures) return fail(c, SYM_EHIP, "beam_select: this build has no kernels");
     const OnDevice on(c);
     hipStream_t st = (hipStream_t)stream;
-    const SelectCut cut = select_cut(rows, most, b->vocab);
+    const SelectCut cut = select_cut(rows, most, b->vocab, b->n_best);
     const int64_t parts = rows << cut.bits;
     uint8_t* at = (uint8_t*)b->scratch;
     const auto take = [&](int64_t bytes) {
