@@ -335,6 +335,9 @@ constexpr uint64_t kNone = ~0ull;
 
 constexpr int kFound = 1024;           // choices that are sorted by counting what comes before each
 constexpr int kFoundLists = 512;
+struct RowScore {
+  double base, from;
+};
 constexpr int kHeld = 16;              // lists that a thread holds
 
 // The best choice of what `each` shows to `see` in every thread, behind `last` (k > 0): the threads' best in `best`, then one of them.
@@ -361,8 +364,8 @@ __device__ __forceinline__ Choice next_best(Choice* best, int k, const Choice& l
 template <typename E, bool MASKED, bool TINY, int THREADS>
 __global__ __launch_bounds__(THREADS) void select_best_kernel(SelectArgs a, GroupRows g, int group0) {
   static_assert(THREADS * kHeld >= 64 * kMostParts || THREADS == 256, "a thread holds its share of the lists");
-  __shared__ double base[kBeamsMost];
-  __shared__ float from[kBeamsMost], subset[THREADS];
+  __shared__ RowScore rows[kBeamsMost];
+  __shared__ float subset[THREADS];
   __shared__ Choice list[kFoundLists], found[kFound];
   __shared__ int n_list, n_found;
   const int tid = threadIdx.x, K = a.n_best, bits = a.parts_bits, parts = 1 << bits;
@@ -389,13 +392,12 @@ __global__ __launch_bounds__(THREADS) void select_best_kernel(SelectArgs a, Grou
     for (int d = 1; d < parts; d <<= 1) sum += __shfl_xor(sum, d);
     const double b = (double)score - log(sum);
     if (tid < all && (tid & (parts - 1)) == 0) {
-      base[tid >> bits] = sum > 0.0 && fabs(b) < (double)INFINITY ? b : -(double)INFINITY;
-      from[tid >> bits] = c;
+      rows[tid >> bits] = RowScore{sum > 0.0 && fabs(b) < (double)INFINITY ? b : -(double)INFINITY, (double)c};
     }
   }
   __syncthreads();
   // scores as 32 bits round them, which keeps their order: at most K - 1 are above one that is below the K-th of any K
-  const auto scored = [&](int row, float value) __attribute__((always_inline)) { return ((double)value - (double)from[row]) + base[row]; };
+  const auto scored = [&](int row, float value) __attribute__((always_inline)) { return ((double)value - rows[row].from) + rows[row].base; };
   // The K-th largest of the 256 threads' values, or of as many subsets of four threads', or a little less.
   const auto reached = [&](float top) __attribute__((always_inline)) {
     subset[tid] = top;
@@ -410,20 +412,23 @@ __global__ __launch_bounds__(THREADS) void select_best_kernel(SelectArgs a, Grou
     }
     return reached_by(of, K, K + K / 8);
   };
-  float top = -INFINITY;
+  float top = -INFINITY, score_of[kHeld];
 #pragma unroll
-  for (int i = 0; i < kHeld; ++i)
-    if (tid + i * THREADS < of_group) top = fmaxf(top, (float)scored((tid + i * THREADS) >> (6 + bits), most[i]));
+  for (int i = 0; i < kHeld; ++i) {
+    const int l = tid + i * THREADS;
+    score_of[i] = l < of_group ? (float)scored(l >> (6 + bits), most[i]) : -INFINITY;
+    top = fmaxf(top, score_of[i]);
+  }
   float low = reached(top);
 
   const auto see_lists = [&](auto see) __attribute__((always_inline)) {
     if (!(top >= low)) return;
 #pragma unroll
     for (int i = 0; i < kHeld; ++i) {
-      const int l = tid + i * THREADS, row = l >> (6 + bits);
-      if (l >= of_group) return;
-      const double s = scored(row, most[i]);
-      if ((float)s >= low) see(Choice{s, rest_of(row, most[i], most_at[i])});
+      if (score_of[i] >= low) {
+        const int row = (tid + i * THREADS) >> (6 + bits);
+        see(Choice{scored(row, most[i]), rest_of(row, most[i], most_at[i])});
+      }
     }
   };
   see_lists([&](const Choice& x) __attribute__((always_inline)) {
@@ -488,12 +493,14 @@ __global__ __launch_bounds__(THREADS) void select_best_kernel(SelectArgs a, Grou
     a.best_tokens[out + k] = (int)(x.rest & 0xffffff);
   };
   if (n <= kFound) {
-    for (int i = tid; i < n; i += THREADS) {
+    for (int i = tid >> 2; i < n; i += THREADS / 4) {       // four lanes count for each
       const Choice x = found[i];
       int rank = 0;
-#pragma unroll 8
-      for (int k = 0; k < n; ++k) rank += before(found[k], x);
-      if (rank < K) write(rank, x);
+#pragma unroll 4
+      for (int k = tid & 3; k < n; k += 4) rank += before(found[k], x);
+      rank += __builtin_amdgcn_update_dpp(0, rank, 0xB1, 0xf, 0xf, false);
+      rank += __builtin_amdgcn_update_dpp(0, rank, 0x4E, 0xf, 0xf, false);
+      if (rank < K && (tid & 3) == 0) write(rank, x);
     }
   } else {                                                 // many large ones in few lists: one after the other
     n = K;
@@ -566,7 +573,9 @@ template <typename E, bool MASKED, bool TINY>
 void launch_best(const SelectArgs& a, const GroupRows& g, int32_t group0, int32_t n_groups, hipStream_t st) {
   int most = 0;                                            // parts of the largest group
   for (int32_t i = 0; i < n_groups; ++i) most = std::max(most, (g.first[i + 1] - g.first[i]) * a.parts);
-  if (most * 64 <= 256 * kHeld) select_best_kernel<E, MASKED, TINY, 256><<<dim3((unsigned)n_groups), dim3(256), 0, st>>>(a, g, group0);
+  // four times the threads where they would otherwise hold too many lists, or look at more than four groups each
+  const int deep = a.part_octets * (kOctet / E::kGroup) / 64;
+  if (most * 64 <= 256 * kHeld && a.n_best * deep <= 4 * 256) select_best_kernel<E, MASKED, TINY, 256><<<dim3((unsigned)n_groups), dim3(256), 0, st>>>(a, g, group0);
   else select_best_kernel<E, MASKED, TINY, 1024><<<dim3((unsigned)n_groups), dim3(1024), 0, st>>>(a, g, group0);
 }
 #define SYM_OF_TYPE(launch, E, ...)                                                     \

@@ -44,8 +44,8 @@ constexpr int kSelectWaves = 4096;
 inline SelectCut select_cut(int64_t rows, int32_t most_beams, int32_t vocab, int32_t n_best) {
   const int64_t octets = (vocab + kOctet - 1) / kOctet, want = (kSelectWaves + rows - 1) / rows, most = std::min<int64_t>(kMostParts / most_beams, 64);
   int32_t bits = 0;
-  // enough lists that the best of one row's are a choice's, then wavefronts, but none of less than 2048 logits
-  while ((2ll << bits) <= most && ((32ll << bits) < n_best || ((1ll << bits) < want && (octets >> bits) > 256))) ++bits;
+  // enough lists that the best of one row's are a choice's; then wavefronts, of no more than 8192 logits and no less than 2048
+  while ((2ll << bits) <= most && ((32ll << bits) < n_best || ((octets >> bits) > 256 && ((1ll << bits) < want || (octets >> bits) > 1280)))) ++bits;
   return SelectCut{bits, (int32_t)((((octets + (1ll << bits) - 1) >> bits) + 63) / 64 * 64)};
 }
 
