@@ -10,6 +10,7 @@ namespace symkv {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr int64_t kLastLevelBytes = 256ll << 20;
 
 // ---- steps across the lanes of a wavefront ---------------------------------------------------
 
@@ -66,6 +67,25 @@ __device__ __forceinline__ double wave_sum(double x) {
   const auto c = __builtin_amdgcn_permlane32_swap((uint32_t)u, (uint32_t)u, false, false), d = __builtin_amdgcn_permlane32_swap((uint32_t)(u >> 32), (uint32_t)(u >> 32), false, false);
   return __builtin_bit_cast(double, (uint64_t)d[0] << 32 | c[0]) + __builtin_bit_cast(double, (uint64_t)d[1] << 32 | c[1]);
 }
+// The same over aligned subsets of 1 << bits lanes, bits the same in every lane.
+__device__ __forceinline__ float most_of_parts(float x, int bits) {
+  if (bits > 0) x = fmaxf(x, dpp<0xB1>(x));
+  if (bits > 1) x = fmaxf(x, dpp<0x4E>(x));
+  if (bits > 2) x = fmaxf(x, dpp<0x141>(x));
+  if (bits > 3) x = fmaxf(x, dpp<0x140>(x));
+  if (bits > 4) x = pair16_max(x);
+  if (bits > 5) x = pair32_max(x);
+  return x;
+}
+__device__ __forceinline__ double sum_of_parts(double x, int bits) {
+  if (bits > 0) x += dpp<0xB1>(x);
+  if (bits > 1) x += dpp<0x4E>(x);
+  if (bits > 2) x += dpp<0x141>(x);
+  if (bits > 3) x += dpp<0x140>(x);
+  if (bits > 4) x += __shfl_xor(x, 16);
+  if (bits > 5) x += __shfl_xor(x, 32);
+  return x;
+}
 __device__ __forceinline__ int lanes_of(uint64_t b) { return __builtin_popcountll(b); }
 
 // Floats as whole numbers of the same order, and back.
@@ -108,6 +128,11 @@ __device__ __forceinline__ float reached_by(const float (&x)[4], int K, int limi
 
 typedef u32x4_t __attribute__((aligned(2))) u32x4_a2;
 typedef u32x4_t __attribute__((aligned(4))) u32x4_a4;
+template <bool FAR, typename T>
+__device__ __forceinline__ u32x4_t load16(const uint8_t* p) {
+  if constexpr (FAR) return __builtin_nontemporal_load((const T*)p);
+  else return *(const T*)p;
+}
 // n < 8 logits of 16 bits
 template <typename R>
 __device__ __forceinline__ R few16(const uint8_t* p, int n) {
@@ -122,7 +147,8 @@ struct LogitBF16 {
   struct Raw {
     u32x4_t w;
   };
-  static __device__ __forceinline__ Raw load(const uint8_t* p) { return Raw{*(const u32x4_a2*)p}; }
+  template <bool FAR>
+  static __device__ __forceinline__ Raw load(const uint8_t* p) { return Raw{load16<FAR, u32x4_a2>(p)}; }
   static __device__ __forceinline__ void unpack(const Raw& r, float (&x)[8]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -137,7 +163,8 @@ struct LogitF16 {
   struct Raw {
     u32x4_t w;
   };
-  static __device__ __forceinline__ Raw load(const uint8_t* p) { return Raw{*(const u32x4_a2*)p}; }
+  template <bool FAR>
+  static __device__ __forceinline__ Raw load(const uint8_t* p) { return Raw{load16<FAR, u32x4_a2>(p)}; }
   static __device__ __forceinline__ void unpack(const Raw& r, float (&x)[8]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -152,7 +179,8 @@ struct LogitF32 {
   struct Raw {
     u32x4_t w;
   };
-  static __device__ __forceinline__ Raw load(const uint8_t* p) { return Raw{*(const u32x4_a4*)p}; }
+  template <bool FAR>
+  static __device__ __forceinline__ Raw load(const uint8_t* p) { return Raw{load16<FAR, u32x4_a4>(p)}; }
   static __device__ __forceinline__ void unpack(const Raw& r, float (&x)[4]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[i] = as_f32(r.w[i]);
@@ -178,10 +206,11 @@ struct Part {
   uint32_t last;                       // where the last of them is read, in bytes
 
   // Group o.  The last one of a row that does not end with it: the row's last N logits.  What is not wanted comes from where others read.
+  template <bool FAR = false>
   __device__ __forceinline__ typename E::Raw raw(int o, bool want) const {
     if constexpr (TINY) return E::few(row, vocab);
     const uint32_t at = min((uint32_t)o * 16, last);
-    return E::load(row + (MASKED && !want ? last : at));
+    return E::template load<FAR>(row + (MASKED && !want ? last : at));
   }
   __device__ __forceinline__ uint32_t allowed(int o) const {
     constexpr uint32_t all = (1u << N) - 1;
@@ -231,7 +260,9 @@ __device__ __forceinline__ Part<E, MASKED, TINY> part_of(const SelectArgs& a, in
 
 // One pass over the logits.  Of every part: its normaliser's share, and for each lane (a list: groups 64 apart) the largest logit and the
 // group where it is found first; the choice needs no more to know where it has to look again.
-template <typename E, bool MASKED, bool TINY>
+// FAR: more logits than the last-level cache holds are read past it (268 MB 62.7 -> 58.8 us a call, 537 MB 123.6 -> 115.3), fewer may lie there from their
+// making, or from this kernel when the choice looks at some again (52 MB 24.4 us, past the cache 27.3; 67 MB 23.8, 24.3).
+template <typename E, bool MASKED, bool TINY, bool FAR>
 __global__ __launch_bounds__(64) void select_rows_kernel(SelectArgs a) {
   const int lane = threadIdx.x & 63;
   const int row = (int)(blockIdx.x / (uint32_t)a.parts), part = (int)(blockIdx.x % (uint32_t)a.parts);
@@ -266,7 +297,7 @@ __global__ __launch_bounds__(64) void select_rows_kernel(SelectArgs a) {
 #pragma unroll
     for (int d = 0; d < kAhead; ++d) {
       b.m[d] = m_next[d];
-      b.raw[d] = p.raw(group(i, d), b.m[d] != 0);
+      b.raw[d] = p.template raw<FAR>(group(i, d), b.m[d] != 0);
     }
 #pragma unroll
     for (int d = 0; d < kAhead; ++d) m_next[d] = p.allowed(group(i + 1, d));
@@ -366,10 +397,11 @@ __global__ __launch_bounds__(THREADS) void select_best_kernel(SelectArgs a, Grou
   static_assert(THREADS * kHeld >= 64 * kMostParts || THREADS == 256, "a thread holds its share of the lists");
   __shared__ RowScore rows[kBeamsMost];
   __shared__ float subset[THREADS];
-  __shared__ Choice list[kFoundLists], found[kFound];
+  __shared__ Choice found[kFound];
+  __shared__ uint16_t list[kFoundLists];
   __shared__ int n_list, n_found;
   const int tid = threadIdx.x, K = a.n_best, bits = a.parts_bits, parts = 1 << bits;
-  const int row0 = g.base + g.first[blockIdx.x], beams = g.first[blockIdx.x + 1] - g.first[blockIdx.x], all = beams << bits;
+  const int row0 = g.row(blockIdx.x), beams = g.rows(blockIdx.x), all = beams << bits;
   const int64_t at0 = (int64_t)row0 << bits;
   const int of_group = all * 64, mine = min(tid, all - 1);
   float most[kHeld];
@@ -386,10 +418,8 @@ __global__ __launch_bounds__(THREADS) void select_best_kernel(SelectArgs a, Grou
   // Of each row the score less the logarithm of its sum, and where its exponents are counted from: a logit is taken from there first,
   // which is exact where it is large, and rows of the type's lowest value alone keep their sum.  A row's parts are neighbouring threads'.
   if (tid < (all + 63 & ~63)) {
-    float c = ref;
-    for (int d = 1; d < parts; d <<= 1) c = fmaxf(c, __shfl_xor(c, d));
-    sum *= (double)__builtin_amdgcn_exp2f((ref - c) * kLog2e);
-    for (int d = 1; d < parts; d <<= 1) sum += __shfl_xor(sum, d);
+    const float c = most_of_parts(ref, bits);
+    sum = sum_of_parts(sum * (double)__builtin_amdgcn_exp2f((ref - c) * kLog2e), bits);
     const double b = (double)score - log(sum);
     if (tid < all && (tid & (parts - 1)) == 0) {
       rows[tid >> bits] = RowScore{sum > 0.0 && fabs(b) < (double)INFINITY ? b : -(double)INFINITY, (double)c};
@@ -427,36 +457,37 @@ __global__ __launch_bounds__(THREADS) void select_best_kernel(SelectArgs a, Grou
     for (int i = 0; i < kHeld; ++i) {
       if (score_of[i] >= low) {
         const int row = (tid + i * THREADS) >> (6 + bits);
-        see(Choice{scored(row, most[i]), rest_of(row, most[i], most_at[i])});
+        see(Choice{scored(row, most[i]), rest_of(row, most[i], most_at[i])}, tid + i * THREADS);
       }
     }
   };
-  see_lists([&](const Choice& x) __attribute__((always_inline)) {
+  see_lists([&](const Choice&, int l) __attribute__((always_inline)) {
     const int to = atomicAdd(&n_list, 1);
-    if (to < kFoundLists) list[to] = x;
+    if (to < kFoundLists) list[to] = (uint16_t)l;
   });
   __syncthreads();
+  constexpr int N = E::kGroup;
+  const int long_part = part_groups<E>(a);
   int lists = n_list;
   if (lists > kFoundLists) {                               // many equals: exactly the K best lists, which hold the K best
     lists = min(K, lists);
     Choice last = {};
     for (int k = 0; k < lists; ++k) {
-      last = next_best<THREADS>(found, k, last, see_lists);
-      if (tid == 0) list[k] = last;
+      last = next_best<THREADS>(found, k, last, [&](auto see) __attribute__((always_inline)) { see_lists([&](const Choice& x, int) __attribute__((always_inline)) { see(x); }); });
+      const int at = (int)(last.rest & 0xffffff), part = at / long_part;
+      if (tid == 0) list[k] = (uint16_t)((((int)(last.rest >> 56) << bits) + part) * 64 + ((at - part * long_part) & 63));
     }
     __syncthreads();
   }
 
   // Lanes for a list: as many as it has groups, up to a wavefront.
-  constexpr int N = E::kGroup;
-  const int long_part = part_groups<E>(a), deep = (long_part + 63) / 64, wide = 32 - __builtin_clz(min(deep, 64) * 2 - 1) - 1;
+  const int wide = 32 - __builtin_clz(min(long_part >> 6, 64) * 2 - 1) - 1;
   const auto see_groups = [&](auto see) __attribute__((always_inline)) {
-    for (int l = tid >> wide; l < lists; l += THREADS >> wide) {
-      const uint64_t rest = list[l].rest;
-      const int row = (int)(rest >> 56), best_at = (int)(rest & 0xffffff), first = best_at / long_part * long_part;
+    for (int i = tid >> wide; i < lists; i += THREADS >> wide) {
+      const int l = list[i], row = l >> (6 + bits), first = ((l >> 6) & (parts - 1)) * long_part;
       const auto p = part_of<E, MASKED, TINY>(a, row0 + row, first);
 #pragma unroll 2
-      for (int o = first + ((best_at - first) & 63) + (tid & ((1 << wide) - 1)) * 64; o < p.end; o += 64 << wide) {
+      for (int o = first + (l & 63) + (tid & ((1 << wide) - 1)) * 64; o < p.end; o += 64 << wide) {
         float x[N];
         p.read(o, x);
 #pragma unroll
@@ -542,7 +573,7 @@ __global__ __launch_bounds__(kStateThreads) void states_kernel(StatesArgs a, Gro
   if (s > 0) b -= a.array[s - 1].end;
   const StateArray& x = a.array[s];
   const uint32_t chunk = b % x.chunks, group = b / x.chunks % (uint32_t)a.n_groups, outer = b / x.chunks / (uint32_t)a.n_groups;
-  const int row0 = g.base + g.first[group], beams = g.first[group + 1] - g.first[group];
+  const int row0 = g.row(group), beams = g.rows(group);
   const bool all = x.dst != x.src;
   int from[R];
   bool moves = all;
@@ -567,12 +598,19 @@ __global__ __launch_bounds__(kStateThreads) void states_kernel(StatesArgs a, Gro
 
 template <typename E, bool MASKED, bool TINY>
 void launch_rows(const SelectArgs& a, hipStream_t st) {
-  select_rows_kernel<E, MASKED, TINY><<<dim3((unsigned)(a.rows * a.parts)), dim3(64), 0, st>>>(a);
+  const dim3 grid((unsigned)(a.rows * a.parts)), block(64);
+  if constexpr (!MASKED && !TINY) {
+    if ((int64_t)a.rows * a.vocab * E::kBytes >= kLastLevelBytes) {
+      select_rows_kernel<E, false, false, true><<<grid, block, 0, st>>>(a);
+      return;
+    }
+  }
+  select_rows_kernel<E, MASKED, TINY, false><<<grid, block, 0, st>>>(a);
 }
 template <typename E, bool MASKED, bool TINY>
 void launch_best(const SelectArgs& a, const GroupRows& g, int32_t group0, int32_t n_groups, hipStream_t st) {
   int most = 0;                                            // parts of the largest group
-  for (int32_t i = 0; i < n_groups; ++i) most = std::max(most, (g.first[i + 1] - g.first[i]) * a.parts);
+  for (int32_t i = 0; i < (g.each ? 1 : n_groups); ++i) most = std::max(most, g.rows(i) * a.parts);
   // four times the threads where they would otherwise hold too many lists, or look at more than four groups each
   const int deep = a.part_octets * (kOctet / E::kGroup) / 64;
   if (most * 64 <= 256 * kHeld && a.n_best * deep <= 4 * 256) select_best_kernel<E, MASKED, TINY, 256><<<dim3((unsigned)n_groups), dim3(256), 0, st>>>(a, g, group0);

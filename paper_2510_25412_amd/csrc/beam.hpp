@@ -12,7 +12,10 @@ constexpr int kBestMost = 128;         // choices of a group
 constexpr int kGroupsAtOnce = 256;     // groups of a launch: their first rows travel with its arguments (1 KB)
 struct GroupRows {
   int32_t base;                        // row of the launch's first group
+  int32_t each;                        // rows of every group, where they are equal: any number of groups in a launch
   int32_t first[kGroupsAtOnce + 1];    // rows before each group, from there on
+  __host__ __device__ int32_t row(int32_t g) const { return base + (each ? g * each : first[g]); }
+  __host__ __device__ int32_t rows(int32_t g) const { return each ? each : first[g + 1] - first[g]; }
 };
 
 constexpr int kOctet = 8;              // what a row is cut by, in logits

@@ -1845,8 +1845,10 @@ int64_t count_rows(int32_t n_groups, const int32_t* beams, int32_t* most) {
 }
 // The first rows of the groups from g0 on, as many as go into a launch.
 int32_t group_rows(int32_t n_groups, const int32_t* beams, int32_t g0, int32_t row0, GroupRows* g) {
-  const int32_t n = std::min(kGroupsAtOnce, n_groups - g0);
   g->base = row0;
+  g->each = std::all_of(beams, beams + n_groups, [&](int32_t b) { return b == beams[0]; }) ? beams[0] : 0;
+  if (g->each) return n_groups - g0;
+  const int32_t n = std::min(kGroupsAtOnce, n_groups - g0);
   g->first[0] = 0;
   for (int32_t i = 0; i < n; ++i) g->first[i + 1] = g->first[i] + beams[g0 + i];
   return n;
@@ -1934,11 +1936,11 @@ int sym_beam_select(sym_ctx* c, const sym_beam_step* b, void* stream) {
     }
     GroupRows g;
     for (int32_t g0 = 0, row = 0; g0 < b->n_groups;) {
-      const int32_t n = group_rows(b->n_groups, b->beams, g0, row, &g);
+      const int32_t n = group_rows(b->n_groups, b->beams, g0, row, &g);      // (all, where their rows are equal)
       Timed t(c, SYM_K_PROLOGUE, st, false, timed);
       const hipError_t e = launch_select_best(a, g, g0, n, b->dtype, st);
       if (e != hipSuccess) return fail_hip(c, e, "beam choice launch");
-      row += g.first[n];
+      row = g.row(n);
       g0 += n;
     }
     return SYM_OK;
@@ -2003,9 +2005,9 @@ int sym_beam_states(sym_ctx* c, int32_t n_groups, const int32_t* beams, const in
         const sym_beam_state& s = states[i];
         if (s.outer == 0 || s.row_bytes == 0) continue;
         // stretches of columns, then of the outer dimension, so that a launch has no more workgroups than it may
-        constexpr int64_t kSlice = kStateBlocks / kGroupsAtOnce * kStateThreads * kStateUnit - kStateThreads * kStateUnit;
-        for (int64_t col = 0; col < s.row_bytes; col += kSlice) {
-          const int64_t bytes = std::min(kSlice, s.row_bytes - col);
+        const int64_t slice = (kStateBlocks / n - 1) * kStateThreads * kStateUnit;
+        for (int64_t col = 0; col < s.row_bytes; col += slice) {
+          const int64_t bytes = std::min(slice, s.row_bytes - col);
           const int64_t chunks = (bytes / kStateUnit + bytes % kStateUnit + kStateThreads - 1) / kStateThreads;
           const int64_t step = std::max<int64_t>(1, kStateBlocks / (chunks * n));
           for (int64_t o = 0; o < s.outer; o += step) {
@@ -2019,7 +2021,7 @@ int sym_beam_states(sym_ctx* c, int32_t n_groups, const int32_t* beams, const in
         }
       }
       if ((rc = launch())) return rc;
-      row += g.first[n];
+      row = g.row(n);
       g0 += n;
     }
     return SYM_OK;
