@@ -43,7 +43,7 @@ struct SelectArgs {
 struct SelectCut {
   int32_t bits, part_octets;
 };
-constexpr int kSelectWaves = 4096;
+constexpr int kSelectWaves = 2048;
 inline SelectCut select_cut(int64_t rows, int32_t most_beams, int32_t vocab, int32_t n_best) {
   const int64_t octets = (vocab + kOctet - 1) / kOctet, want = (kSelectWaves + rows - 1) / rows, most = std::min<int64_t>(kMostParts / most_beams, 64);
   int32_t bits = 0;

@@ -2,6 +2,7 @@
 #include "kvfs.hpp"
 
 #include <algorithm>
+#include <cstring>
 #include <numeric>
 
 #include "../../include/symphony_kv.h"
@@ -94,12 +95,12 @@ int32_t Kvfs::new_file() {
 
 int32_t Kvfs::new_handle(int32_t file_id) {
   int32_t h;
-  if (!free_handles_.empty()) {
-    h = free_handles_.top();               // lowest free handle slot
-    free_handles_.pop();
+  if (free_handles_.size()) {
+    h = free_handles_.pop_lowest();        // lowest free handle slot
   } else {
     h = (int32_t)handle_file_.size();
     handle_file_.push_back(-1);
+    free_handles_.reach(h + 1);
   }
   handle_file_[h] = file_id;
   files_[file_id].handles.push_back(h);
@@ -113,7 +114,7 @@ void Kvfs::drop_file(int32_t id) {
   f.waiting = false;
   for (int32_t h : f.handles) {
     handle_file_[h] = -1;
-    free_handles_.push(h);
+    free_handles_.insert(h);
   }
   f.handles.clear();
   if (f.named) names_.erase(f.name);
@@ -162,7 +163,7 @@ int Kvfs::close(int32_t h) {
   KvFile& f = files_[id];
   f.handles.erase(std::find(f.handles.begin(), f.handles.end(), h));
   handle_file_[h] = -1;
-  free_handles_.push(h);
+  free_handles_.insert(h);
   if (!f.named && f.handles.empty()) drop_file(id);   // nobody can reach it any more
   return SYM_OK;
 }
@@ -518,6 +519,15 @@ bool Kvfs::copy_last(int32_t id, CopyPlan* plan) {
   return true;
 }
 
+// How many leading entries two tables share: by 64 at a time while they do (memcmp has wide loads, a search for the first difference has not).
+static size_t same_pages(const std::vector<int32_t>& a, const std::vector<int32_t>& b) {
+  const size_t n = std::min(a.size(), b.size());
+  size_t i = 0;
+  while (i + 64 <= n && !std::memcmp(a.data() + i, b.data() + i, 64 * 4)) i += 64;
+  while (i < n && a[i] == b[i]) ++i;
+  return i;
+}
+
 int Kvfs::fork_batch(int32_t n, const int32_t* parents, bool own_last, int32_t* out, CopyPlan* plan, std::string* err) {
   plan->copies.clear();
   int64_t need = 0;
@@ -534,9 +544,19 @@ int Kvfs::fork_batch(int32_t n, const int32_t* parents, bool own_last, int32_t* 
     return SYM_ENOSPC;
   }
   plan->copies.reserve(3 * (size_t)need);
-  for (int32_t i = 0; i < n; ++i) {
-    out[i] = fork(parents[i]);
-    if (own_last) copy_last(handle_file_[out[i]], plan);
+  // A parent's forks one after the other: its pages are counted once for all of them.
+  for (int32_t i = 0, j; i < n; i = j) {
+    const int32_t pid = handle_file_[parents[i]];
+    for (j = i + 1; j < n && handle_file_[parents[j]] == pid;) ++j;
+    for (int32_t p : files_[pid].pages) refcount_[p] += (uint32_t)(j - i);
+    for (int32_t k = i; k < j; ++k) {
+      const int32_t id = new_file();            // may grow files_: the parent by index
+      files_[id].pages = files_[pid].pages;
+      files_[id].len = files_[pid].len;
+      files_[id].bounded = files_[pid].bounded;
+      out[k] = new_handle(id);
+      if (own_last) copy_last(id, plan);
+    }
   }
   return SYM_OK;
 }
@@ -567,14 +587,15 @@ int Kvfs::reorder(int32_t n, const int32_t* handles, const int32_t* from, bool o
     size_t same, tail, tail_n;
   };
   std::vector<Take> takes;
-  std::vector<int32_t> tails, freed;
+  std::vector<int32_t> tails, freed, left;
   size_t dropped = 0;
+  takes.reserve((size_t)n);
+  left.reserve((size_t)n);
   for (int32_t i = 0; i < n; ++i) {
     if (from[i] < 0 || from[i] == i) continue;
     KvFile& f = files_[handle_file_[handles[i]]];
     const KvFile& s = files_[handle_file_[handles[from[i]]]];
-    const size_t both = std::min(f.pages.size(), s.pages.size());
-    const size_t same = (size_t)(std::mismatch(f.pages.begin(), f.pages.begin() + (ptrdiff_t)both, s.pages.begin()).first - f.pages.begin());
+    const size_t same = same_pages(f.pages, s.pages);
     takes.push_back({handle_file_[handles[i]], s.len, s.bounded, same, tails.size(), s.pages.size() - same});
     tails.insert(tails.end(), s.pages.begin() + (ptrdiff_t)same, s.pages.end());
     f.pages.reserve(s.pages.size());
@@ -591,20 +612,18 @@ int Kvfs::reorder(int32_t n, const int32_t* handles, const int32_t* from, bool o
   // The copies: of a page that several have, the last that is asked keeps it.
   int64_t need = 0;
   if (own_last) {
-    pending_.clear();
     const auto ask = [&](int32_t last, int64_t len) {
-      if (len % P_ == 0) return;
-      int32_t& gone = pending_[last];
-      if ((int64_t)refcount_[last] - gone > 1) {
-        ++need;
-        ++gone;
-      }
+      if (len % P_ == 0 || refcount_[last] < 2) return;
+      ++need;
+      --refcount_[last];
+      left.push_back(last);
     };
     for (const Take& t : takes) ask(t.tail_n ? tails[t.tail + t.tail_n - 1] : t.same ? files_[t.file].pages[t.same - 1] : -1, t.len);
     for (int32_t i = 0; i < n; ++i) {
       const KvFile& f = files_[handle_file_[handles[i]]];
       if (from[i] < 0 || from[i] == i) ask(f.pages.empty() ? -1 : f.pages.back(), f.len);
     }
+    for (int32_t p : left) ++refcount_[p];
   }
   if (need > free_pages() + (int64_t)freed.size()) {
     for (const Take& t : takes)
@@ -641,7 +660,37 @@ int Kvfs::remove_batch(int32_t n, const int32_t* handles, std::string* err) {
       return SYM_EBUSY;
     }
   }
-  for (int32_t i = 0; i < n; ++i) drop_file(handle_file_[handles[i]]);
+  // Forks of one file share most of their tables, and come one after the other: an entry that a file has at the same place as the file
+  // before it is counted down with that one's.  began[k]: the file with which entry k of `spine` began to be shared.
+  std::vector<int32_t> spine, began;
+  size_t most = 0;
+  for (int32_t i = 0; i < n; ++i) most = std::max(most, file_of(handles[i])->pages.size());
+  spine.reserve(most);                            // (no allocation between here and the end)
+  began.reserve(most);
+  const auto flush = [&](size_t keep, int32_t now) {
+    for (size_t k = keep; k < spine.size(); ++k) {
+      const int32_t page = spine[k];
+      refcount_[page] -= (uint32_t)(now - began[k]);
+      if (refcount_[page] == 0) free_ranks_.insert(rank_[page]);
+    }
+    spine.resize(keep);
+    began.resize(keep);
+  };
+  for (int32_t i = 0; i < n; ++i) {
+    const int32_t id = handle_file_[handles[i]];
+    KvFile& f = files_[id];
+    if (!f.waiting) {
+      const size_t same = same_pages(f.pages, spine);
+      flush(same, i);
+      spine.insert(spine.end(), f.pages.begin() + (ptrdiff_t)same, f.pages.end());
+      began.resize(spine.size(), i);
+      f.pages.clear();
+    } else {
+      flush(0, i);                                // its entries are kept track of one by one
+    }
+    drop_file(id);
+  }
+  flush(0, n);
   return SYM_OK;
 }
 

@@ -41,6 +41,11 @@ class RankSet {
     count_ = n;
     hint_ = 0;
   }
+  void reach(int64_t n) {                     // room for ranks up to n - 1, none of the new ones free
+    if ((int64_t)l0_.size() * 64 >= n) return;
+    l0_.resize((size_t)((n + 63) / 64 * 2), 0);
+    l1_.resize((l0_.size() + 63) / 64, 0);
+  }
   int64_t size() const { return count_; }
   int32_t pop_lowest() {                      // the caller has checked size() > 0
     size_t i = hint_;
@@ -223,7 +228,7 @@ class Kvfs {
   std::vector<KvFile> files_;
   std::vector<int32_t> free_file_ids_;
   std::vector<int32_t> handle_file_;        // handle -> file id or -1
-  std::priority_queue<int32_t, std::vector<int32_t>, std::greater<int32_t>> free_handles_;
+  RankSet free_handles_;
   std::unordered_map<std::string, int32_t> names_;
   typedef std::vector<std::pair<int32_t, int32_t>> RefList;          // (file id, table index) entries
   std::unordered_map<int32_t, RefList> waiters_;    // resident page -> entries of waiting files that reference it

@@ -14,7 +14,7 @@ struct CopyList {
 // The filled slots of pages, bit for bit.  A page is 4 * Hkv pieces (kv head, K or V, row half) of 16 slots of 128 bytes; the first r
 // slots of a piece lie together, so the 16-byte chunks of a copy are counted through, r * 8 to a piece.  Sources and destinations are
 // different pages.  Bound: HBM, read + write.
-constexpr int kCopyChunks = 8;         // chunks of a thread, all in flight
+constexpr int kCopyChunks = 4;         // chunks of a thread, all in flight
 template <bool BY_ARGS, int N>
 __global__ __launch_bounds__(256) void copy_kernel(CopyArgs a, CopyList<N> l) {
   const int e = 3 * (int)blockIdx.y;
@@ -29,20 +29,22 @@ __global__ __launch_bounds__(256) void copy_kernel(CopyArgs a, CopyList<N> l) {
   const uint8_t* s = pool + (int64_t)src * a.page_bytes;
   uint8_t* d = pool + (int64_t)dst * a.page_bytes;
   const uint32_t first = blockIdx.x * (256 * kCopyChunks) + threadIdx.x;
-  const float inv = 1.0f / (float)per;
-  u32x4_t v[kCopyChunks];
-  uint32_t at[kCopyChunks];
+  if (blockIdx.x * (256 * kCopyChunks) < total) {
+    const float inv = 1.0f / (float)per;
+    u32x4_t v[kCopyChunks];
+    uint32_t at[kCopyChunks];
 #pragma unroll
-  for (int u = 0; u < kCopyChunks; ++u) {
-    const uint32_t i = first + u * 256;
-    // i / per: with a half added, no quotient of an i below 2^21 is within its roundings of a whole number
-    const uint32_t piece = (uint32_t)(((float)i + 0.5f) * inv);
-    at[u] = piece * (kP * kHalfBytes) + (i - piece * per) * 16;
-    if (i < total) v[u] = *(const u32x4_t*)(s + at[u]);
+    for (int u = 0; u < kCopyChunks; ++u) {
+      const uint32_t i = min(first + u * 256, total - 1);
+      // i / per: with a half added, no quotient of an i below 2^21 is within its roundings of a whole number
+      const uint32_t piece = (uint32_t)(((float)i + 0.5f) * inv);
+      at[u] = (i + piece * (kP * 8 - per)) * 16;
+      v[u] = __builtin_nontemporal_load((const u32x4_t*)(s + at[u]));
+    }
+#pragma unroll
+    for (int u = 0; u < kCopyChunks; ++u)
+      if (first + u * 256 < total) *(u32x4_t*)(d + at[u]) = v[u];
   }
-#pragma unroll
-  for (int u = 0; u < kCopyChunks; ++u)
-    if (first + u * 256 < total) *(u32x4_t*)(d + at[u]) = v[u];
   if (blockIdx.x == 0 && (what >> 8) && a.bounds) {
     uint8_t* b = a.bounds + (int64_t)blockIdx.z * a.layer_bounds;
     const int64_t n = (int64_t)a.Hkv * 512;
