@@ -392,6 +392,7 @@ int sym_pred_layer_sparse(sym_ctx* ctx, int32_t layer, const void* q, const void
 typedef struct sym_beam_step {
   int32_t n_groups, n_best;
   const int32_t* beams;            /* [n_groups], 1 .. SYM_BEAMS_MOST each                */
+  int64_t rows;                    /* of logits, scores, allowed: the sum of beams, or SYM_EINVAL */
   int32_t vocab, dtype;            /* 1 .. 2^24; SYM_F32, SYM_BF16 or SYM_F16             */
   const void* logits;              /* [rows][logits_stride], aligned to an element        */
   int64_t logits_stride;           /* elements from row to row, >= vocab (0: vocab)       */
@@ -408,7 +409,7 @@ int64_t sym_beam_scratch_bytes(int32_t n_groups, const int32_t* beams, int32_t v
 int     sym_beam_select(sym_ctx* ctx, const sym_beam_step* step, void* stream);
 
 /* Rows of per-beam state (token histories, recurrent states) after the beams: in each of n_states arrays [outer][rows][row_bytes], row r
- * of group g receives row parents[r] of the group (device int32 [rows], index within the group).  A parent outside the group, -1 above
+ * of group g receives row parents[r] of the group (device int32 [rows], index within the group; rows: the sum of beams, or SYM_EINVAL).  A parent outside the group, -1 above
  * all, leaves the row as it is.  dst may be src (in place) or apart from it, then every row is written; nothing else may overlap.  Rows
  * of any alignment; 16-byte aligned ones move fastest.  Like sym_beam_select allowed while a batch is open and in graphs.  */
 #define SYM_STATES_MOST 64
@@ -418,7 +419,7 @@ typedef struct sym_beam_state {
   int64_t outer, outer_stride;     /* bytes from one [rows][row_bytes] to the next        */
   int64_t row_stride, row_bytes;   /* bytes from row to row, >= row_bytes; bytes that move */
 } sym_beam_state;
-int     sym_beam_states(sym_ctx* ctx, int32_t n_groups, const int32_t* beams, const int32_t* parents,
+int     sym_beam_states(sym_ctx* ctx, int32_t n_groups, const int32_t* beams, int64_t rows, const int32_t* parents,
                         int32_t n_states, const sym_beam_state* states, void* stream);
 
 /* The files of beams.  All on the host but the copies, one launch for all of them and all layers, on `stream`:

@@ -13,7 +13,6 @@ LIB_PATH = os.environ.get("SYMPHONY_KV_LIB") or os.path.join(_HERE, "libsymphony
 
 SYM_OK, SYM_EINVAL, SYM_EBADF, SYM_ENOSPC, SYM_ENOENT, SYM_EEXIST, SYM_EBUSY, SYM_EHIP = 0, -1, -2, -3, -4, -5, -6, -7
 SYM_F32, SYM_BF16, SYM_F16 = 0, 1, 2
-LOGIT_TYPES = {"torch.float32": SYM_F32, "torch.bfloat16": SYM_BF16, "torch.float16": SYM_F16}
 ROPE_LAYOUTS = {"halves": 0, "interleaved": 1}
 K_PROLOGUE, K_ATTN, K_MERGE, K_MOVE, K_SWAP = 0, 1, 2, 3, 4
 
@@ -54,7 +53,7 @@ class SymSparse(C.Structure):
 
 
 class SymBeamStep(C.Structure):
-    _fields_ = [("n_groups", C.c_int32), ("n_best", C.c_int32), ("beams", C.c_void_p), ("vocab", C.c_int32), ("dtype", C.c_int32),
+    _fields_ = [("n_groups", C.c_int32), ("n_best", C.c_int32), ("beams", C.c_void_p), ("rows", C.c_int64), ("vocab", C.c_int32), ("dtype", C.c_int32),
                 ("logits", C.c_void_p), ("logits_stride", C.c_int64), ("scores", C.c_void_p), ("allowed", C.c_void_p), ("allowed_stride", C.c_int64),
                 ("best_scores", C.c_void_p), ("best_beams", C.c_void_p), ("best_tokens", C.c_void_p), ("scratch", C.c_void_p), ("scratch_bytes", C.c_int64)]
 
@@ -113,7 +112,7 @@ _SIGNATURES = {
     "sym_pred_layer_sparse": (C.c_int, [C.c_void_p, C.c_int32] + [C.c_void_p] * 6),
     "sym_beam_scratch_bytes": (C.c_int64, [C.c_int32, _I32P, C.c_int32, C.c_int32]),
     "sym_beam_select": (C.c_int, [C.c_void_p, C.POINTER(SymBeamStep), C.c_void_p]),
-    "sym_beam_states": (C.c_int, [C.c_void_p, C.c_int32, _I32P, C.c_void_p, C.c_int32, C.POINTER(SymBeamState), C.c_void_p]),
+    "sym_beam_states": (C.c_int, [C.c_void_p, C.c_int32, _I32P, C.c_int64, C.c_void_p, C.c_int32, C.POINTER(SymBeamState), C.c_void_p]),
     "sym_kv_fork_batch": (C.c_int, [C.c_void_p, C.c_int32, _I32P, C.c_int32, _I32P, C.c_void_p]),
     "sym_kv_reorder": (C.c_int, [C.c_void_p, C.c_int32, _I32P, _I32P, C.c_int32, C.c_void_p]),
     "sym_kv_remove_batch": (C.c_int, [C.c_void_p, C.c_int32, _I32P]),
@@ -216,6 +215,18 @@ def _positions(t):
     if t.element_size() != 4 or t.is_floating_point():
         raise TypeError(f"positions must be int32, got {t.dtype}")
     return _ptr(t)
+
+
+_F32 = _I32 = None
+_logit_types = {}
+
+
+def _torch_types():
+    """Names of element types, from the first call that looks at tensors on: this module loads without torch."""
+    global _F32, _I32
+    import torch
+    _logit_types.update({torch.float32: SYM_F32, torch.bfloat16: SYM_BF16, torch.float16: SYM_F16})
+    _F32, _I32 = torch.float32, torch.int32
 
 
 def _rows(t, count):
@@ -519,37 +530,44 @@ class Context:
     def beam_select(self, beams, n_best, logits, scores, best_scores, best_beams, best_tokens, scratch, allowed=None, stream=None):
         """beams: rows of each request.  logits [rows, vocab] (rows may lie apart), scores [rows] float32, allowed: int32 words [rows, ...] of bits or
         None; best_*: [requests, n_best]; scratch: a tensor of beam_scratch_bytes().  All on the device but beams."""
+        if _F32 is None:
+            _torch_types()
         b_a, b_p = _i32(beams)
         (rows, vocab), groups = logits.shape, len(b_a)
-        if int(b_a.sum()) != rows or vocab > 1 and logits.stride(1) != 1:
-            raise ValueError(f"logits of shape {tuple(logits.shape)} for {int(b_a.sum())} beams, each row contiguous")
-        for t, n, size in ((scores, rows, 4), (best_scores, groups * n_best, 4), (best_beams, groups * n_best, 4), (best_tokens, groups * n_best, 4)):
-            if t.numel() != n or t.element_size() != size:
-                raise ValueError(f"{tuple(t.shape)} of {t.dtype} for {n} values of 4 bytes")
-        if not (scores.is_floating_point() and best_scores.is_floating_point()) or best_beams.is_floating_point() or best_tokens.is_floating_point():
-            raise TypeError("scores are float32, beams and tokens int32")
-        kind = LOGIT_TYPES.get(str(logits.dtype))
+        far, step = logits.stride()
+        if vocab > 1 and step != 1:
+            raise ValueError(f"logits of strides {logits.stride()}: each row has to be contiguous")
+        kind = _logit_types.get(logits.dtype)
         if kind is None:
             raise TypeError(f"logits of {logits.dtype}")
-        a_ptr, a_stride = None, 0
+        if scores.dtype is not _F32 or best_scores.dtype is not _F32 or best_beams.dtype is not _I32 or best_tokens.dtype is not _I32:
+            raise TypeError("scores are float32, beams and tokens int32")
+        n = groups * n_best
+        if scores.numel() != rows or best_scores.numel() != n or best_beams.numel() != n or best_tokens.numel() != n:
+            raise ValueError(f"scores of {scores.numel()} rows for {rows}, or outputs of {best_scores.numel()}, {best_beams.numel()}, {best_tokens.numel()} values for {n}")
+        a_ptr, a_far = None, 0
         if allowed is not None:
-            if allowed.element_size() != 4 or allowed.is_floating_point() or allowed.dim() != 2 or allowed.shape[0] != rows or allowed.shape[1] * 32 < vocab or \
-                    allowed.shape[1] > 1 and allowed.stride(1) != 1:
+            if allowed.dtype is not _I32 or allowed.dim() != 2 or allowed.shape[0] != rows or allowed.shape[1] * 32 < vocab or allowed.shape[1] > 1 and allowed.stride(1) != 1:
                 raise ValueError(f"allowed tokens: int32 words [{rows}, {(vocab + 31) // 32}], got {tuple(allowed.shape)} of {allowed.dtype}")
-            a_ptr, a_stride = allowed.data_ptr(), allowed.stride(0) if rows > 1 else 0
-        step = SymBeamStep(groups, n_best, b_p, vocab, kind, logits.data_ptr(), logits.stride(0) if rows > 1 else 0, _ptr(scores), a_ptr, a_stride,
-                           _ptr(best_scores), _ptr(best_beams), _ptr(best_tokens), _ptr(scratch), scratch.numel() * scratch.element_size())
-        rc = self.lib.sym_beam_select(self.h, C.byref(step), stream)
+            a_ptr = allowed.data_ptr()
+            a_far = allowed.stride(0) if rows > 1 else 0
+            if rows > 1 and a_far == 0:
+                raise ValueError("rows of allowed tokens share their memory")
+        if rows > 1 and far == 0:
+            raise ValueError("rows of logits share their memory")
+        arg = SymBeamStep(groups, n_best, b_p, rows, vocab, kind, logits.data_ptr(), far if rows > 1 else 0, _ptr(scores), a_ptr, a_far,
+                          _ptr(best_scores), _ptr(best_beams), _ptr(best_tokens), _ptr(scratch), scratch.numel() * scratch.element_size())
+        rc = self.lib.sym_beam_select(self.h, C.byref(arg), stream)
         if rc < 0:
             self._chk(rc)
 
     def beam_states(self, beams, parents, states, stream=None):
         """Rows of the arrays of make_states() after their beams.  parents: int32 [rows] on the device, index within the request; -1: the row stays."""
         b_a, b_p = _i32(beams)
-        rows = int(b_a.sum())
-        if states._rows is not None and states._rows != rows or parents.numel() != rows:
-            raise ValueError(f"{rows} beams, states of {states._rows} rows, {parents.numel()} parents")
-        rc = self._fn.sym_beam_states(self.h, len(b_a), b_p, _positions(parents), states._n, states, stream)
+        rows = parents.numel()
+        if states._rows is not None and states._rows != rows:
+            raise ValueError(f"{rows} parents for states of {states._rows} rows")
+        rc = self._fn.sym_beam_states(self.h, len(b_a), b_p, rows, _positions(parents), states._n, states, stream)
         if rc < 0:
             self._chk(rc)
 

@@ -551,21 +551,10 @@ __global__ __launch_bounds__(THREADS) void select_best_kernel(SelectArgs a, Grou
 
 typedef u32x4_t __attribute__((aligned(1))) u32x4_a1;
 
-// A thread moves one column (16 bytes; the last ones of a row that is no multiple of that, single) of all rows of a group: every row's
+// A thread moves columns (16 bytes; the last ones of a row that is no multiple of that, single) of all rows of a group: every row's
 // new value is read before the first is written, and no other thread touches the column, so a group may be moved in place.
-// Rows that stay are neither read nor written there.  Bound: HBM, read + write.
-template <int R, typename V>
-__device__ __forceinline__ void move_column(uint8_t* dst, const uint8_t* src, int64_t stride, int beams, const int (&from)[R], bool all) {
-  V v[R];
-#pragma unroll
-  for (int r = 0; r < R; ++r)
-    if (r < beams && (all || from[r] != r)) v[r] = *(const V*)(src + from[r] * stride);
-#pragma unroll
-  for (int r = 0; r < R; ++r)
-    if (r < beams && (all || from[r] != r)) *(V*)(dst + r * stride) = v[r];
-}
-
-template <int R>
+// Rows that stay are neither read nor written there.  Bound: HBM, read + write.  U columns of R rows are under way at a time.
+template <int R, int U>
 __global__ __launch_bounds__(kStateThreads) void states_kernel(StatesArgs a, GroupRows g) {
   uint32_t b = blockIdx.x;
   int s = 0;
@@ -576,23 +565,45 @@ __global__ __launch_bounds__(kStateThreads) void states_kernel(StatesArgs a, Gro
   const int row0 = g.row(group), beams = g.rows(group);
   const bool all = x.dst != x.src;
   int from[R];
-  bool moves = all;
+  uint64_t moves = 0;                                      // rows that change
 #pragma unroll
   for (int r = 0; r < R; ++r) {
-    from[r] = r;
-    if (r < beams) {
-      const int p = sload(a.parents + row0 + r);
-      from[r] = (uint32_t)p < (uint32_t)beams ? p : r;
-      moves = moves || from[r] != r;
-    }
+    const int p = sload(a.parents + row0 + min(r, beams - 1));
+    from[r] = (uint32_t)p < (uint32_t)beams ? p : r;
+    if (r < beams && (all || from[r] != r)) moves |= 1ull << r;
   }
   if (!moves) return;
-  const int64_t units = x.row_bytes / kStateUnit, unit = (int64_t)chunk * kStateThreads + threadIdx.x;
-  const int64_t rest = x.row_bytes % kStateUnit, at = (int64_t)outer * x.outer_stride + row0 * x.row_stride;
-  if (unit < units) move_column<R, u32x4_a1>(x.dst + at + unit * kStateUnit, x.src + at + unit * kStateUnit, x.row_stride, beams, from, all);
-  else if (unit < units + rest) {
-    const int64_t byte = units * kStateUnit + (unit - units);
-    move_column<R, uint8_t>(x.dst + at + byte, x.src + at + byte, x.row_stride, beams, from, all);
+  // a stretch of U * 4 KB of every row, from a base that is the same for all threads
+  const int64_t begin = (int64_t)chunk * (U * kStateThreads * kStateUnit), stretch = min(x.row_bytes - begin, (int64_t)(U * kStateThreads * kStateUnit));
+  const int64_t at = (int64_t)outer * x.outer_stride + row0 * x.row_stride + begin;
+  const uint8_t* src = x.src + at;
+  uint8_t* dst = x.dst + at;
+  const uint32_t whole = (uint32_t)stretch / kStateUnit * kStateUnit, rest = (uint32_t)stretch % kStateUnit, mine = threadIdx.x * kStateUnit;
+  u32x4_t v[R][U];
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+    if (moves >> r & 1) {
+      const uint8_t* row = src + from[r] * x.row_stride;
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (mine + u * (kStateThreads * kStateUnit) < whole) v[r][u] = __builtin_nontemporal_load((const u32x4_a1*)(row + (mine + u * (kStateThreads * kStateUnit))));
+    }
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+    if (moves >> r & 1) {
+      uint8_t* row = dst + r * x.row_stride;
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (mine + u * (kStateThreads * kStateUnit) < whole) *(u32x4_a1*)(row + (mine + u * (kStateThreads * kStateUnit))) = v[r][u];
+    }
+  if (threadIdx.x < rest) {
+    uint8_t c[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+      if (moves >> r & 1) c[r] = src[from[r] * x.row_stride + whole + threadIdx.x];
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+      if (moves >> r & 1) dst[r * x.row_stride + whole + threadIdx.x] = c[r];
   }
 }
 
@@ -640,11 +651,11 @@ hipError_t launch_select_best(const SelectArgs& a, const GroupRows& g, int32_t g
 
 hipError_t launch_states(const StatesArgs& a, const GroupRows& g, int32_t most_beams, hipStream_t st) {
   const dim3 grid(a.array[a.n_arrays - 1].end), block(kStateThreads);
-  if (most_beams <= 4) states_kernel<4><<<grid, block, 0, st>>>(a, g);
-  else if (most_beams <= 8) states_kernel<8><<<grid, block, 0, st>>>(a, g);
-  else if (most_beams <= 16) states_kernel<16><<<grid, block, 0, st>>>(a, g);
-  else if (most_beams <= 32) states_kernel<32><<<grid, block, 0, st>>>(a, g);
-  else states_kernel<kBeamsMost><<<grid, block, 0, st>>>(a, g);
+  if (most_beams <= 4) states_kernel<4, state_columns(4)><<<grid, block, 0, st>>>(a, g);
+  else if (most_beams <= 8) states_kernel<8, state_columns(8)><<<grid, block, 0, st>>>(a, g);
+  else if (most_beams <= 16) states_kernel<16, state_columns(16)><<<grid, block, 0, st>>>(a, g);
+  else if (most_beams <= 32) states_kernel<32, state_columns(32)><<<grid, block, 0, st>>>(a, g);
+  else states_kernel<kBeamsMost, state_columns(kBeamsMost)><<<grid, block, 0, st>>>(a, g);
   return hipGetLastError();
 }
 

@@ -67,6 +67,8 @@ struct StatesArgs {
 };
 constexpr int kStateUnit = 16;         // bytes of each row that a thread moves
 constexpr int kStateThreads = 256;
+// Columns of a thread, by the rows of the largest group.
+constexpr int state_columns(int beams) { return beams <= 4 ? 4 : beams <= 8 ? 2 : 1; }
 
 constexpr int kArgCopies = 256;        // copies that travel with the arguments (3 KB of the 4 KB that a launch may have)
 struct CopyArgs {

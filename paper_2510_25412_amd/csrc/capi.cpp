@@ -1875,6 +1875,7 @@ int sym_beam_select(sym_ctx* c, const sym_beam_step* b, void* stream) {
     int32_t most;
     const int64_t rows = count_rows(b->n_groups, b->beams, &most);
     if (rows < 0) return fail(c, SYM_EINVAL, "beam_select: groups of 1 .. 64 beams, 65536 of them at most");
+    if (rows != b->rows) return fail(c, SYM_EINVAL, "beam_select: as many rows as the groups have beams");
     if (b->n_best < 1 || b->n_best > kBestMost) return fail(c, SYM_EINVAL, "beam_select: n_best must be 1 .. 128");
     if (b->vocab < 1 || b->vocab > (1 << 24)) return fail(c, SYM_EINVAL, "beam_select: vocab must be 1 .. 2^24");
     if (b->dtype != SYM_F32 && b->dtype != SYM_BF16 && b->dtype != SYM_F16) return fail(c, SYM_EINVAL, "beam_select: unknown type of logits");
@@ -1947,13 +1948,14 @@ int sym_beam_select(sym_ctx* c, const sym_beam_step* b, void* stream) {
   });
 }
 
-int sym_beam_states(sym_ctx* c, int32_t n_groups, const int32_t* beams, const int32_t* parents, int32_t n_states, const sym_beam_state* states, void* stream) {
+int sym_beam_states(sym_ctx* c, int32_t n_groups, const int32_t* beams, int64_t n_rows, const int32_t* parents, int32_t n_states, const sym_beam_state* states, void* stream) {
   if (!c || n_states < 0 || n_states > SYM_STATES_MOST || (n_states > 0 && !states)) return SYM_EINVAL;
   std::lock_guard<std::mutex> lk(c->mu);
   return guarded(c, [&]() -> int {
     int32_t most;
     const int64_t rows = count_rows(n_groups, beams, &most);
     if (rows < 0) return fail(c, SYM_EINVAL, "beam_states: groups of 1 .. 64 beams, 65536 of them at most");
+    if (rows != n_rows) return fail(c, SYM_EINVAL, "beam_states: as many rows as the groups have beams");
     struct Area {
       const void* p;
       int64_t n;
@@ -2005,10 +2007,10 @@ int sym_beam_states(sym_ctx* c, int32_t n_groups, const int32_t* beams, const in
         const sym_beam_state& s = states[i];
         if (s.outer == 0 || s.row_bytes == 0) continue;
         // stretches of columns, then of the outer dimension, so that a launch has no more workgroups than it may
-        const int64_t slice = (kStateBlocks / n - 1) * kStateThreads * kStateUnit;
+        const int64_t chunk = (int64_t)state_columns(most) * kStateThreads * kStateUnit, slice = (kStateBlocks / n - 1) * chunk;
         for (int64_t col = 0; col < s.row_bytes; col += slice) {
           const int64_t bytes = std::min(slice, s.row_bytes - col);
-          const int64_t chunks = (bytes / kStateUnit + bytes % kStateUnit + kStateThreads - 1) / kStateThreads;
+          const int64_t chunks = (bytes + chunk - 1) / chunk;
           const int64_t step = std::max<int64_t>(1, kStateBlocks / (chunks * n));
           for (int64_t o = 0; o < s.outer; o += step) {
             const int64_t blocks = std::min(step, s.outer - o) * chunks * n, before = a.n_arrays ? a.array[a.n_arrays - 1].end : 0;

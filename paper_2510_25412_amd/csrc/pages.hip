@@ -14,7 +14,7 @@ struct CopyList {
 // The filled slots of pages, bit for bit.  A page is 4 * Hkv pieces (kv head, K or V, row half) of 16 slots of 128 bytes; the first r
 // slots of a piece lie together, so the 16-byte chunks of a copy are counted through, r * 8 to a piece.  Sources and destinations are
 // different pages.  Bound: HBM, read + write.
-constexpr int kCopyChunks = 4;         // chunks of a thread, all in flight
+constexpr int kCopyChunks = 2;         // chunks of a thread
 template <bool BY_ARGS, int N>
 __global__ __launch_bounds__(256) void copy_kernel(CopyArgs a, CopyList<N> l) {
   const int e = 3 * (int)blockIdx.y;
@@ -43,7 +43,7 @@ __global__ __launch_bounds__(256) void copy_kernel(CopyArgs a, CopyList<N> l) {
     }
 #pragma unroll
     for (int u = 0; u < kCopyChunks; ++u)
-      if (first + u * 256 < total) *(u32x4_t*)(d + at[u]) = v[u];
+      if (first + u * 256 < total) __builtin_nontemporal_store(v[u], (u32x4_t*)(d + at[u]));
   }
   if (blockIdx.x == 0 && (what >> 8) && a.bounds) {
     uint8_t* b = a.bounds + (int64_t)blockIdx.z * a.layer_bounds;

@@ -179,7 +179,7 @@ def test_rows_that_lie_apart(ctx):
     compare(choose(ctx, far[:, 3:1206], s, [2, 4], 9), x, s, [2, 4], 9)
     compare(choose(ctx, far[:, 3:1206], s, [2, 4], 9, allowed, wide[:, 5:43]), x, s, [2, 4], 9, allowed)
     shared = words_of(allowed[:1]).expand(6, 38)              # one mask for all rows has to be written out
-    with pytest.raises(binding.SymError):
+    with pytest.raises(ValueError):
         choose(ctx, x, s, [2, 4], 9, allowed, shared)
 
 
@@ -205,7 +205,9 @@ def test_binding_refuses(ctx):
     x, s = make(4, 100, "bf16", 1)
     out = [torch.empty((1, 8), dtype=t, device="cuda") for t in (torch.float32, torch.int32, torch.int32)]
     scratch = torch.empty(binding.beam_scratch_bytes([4], 100, 8), dtype=torch.uint8, device="cuda")
-    for bad in [dict(beams=[3]), dict(logits=x.t().contiguous().t()), dict(logits=x.double()), dict(scores=s[:3]), dict(scores=s.double()), dict(scores=s.int()), dict(best=9),
+    with pytest.raises(binding.SymError):                     # as many rows as beams
+        ctx.beam_select([3], 8, x, s, *out, scratch, None, stream())
+    for bad in [dict(logits=x[:1].expand(4, 100)), dict(logits=x.t().contiguous().t()), dict(logits=x.double()), dict(scores=s[:3]), dict(scores=s.double()), dict(scores=s.int()), dict(best=9),
                 dict(allowed=torch.zeros((4, 3), dtype=torch.int32, device="cuda")), dict(allowed=torch.zeros((3, 4), dtype=torch.int32, device="cuda")),
                 dict(allowed=torch.zeros((4, 4), device="cuda"))]:
         a = dict(dict(beams=[4], best=8, logits=x, scores=s, allowed=None), **bad)
@@ -291,8 +293,9 @@ def test_plans_of_states_are_checked(ctx):
         with pytest.raises(ValueError):
             binding.make_states(bad)
     plan = binding.make_states([(x, x, 1)])
-    for beams, parents in [([7], torch.zeros(7, dtype=torch.int32, device="cuda")), ([8], torch.zeros(7, dtype=torch.int32, device="cuda"))]:
-        with pytest.raises(ValueError):
+    for beams, parents, error in [([7], torch.zeros(7, dtype=torch.int32, device="cuda"), ValueError), ([8], torch.zeros(7, dtype=torch.int32, device="cuda"), ValueError),
+                                  ([7], torch.zeros(8, dtype=torch.int32, device="cuda"), binding.SymError)]:
+        with pytest.raises(error):
             ctx.beam_states(beams, parents, plan, stream())
     with pytest.raises(TypeError):
         ctx.beam_states([8], torch.zeros(8, device="cuda"), plan, stream())

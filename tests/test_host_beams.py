@@ -282,7 +282,7 @@ def test_scratch_of_a_choice():
 def step_of(**kw):
     """A well-formed step on addresses that a host-only context never follows."""
     beams = np.array(kw.pop("beams", [4, 3]), np.int32)
-    d = dict(n_groups=len(beams), n_best=8, beams=beams.ctypes.data, vocab=1000, dtype=binding.SYM_BF16, logits=1 << 30, logits_stride=0, scores=1 << 28, allowed=1 << 27, allowed_stride=0,
+    d = dict(n_groups=len(beams), n_best=8, beams=beams.ctypes.data, rows=int(beams.sum()), vocab=1000, dtype=binding.SYM_BF16, logits=1 << 30, logits_stride=0, scores=1 << 28, allowed=1 << 27, allowed_stride=0,
              best_scores=1 << 20, best_beams=1 << 21, best_tokens=1 << 22, scratch=1 << 40, scratch_bytes=1 << 30)
     d.update(kw)
     s = binding.SymBeamStep(**d)
@@ -295,7 +295,7 @@ def test_choice_arguments():
     call = lambda **kw: (ctx.lib.sym_beam_select(ctx.h, C.byref(step_of(**kw)), None), ctx.lib.sym_strerror(ctx.h).decode())  # noqa: E731
     assert call() == (EINVAL, "host-only context")            # everything else was well-formed
     assert call(allowed=None) == (EINVAL, "host-only context")
-    for kw in [dict(beams=[0, 1]), dict(beams=[65]), dict(n_groups=-1), dict(n_best=0), dict(n_best=129), dict(vocab=0), dict(vocab=(1 << 24) + 1), dict(dtype=3), dict(logits_stride=999),
+    for kw in [dict(beams=[0, 1]), dict(beams=[65]), dict(n_groups=-1), dict(rows=6), dict(rows=8), dict(n_best=0), dict(n_best=129), dict(vocab=0), dict(vocab=(1 << 24) + 1), dict(dtype=3), dict(logits_stride=999),
                dict(logits_stride=-1), dict(allowed_stride=31), dict(logits=None), dict(scores=None), dict(best_scores=None), dict(best_beams=None), dict(best_tokens=None), dict(scratch=None),
                dict(logits=(1 << 30) + 1), dict(dtype=0, logits=(1 << 30) + 2), dict(scores=(1 << 28) + 2), dict(allowed=(1 << 27) + 1), dict(best_scores=(1 << 20) + 2),
                dict(scratch=(1 << 40) + 8), dict(best_beams=(1 << 20) + 60), dict(best_tokens=1 << 28), dict(best_tokens=(1 << 30) + 7 * 2000 - 4), dict(scratch=(1 << 30) + 13984),
@@ -312,15 +312,15 @@ def test_state_arguments():
     beams = np.array([4, 3], np.int32)
     good = dict(dst=1 << 30, src=1 << 30, outer=2, outer_stride=7000, row_stride=1000, row_bytes=1000)
 
-    def call(*states, parents=1 << 20, n=2):
+    def call(*states, parents=1 << 20, n=2, rows=7):
         plan = (binding.SymBeamState * max(len(states), 1))(*[binding.SymBeamState(**dict(good, **s)) for s in states])
-        return ctx.lib.sym_beam_states(ctx.h, n, beams.ctypes.data_as(C.POINTER(C.c_int32)), parents, len(states), plan, None), ctx.lib.sym_strerror(ctx.h).decode()
+        return ctx.lib.sym_beam_states(ctx.h, n, beams.ctypes.data_as(C.POINTER(C.c_int32)), rows, parents, len(states), plan, None), ctx.lib.sym_strerror(ctx.h).decode()
 
     host_only = (EINVAL, "host-only context")
     assert call({}) == host_only and call({}, dict(dst=1 << 31, src=(1 << 31) + 14000)) == host_only
     for states, kw in [(({}, {}), {}), (({}, dict(dst=(1 << 30) + 13999, src=1 << 32)), {}), ((dict(src=(1 << 30) + 1),), {}), ((dict(row_bytes=1001),), {}), ((dict(outer_stride=6999),), {}),
-                       ((dict(outer=-1),), {}), ((dict(row_bytes=-1),), {}), ((dict(dst=None),), {}), ((dict(src=None),), {}), (({},), dict(parents=None)), (({},), dict(parents=(1 << 20) + 2)),
+                       ((dict(outer=-1),), {}), ((dict(row_bytes=-1),), {}), ((dict(dst=None),), {}), ((dict(src=None),), {}), (({},), dict(parents=None)), (({},), dict(rows=8)), (({},), dict(parents=(1 << 20) + 2)),
                        (({},), dict(parents=(1 << 30) + 400)), ((dict(row_stride=1 << 50),), {}), ((dict(outer=1 << 40, outer_stride=1 << 40),), {})]:
         code, what = call(*states, **kw)
         assert code == EINVAL and what != "host-only context", (states, kw, what)
-    assert call(dict(row_bytes=0))[0] == 0 and call(dict(outer=0))[0] == 0 and call({}, n=0)[0] == 0 and call()[0] == 0
+    assert call(dict(row_bytes=0))[0] == 0 and call(dict(outer=0))[0] == 0 and call({}, n=0, rows=0)[0] == 0 and call()[0] == 0
