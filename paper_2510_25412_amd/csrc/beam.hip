@@ -366,10 +366,10 @@ constexpr uint64_t kNone = ~0ull;
 
 constexpr int kFound = 1024;           // choices that are sorted by counting what comes before each
 constexpr int kFoundLists = 512;
+constexpr int kFewLists = 4096, kFewThreads = 512;
 struct RowScore {
   double base, from;
 };
-constexpr int kHeld = 16;              // lists that a thread holds
 
 // The best choice of what `each` shows to `see` in every thread, behind `last` (k > 0): the threads' best in `best`, then one of them.
 template <int THREADS, typename F>
@@ -392,9 +392,8 @@ __device__ __forceinline__ Choice next_best(Choice* best, int k, const Choice& l
 // One workgroup for a group.  A value that the K best reach comes from 256 disjoint subsets' largest: of every row some lists, since the best
 // may all be one row's.  Lists that reach it are read again, and what reaches it in them is sorted.  What is read of the rows' pass is
 // requested at once and kept, so that a choice is three round trips: where the group's rows are, their lists, the logits looked at again.
-template <typename E, bool MASKED, bool TINY, int THREADS>
+template <typename E, bool MASKED, bool TINY, int THREADS, int kHeld>
 __global__ __launch_bounds__(THREADS) void select_best_kernel(SelectArgs a, GroupRows g, int group0) {
-  static_assert(THREADS * kHeld >= 64 * kMostParts || THREADS == 256, "a thread holds its share of the lists");
   __shared__ RowScore rows[kBeamsMost];
   __shared__ float subset[THREADS];
   __shared__ Choice found[kFound];
@@ -622,10 +621,11 @@ template <typename E, bool MASKED, bool TINY>
 void launch_best(const SelectArgs& a, const GroupRows& g, int32_t group0, int32_t n_groups, hipStream_t st) {
   int most = 0;                                            // parts of the largest group
   for (int32_t i = 0; i < (g.each ? 1 : n_groups); ++i) most = std::max(most, g.rows(i) * a.parts);
-  // four times the threads where they would otherwise hold too many lists, or look at more than four groups each
-  const int deep = a.part_octets * (kOctet / E::kGroup) / 64;
-  if (most * 64 <= 256 * kHeld && a.n_best * deep <= 4 * 256) select_best_kernel<E, MASKED, TINY, 256><<<dim3((unsigned)n_groups), dim3(256), 0, st>>>(a, g, group0);
-  else select_best_kernel<E, MASKED, TINY, 1024><<<dim3((unsigned)n_groups), dim3(1024), 0, st>>>(a, g, group0);
+  const int lists = most * 64, deep = a.part_octets * (kOctet / E::kGroup) / 64;
+  const dim3 grid((unsigned)n_groups);
+  static_assert(1024 * 16 == 64 * kMostParts, "a thread holds its share of the lists");
+  if (lists <= kFewLists && a.n_best * deep <= 1024) select_best_kernel<E, MASKED, TINY, kFewThreads, kFewLists / kFewThreads><<<grid, dim3(kFewThreads), 0, st>>>(a, g, group0);
+  else select_best_kernel<E, MASKED, TINY, 1024, 16><<<grid, dim3(1024), 0, st>>>(a, g, group0);
 }
 #define SYM_OF_TYPE(launch, E, ...)                                                     \
   (a.vocab < E::kGroup ? (a.allowed ? launch<E, true, true>(__VA_ARGS__) : launch<E, false, true>(__VA_ARGS__)) \
