@@ -293,11 +293,13 @@ def bench_rag(args, np, torch, binding, synth, HipSession, dev):
     n_req = args.steps if args.steps is not None else 1500
     rows = []
     for pareto, retain in ((0.5, 20), (1.0, 20), (2.0, 20), (1.0, 0)):
-        cfg = rag.RagConfig(pareto_index=pareto, retain=retain, n_requests=n_req, rate_per_s=args.rag_rate)
+        cfg = rag.RagConfig(pareto_index=pareto, retain=retain, n_requests=n_req, rate_per_s=args.rag_rate, beams=args.rag_beams)
         # room for every request's file at once (no admission control here) + the retained documents
         n_pages = (n_req + retain + 8) * ((cfg.doc_tokens + cfg.answer_tokens) // 16 + 2)
-        s = HipSession(shape, n_pages, None, dev, max_lips=cfg.max_batch, max_tokens=cfg.max_batch * cfg.prefill_chunk + 64,
-                       max_entries=cfg.max_batch * ((cfg.doc_tokens + cfg.answer_tokens) // 16 + 2) + 64)
+        if cfg.beams > 1:                                    # and for the beams' own pages
+            n_pages += n_req * cfg.beams * (cfg.answer_tokens // 16 + 2)
+        s = HipSession(shape, n_pages, None, dev, max_lips=cfg.max_batch * cfg.beams, max_tokens=cfg.max_batch * cfg.prefill_chunk + 64,
+                       max_entries=cfg.max_batch * cfg.beams * ((cfg.doc_tokens + cfg.answer_tokens) // 16 + 2) + 64)
         d = rag.RagDriver(s, cfg)
         with timed_region():
             r = d.run()
@@ -313,7 +315,8 @@ def bench_rag(args, np, torch, binding, synth, HipSession, dev):
             "scaling": "weak", "vs_baseline": None, "dtype": "bf16", "data": "synthetic",
             "config": {"workload": f"rag: 100 documents x 3000 tokens, 32 answer tokens, top-20 topics retained (prompt caching by fork), Poisson "
                                    f"requests at {args.rag_rate:.0f}/s, Pareto topic popularity, 32Q/8KV bf16, batches fired by sym_sched; virtual time "
-                                   "advanced by measured batch wall time; value quoted at Pareto index 1.0"},
+                                   "advanced by measured batch wall time; value quoted at Pareto index 1.0"
+                                   + (f"; {args.rag_beams} beams to an answer" if args.rag_beams > 1 else "")},
             "by_pareto_index": [{k: (round(v, 4) if isinstance(v, float) else v) for k, v in r.items() if k != "scheduler"} for r in rows],
             "roofline": None, "cpu_baseline": None}
     print(json.dumps(line))
@@ -570,6 +573,7 @@ def main():
                                                  "(the fields of sym_tuning); the attention workloads only")
     ap.add_argument("--decode-waves", type=int, default=0, help="sym_config.decode_waves (0 = the library's choice)")
     ap.add_argument("--no-extra", action="store_true", help="headline workload only")
+    ap.add_argument("--rag-beams", type=int, default=1, help="beams of an answer in the rag workload")
     ap.add_argument("--rag-rate", type=float, default=6000.0, help="request arrivals per second of the rag workload")
     args = ap.parse_args()
     args.tuning_dict = {k.strip(): int(v) for k, v in (kv.split("=") for kv in args.tuning.split(",") if kv.strip())} or None

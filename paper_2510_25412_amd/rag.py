@@ -13,6 +13,9 @@ Time is virtual: requests arrive by a seeded Poisson process, and every fired ba
 clock by its measured wall time (host work + GPU, synchronised), so throughput and latency are
 those of a server that does nothing but this path.  Only attention is computed (no weights on
 this path): Q/K/V rows are slices of fixed seeded random arrays, and sampled tokens do not exist.
+With `beams` > 1 an answer is searched for with that many beams: the document's file is forked for each, every step's
+preds are followed by the choice among their continuations (logits: slices of a fixed seeded random array), and the
+beams' scores, tokens and files follow it.
 Host logic and argument marshalling only; none of the method's arithmetic.
 """
 import math
@@ -38,6 +41,8 @@ class RagConfig:
     max_batch: int = 64
     max_wait_us: float = 300.0
     seed: int = 2025
+    beams: int = 1                      # of an answer; > 1: a pred call of an answer is as many rows
+    vocab: int = 32768                  # of the logits that beams choose from
 
 
 def topic_probabilities(n_docs, pareto_index, rng):
@@ -48,12 +53,12 @@ def topic_probabilities(n_docs, pareto_index, rng):
 
 
 class _Lip:
-    __slots__ = ("rid", "topic", "arrival", "fid", "to_prefill", "to_decode", "hit")
+    __slots__ = ("rid", "topic", "arrival", "fid", "to_prefill", "to_decode", "hit", "beams")
 
 
 class RagDriver:
-    """sess: a driver.HipSession whose pool, workspace (max_lips >= max_batch, max_tokens >=
-    max_batch * prefill_chunk) are large enough.  trace=True records every file operation and batch
+    """sess: a driver.HipSession whose pool, workspace (max_lips >= max_batch * beams, max_tokens >=
+    max_batch * max(prefill_chunk, beams)) are large enough.  trace=True records every file operation and batch
     (and keeps the outputs) so that the run can be replayed on the CPU model."""
 
     def __init__(self, sess, cfg, trace=False, timer=None):
@@ -62,7 +67,7 @@ class RagDriver:
         self.sess, self.cfg = sess, cfg
         self.timer = timer or binding.BatchTimer(cfg.max_batch, cfg.max_wait_us)
         s = sess.shape
-        self.max_rows = cfg.max_batch * max(cfg.prefill_chunk, 1)
+        self.max_rows = cfg.max_batch * max(cfg.prefill_chunk, cfg.beams, 1)
         st = np.random.SeedSequence(cfg.seed).spawn(4)
         self.rng = np.random.Generator(np.random.PCG64(st[0]))
         # fixed seeded rows; a batch with T new tokens uses rows [0, T) of each
@@ -72,6 +77,20 @@ class RagDriver:
         from .driver import to_device
         self.q, self.k, self.v = (to_device(a, sess.device) for a in (self.q_host, self.k_host, self.v_host))
         self.out = torch.empty((self.max_rows, s.n_q_heads, s.head_dim), dtype=torch.float32, device=sess.device)
+        if cfg.beams > 1:
+            rows, B = cfg.max_batch * cfg.beams, cfg.beams
+            g = torch.Generator().manual_seed(cfg.seed)
+            self.logits = (2.0 * torch.randn((rows, cfg.vocab), generator=g)).to(sess.device, torch.bfloat16)
+            # of every request: its beams' scores (at first they are one and the same) and tokens
+            self.scores = torch.full((cfg.n_requests, B), -math.inf, device=sess.device)
+            self.scores[:, 0] = 0.0
+            self.tokens = torch.full((cfg.n_requests * B, cfg.answer_tokens), -1, dtype=torch.int32, device=sess.device)
+            self.parents = torch.empty(cfg.n_requests * B, dtype=torch.int32, device=sess.device)
+            self.states = binding.make_states([(self.tokens, self.tokens, 0)])
+            self.every = np.full(cfg.n_requests, B, np.int32)
+            self.best = [torch.empty(rows, dtype=t, device=sess.device) for t in (torch.float32, torch.int32, torch.int32)]
+            self.scratch = torch.empty(max(binding.beam_scratch_bytes(self.every[:n], cfg.vocab, B) for n in range(1, min(cfg.max_batch, cfg.n_requests) + 1)),
+                                       dtype=torch.uint8, device=sess.device)
         self.trace = [] if trace else None
         self.outputs = [] if trace else None
         self.next_fid = 0
@@ -99,6 +118,40 @@ class RagDriver:
         if self.trace is not None:
             self.trace.append(("remove", fid))
 
+    def _spread(self, parent):
+        """A fork of the file for every beam, last pages their own."""
+        fids = list(range(self.next_fid, self.next_fid + self.cfg.beams))
+        self.next_fid += len(fids)
+        self.h.update(zip(fids, map(int, self.sess.ctx.kv_fork_batch([self.h[parent]] * len(fids), True, self.sess.stream))))
+        if self.trace is not None:
+            self.trace.append(("fork_batch", fids, [parent] * len(fids)))
+        return fids
+
+    def _remove_all(self, fids):
+        self.sess.ctx.kv_remove_batch([self.h.pop(f) for f in fids])
+        if self.trace is not None:
+            self.trace.append(("remove_batch", list(fids)))
+
+    def _choose(self, lips):
+        """A step of these requests' searches: the best continuations of their beams, whose scores, tokens and files follow them."""
+        torch, ctx, B, n, stream = self.torch, self.sess.ctx, self.cfg.beams, len(lips), self.sess.stream
+        rid = torch.tensor([lip.rid for lip in lips], device=self.sess.device)
+        best, beam, token = (x[:n * B] for x in self.best)
+        ctx.beam_select(self.every[:n], B, self.logits[:n * B], self.scores[rid].flatten(), best, beam, token, self.scratch, None, stream)
+        self.scores[rid] = best.view(n, B)
+        self.parents.fill_(-1)
+        rows = (rid[:, None] * B + torch.arange(B, device=rid.device)).flatten()
+        self.parents[rows] = beam
+        ctx.beam_states(self.every, self.parents, self.states, stream)
+        at = torch.tensor([self.cfg.answer_tokens - lip.to_decode for lip in lips], device=rid.device).repeat_interleave(B)
+        self.tokens[rows, at] = token
+        files = [f for lip in lips for f in lip.beams]
+        sources = beam.cpu().numpy()
+        sources = np.where(sources < 0, -1, sources + np.repeat(np.arange(n) * B, B))
+        ctx.kv_reorder([self.h[f] for f in files], sources, True, stream)
+        if self.trace is not None:
+            self.trace.append(("reorder", files, sources.tolist()))
+
     # ---- the run -------------------------------------------------------------------
     def run(self):
         cfg, torch = self.cfg, self.torch
@@ -123,9 +176,13 @@ class RagDriver:
             lip = _Lip()
             lip.rid, lip.topic, lip.arrival = rid, int(topics[rid]), t
             counts[lip.topic] += 1
-            lip.to_decode = cfg.answer_tokens
+            lip.to_decode, lip.beams = cfg.answer_tokens, None
             if lip.topic in cache:       # prompt cache hit: share the document's pages
-                lip.fid, lip.to_prefill, lip.hit = self._fork(cache[lip.topic]), 0, True
+                lip.to_prefill, lip.hit = 0, True
+                if cfg.beams > 1:
+                    lip.fid, lip.beams = None, self._spread(cache[lip.topic])
+                else:
+                    lip.fid = self._fork(cache[lip.topic])
                 hits += 1
             else:
                 lip.fid, lip.to_prefill, lip.hit = self._open(), cfg.doc_tokens, False
@@ -155,15 +212,22 @@ class RagDriver:
                 continue
             self.timer.fired(fire)
             batch = [calls.popleft() for _ in range(fire)]
-            kv = [self.h[lip.fid] for lip, _ in batch]
-            nt = [n for _, n in batch]
+            fids, nt = [], []
+            for lip, n in batch:
+                fids += lip.beams or [lip.fid]
+                nt += [n] * (len(lip.beams) if lip.beams else 1)
+            kv = [self.h[f] for f in fids]
             T = sum(nt)
             t0 = time.perf_counter()
             self.sess.ctx.pred_batch(kv, nt, self.q, self.k, self.v, self.out, stream)
+            if self.trace is not None:
+                self.trace.append(("pred", fids, nt))
+            searching = [lip for lip, _ in batch if lip.beams]
+            if searching:
+                self._choose(searching)
             torch.cuda.current_stream(self.sess.device).synchronize()
             dt = (time.perf_counter() - t0) * 1e6
             if self.trace is not None:
-                self.trace.append(("pred", [lip.fid for lip, _ in batch], nt))
                 self.outputs.append(self.out[:T].cpu().numpy().copy())
             now += dt
             busy += dt
@@ -176,10 +240,16 @@ class RagDriver:
                     prefilled += n
                     if lip.to_prefill == 0:
                         retain_after_prefill(lip)
+                        if cfg.beams > 1:
+                            lip.beams = self._spread(lip.fid)
+                            self._remove(lip.fid)
                 else:
                     lip.to_decode -= 1
                 if lip.to_prefill == 0 and lip.to_decode == 0:
-                    self._remove(lip.fid)
+                    if lip.beams:
+                        self._remove_all(lip.beams)
+                    else:
+                        self._remove(lip.fid)
                     lat.append(now - lip.arrival)
                     done += 1
                 else:

@@ -604,3 +604,52 @@ def test_a_search(layers):
     f.ctx.kv_remove_batch(kv)
     assert f.ctx.free_pages() == 260
     f.sess.close()
+
+
+@pytest.mark.parametrize("pareto_index", [0.5, 2.0])
+def test_rag_answers_with_beams(pareto_index):
+    """The RAG driver with three beams to an answer, replayed operation by operation on the state model: every batch's outputs, the
+    page tables at the end; its scores fall from beam to beam."""
+    from oracle.driver import OracleSession
+    from paper_2510_25412_amd import rag
+    shape = synth.Shape(32, 8, 128, 16, synth.BF16)
+    cfg = rag.RagConfig(n_docs=6, doc_tokens=75, answer_tokens=4, retain=2, pareto_index=pareto_index, rate_per_s=20000.0, n_requests=16, prefill_chunk=64,
+                        max_batch=6, max_wait_us=200.0, seed=17, beams=3, vocab=1001)
+    sess = driver.HipSession(shape, 600, max_lips=18, max_tokens=6 * 64 + 64, max_entries=18 * 10 + 64, poison=True)
+    print(f"[case] rag with beams, pareto={pareto_index}", flush=True)
+    d = rag.RagDriver(sess, cfg, trace=True)
+    res = d.run()
+    assert res["requests"] == 16 and res["cached_topics"] <= 2
+    osess = OracleSession(shape, 600)
+    osess.model = oracle.BeamFiles(600, 16)
+    outputs = iter(d.outputs)
+    for op in d.trace:
+        h = osess.h
+        if op[0] == "pred":
+            T = sum(op[2])
+            ref = osess.pred(dict(files=op[1], n_tokens=op[2], q=d.q_host[:T], k_new=d.k_host[:T], v_new=d.v_host[:T]), dtype=np.float64)
+            got = next(outputs)
+            assert (np.abs(got - ref) <= 2e-3 * np.maximum(1.0, np.abs(ref))).all()      # the bar of every bf16 pred
+        elif op[0] == "fork_batch":
+            new, copies = osess.model.kv_fork_batch([h[f] for f in op[2]], True)
+            h.update(zip(op[1], new))
+            for c in copies:
+                osess.pool.copy_slots(*c)
+        elif op[0] == "reorder":
+            for c in osess.model.kv_reorder([h[f] for f in op[1]], op[2], True):
+                osess.pool.copy_slots(*c)
+        elif op[0] == "remove_batch":
+            osess.model.kv_remove_batch([h.pop(f) for f in op[1]])
+        else:
+            osess.setup([op])
+    assert set(d.h) == set(osess.h) and sess.ctx.free_pages() == osess.model.free_pages()
+    for fid in d.h:
+        assert sess.ctx.kv_pages(d.h[fid]) == osess.model.kv_pages(osess.h[fid])
+    osess.model.audit()
+    # every request ends with the best of its beams first, and a token for every step
+    scores, tokens = d.scores.cpu().numpy(), d.tokens.cpu().numpy()
+    assert np.isfinite(scores).all() and (np.diff(scores, axis=1) <= 0).all()
+    assert (tokens >= 0).all() and (tokens < 1001).all()
+    d.close()
+    assert sess.ctx.free_pages() == 600
+    sess.close()
