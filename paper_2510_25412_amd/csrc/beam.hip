@@ -156,6 +156,15 @@ struct LogitBF16 {
       x[2 * i + 1] = as_f32(r.w[i] & 0xffff0000u);
     }
   }
+  // from the upper half of the first word on, to the lower half of the word behind
+  static __device__ __forceinline__ void unpack_late(const Raw& r, uint32_t behind, float (&x)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t next = i < 3 ? r.w[i + 1] : behind;
+      x[2 * i] = as_f32(r.w[i] & 0xffff0000u);
+      x[2 * i + 1] = as_f32(next << 16);
+    }
+  }
   static __device__ __forceinline__ Raw few(const uint8_t* p, int n) { return few16<Raw>(p, n); }
 };
 struct LogitF16 {
@@ -170,6 +179,15 @@ struct LogitF16 {
     for (int i = 0; i < 4; ++i) {
       x[2 * i] = (float)__builtin_bit_cast(_Float16, (uint16_t)r.w[i]);
       x[2 * i + 1] = (float)__builtin_bit_cast(_Float16, (uint16_t)(r.w[i] >> 16));
+    }
+  }
+  // from the upper half of the first word on, to the lower half of the word behind
+  static __device__ __forceinline__ void unpack_late(const Raw& r, uint32_t behind, float (&x)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t next = i < 3 ? r.w[i + 1] : behind;
+      x[2 * i] = (float)__builtin_bit_cast(_Float16, (uint16_t)(r.w[i] >> 16));
+      x[2 * i + 1] = (float)__builtin_bit_cast(_Float16, (uint16_t)next);
     }
   }
   static __device__ __forceinline__ Raw few(const uint8_t* p, int n) { return few16<Raw>(p, n); }
@@ -262,12 +280,12 @@ __device__ __forceinline__ Part<E, MASKED, TINY> part_of(const SelectArgs& a, in
 // group where it is found first; the choice needs no more to know where it has to look again.
 // FAR: more logits than the last-level cache holds are read past it (268 MB 62.7 -> 58.8 us a call, 537 MB 123.6 -> 115.3), fewer may lie there from their
 // making, or from this kernel when the choice looks at some again (52 MB 24.4 us, past the cache 27.3; 67 MB 23.8, 24.3).
-template <typename E, bool MASKED, bool TINY, bool FAR>
+template <typename E, bool MASKED, bool TINY, bool FAR, bool HALVES = false>
 __global__ __launch_bounds__(64) void select_rows_kernel(SelectArgs a) {
   const int lane = threadIdx.x & 63;
   const int row = (int)(blockIdx.x / (uint32_t)a.parts), part = (int)(blockIdx.x % (uint32_t)a.parts);
   const int64_t at = blockIdx.x;
-  const float score = a.scores[row];
+  const float score = as_f32((uint32_t)sload((const int32_t*)a.scores + row));
   const auto p = part_of<E, MASKED, TINY>(a, row, part * part_groups<E>(a));
   if (p.first >= p.end || !(fabsf(score) < INFINITY)) {    // behind the row's end, or no beam lives here
     a.most[at * 64 + lane] = -INFINITY;
@@ -288,24 +306,54 @@ __global__ __launch_bounds__(64) void select_rows_kernel(SelectArgs a) {
   int most_at = p.first + lane;
   const int batches = (p.end - p.first + 64 * kAhead - 1) / (64 * kAhead);
   const auto group = [&](int i, int d) __attribute__((always_inline)) { return p.first + (i * kAhead + d) * 64 + lane; };
+  // HALVES: rows of 16-bit logits some of which begin in the middle of a word (every other one of an odd vocabulary).  16 bytes from there cost the
+  // memory more than from a word's beginning, so batches that are not at an end of such a row read a half word early, and each lane
+  // takes its last logit from the next one (2048 rows of 131071 bf16 logits 144 -> 119 us a call; where no row begins so the
+  // registers that this takes cost 67 MB 1.8 us of 23.3).
+  const bool late = HALVES && ((uintptr_t)p.row & 2);
+  const auto early = [&](int i) __attribute__((always_inline)) {
+    const int from = p.first + i * kAhead * 64, to = from + kAhead * 64;
+    return late && from > 0 && to <= p.end && to * N < p.vocab;
+  };
   struct Batch {
     typename E::Raw raw[kAhead];
-    uint32_t m[kAhead];
+    uint32_t m[kAhead], behind;                            // the word behind the last lane's
   };
   uint32_t m_next[kAhead];                                 // allowed bits are known a batch before the logits that they ask for
   const auto load = [&](Batch& b, int i) __attribute__((always_inline)) {
+    if (HALVES && early(i)) {
+      const uint8_t* row = p.row - 2;
 #pragma unroll
-    for (int d = 0; d < kAhead; ++d) {
-      b.m[d] = m_next[d];
-      b.raw[d] = p.template raw<FAR>(group(i, d), b.m[d] != 0);
+      for (int d = 0; d < kAhead; ++d) b.raw[d] = E::template load<FAR>(row + (uint32_t)group(i, d) * 16);
+      if (lane == 63) b.behind = *(const uint32_t*)(row + (uint32_t)(group(i, kAhead - 1) + 1) * 16);
+    } else {
+#pragma unroll
+      for (int d = 0; d < kAhead; ++d) {
+        b.m[d] = m_next[d];
+        b.raw[d] = p.template raw<FAR>(group(i, d), b.m[d] != 0);
+      }
     }
 #pragma unroll
     for (int d = 0; d < kAhead; ++d) m_next[d] = p.allowed(group(i + 1, d));
   };
   const auto add = [&](const Batch& b, int i) __attribute__((always_inline)) {
     float x[kAhead][N];
+    if constexpr (HALVES) {
+      if (early(i)) {
 #pragma unroll
-    for (int d = 0; d < kAhead; ++d) E::unpack(b.raw[d], x[d]);
+        for (int d = 0; d < kAhead; ++d) {
+          const uint32_t first = b.raw[d].w[0], last = d + 1 < kAhead ? __builtin_amdgcn_readfirstlane(b.raw[d + 1 < kAhead ? d + 1 : d].w[0]) : b.behind;
+          const uint32_t next = __builtin_amdgcn_update_dpp(first, first, 0x130, 0xf, 0xf, false);      // wave_shl:1
+          E::unpack_late(b.raw[d], lane == 63 ? last : next, x[d]);
+        }
+      } else {
+#pragma unroll
+        for (int d = 0; d < kAhead; ++d) E::unpack(b.raw[d], x[d]);
+      }
+    } else {
+#pragma unroll
+      for (int d = 0; d < kAhead; ++d) E::unpack(b.raw[d], x[d]);
+    }
     if (MASKED || TINY || p.first + (i + 1) * kAhead * 64 > whole) {
 #pragma unroll
       for (int d = 0; d < kAhead; ++d) p.mask(x[d], group(i, d), b.m[d]);
@@ -610,7 +658,15 @@ template <typename E, bool MASKED, bool TINY>
 void launch_rows(const SelectArgs& a, hipStream_t st) {
   const dim3 grid((unsigned)(a.rows * a.parts)), block(64);
   if constexpr (!MASKED && !TINY) {
-    if ((int64_t)a.rows * a.vocab * E::kBytes >= kLastLevelBytes) {
+    const bool far = (int64_t)a.rows * a.vocab * E::kBytes >= kLastLevelBytes;
+    if constexpr (E::kBytes == 2) {
+      if (((uintptr_t)a.logits & 2) || (a.rows > 1 && (a.stride & 1))) {
+        if (far) select_rows_kernel<E, false, false, true, true><<<grid, block, 0, st>>>(a);
+        else select_rows_kernel<E, false, false, false, true><<<grid, block, 0, st>>>(a);
+        return;
+      }
+    }
+    if (far) {
       select_rows_kernel<E, false, false, true><<<grid, block, 0, st>>>(a);
       return;
     }
