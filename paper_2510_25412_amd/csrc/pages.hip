@@ -13,8 +13,17 @@ struct CopyList {
 
 // The filled slots of pages, bit for bit.  A page is 4 * Hkv pieces (kv head, K or V, row half) of 16 slots of 128 bytes; the first r
 // slots of a piece lie together, so the 16-byte chunks of a copy are counted through, r * 8 to a piece.  Sources and destinations are
-// different pages.  Bound: HBM, read + write.
+// different pages.  Bound: HBM, read + write.  Half of a server's pool (9837 pages, 2 layers, 1.29 GB read, as much written) 409..422 us = 6.1..6.3 TB/s,
+// with two chunks to a thread, past the caches both ways (plain stores 438, plain loads 425, four chunks 420..437, eight 445..468).
+// Few copies are of last pages, which several forks take: plain loads (239 copies x 8 layers, a call 24.2 us; 26.0 past the caches).
+// A copy of r slots takes nearly as long as one of 16: the beginnings of pieces, 2 KB apart, lie in the same few of the memory's channels, and what
+// those move decides (240 copies x 8 layers of 1, 4, 15 slots: 23, 28, 38 us, 8, 31 and 118 MB written).
 constexpr int kCopyChunks = 2;         // chunks of a thread
+template <bool PAST>
+__device__ __forceinline__ u32x4_t load16(const uint8_t* p) {
+  if constexpr (PAST) return __builtin_nontemporal_load((const u32x4_t*)p);
+  else return *(const u32x4_t*)p;
+}
 template <bool BY_ARGS, int N>
 __global__ __launch_bounds__(256) void copy_kernel(CopyArgs a, CopyList<N> l) {
   const int e = 3 * (int)blockIdx.y;
@@ -39,7 +48,7 @@ __global__ __launch_bounds__(256) void copy_kernel(CopyArgs a, CopyList<N> l) {
       // i / per: with a half added, no quotient of an i below 2^21 is within its roundings of a whole number
       const uint32_t piece = (uint32_t)(((float)i + 0.5f) * inv);
       at[u] = (i + piece * (kP * 8 - per)) * 16;
-      v[u] = __builtin_nontemporal_load((const u32x4_t*)(s + at[u]));
+      v[u] = load16<!BY_ARGS>(s + at[u]);
     }
 #pragma unroll
     for (int u = 0; u < kCopyChunks; ++u)
