@@ -1858,7 +1858,7 @@ int64_t select_scratch(int64_t rows, int32_t most, int32_t vocab, int32_t n_best
   return align_up(parts * 8, 16) + align_up(parts * 4, 16) + 2 * parts * 64 * 4;
 }
 static_assert(kBeamsMost == SYM_BEAMS_MOST && kBestMost == SYM_BEST_MOST, "the header's limits");
-constexpr int64_t kStateBlocks = 1 << 22;              // workgroups of a launch
+constexpr int64_t kStateBlocks = 1 << 16;              // workgroups of an array in a launch, about: a gigabyte and more
 }  // namespace
 
 int64_t sym_beam_scratch_bytes(int32_t n_groups, const int32_t* beams, int32_t vocab, int32_t n_best) {
@@ -2007,7 +2007,7 @@ int sym_beam_states(sym_ctx* c, int32_t n_groups, const int32_t* beams, int64_t 
         const sym_beam_state& s = states[i];
         if (s.outer == 0 || s.row_bytes == 0) continue;
         // stretches of columns, then of the outer dimension, so that a launch has no more workgroups than it may
-        const int64_t chunk = (int64_t)state_columns(most) * kStateThreads * kStateUnit, slice = (kStateBlocks / n - 1) * chunk;
+        const int64_t chunk = (int64_t)state_columns(most) * kStateThreads * kStateUnit, slice = std::max<int64_t>(1, kStateBlocks / n) * chunk;
         for (int64_t col = 0; col < s.row_bytes; col += slice) {
           const int64_t bytes = std::min(slice, s.row_bytes - col);
           const int64_t chunks = (bytes + chunk - 1) / chunk;

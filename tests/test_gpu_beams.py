@@ -183,6 +183,49 @@ def test_rows_that_lie_apart(ctx):
         choose(ctx, x, s, [2, 4], 9, allowed, shared)
 
 
+def test_many_requests_of_unlike_widths(ctx):
+    # more than travel with a launch
+    beams = np.random.default_rng(6).integers(1, 6, 700).tolist()
+    x, s = make(sum(beams), 300, "bf16", 60)
+    s[torch.rand(len(s), generator=torch.Generator().manual_seed(1)).cuda() < 0.4] = -math.inf      # some requests have no beam left
+    compare(choose(ctx, x, s, beams, 6), x, s, beams, 6)
+
+
+def test_the_largest_vocabulary(ctx):
+    for dtype in ("bf16", "f32"):
+        print(f"[case] largest vocabulary {dtype}", flush=True)
+        x, s = make(2, 1 << 24, dtype, 61)
+        x[1, -1], x[0, 0] = 30.0, 29.0
+        compare(choose(ctx, x, s, [2], 5), x, s, [2], 5)
+
+
+@pytest.mark.parametrize("rows,vocab,dtype,beams,best", [(1060, 131071, "bf16", 4, 8), (528, 131072, "f32", 4, 8), (2050, 65536, "f16", 5, 40)])
+def test_logits_beyond_the_last_level_cache(ctx, rows, vocab, dtype, beams, best):
+    print(f"[case] {rows} rows of {vocab} {dtype}", flush=True)
+    x, s = torch.empty((rows, vocab), dtype=TYPES[dtype], device="cuda").normal_(generator=torch.Generator(device="cuda").manual_seed(3)).mul_(2.5), -20 * torch.rand(rows, device="cuda")
+    groups = rows // beams
+    got = choose(ctx, x, s, [beams] * groups, best)
+    for g in [0, 1, groups // 2, groups - 1]:
+        at = slice(g * beams, (g + 1) * beams)
+        compare([o[g:g + 1] for o in got], x[at], s[at], [beams], best)
+
+
+def test_two_calls_at_once(ctx):
+    # on two streams, with scratch of their own
+    jobs, streams = [], [torch.cuda.Stream() for _ in range(2)]
+    for k in range(2):
+        x, s = make(64, 30011 + k, "bf16", 70 + k)
+        jobs.append((x, s, [torch.empty((16, 8), dtype=t, device="cuda") for t in (torch.float32, torch.int32, torch.int32)],
+                     torch.empty(binding.beam_scratch_bytes([4] * 16, 30011 + k, 8), dtype=torch.uint8, device="cuda")))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for (x, s, out, scratch), st in zip(jobs, streams):
+            ctx.beam_select([4] * 16, 8, x, s, *out, scratch, None, st.cuda_stream)
+    torch.cuda.synchronize()
+    for x, s, out, _ in jobs:
+        compare([o.cpu().numpy() for o in out], x, s, [4] * 16, 8)
+
+
 def test_far_rows(ctx):
     # row offsets beyond 2^32 bytes, and beyond 2^31 elements
     stride, rows = 1 << 29, 6
@@ -279,6 +322,17 @@ def test_many_groups_and_long_rows(ctx):
     y = x.clone()
     ctx.beam_states([3], torch.tensor([1, 2, 0], dtype=torch.int32, device="cuda"), binding.make_states([(y, y, 0)]), stream())
     assert torch.equal(y, x[[1, 2, 0]])
+    x = torch.randint(-128, 127, (1300, 900001), dtype=torch.int8, device="cuda")          # many groups of rows that are cut, and of an odd length
+    p = torch.from_numpy(np.tile([1, 0], 650).astype(np.int32)).cuda()
+    y = x.clone()
+    ctx.beam_states([2] * 650, p, binding.make_states([(y, y, 0)]), stream())
+    assert torch.equal(y.view(650, 2, -1)[:, 0], x.view(650, 2, -1)[:, 1]) and torch.equal(y.view(650, 2, -1)[:, 1], x.view(650, 2, -1)[:, 0])
+    del x, y
+    x = torch.randint(-1000, 1000, (700, 8, 70000), dtype=torch.int16, device="cuda")      # an outer dimension that is cut
+    y = torch.empty_like(x)
+    ctx.beam_states([2] * 4, p[:8], binding.make_states([(y, x, 1)] * 1 + [(x[:, :, :0], x[:, :, :0], 1)]), stream())
+    assert torch.equal(y[:, 0::2], x[:, 1::2]) and torch.equal(y[:, 1::2], x[:, 0::2])
+    del x, y
     far = torch.empty((5, 3, 1 << 30), dtype=torch.int8, device="cuda")                    # an array beyond 2^32 bytes, strides too
     view = far[:, :, :1000]
     view.copy_(torch.randint(-128, 127, (5, 3, 1000), dtype=torch.int8, device="cuda"))
