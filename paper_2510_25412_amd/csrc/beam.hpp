@@ -43,12 +43,22 @@ struct SelectArgs {
 struct SelectCut {
   int32_t bits, part_octets;
 };
-constexpr int kSelectWaves = 2048;
-inline SelectCut select_cut(int64_t rows, int32_t most_beams, int32_t vocab, int32_t n_best) {
-  const int64_t octets = (vocab + kOctet - 1) / kOctet, want = (kSelectWaves + rows - 1) / rows, most = std::min<int64_t>(kMostParts / most_beams, 64);
+// Parts, first, until the lists of one row can hold a choice.  Then, while a part has more than 2048 logits (a wavefront's loads under way), until there
+// are 2048 wavefronts, but no more parts of a group than 512 threads hold in the second launch (rows of 131072 bf16 logits, calls of 4, 16, 64 requests
+// of 4 beams: 11.7, 13.9, 22 us; with up to 256 parts of a group 16.0, 15.2, 22; wavefronts 1024 or 4096: 13.9 and 19.8 us for 16 requests), or until a
+// part has no more than 40960 logits of 16 bits (2048 rows of 131072: 97 us; 20480 101, 10240 105, 81920 100), 10240 of fp32 (1024 rows of 65537, 32
+// choices of 16 beams: 58 us; 62 with half as many or four times as many: what is looked at again is a list, a 64th of a part).
+constexpr int kSelectWaves = 2048, kSelectParts = 64;
+inline SelectCut select_cut(int64_t rows, int32_t most_beams, int32_t vocab, int32_t n_best, int32_t logit_bytes) {
+  const int64_t octets = (vocab + kOctet - 1) / kOctet, most = std::min<int64_t>(kMostParts / most_beams, 64);
+  const int64_t longest = logit_bytes == 4 ? 1280 : 5120;
   int32_t bits = 0;
-  // enough lists that the best of one row's are a choice's; then wavefronts, of no more than 8192 logits and no less than 2048
-  while ((2ll << bits) <= most && ((32ll << bits) < n_best || ((octets >> bits) > 256 && ((1ll << bits) < want || (octets >> bits) > 1280)))) ++bits;
+  const auto more = [&] {
+    if ((32ll << bits) < n_best) return true;
+    if ((octets >> bits) <= 256) return false;
+    return (octets >> bits) > longest || ((rows << bits) < kSelectWaves && ((int64_t)most_beams << (bits + 1)) <= kSelectParts);
+  };
+  while ((2ll << bits) <= most && more()) ++bits;
   return SelectCut{bits, (int32_t)((((octets + (1ll << bits) - 1) >> bits) + 63) / 64 * 64)};
 }
 

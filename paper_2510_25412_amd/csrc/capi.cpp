@@ -1854,7 +1854,7 @@ int32_t group_rows(int32_t n_groups, const int32_t* beams, int32_t g0, int32_t r
   return n;
 }
 int64_t select_scratch(int64_t rows, int32_t most, int32_t vocab, int32_t n_best) {
-  const int64_t parts = rows << select_cut(rows, most, vocab, n_best).bits;
+  const int64_t parts = rows << select_cut(rows, most, vocab, n_best, 4).bits;      // (16-bit logits have no more)
   return align_up(parts * 8, 16) + align_up(parts * 4, 16) + 2 * parts * 64 * 4;
 }
 static_assert(kBeamsMost == SYM_BEAMS_MOST && kBestMost == SYM_BEST_MOST, "the header's limits");
@@ -1902,7 +1902,7 @@ int sym_beam_select(sym_ctx* c, const sym_beam_step* b, void* stream) {
     if (!launch_select_rows || !stream_captures) return fail(c, SYM_EHIP, "beam_select: this build has no kernels");
     const OnDevice on(c);
     hipStream_t st = (hipStream_t)stream;
-    const SelectCut cut = select_cut(rows, most, b->vocab, b->n_best);
+    const SelectCut cut = select_cut(rows, most, b->vocab, b->n_best, (int32_t)es);
     const int64_t parts = rows << cut.bits;
     uint8_t* at = (uint8_t*)b->scratch;
     const auto take = [&](int64_t bytes) {
