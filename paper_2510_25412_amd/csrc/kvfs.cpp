@@ -519,11 +519,12 @@ bool Kvfs::copy_last(int32_t id, CopyPlan* plan) {
   return true;
 }
 
-// How many leading entries two tables share: by 64 at a time while they do (memcmp has wide loads, a search for the first difference has not).
+// How many leading entries two tables share: by 64, 8 and 1 at a time while they do (memcmp has wide loads, a search for the first difference has not).
 static size_t same_pages(const std::vector<int32_t>& a, const std::vector<int32_t>& b) {
   const size_t n = std::min(a.size(), b.size());
   size_t i = 0;
   while (i + 64 <= n && !std::memcmp(a.data() + i, b.data() + i, 64 * 4)) i += 64;
+  while (i + 8 <= n && !std::memcmp(a.data() + i, b.data() + i, 8 * 4)) i += 8;
   while (i < n && a[i] == b[i]) ++i;
   return i;
 }
