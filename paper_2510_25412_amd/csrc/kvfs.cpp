@@ -79,6 +79,8 @@ int32_t Kvfs::new_file() {
     free_file_ids_.pop_back();
   } else {
     id = (int32_t)files_.size();
+    if (files_.size() == files_.capacity()) files_.reserve(std::max<size_t>(64, 2 * files_.size()));
+    free_file_ids_.reserve(files_.capacity());      // so that no file's end allocates
     files_.emplace_back();
   }
   KvFile& f = files_[id];
@@ -94,16 +96,18 @@ int32_t Kvfs::new_file() {
 }
 
 int32_t Kvfs::new_handle(int32_t file_id) {
+  std::vector<int32_t>& of = files_[file_id].handles;
+  if (of.size() == of.capacity()) of.reserve(2 * of.size() + 1);      // what may fail comes first
   int32_t h;
   if (free_handles_.size()) {
     h = free_handles_.pop_lowest();        // lowest free handle slot
   } else {
     h = (int32_t)handle_file_.size();
-    handle_file_.push_back(-1);
     free_handles_.reach(h + 1);
+    handle_file_.push_back(-1);
   }
   handle_file_[h] = file_id;
-  files_[file_id].handles.push_back(h);
+  of.push_back(h);
   return h;
 }
 
@@ -545,19 +549,32 @@ int Kvfs::fork_batch(int32_t n, const int32_t* parents, bool own_last, int32_t* 
     return SYM_ENOSPC;
   }
   plan->copies.reserve(3 * (size_t)need);
+  // The files first, without their entries' counts: what may fail.
+  int32_t made = 0, id = -1;
+  try {
+    for (; made < n; ++made, id = -1) {
+      const int32_t pid = handle_file_[parents[made]];
+      id = new_file();                          // may grow files_: the parent by index
+      files_[id].pages = files_[pid].pages;
+      files_[id].len = files_[pid].len;
+      files_[id].bounded = files_[pid].bounded;
+      out[made] = new_handle(id);
+    }
+  } catch (...) {
+    const auto drop = [&](int32_t file) {
+      files_[file].pages.clear();
+      drop_file(file);
+    };
+    if (id >= 0) drop(id);
+    while (made > 0) drop(handle_file_[out[--made]]);
+    throw;
+  }
   // A parent's forks one after the other: its pages are counted once for all of them.
   for (int32_t i = 0, j; i < n; i = j) {
     const int32_t pid = handle_file_[parents[i]];
     for (j = i + 1; j < n && handle_file_[parents[j]] == pid;) ++j;
     for (int32_t p : files_[pid].pages) refcount_[p] += (uint32_t)(j - i);
-    for (int32_t k = i; k < j; ++k) {
-      const int32_t id = new_file();            // may grow files_: the parent by index
-      files_[id].pages = files_[pid].pages;
-      files_[id].len = files_[pid].len;
-      files_[id].bounded = files_[pid].bounded;
-      out[k] = new_handle(id);
-      if (own_last) copy_last(id, plan);
-    }
+    for (int32_t k = i; own_last && k < j; ++k) copy_last(handle_file_[out[k]], plan);
   }
   return SYM_OK;
 }

@@ -43,8 +43,9 @@ class RankSet {
   }
   void reach(int64_t n) {                     // room for ranks up to n - 1, none of the new ones free
     if ((int64_t)l0_.size() * 64 >= n) return;
-    l0_.resize((size_t)((n + 63) / 64 * 2), 0);
-    l1_.resize((l0_.size() + 63) / 64, 0);
+    const size_t words = (size_t)((n + 63) / 64 * 2);
+    l1_.resize((words + 63) / 64, 0);         // (first: where there is room for a rank, there is room above)
+    l0_.resize(words, 0);
   }
   int64_t size() const { return count_; }
   int32_t pop_lowest() {                      // the caller has checked size() > 0
