@@ -277,7 +277,8 @@ __device__ __forceinline__ Part<E, MASKED, TINY> part_of(const SelectArgs& a, in
 }
 
 // One pass over the logits.  Of every part: its normaliser's share, and for each lane (a list: groups 64 apart) the largest logit and the
-// group where it is found first; the choice needs no more to know where it has to look again.
+// group where it is found first; the choice needs no more to know where it has to look again.  Bound: HBM where the rows are many (1024 rows of 65537
+// fp32 logits, 268 MB: 46 us, 5.9 TB/s), what is under way where they are few (256 rows of 131072 bf16 logits, 67 MB: 14 us, 4.7 TB/s).
 // FAR: more logits than the last-level cache holds are read past it (268 MB 62.7 -> 58.8 us a call, 537 MB 123.6 -> 115.3), fewer may lie there from their
 // making, or from this kernel when the choice looks at some again (52 MB 24.4 us, past the cache 27.3; 67 MB 23.8, 24.3).
 template <typename E, bool MASKED, bool TINY, bool FAR, bool HALVES = false>
@@ -412,40 +413,76 @@ __device__ __forceinline__ uint64_t rest_of(int row, float value, int token) { r
 __device__ __forceinline__ bool before(const Choice& a, const Choice& b) { return a.score > b.score || (a.score == b.score && a.rest < b.rest); }
 constexpr uint64_t kNone = ~0ull;
 
-constexpr int kFound = 1024;           // choices that are sorted by counting what comes before each
-constexpr int kFoundLists = 512;
 constexpr int kFewLists = 4096, kFewThreads = 512;
 struct RowScore {
   double base, from;
 };
 
-// The best choice of what `each` shows to `see` in every thread, behind `last` (k > 0): the threads' best in `best`, then one of them.
-template <int THREADS, typename F>
-__device__ __forceinline__ Choice next_best(Choice* best, int k, const Choice& last, F each) {
+__device__ __forceinline__ double of_order(uint64_t k) { return __builtin_bit_cast(double, k >> 63 ? k ^ 1ull << 63 : ~k); }
+// The K-th of the threads' choices, from the highest bit down, of the scores first.
+__device__ __forceinline__ Choice kth_best(const Choice& mine, int K) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, mine.score + 0.0), key = u ^ ((uint64_t)((int64_t)u >> 63) | 1ull << 63);
+  uint64_t score = 0, rest = kNone;
+  for (uint64_t bit = 1ull << 63; bit; bit >>= 1)
+    if (__syncthreads_count(key >= (score | bit)) >= K) score |= bit;
+  const int left = K - __syncthreads_count(key > score);
+  if (__syncthreads_count(key == score) == left) return Choice{of_order(score), kNone - 1};      // (all of them)
+  for (uint64_t bit = 1ull << 63; bit; bit >>= 1)
+    if (__syncthreads_count(key == score && mine.rest <= (rest ^ bit)) >= left) rest ^= bit;
+  return Choice{of_order(score), rest};
+}
+
+// The K best of many, in `found` in any order, or all where they are fewer; returns how many.  What `of` makes of turn t in a thread (N choices at
+// most; a bit for each that counts) goes there, and whenever it is full the K best stay and nothing behind them comes in any more.  Equal logits by
+// the thousand take this way: a choice of 64 requests of 4 beams of 131072 equal logits takes 0.31 ms with 8, 0.53 ms with 128.
+template <int THREADS, int N, typename F>
+__device__ __forceinline__ int keep_best(Choice* found, int* n_found, int K, int turns, F of) {
   const int tid = threadIdx.x;
-  Choice b = {0.0, kNone};
-  each([&](const Choice& x) __attribute__((always_inline)) {
-    if ((k == 0 || before(last, x)) && (b.rest == kNone || before(x, b))) b = x;
-  });
-  __syncthreads();                                         // the last one has been read
-  best[tid] = b;
+  Choice cut = {0.0, kNone};
+  __syncthreads();                                         // everyone has read how many there were
+  if (tid == 0) *n_found = 0;
   __syncthreads();
-  for (int d = THREADS / 2; d; d >>= 1) {
-    if (tid < d && best[tid + d].rest != kNone && (best[tid].rest == kNone || before(best[tid + d], best[tid]))) best[tid] = best[tid + d];
-    __syncthreads();
+  for (int t = 0; t < turns; ++t) {
+    Choice x[N];
+    uint32_t left = of(t, x);
+    for (bool last = false;;) {
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        if (!(left >> j & 1)) continue;
+        if (cut.rest != kNone && !before(x[j], cut)) {
+          left &= ~(1u << j);
+          continue;
+        }
+        const int to = atomicAdd(n_found, 1);
+        if (to >= THREADS) continue;
+        found[to] = x[j];
+        left &= ~(1u << j);
+      }
+      const bool over = __syncthreads_or(left);
+      const int n = min(*n_found, THREADS);
+      if (!over && (last || t + 1 < turns || n <= K)) break;
+      last = !over;
+      const Choice mine = tid < n ? found[tid] : Choice{-(double)INFINITY, kNone};
+      cut = kth_best(mine, K);
+      if (tid == 0) *n_found = 0;
+      __syncthreads();
+      if (tid < n && !before(cut, mine)) found[atomicAdd(n_found, 1)] = mine;
+      __syncthreads();
+    }
   }
-  return best[0];
+  return *n_found;
 }
 
 // One workgroup for a group.  A value that the K best reach comes from 256 disjoint subsets' largest: of every row some lists, since the best
 // may all be one row's.  Lists that reach it are read again, and what reaches it in them is sorted.  What is read of the rows' pass is
-// requested at once and kept, so that a choice is three round trips: where the group's rows are, their lists, the logits looked at again.
+// requested at once and kept, so that a choice is three round trips: where the group's rows are, their lists, the logits looked at again.  Bound: those
+// and the steps between (6..8 us for 1..64 requests of 4 beams, 8 choices; 12 for 32 choices of 16 beams).
 template <typename E, bool MASKED, bool TINY, int THREADS, int kHeld>
 __global__ __launch_bounds__(THREADS) void select_best_kernel(SelectArgs a, GroupRows g, int group0) {
   __shared__ RowScore rows[kBeamsMost];
   __shared__ float subset[THREADS];
-  __shared__ Choice found[kFound];
-  __shared__ uint16_t list[kFoundLists];
+  __shared__ Choice found[THREADS];      // choices that are sorted by counting what comes before each
+  __shared__ uint16_t list[THREADS];
   __shared__ int n_list, n_found;
   const int tid = threadIdx.x, K = a.n_best, bits = a.parts_bits, parts = 1 << bits;
   const int row0 = g.row(blockIdx.x), beams = g.rows(blockIdx.x), all = beams << bits;
@@ -475,20 +512,6 @@ __global__ __launch_bounds__(THREADS) void select_best_kernel(SelectArgs a, Grou
   __syncthreads();
   // scores as 32 bits round them, which keeps their order: at most K - 1 are above one that is below the K-th of any K
   const auto scored = [&](int row, float value) __attribute__((always_inline)) { return ((double)value - rows[row].from) + rows[row].base; };
-  // The K-th largest of the 256 threads' values, or of as many subsets of four threads', or a little less.
-  const auto reached = [&](float top) __attribute__((always_inline)) {
-    subset[tid] = top;
-    __syncthreads();
-    float of[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int at = j * 64 + (tid & 63);
-      of[j] = subset[at];
-#pragma unroll
-      for (int more = 256; more < THREADS; more += 256) of[j] = fmaxf(of[j], subset[more + at]);
-    }
-    return reached_by(of, K, K + K / 8);
-  };
   float top = -INFINITY, score_of[kHeld];
 #pragma unroll
   for (int i = 0; i < kHeld; ++i) {
@@ -496,7 +519,18 @@ __global__ __launch_bounds__(THREADS) void select_best_kernel(SelectArgs a, Grou
     score_of[i] = l < of_group ? (float)scored(l >> (6 + bits), most[i]) : -INFINITY;
     top = fmaxf(top, score_of[i]);
   }
-  float low = reached(top);
+  // the K-th largest of 256 subsets' values, or a little less
+  subset[tid] = top;
+  __syncthreads();
+  float of[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int at = j * 64 + (tid & 63);
+    of[j] = subset[at];
+#pragma unroll
+    for (int more = 256; more < THREADS; more += 256) of[j] = fmaxf(of[j], subset[more + at]);
+  }
+  const float low = reached_by(of, K, K + K / 8);
 
   const auto see_lists = [&](auto see) __attribute__((always_inline)) {
     if (!(top >= low)) return;
@@ -510,59 +544,78 @@ __global__ __launch_bounds__(THREADS) void select_best_kernel(SelectArgs a, Grou
   };
   see_lists([&](const Choice&, int l) __attribute__((always_inline)) {
     const int to = atomicAdd(&n_list, 1);
-    if (to < kFoundLists) list[to] = (uint16_t)l;
+    if (to < THREADS) list[to] = (uint16_t)l;
   });
   __syncthreads();
   constexpr int N = E::kGroup;
   const int long_part = part_groups<E>(a);
   int lists = n_list;
-  if (lists > kFoundLists) {                               // many equals: exactly the K best lists, which hold the K best
-    lists = min(K, lists);
-    Choice last = {};
-    for (int k = 0; k < lists; ++k) {
-      last = next_best<THREADS>(found, k, last, [&](auto see) __attribute__((always_inline)) { see_lists([&](const Choice& x, int) __attribute__((always_inline)) { see(x); }); });
-      const int at = (int)(last.rest & 0xffffff), part = at / long_part;
-      if (tid == 0) list[k] = (uint16_t)((((int)(last.rest >> 56) << bits) + part) * 64 + ((at - part * long_part) & 63));
+  if (lists > THREADS) {                                   // many equals: the K best lists hold the K best
+    lists = keep_best<THREADS, 1>(found, &n_found, K, (of_group + THREADS - 1) / THREADS, [&](int t, Choice* x) {
+      const int l = tid + t * THREADS, row = l >> (6 + bits);
+      if (l >= of_group) return 0u;
+      const float value = a.most[at0 * 64 + l];
+      x[0] = Choice{scored(row, value), rest_of(row, value, a.most_at[at0 * 64 + l])};
+      return (float)x[0].score >= low ? 1u : 0u;
+    });
+    if (tid < lists) {
+      const uint64_t of = found[tid].rest;
+      const int at = (int)(of & 0xffffff), part = at / long_part;
+      list[tid] = (uint16_t)((((int)(of >> 56) << bits) + part) * 64 + ((at - part * long_part) & 63));
     }
+    __syncthreads();
+    if (tid == 0) n_found = 0;
     __syncthreads();
   }
 
   // Lanes for a list: as many as it has groups, up to a wavefront.
   const int wide = 32 - __builtin_clz(min(long_part >> 6, 64) * 2 - 1) - 1;
-  const auto see_groups = [&](auto see) __attribute__((always_inline)) {
-    for (int i = tid >> wide; i < lists; i += THREADS >> wide) {
-      const int l = list[i], row = l >> (6 + bits), first = ((l >> 6) & (parts - 1)) * long_part;
-      const auto p = part_of<E, MASKED, TINY>(a, row0 + row, first);
+  const int side = tid & ((1 << wide) - 1), at_once = THREADS >> wide;
+  const auto list_of = [&](int i, int* row, int* first) __attribute__((always_inline)) {
+    const int l = list[i];
+    *row = l >> (6 + bits);
+    *first = ((l >> 6) & (parts - 1)) * long_part;
+    return *first + (l & 63) + side * 64;
+  };
+  for (int i = tid >> wide; i < lists; i += at_once) {
+    int row, first;
+    const int from = list_of(i, &row, &first);
+    const auto p = part_of<E, MASKED, TINY>(a, row0 + row, first);
 #pragma unroll 2
-      for (int o = first + (l & 63) + (tid & ((1 << wide) - 1)) * 64; o < p.end; o += 64 << wide) {
-        float x[N];
-        p.read(o, x);
+    for (int o = from; o < p.end; o += 64 << wide) {
+      float x[N];
+      p.read(o, x);
 #pragma unroll
-        for (int j = 0; j < N; ++j) {
-          const double s = scored(row, x[j]);
-          if ((float)s >= low) see(Choice{s, rest_of(row, x[j], p.token(o, j))});
+      for (int j = 0; j < N; ++j) {
+        const double s = scored(row, x[j]);
+        if ((float)s >= low) {
+          const int to = atomicAdd(&n_found, 1);
+          if (to < THREADS) found[to] = Choice{s, rest_of(row, x[j], p.token(o, j))};
         }
       }
     }
-  };
-  // What reaches it, or, where that is too much, the K-th largest of what the threads see of it.
-  int n;
-  for (int turn = 0;; ++turn) {
-    float seen = -INFINITY;
-    see_groups([&](const Choice& x) __attribute__((always_inline)) {
-      const int to = atomicAdd(&n_found, 1);
-      if (to < kFound) found[to] = x;
-      seen = fmaxf(seen, (float)x.score);
+  }
+  __syncthreads();
+  int n = n_found;
+  if (n > THREADS) {
+    const int steps = (long_part + (64 << wide) - 1) / (64 << wide);
+    n = keep_best<THREADS, N>(found, &n_found, K, (lists + at_once - 1) / at_once * steps, [&](int t, Choice* best) {
+      const int i = (tid >> wide) + t / steps * at_once;
+      if (i >= lists) return 0u;
+      int row, first;
+      const int o = list_of(i, &row, &first) + t % steps * (64 << wide);
+      const auto p = part_of<E, MASKED, TINY>(a, row0 + row, first);
+      if (o >= p.end) return 0u;
+      float x[N];
+      p.read(o, x);
+      uint32_t reach = 0;
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        best[j] = Choice{scored(row, x[j]), rest_of(row, x[j], p.token(o, j))};
+        if ((float)best[j].score >= low) reach |= 1u << j;
+      }
+      return reach;
     });
-    __syncthreads();
-    n = n_found;
-    if (n <= kFound || turn == 3) break;
-    const float higher = reached(seen);
-    if (!(higher > low)) break;
-    low = higher;
-    __syncthreads();                                       // everyone has read the subsets, and what was found
-    if (tid == 0) n_found = 0;
-    __syncthreads();
   }
   const int64_t out = (int64_t)(group0 + blockIdx.x) * K;
   const auto write = [&](int k, const Choice& x) __attribute__((always_inline)) {
@@ -570,23 +623,14 @@ __global__ __launch_bounds__(THREADS) void select_best_kernel(SelectArgs a, Grou
     a.best_beams[out + k] = (int)(x.rest >> 56);
     a.best_tokens[out + k] = (int)(x.rest & 0xffffff);
   };
-  if (n <= kFound) {
-    for (int i = tid >> 2; i < n; i += THREADS / 4) {       // four lanes count for each
-      const Choice x = found[i];
-      int rank = 0;
+  for (int i = tid >> 2; i < n; i += THREADS / 4) {         // four lanes count for each
+    const Choice x = found[i];
+    int rank = 0;
 #pragma unroll 4
-      for (int k = tid & 3; k < n; k += 4) rank += before(found[k], x);
-      rank += __builtin_amdgcn_update_dpp(0, rank, 0xB1, 0xf, 0xf, false);
-      rank += __builtin_amdgcn_update_dpp(0, rank, 0x4E, 0xf, 0xf, false);
-      if (rank < K && (tid & 3) == 0) write(rank, x);
-    }
-  } else {                                                 // many large ones in few lists: one after the other
-    n = K;
-    Choice last = {};
-    for (int k = 0; k < K; ++k) {
-      last = next_best<THREADS>(found, k, last, see_groups);
-      if (tid == 0) write(k, last);
-    }
+    for (int k = tid & 3; k < n; k += 4) rank += before(found[k], x);
+    rank += __builtin_amdgcn_update_dpp(0, rank, 0xB1, 0xf, 0xf, false);
+    rank += __builtin_amdgcn_update_dpp(0, rank, 0x4E, 0xf, 0xf, false);
+    if (rank < K && (tid & 3) == 0) write(rank, x);
   }
   for (int k = n + tid; k < K; k += THREADS) {
     a.best_scores[out + k] = -INFINITY;
@@ -682,6 +726,8 @@ void launch_best(const SelectArgs& a, const GroupRows& g, int32_t group0, int32_
   const int lists = most * 64, deep = a.part_octets * (kOctet / E::kGroup) / 64;
   const dim3 grid((unsigned)n_groups);
   static_assert(1024 * 16 == 64 * kMostParts, "a thread holds its share of the lists");
+  // Half the threads where they hold the lists and what is looked at again is little: calls of 16 and 64 requests of 4 beams of 131072 bf16 logits, 8
+  // choices: 14.5 and 22.7 us, with 1024 threads 16.5 and 25.4; 64 requests with 128 choices (a list there is 32 groups): 33, with 512 threads 42.
   if (lists <= kFewLists && a.n_best * deep <= 1024) select_best_kernel<E, MASKED, TINY, kFewThreads, kFewLists / kFewThreads><<<grid, dim3(kFewThreads), 0, st>>>(a, g, group0);
   else select_best_kernel<E, MASKED, TINY, 1024, 16><<<grid, dim3(1024), 0, st>>>(a, g, group0);
 }

@@ -109,6 +109,23 @@ def test_equal_logits(ctx, dtype, vocab):
                 compare(got, x, same, beams, best)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("best", [8, 100, 128])
+def test_many_equals_in_few_places(ctx, dtype, best):
+    # rows 0..6 of a group have their largest logits in the first 512 of 40960, where a sixteenth of the threads look; then 640 places of one
+    # row that a sixth of them have looked at, among equal smaller ones
+    print(f"[case] equals in few places best={best} {dtype}", flush=True)
+    x = torch.full((64, 40960), -1.0, dtype=TYPES[dtype], device="cuda")
+    x[:7, :512] = 3
+    s = torch.full((64,), -2.0, device="cuda")
+    compare(choose(ctx, x, s, [64], best), x, s, [64], best)
+    y = torch.full((1, 131072), -1.0, dtype=TYPES[dtype], device="cuda")
+    part = y.view(64, 4, 64, 8)
+    part[0::8, 0, :, 0] = 3
+    part[1::8, 0, :16, 0] = 3
+    compare(choose(ctx, y, s[:1], [1], best), y, s[:1], [1], best)
+
+
 def test_equal_rows_at_unlike_addresses(ctx):
     # rows of an odd number of logits begin at every alignment: their scores have to be equal to the bit
     row = make(1, 4099, "bf16", 5)[0]
