@@ -550,6 +550,7 @@ int Kvfs::fork_batch(int32_t n, const int32_t* parents, bool own_last, int32_t* 
   }
   plan->copies.reserve(3 * (size_t)need);
   // The files first, without their entries' counts: what may fail.
+  std::vector<int32_t> ids((size_t)n);
   int32_t made = 0, id = -1;
   try {
     for (; made < n; ++made, id = -1) {
@@ -558,7 +559,8 @@ int Kvfs::fork_batch(int32_t n, const int32_t* parents, bool own_last, int32_t* 
       files_[id].pages = files_[pid].pages;
       files_[id].len = files_[pid].len;
       files_[id].bounded = files_[pid].bounded;
-      out[made] = new_handle(id);
+      ids[(size_t)made] = id;
+      new_handle(id);
     }
   } catch (...) {
     const auto drop = [&](int32_t file) {
@@ -566,7 +568,7 @@ int Kvfs::fork_batch(int32_t n, const int32_t* parents, bool own_last, int32_t* 
       drop_file(file);
     };
     if (id >= 0) drop(id);
-    while (made > 0) drop(handle_file_[out[--made]]);
+    while (made > 0) drop(ids[(size_t)--made]);
     throw;
   }
   // A parent's forks one after the other: its pages are counted once for all of them.
@@ -574,8 +576,9 @@ int Kvfs::fork_batch(int32_t n, const int32_t* parents, bool own_last, int32_t* 
     const int32_t pid = handle_file_[parents[i]];
     for (j = i + 1; j < n && handle_file_[parents[j]] == pid;) ++j;
     for (int32_t p : files_[pid].pages) refcount_[p] += (uint32_t)(j - i);
-    for (int32_t k = i; own_last && k < j; ++k) copy_last(handle_file_[out[k]], plan);
+    for (int32_t k = i; own_last && k < j; ++k) copy_last(ids[(size_t)k], plan);
   }
+  for (int32_t i = 0; i < n; ++i) out[i] = files_[ids[(size_t)i]].handles[0];      // (last: it may be the list of parents)
   return SYM_OK;
 }
 

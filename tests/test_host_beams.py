@@ -324,3 +324,21 @@ def test_state_arguments():
         code, what = call(*states, **kw)
         assert code == EINVAL and what != "host-only context", (states, kw, what)
     assert call(dict(row_bytes=0))[0] == 0 and call(dict(outer=0))[0] == 0 and call({}, n=0, rows=0)[0] == 0 and call()[0] == 0
+
+
+def test_forks_into_the_list_of_parents():
+    # the same array for both, and one entry further on
+    for shift in (0, 1):
+        ctx = host_ctx(64)
+        f = [ctx.kv_open(None) for _ in range(3)]
+        ctx.plan_append(f, [20, 33, 5])
+        arr = (C.c_int32 * 4)(f[0], f[1], f[1], f[2])
+        n = 4 - shift
+        out = C.cast(C.addressof(arr) + 4 * shift, C.POINTER(C.c_int32))
+        assert ctx.lib.sym_kv_fork_batch(ctx.h, n, arr, 1, out, None) == 0
+        new = list(arr)[shift:]
+        assert len(set(new) | set(f)) == n + 3
+        assert [ctx.kv_len(h) for h in new] == [20, 33, 33, 5][:n]
+        assert [list(c)[2] for c in ctx.last_copies()] == [4, 1, 1, 5][:n]
+        ctx.kv_remove_batch(f + new)
+        assert ctx.free_pages() == 64
