@@ -305,7 +305,8 @@ def make_states(arrays):
                 raise ValueError("the dimensions before the rows' must be one stretch")
             outer_stride = step if outer == 1 else outer_stride
             outer *= n
-        s.dst, s.src, s.outer, s.outer_stride, s.row_stride, s.row_bytes = dst.data_ptr(), src.data_ptr(), outer, outer_stride * es, stride[dim] * es, inner * es
+        step = stride[dim] if shape[dim] > 1 else inner                  # (of one row it says nothing)
+        s.dst, s.src, s.outer, s.outer_stride, s.row_stride, s.row_bytes = dst.data_ptr(), src.data_ptr(), outer, outer_stride * es, step * es, inner * es
     rows = {a[0].shape[a[2]] for a in arrays}
     if len(rows) > 1:
         raise ValueError(f"states of {sorted(rows)} rows")

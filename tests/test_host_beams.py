@@ -342,3 +342,16 @@ def test_forks_into_the_list_of_parents():
         assert [list(c)[2] for c in ctx.last_copies()] == [4, 1, 1, 5][:n]
         ctx.kv_remove_batch(f + new)
         assert ctx.free_pages() == 64
+
+
+def test_states_of_one_row():
+    # torch gives a dimension of one any stride
+    import torch
+    for x, dim in [(torch.zeros(5, 1).t(), 0), (torch.zeros(3, 8)[:, None], 1), (torch.zeros(4, 1, 6).expand(4, 1, 6), 1), (torch.zeros(7).as_strided((1, 7), (0, 1)), 0)]:
+        plan = binding.make_states([(x, x, dim)])
+        s = plan[0]
+        assert plan._rows == 1 and s.row_bytes == 4 * x[0].numel() if dim == 0 else s.row_bytes == 4 * x.shape[-1]
+        assert s.row_stride >= s.row_bytes and s.outer == (1 if dim == 0 else x.shape[0])
+        host = host_ctx()
+        refused(EINVAL, host.beam_states, [1], torch.zeros(1, dtype=torch.int32), plan)         # (of a host-only context)
+        assert host.lib.sym_strerror(host.h).decode() == "host-only context"
