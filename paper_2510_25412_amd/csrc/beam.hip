@@ -476,7 +476,7 @@ __device__ __forceinline__ int keep_best(Choice* found, int* n_found, int K, int
 // One workgroup for a group.  A value that the K best reach comes from 256 disjoint subsets' largest: of every row some lists, since the best
 // may all be one row's.  Lists that reach it are read again, and what reaches it in them is sorted.  What is read of the rows' pass is
 // requested at once and kept, so that a choice is three round trips: where the group's rows are, their lists, the logits looked at again.  Bound: those
-// and the steps between (6..8 us for 1..64 requests of 4 beams, 8 choices; 12 for 32 choices of 16 beams).
+// and the steps between (6..9 us for 1..64 requests of 4 beams, 8 choices; 12 for 32 choices of 16 beams).
 template <typename E, bool MASKED, bool TINY, int THREADS, int kHeld>
 __global__ __launch_bounds__(THREADS) void select_best_kernel(SelectArgs a, GroupRows g, int group0) {
   __shared__ RowScore rows[kBeamsMost];
