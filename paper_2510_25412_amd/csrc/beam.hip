@@ -413,34 +413,85 @@ __device__ __forceinline__ uint64_t rest_of(int row, float value, int token) { r
 __device__ __forceinline__ bool before(const Choice& a, const Choice& b) { return a.score > b.score || (a.score == b.score && a.rest < b.rest); }
 constexpr uint64_t kNone = ~0ull;
 
-constexpr int kFewLists = 4096, kFewThreads = 512;
+constexpr int kFewLists = 4096, kFewThreads = 512, kRanked = 256;
+static_assert(kRanked >= kBestMost, "more than the K best");
 struct RowScore {
   double base, from;
 };
 
 __device__ __forceinline__ double of_order(uint64_t k) { return __builtin_bit_cast(double, k >> 63 ? k ^ 1ull << 63 : ~k); }
-// The K-th of the threads' choices, from the highest bit down, of the scores first.
-__device__ __forceinline__ Choice kth_best(const Choice& mine, int K) {
-  const uint64_t u = __builtin_bit_cast(uint64_t, mine.score + 0.0), key = u ^ ((uint64_t)((int64_t)u >> 63) | 1ull << 63);
-  uint64_t score = 0, rest = kNone;
-  for (uint64_t bit = 1ull << 63; bit; bit >>= 1)
-    if (__syncthreads_count(key >= (score | bit)) >= K) score |= bit;
-  const int left = K - __syncthreads_count(key > score);
-  if (__syncthreads_count(key == score) == left) return Choice{of_order(score), kNone - 1};      // (all of them)
-  for (uint64_t bit = 1ull << 63; bit; bit >>= 1)
-    if (__syncthreads_count(key == score && mine.rest <= (rest ^ bit)) >= left) rest ^= bit;
+// In how many threads x holds, in every thread.  One barrier: the wavefronts' counts lie in one half of `counts` (32) and the next call's in the other.
+template <int THREADS>
+__device__ __forceinline__ int threads_with(bool x, int* counts, int* half) {
+  static_assert(THREADS <= 1024, "16 counts to a half");
+  const int lane = threadIdx.x & 63;
+  const int of_wave = lanes_of(__ballot(x));
+  if (lane == 0) counts[*half + (threadIdx.x >> 6)] = of_wave;
+  __syncthreads();
+  int n = (lane & 15) < THREADS / 64 ? counts[*half + (lane & 15)] : 0;
+  *half ^= 16;
+  n += __builtin_amdgcn_update_dpp(0, n, 0xB1, 0xf, 0xf, false);
+  n += __builtin_amdgcn_update_dpp(0, n, 0x4E, 0xf, 0xf, false);
+  n += __builtin_amdgcn_update_dpp(0, n, 0x141, 0xf, 0xf, false);
+  n += __builtin_amdgcn_update_dpp(0, n, 0x140, 0xf, 0xf, false);
+  return __builtin_amdgcn_readfirstlane(n);
+}
+
+// The K-th of the threads' choices (those of the first n, n >= K), from the highest bit down, of the scores first.  Bits that all have alike are
+// passed over: of equal logits only the tokens' differ (64 requests of 4 beams of 131072 equal logits, 128 choices: 0.53 -> 0.26 ms).
+template <int THREADS>
+__device__ __forceinline__ Choice kth_best(const Choice& mine, const Choice& one, bool is, int K) {
+  __shared__ uint32_t unlike[4];
+  __shared__ int counts[32];
+  int half = 0;
+  const auto in = [&](bool x) __attribute__((always_inline)) { return threads_with<THREADS>(x, counts, &half); };
+  const auto key_of_score = [](double x) __attribute__((always_inline)) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, x + 0.0);
+    return u ^ ((uint64_t)((int64_t)u >> 63) | 1ull << 63);
+  };
+  const uint64_t key = key_of_score(mine.score), of_one = key_of_score(one.score);
+  if (threadIdx.x < 4) unlike[threadIdx.x] = 0;
+  __syncthreads();
+  if (is) {
+    const uint64_t d = key ^ of_one, e = mine.rest ^ one.rest;
+    atomicOr(&unlike[0], (uint32_t)d);
+    atomicOr(&unlike[1], (uint32_t)(d >> 32));
+    atomicOr(&unlike[2], (uint32_t)e);
+    atomicOr(&unlike[3], (uint32_t)(e >> 32));
+  }
+  __syncthreads();
+  const uint64_t scores = (uint64_t)unlike[1] << 32 | unlike[0], rests = (uint64_t)unlike[3] << 32 | unlike[2];
+  const auto highest = [](uint64_t x) __attribute__((always_inline)) { return 1ull << (63 - __builtin_clzll(x)); };
+  uint64_t score = of_one & ~scores, rest = one.rest | rests;
+  for (uint64_t m = scores; m; m &= ~highest(m))
+    if (in(is && key >= (score | highest(m))) >= K) score |= highest(m);
+  const int left = K - in(is && key > score);
+  if (in(is && key == score) == left) return Choice{of_order(score), kNone - 1};      // (all of them)
+  for (uint64_t m = rests; m; m &= ~highest(m))
+    if (in(is && key == score && mine.rest <= (rest ^ highest(m))) >= left) rest ^= highest(m);
   return Choice{of_order(score), rest};
+}
+
+// Of the n > K choices in `found` the K best stay, in any order; the K-th of them, or what none of the others reaches.
+template <int THREADS>
+__device__ __forceinline__ Choice keep_k(Choice* found, int* n_found, int n, int K) {
+  const int tid = threadIdx.x;
+  const Choice mine = found[min(tid, n - 1)], cut = kth_best<THREADS>(mine, found[0], tid < n, K);
+  if (tid == 0) *n_found = 0;
+  __syncthreads();
+  if (tid < n && !before(cut, mine)) found[atomicAdd(n_found, 1)] = mine;
+  __syncthreads();
+  return cut;
 }
 
 // The K best of many, in `found` in any order, or all where they are fewer; returns how many.  What `of` makes of turn t in a thread (N choices at
 // most; a bit for each that counts) goes there, and whenever it is full the K best stay and nothing behind them comes in any more.  Equal logits by
-// the thousand take this way: a choice of 64 requests of 4 beams of 131072 equal logits takes 0.31 ms with 8, 0.53 ms with 128.
+// the thousand take this way: a choice of 64 requests of 4 beams of 131072 equal logits takes 0.18 ms with 8, 0.23 ms with 128.
 template <int THREADS, int N, typename F>
 __device__ __forceinline__ int keep_best(Choice* found, int* n_found, int K, int turns, F of) {
-  const int tid = threadIdx.x;
   Choice cut = {0.0, kNone};
   __syncthreads();                                         // everyone has read how many there were
-  if (tid == 0) *n_found = 0;
+  if (threadIdx.x == 0) *n_found = 0;
   __syncthreads();
   for (int t = 0; t < turns; ++t) {
     Choice x[N];
@@ -462,12 +513,7 @@ __device__ __forceinline__ int keep_best(Choice* found, int* n_found, int K, int
       const int n = min(*n_found, THREADS);
       if (!over && (last || t + 1 < turns || n <= K)) break;
       last = !over;
-      const Choice mine = tid < n ? found[tid] : Choice{-(double)INFINITY, kNone};
-      cut = kth_best(mine, K);
-      if (tid == 0) *n_found = 0;
-      __syncthreads();
-      if (tid < n && !before(cut, mine)) found[atomicAdd(n_found, 1)] = mine;
-      __syncthreads();
+      cut = keep_k<THREADS>(found, n_found, n, K);
     }
   }
   return *n_found;
@@ -616,6 +662,9 @@ __global__ __launch_bounds__(THREADS) void select_best_kernel(SelectArgs a, Grou
       }
       return reach;
     });
+  } else if (n > kRanked) {                                // ranking takes n * n looks (256 rows of logits rounded to whole numbers, 64 choices: 131 -> 76 us)
+    keep_k<THREADS>(found, &n_found, n, K);
+    n = K;
   }
   const int64_t out = (int64_t)(group0 + blockIdx.x) * K;
   const auto write = [&](int k, const Choice& x) __attribute__((always_inline)) {
