@@ -390,12 +390,12 @@ int sym_pred_layer_sparse(sym_ctx* ctx, int32_t layer, const void* q, const void
 #define SYM_BEAMS_MOST 64       /* rows of a group   */
 #define SYM_BEST_MOST  128      /* choices of a group */
 typedef struct sym_beam_step {
-  int32_t n_groups, n_best;
+  int32_t n_groups, n_best;        /* 0 .. 65536, 1 .. SYM_BEST_MOST                      */
   const int32_t* beams;            /* [n_groups], 1 .. SYM_BEAMS_MOST each                */
   int64_t rows;                    /* of logits, scores, allowed: the sum of beams, or SYM_EINVAL */
   int32_t vocab, dtype;            /* 1 .. 2^24; SYM_F32, SYM_BF16 or SYM_F16             */
   const void* logits;              /* [rows][logits_stride], aligned to an element        */
-  int64_t logits_stride;           /* elements from row to row, >= vocab (0: vocab)       */
+  int64_t logits_stride;           /* elements from row to row, >= vocab (0: vocab); rows of an array span 2^46 bytes at most */
   const float* scores;             /* [rows]                                              */
   const uint32_t* allowed;         /* NULL, or [rows][allowed_stride]: bit v % 32 of word v / 32 */
   int64_t allowed_stride;          /* words from row to row, >= (vocab + 31) / 32 (0: that) */
@@ -410,7 +410,7 @@ int     sym_beam_select(sym_ctx* ctx, const sym_beam_step* step, void* stream);
 
 /* Rows of per-beam state (token histories, recurrent states) after the beams: in each of n_states arrays [outer][rows][row_bytes], row r
  * of group g receives row parents[r] of the group (device int32 [rows], index within the group; rows: the sum of beams, or SYM_EINVAL).  A parent outside the group, -1 above
- * all, leaves the row as it is.  dst may be src (in place) or apart from it, then every row is written; nothing else may overlap.  Rows
+ * all, leaves the row as it is.  Up to 65536 groups.  dst may be src (in place) or apart from it, then every row is written; nothing else may overlap.  Rows
  * of any alignment; 16-byte aligned ones move fastest.  Like sym_beam_select allowed while a batch is open and in graphs.  */
 #define SYM_STATES_MOST 64
 typedef struct sym_beam_state {

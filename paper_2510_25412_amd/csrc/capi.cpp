@@ -1831,6 +1831,7 @@ int sym_pred_sparse(sym_ctx* c, int32_t n_lips, const sym_kv* kv, const int32_t*
 
 namespace {
 constexpr int32_t kGroupsMost = 1 << 16;
+constexpr int64_t kFar = (int64_t)1 << 46;             // bytes of an array at most, from its first row to its last: what is computed of them stays within 64 bits
 // Rows of all groups and of the largest, or a negative status.
 int64_t count_rows(int32_t n_groups, const int32_t* beams, int32_t* most) {
   if (n_groups < 0 || n_groups > kGroupsMost || (n_groups > 0 && !beams)) return SYM_EINVAL;
@@ -1883,7 +1884,10 @@ int sym_beam_select(sym_ctx* c, const sym_beam_step* b, void* stream) {
     if (stride < b->vocab || stride > (int64_t)1 << 40) return fail(c, SYM_EINVAL, "beam_select: rows of logits overlap, or lie too far apart");
     if (b->allowed && (bit_stride < words || bit_stride > (int64_t)1 << 40)) return fail(c, SYM_EINVAL, "beam_select: rows of allowed tokens overlap, or lie too far apart");
     if (rows == 0) return SYM_OK;
-    const int64_t es = b->dtype == SYM_F32 ? 4 : 2, scratch = select_scratch(rows, most, b->vocab, b->n_best), out = (int64_t)b->n_groups * b->n_best * 4;
+    const int64_t es = b->dtype == SYM_F32 ? 4 : 2;
+    if (rows > 1 && stride > kFar / (rows * es)) return fail(c, SYM_EINVAL, "beam_select: rows of logits overlap, or lie too far apart");
+    if (rows > 1 && b->allowed && bit_stride > kFar / (rows * 4)) return fail(c, SYM_EINVAL, "beam_select: rows of allowed tokens overlap, or lie too far apart");
+    const int64_t scratch = select_scratch(rows, most, b->vocab, b->n_best), out = (int64_t)b->n_groups * b->n_best * 4;
     if (!b->logits || !b->scores || !b->best_scores || !b->best_beams || !b->best_tokens || !b->scratch) return fail(c, SYM_EINVAL, "beam_select: a pointer is missing");
     if (!aligned(b->logits, (uintptr_t)es) || !aligned(b->scores, 4) || !aligned(b->allowed, 4) || !aligned(b->best_scores, 4) || !aligned(b->best_beams, 4) ||
         !aligned(b->best_tokens, 4) || !aligned(b->scratch, 16))
@@ -1965,7 +1969,6 @@ int sym_beam_states(sym_ctx* c, int32_t n_groups, const int32_t* beams, int64_t 
     std::vector<Area> area;
     area.reserve(2 * (size_t)n_states + 1);
     if (rows > 0) area.push_back({parents, rows * 4, -1, false});
-    constexpr int64_t kFar = (int64_t)1 << 46;             // bytes of an array at most
     for (int32_t i = 0; i < n_states; ++i) {
       const sym_beam_state& s = states[i];
       if (s.outer < 0 || s.row_bytes < 0 || (s.row_bytes > 0 && s.row_stride < s.row_bytes) || s.row_stride > kFar || s.outer > kFar)

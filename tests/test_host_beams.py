@@ -355,3 +355,26 @@ def test_states_of_one_row():
         host = host_ctx()
         refused(EINVAL, host.beam_states, [1], torch.zeros(1, dtype=torch.int32), plan)         # (of a host-only context)
         assert host.lib.sym_strerror(host.h).decode() == "host-only context"
+
+
+def test_far_strides_of_a_choice():
+    # 65536 requests of 64 beams, rows as far apart as an address space is wide: the arrays' ends lie beyond 64 bits, and an output in
+    # the midst of the logits would go unnoticed
+    ctx = host_ctx()
+    call = lambda **kw: (ctx.lib.sym_beam_select(ctx.h, C.byref(step_of(**kw)), None), ctx.lib.sym_strerror(ctx.h).decode())  # noqa: E731
+    many = [64] * 65536
+    apart = dict(scores=1 << 50, best_scores=1 << 51, best_beams=1 << 52, best_tokens=1 << 53, scratch=1 << 54, scratch_bytes=1 << 40)
+    far = dict(apart, beams=many, allowed=None, n_best=1)
+    assert call(**far) == (EINVAL, "host-only context")
+    for dtype, size in ((binding.SYM_F32, 4), (binding.SYM_BF16, 2), (binding.SYM_F16, 2)):
+        most = (1 << 46) // (size << 22)                      # 64 TB of logits, no more
+        assert call(**dict(far, dtype=dtype, logits_stride=most)) == (EINVAL, "host-only context")
+        for stride in (most + 1, 1 << 39, (1 << 40) - 1, 1 << 40):
+            assert call(**dict(far, dtype=dtype, logits_stride=stride)) == (EINVAL, "beam_select: rows of logits overlap, or lie too far apart")
+            assert call(**dict(far, dtype=dtype, logits_stride=stride, best_tokens=1 << 31))[1] != "host-only context"
+    words = dict(far, logits=1 << 49, allowed=1 << 27)
+    assert call(**dict(words, allowed_stride=1 << 22)) == (EINVAL, "host-only context")
+    for stride in ((1 << 22) + 1, 1 << 39, 1 << 40):
+        assert call(**dict(words, allowed_stride=stride)) == (EINVAL, "beam_select: rows of allowed tokens overlap, or lie too far apart")
+    assert call(**dict(apart, logits_stride=1 << 40, allowed=None, beams=[1])) == (EINVAL, "host-only context")      # (one row: its stride says nothing)
+    assert call(**dict(apart, logits_stride=1 << 41, allowed=None, beams=[1]))[1] != "host-only context"
