@@ -85,11 +85,9 @@ class RagDriver:
             self.scores = torch.full((cfg.n_requests, B), -math.inf, device=sess.device)
             self.scores[:, 0] = 0.0
             self.tokens = torch.full((cfg.n_requests * B, cfg.answer_tokens), -1, dtype=torch.int32, device=sess.device)
-            self.parents = torch.empty(cfg.n_requests * B, dtype=torch.int32, device=sess.device)
-            self.states = binding.make_states([(self.tokens, self.tokens, 0)])
-            self.every = np.full(cfg.n_requests, B, np.int32)
+            self.every = np.full(min(cfg.max_batch, cfg.n_requests), B, np.int32)
             self.best = [torch.empty(rows, dtype=t, device=sess.device) for t in (torch.float32, torch.int32, torch.int32)]
-            self.scratch = torch.empty(max(binding.beam_scratch_bytes(self.every[:n], cfg.vocab, B) for n in range(1, min(cfg.max_batch, cfg.n_requests) + 1)),
+            self.scratch = torch.empty(max(binding.beam_scratch_bytes(self.every[:n], cfg.vocab, B) for n in range(1, len(self.every) + 1)),
                                        dtype=torch.uint8, device=sess.device)
         self.trace = [] if trace else None
         self.outputs = [] if trace else None
@@ -139,12 +137,12 @@ class RagDriver:
         best, beam, token = (x[:n * B] for x in self.best)
         ctx.beam_select(self.every[:n], B, self.logits[:n * B], self.scores[rid].flatten(), best, beam, token, self.scratch, None, stream)
         self.scores[rid] = best.view(n, B)
-        self.parents.fill_(-1)
         rows = (rid[:, None] * B + torch.arange(B, device=rid.device)).flatten()
-        self.parents[rows] = beam
-        ctx.beam_states(self.every, self.parents, self.states, stream)
+        tokens = self.tokens[rows]                           # of this batch alone, whatever the run's length
+        ctx.beam_states(self.every[:n], beam, binding.make_states([(tokens, tokens, 0)]), stream)
         at = torch.tensor([self.cfg.answer_tokens - lip.to_decode for lip in lips], device=rid.device).repeat_interleave(B)
-        self.tokens[rows, at] = token
+        tokens[torch.arange(n * B, device=rid.device), at] = token
+        self.tokens[rows] = tokens
         files = [f for lip in lips for f in lip.beams]
         sources = beam.cpu().numpy()
         sources = np.where(sources < 0, -1, sources + np.repeat(np.arange(n) * B, B))
