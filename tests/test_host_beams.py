@@ -378,3 +378,16 @@ def test_far_strides_of_a_choice():
         assert call(**dict(words, allowed_stride=stride)) == (EINVAL, "beam_select: rows of allowed tokens overlap, or lie too far apart")
     assert call(**dict(apart, logits_stride=1 << 40, allowed=None, beams=[1])) == (EINVAL, "host-only context")      # (one row: its stride says nothing)
     assert call(**dict(apart, logits_stride=1 << 41, allowed=None, beams=[1]))[1] != "host-only context"
+
+
+def test_one_row_in_any_dimension():
+    # rows, bytes and strides of each, whichever dimension the row is
+    import torch
+    x = torch.zeros(3, 1, 5, 2, dtype=torch.int16)
+    for dim, row_bytes, outer in [(1, 20, 3), (-3, 20, 3)]:
+        plan = binding.make_states([(x, x, dim)])
+        assert (plan._rows, plan[0].row_bytes, plan[0].outer) == (1, row_bytes, outer) and plan[0].row_stride >= row_bytes
+    for shape, dim in [((1, 6), 0), ((6, 1), 1), ((1,), 0), ((2, 3, 1), 2), ((2, 1, 3), 1)]:
+        x = torch.zeros(shape)
+        plan = binding.make_states([(x, x, dim)])
+        assert plan._rows == 1 and plan[0].row_bytes * plan[0].outer == 4 * x.numel() and plan[0].row_stride >= plan[0].row_bytes
