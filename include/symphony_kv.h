@@ -383,7 +383,9 @@ int sym_pred_layer_sparse(sym_ctx* ctx, int32_t layer, const void* q, const void
  * n_best (beam, token) pairs of largest score, best first; of equal ones the lower beam, then the lower token.  A pair of a score that is
  * not finite in 32 bits is never chosen: rows whose running score is not finite (-inf: a beam that does not live; its logits are not read),
  * rows that allow nothing, and rows with a NaN or +inf among what they allow have none.  Places that nothing fills
- * hold -inf, -1, -1.  Compared in 64 bits, returned in 32; exponentials in 32 bits, summed in 32 by each lane (a part of a row has 256 or 512 sums) and in 64 beyond.
+ * hold -inf, -1, -1.  Equal are scores that come out equal: of rows that hold the same logits in the same order always; rows of the same
+ * logits in another order may have normalisers that differ in their last bits.  Compared in 64 bits, returned in 32; exponentials in 32
+ * bits, summed in 32 by each lane (a part of a row has 256 or 512 sums) and in 64 beyond.
  * All pointers are device memory of the caller but `beams` (host, read before the call returns); scratch is written and read by the call alone:
  * two calls that may run at one time (graphs among them) need one each.  An output that overlaps anything else is refused (what lies between rows that are apart belongs to the array).  Touches
  * neither files nor workspace: allowed while a batch is open, and may be recorded into a graph.              */

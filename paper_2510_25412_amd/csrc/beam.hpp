@@ -45,9 +45,12 @@ struct SelectCut {
 };
 // Parts, first, until the lists of one row can hold a choice.  Then, while a part has more than 2048 logits (a wavefront's loads under way), until there
 // are 2048 wavefronts, but no more parts of a group than 512 threads hold in the second launch (rows of 131072 bf16 logits, calls of 4, 16, 64 requests
-// of 4 beams: 11.7, 13.9, 22 us; with up to 256 parts of a group 16.0, 15.2, 22; wavefronts 1024 or 4096: 13.9 and 19.8 us for 16 requests), or until a
+// of 4 beams: 12, 14, 23 us; with up to 256 parts of a group 14, 18, 23; wavefronts 1024 or 4096: 13.9 and 19.8 us for 16 requests), or until a
 // part has no more than 40960 logits of 16 bits (2048 rows of 131072: 97 us; 20480 101, 10240 105, 81920 100), 10240 of fp32 (1024 rows of 65537, 32
 // choices of 16 beams: 58 us; 62 with half as many or four times as many: what is looked at again is a list, a 64th of a part).
+// The bound of 64 parts is the one that 4 beams want.  Few wide requests of 16-bit logits lose by it: 1 and 4 requests of 16 beams of 131072 take 17.4 and
+// 18.9 us, with 256 parts 12.4 and 14.3, of 32 beams 20 and 22 against 15 and 18, of 64 beams of 40960 22 and 23 against 17 and 20; with 16 requests
+// of 16 beams and more, and with fp32 logits of so many, the two are alike within 2 us.
 constexpr int kSelectWaves = 2048, kSelectParts = 64;
 inline SelectCut select_cut(int64_t rows, int32_t most_beams, int32_t vocab, int32_t n_best, int32_t logit_bytes) {
   const int64_t octets = (vocab + kOctet - 1) / kOctet, most = std::min<int64_t>(kMostParts / most_beams, 64);

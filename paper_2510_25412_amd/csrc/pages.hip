@@ -16,8 +16,9 @@ struct CopyList {
 // different pages.  Bound: HBM, read + write.  Half of a server's pool (9837 pages, 2 layers, 1.29 GB read, as much written) 409..422 us = 6.1..6.3 TB/s,
 // with two chunks to a thread, past the caches both ways (plain stores 438, plain loads 425, four chunks 420..437, eight 445..468).
 // Few copies are of last pages, which several forks take: plain loads (239 copies x 8 layers, a call 24.2 us; 26.0 past the caches).
-// A copy of r slots takes nearly as long as one of 16: the beginnings of pieces, 2 KB apart, lie in the same few of the memory's channels, and what
-// those move decides (240 copies x 8 layers of 1, 4, 15 slots: 23, 28, 38 us, 8, 31 and 118 MB written).
+// The grid is a full page's whatever the slots, and of a copy of few slots most workgroups start, read the list and leave: 240 copies x 8 layers x 8
+// heads of 1, 4, 8, 15 slots take 13, 26, 26, 36 us (8, 31, 63, 118 MB written); with a grid for the longest copy of the list 3.6, 8.8, 20, 36. The
+// calls that copy so are the host's time (next to which this is not seen).
 constexpr int kCopyChunks = 2;         // chunks of a thread
 template <bool PAST>
 __device__ __forceinline__ u32x4_t load16(const uint8_t* p) {
