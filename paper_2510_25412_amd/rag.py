@@ -86,6 +86,7 @@ class RagDriver:
             self.scores[:, 0] = 0.0
             self.tokens = torch.full((cfg.n_requests * B, cfg.answer_tokens), -1, dtype=torch.int32, device=sess.device)
             self.every = np.full(min(cfg.max_batch, cfg.n_requests), B, np.int32)
+            self.nth = torch.arange(len(self.every), device=sess.device)
             self.best = [torch.empty(rows, dtype=t, device=sess.device) for t in (torch.float32, torch.int32, torch.int32)]
             self.scratch = torch.empty(max(binding.beam_scratch_bytes(self.every[:n], cfg.vocab, B) for n in range(1, len(self.every) + 1)),
                                        dtype=torch.uint8, device=sess.device)
@@ -133,16 +134,16 @@ class RagDriver:
     def _choose(self, lips):
         """A step of these requests' searches: the best continuations of their beams, whose scores, tokens and files follow them."""
         torch, ctx, B, n, stream = self.torch, self.sess.ctx, self.cfg.beams, len(lips), self.sess.stream
-        rid = torch.tensor([lip.rid for lip in lips], device=self.sess.device)
+        rid, at = torch.tensor([[lip.rid for lip in lips], [self.cfg.answer_tokens - lip.to_decode for lip in lips]], device=self.sess.device)
         best, beam, token = (x[:n * B] for x in self.best)
         ctx.beam_select(self.every[:n], B, self.logits[:n * B], self.scores[rid].flatten(), best, beam, token, self.scratch, None, stream)
         self.scores[rid] = best.view(n, B)
-        rows = (rid[:, None] * B + torch.arange(B, device=rid.device)).flatten()
-        tokens = self.tokens[rows]                           # of this batch alone, whatever the run's length
-        ctx.beam_states(self.every[:n], beam, binding.make_states([(tokens, tokens, 0)]), stream)
-        at = torch.tensor([self.cfg.answer_tokens - lip.to_decode for lip in lips], device=rid.device).repeat_interleave(B)
-        tokens[torch.arange(n * B, device=rid.device), at] = token
-        self.tokens[rows] = tokens
+        of_request = self.tokens.view(-1, B, self.cfg.answer_tokens)
+        tokens = of_request[rid]                             # this batch's alone, whatever the run's length
+        rows = tokens.flatten(0, 1)
+        ctx.beam_states(self.every[:n], beam, binding.make_states([(rows, rows, 0)]), stream)
+        tokens[self.nth[:n], :, at] = token.view(n, B)
+        of_request[rid] = tokens
         files = [f for lip in lips for f in lip.beams]
         sources = beam.cpu().numpy()
         sources = np.where(sources < 0, -1, sources + np.repeat(np.arange(n) * B, B))
